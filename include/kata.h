@@ -418,6 +418,160 @@ KATA_API int kata_bwd_form(int B, int H, int T, int d, int dv, int C, int g, kat
 KATA_API int kata_bwd_fused_scan(int B, int H, int T, int d, int dv, int C, int g,
                                  kata_dtype_t dtype);
 
+/*
+ * Operators around a recurrent mixer: the short convolution over a projection's
+ * channels, the norms of query and key heads with their position rotation, and
+ * the selective state space scan.  Conventions that differ from the ones above:
+ *  - Activations are token-major, as a projection writes them, and may be views
+ *    of a wider tensor: each has element strides (>= 0) over its outer
+ *    dimensions, the innermost dimension being contiguous.  Their base addresses
+ *    need the alignment of one element only; rows of aligned 16-byte pieces
+ *    are read and written as such.  The rows of an output must not overlap.
+ *  - Inputs, outputs and gradients of activations are fp32 or bf16 (dtype), each
+ *    output rounded once; parameters, their gradients and states are fp32 unless
+ *    stated, 4-byte aligned and contiguous.  Sums are held in fp32 or fp64.
+ *  - lengths (nullable): int32 [B] on the device, the tokens of each sequence of
+ *    a padded batch (clamped to 0..T).  Rows past a sequence's end are neither
+ *    read nor written; a returned state is the one after its last token (of
+ *    no tokens: the given state, or zeros).
+ *  - No output may alias or overlap an input, except the states that a step
+ *    updates in place; equal base addresses are KATA_ERR_INVALID_ARG.
+ *  - Non-finite inputs reach no output of an earlier token, another sequence or
+ *    (where heads are separate) another head; in gradients they may reach
+ *    every output of their sequence, and the parameters'.
+ *  - Every call enqueues kernel launches only and can be captured into a HIP
+ *    graph; results do not depend on the order in which workgroups run.
+ *    T <= 2^30; larger T and launches of more than 2^31 - 1 workgroups are
+ *    KATA_ERR_UNSUPPORTED.
+ */
+
+/*
+ * Causal depthwise convolution of W taps (2, 3 or 4; else KATA_ERR_UNSUPPORTED) over
+ * D <= 2^20 channels:
+ *     pre[t] = bias + sum_{j<W} w[j] x[t - (W-1) + j],   y = act(pre).
+ *   x, y : [B][T][D], strides x_batch, x_token, y_batch, y_token;  w : [D][W];
+ *   bias : [D], nullable.
+ *   state_in  (nullable: zeros) : [B][W-1][D] in dtype, the rows before x[0],
+ *   state_out (nullable) : the last W-1 rows, for kata_conv_step or a next call.
+ */
+typedef enum { KATA_CONV_NONE = 0, KATA_CONV_SILU = 1 } kata_conv_act_t;
+KATA_API kata_status_t kata_conv_fwd(const void* x, const float* w, const float* bias,
+                                     const void* state_in, const int* lengths, void* y,
+                                     void* state_out, int B, int T, int D, int W,
+                                     long long x_batch, long long x_token, long long y_batch,
+                                     long long y_token, kata_conv_act_t act, kata_dtype_t dtype,
+                                     hipStream_t stream);
+/* One token of every sequence: x, y [B][D] (strides x_batch, y_batch); the rows of
+ * state [B][W-1][D] move up by one. */
+KATA_API kata_status_t kata_conv_step(void* state, const void* x, const float* w,
+                                      const float* bias, void* y, int B, int D, int W,
+                                      long long x_batch, long long y_batch, kata_conv_act_t act,
+                                      kata_dtype_t dtype, hipStream_t stream);
+/* Gradients of kata_conv_fwd without state and lengths: dx [B][T][D] (strides), dw [D][W],
+ * dbias [D] (either nullable) from dy [B][T][D] (strides).  workspace: at least
+ * kata_conv_bwd_workspace_bytes(...) bytes (0: invalid or unsupported arguments),
+ * 256-byte aligned, contents undefined on exit. */
+KATA_API kata_status_t kata_conv_bwd_ws(const void* x, const float* w, const float* bias,
+                                        const void* dy, void* dx, float* dw, float* dbias, int B,
+                                        int T, int D, int W, long long x_batch, long long x_token,
+                                        long long dy_batch, long long dy_token,
+                                        long long dx_batch, long long dx_token,
+                                        kata_conv_act_t act, kata_dtype_t dtype, void* workspace,
+                                        size_t workspace_bytes, hipStream_t stream);
+KATA_API size_t kata_conv_bwd_workspace_bytes(int B, int T, int D, int W, kata_dtype_t dtype);
+
+/*
+ * Norms of query and key heads with the position rotation in the same pass, from a
+ * projection's rows to the head-major tensors of the attention calls above (at T = 1:
+ * of the decode step).  For every head row x of width d:
+ *     hat = x / sqrt(mean(x^2) + eps)  (KATA_NORM_RMS; KATA_NORM_L2: the sum for the mean;
+ *           KATA_NORM_NONE: x),        y = R (w hat),
+ * R turning pair i < r/2 of the first r coordinates by the angle pos * freq[i]:
+ * coordinates (i, i + r/2), or with pairs = 1 (2i, 2i+1).
+ *   q : [B][T][Hq][d], k : [B][T][Hk][d] with strides (batch, token, head); k, wk and the
+ *   key outputs are null where Hk = 0.  wq, wk : [d], nullable (ones).
+ *   pos : int32 [B][T], nullable (0..T-1);  freq : fp64 [r/2], null where r = 0 (angles are
+ *   formed in fp64: positions up to 2^31 lose nothing).
+ *   yq : [B][Hq][T][d], yk : [B][Hk][T][d], contiguous, in dtype.
+ *   d <= 256 (else KATA_ERR_UNSUPPORTED), r even, 0 <= r <= d, eps >= 0 and finite (a row of
+ *   zeros needs eps > 0); Hq + Hk <= 65535.  Squares are summed in fp32.
+ */
+typedef enum { KATA_NORM_NONE = 0, KATA_NORM_RMS = 1, KATA_NORM_L2 = 2 } kata_norm_t;
+KATA_API kata_status_t kata_qk_norm_fwd(const void* q, const void* k, const float* wq,
+                                        const float* wk, const int* pos, const double* freq,
+                                        void* yq, void* yk, int B, int T, int Hq, int Hk, int d,
+                                        int r, long long q_batch, long long q_token,
+                                        long long q_head, long long k_batch, long long k_token,
+                                        long long k_head, kata_norm_t norm, float eps, int pairs,
+                                        kata_dtype_t dtype, hipStream_t stream);
+/* Its gradients: dq, dk of the outputs, head-major as yq and yk, in dy_dtype (fp32 as the
+ * attention's gradients, or dtype); dxq [B][T][Hq][d] and dxk [B][T][Hk][d] in dtype, with
+ * strides of their own; dwq, dwk [d], nullable.  workspace as for kata_conv_bwd_ws. */
+KATA_API kata_status_t kata_qk_norm_bwd_ws(
+    const void* q, const void* k, const float* wq, const float* wk, const int* pos,
+    const double* freq, const void* dq, const void* dk, void* dxq, void* dxk, float* dwq,
+    float* dwk, int B, int T, int Hq, int Hk, int d, int r, long long q_batch, long long q_token,
+    long long q_head, long long k_batch, long long k_token, long long k_head, long long dxq_batch,
+    long long dxq_token, long long dxq_head, long long dxk_batch, long long dxk_token,
+    long long dxk_head, kata_norm_t norm, float eps, int pairs, kata_dtype_t dtype,
+    kata_dtype_t dy_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
+KATA_API size_t kata_qk_norm_bwd_workspace_bytes(int B, int T, int Hq, int Hk, int d,
+                                                 kata_dtype_t dtype);
+
+/*
+ * Selective state space scan, per head with a state S [N][P]:
+ *     step_t = softplus(dt_t + bias)   (softplus = 0: dt_t + bias),
+ *     S_t = exp(step_t A) S_{t-1} + step_t B_t x_t^T,    y_t = C_t^T S_t + D x_t.
+ *   x, y : [B][T][H][P];  dt : [B][T][H];  Bm, Cm : [B][T][G][N], a group's rows shared by its
+ *   H / G heads (G divides H, else KATA_ERR_INVALID_ARG); all in dtype, with strides.
+ *   A : [H] (negative for a decaying state), D, dt_bias : [H], nullable.
+ *   S_in (nullable: zeros), S_out (nullable) : fp32 [B][H][N][P], 16-byte aligned.
+ *   N <= 128, P <= 256, B*H <= 65535, else KATA_ERR_UNSUPPORTED.
+ *   Computed in chunks of 64 (fp32: 32) tokens on the matrix cores; long sequences of few
+ *   heads are split into spans whose states are joined.  bf16: products accumulate in fp32,
+ *   the weights of a chunk's pairs and the state that y reads are rounded to bf16 once, the
+ *   state itself keeps 2^-18 of every term.  A positive A or a negative step grows the state
+ *   as the formula says, until it overflows.
+ *   strides : element strides over batch, token and head (group); null: contiguous.
+ *   workspace : at least kata_ssm_workspace_bytes(..., backward) bytes (0: invalid or
+ *   unsupported arguments), 256-byte aligned, contents undefined on exit.
+ */
+typedef struct {
+  long long x_batch, x_token, x_head;
+  long long dt_batch, dt_token, dt_head;
+  long long b_batch, b_token, b_group;
+  long long c_batch, c_token, c_group;
+  long long y_batch, y_token, y_head; /* y, or dy in the backward */
+} kata_ssm_strides_t;
+KATA_API kata_status_t kata_ssm_fwd_ws(const void* x, const void* dt, const float* A,
+                                       const void* Bm, const void* Cm, const float* D,
+                                       const float* dt_bias, const float* S_in,
+                                       const int* lengths, void* y, float* S_out, int B, int T,
+                                       int H, int G, int N, int P,
+                                       const kata_ssm_strides_t* strides, int softplus,
+                                       kata_dtype_t dtype, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream);
+/* Gradients of kata_ssm_fwd_ws from a zero state, without lengths: dx, ddt, dBm, dCm in
+ * dtype, contiguous and shaped as x, dt, Bm, Cm (those of a group summed over its heads);
+ * dA, dD, dt_dbias [H], each nullable. */
+KATA_API kata_status_t kata_ssm_bwd_ws(const void* x, const void* dt, const float* A,
+                                       const void* Bm, const void* Cm, const float* D,
+                                       const float* dt_bias, const void* dy, void* dx, void* ddt,
+                                       float* dA, void* dBm, void* dCm, float* dD,
+                                       float* dt_dbias, int B, int T, int H, int G, int N, int P,
+                                       const kata_ssm_strides_t* strides, int softplus,
+                                       kata_dtype_t dtype, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream);
+KATA_API size_t kata_ssm_workspace_bytes(int B, int T, int H, int G, int N, int P,
+                                         kata_dtype_t dtype, int backward);
+/* One token: x, y [B][H][P], dt [B][H], Bm, Cm [B][G][N] (the token strides are not read);
+ * S [B][H][N][P], 16-byte aligned, updated in place. */
+KATA_API kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, const float* A,
+                                     const void* Bm, const void* Cm, const float* D,
+                                     const float* dt_bias, void* y, int B, int H, int G, int N,
+                                     int P, const kata_ssm_strides_t* strides, int softplus,
+                                     kata_dtype_t dtype, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 KATA_API const char* kata_status_string(kata_status_t s);
 

@@ -9,15 +9,24 @@ fallback: if libkata.so is missing or fails to load, every call raises.
     out = kata.fwd_chunked(q, k, v, C=64)           # q, k: [B,H,T,d]; v: [B,H,T,dv]
     S, z = kata.prefill_state(k, v)                 # packed state after T tokens
     o = kata.decode_step(S, z, q1, k1, v1)          # one token per head, in place
+
+Around a recurrent mixer, on token-major rows (views of a projection's output):
+
+    u = kata.conv_fwd(x, w, bias)                   # short causal convolution, [B,T,D]
+    q, k = kata.qk_norm_fwd(q, k, wq, wk, freq)     # norms and rotation, to [B,H,T,d]
+    y = kata.ssm_fwd(x, dt, A, Bm, Cm, D, bias)     # selective scan, [B,T,H,P]
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 __all__ = [
     "KataError", "lib", "fwd_chunked", "fwd_chunked_timed", "fwd_chunked_alloc", "workspace_bytes",
     "default_span", "prefill_state", "decode_step", "packed_dim", "LIB_PATH",
+    "conv_fwd", "conv_step", "conv_bwd", "qk_norm_fwd", "qk_norm_bwd", "rope_frequencies",
+    "ssm_fwd", "ssm_step", "ssm_bwd",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkata.so")
@@ -40,6 +49,9 @@ EXPORTED = (
     "kata_bwd_workspace_bytes", "kata_bwd_fused_scan", "kata_bwd_form",
     "kata_fwd_chunked_noalloc", "kata_noalloc_scratch_bytes",
     "kata_status_string", "kata_abi_version",
+    "kata_conv_fwd", "kata_conv_step", "kata_conv_bwd_ws", "kata_conv_bwd_workspace_bytes",
+    "kata_qk_norm_fwd", "kata_qk_norm_bwd_ws", "kata_qk_norm_bwd_workspace_bytes",
+    "kata_ssm_fwd_ws", "kata_ssm_bwd_ws", "kata_ssm_workspace_bytes", "kata_ssm_step",
 )
 
 # what kata_fwd_form and kata_bwd_form return (-1: unsupported)
@@ -48,6 +60,10 @@ BWD_STATES, BWD_FUSED_STATES, BWD_QUADRATIC = 0, 1, 2
 
 # kata_lin_feature_t
 LIN_IDENTITY, LIN_RELU, LIN_ELU, LIN_LORENTZ, LIN_LORENTZ_S = 0, 1, 2, 3, 4
+
+# kata_conv_act_t, kata_norm_t
+CONV_NONE, CONV_SILU = 0, 1
+NORM_NONE, NORM_RMS, NORM_L2 = 0, 1, 2
 
 
 class KataError(RuntimeError):
@@ -146,6 +162,25 @@ def lib():
     L.kata_bwd_fused_scan.restype = i
     L.kata_bwd_form.argtypes = [i, i, i, i, i, i, i, i]
     L.kata_bwd_form.restype = i
+    ll = ctypes.c_longlong
+    L.kata_conv_fwd.argtypes = [vp] * 7 + [i] * 4 + [ll] * 4 + [i, i, vp]
+    L.kata_conv_step.argtypes = [vp] * 5 + [i] * 3 + [ll] * 2 + [i, i, vp]
+    L.kata_conv_bwd_ws.argtypes = [vp] * 7 + [i] * 4 + [ll] * 6 + [i, i, vp, sz, vp]
+    L.kata_conv_bwd_workspace_bytes.argtypes = [i] * 5
+    L.kata_qk_norm_fwd.argtypes = [vp] * 8 + [i] * 6 + [ll] * 6 + [i, f, i, i, vp]
+    L.kata_qk_norm_bwd_ws.argtypes = ([vp] * 12 + [i] * 6 + [ll] * 12
+                                      + [i, f, i, i, i, vp, sz, vp])
+    L.kata_qk_norm_bwd_workspace_bytes.argtypes = [i] * 6
+    L.kata_ssm_fwd_ws.argtypes = [vp] * 11 + [i] * 6 + [vp, i, i, vp, sz, vp]
+    L.kata_ssm_bwd_ws.argtypes = [vp] * 15 + [i] * 6 + [vp, i, i, vp, sz, vp]
+    L.kata_ssm_workspace_bytes.argtypes = [i] * 8
+    L.kata_ssm_step.argtypes = [vp] * 9 + [i] * 5 + [vp, i, i, vp]
+    for name in ("kata_conv_fwd", "kata_conv_step", "kata_conv_bwd_ws", "kata_qk_norm_fwd",
+                 "kata_qk_norm_bwd_ws", "kata_ssm_fwd_ws", "kata_ssm_bwd_ws", "kata_ssm_step"):
+        getattr(L, name).restype = i
+    for name in ("kata_conv_bwd_workspace_bytes", "kata_qk_norm_bwd_workspace_bytes",
+                 "kata_ssm_workspace_bytes"):
+        getattr(L, name).restype = sz
     L.kata_status_string.argtypes = [i]
     L.kata_status_string.restype = ctypes.c_char_p
     L.kata_abi_version.argtypes = []
@@ -633,3 +668,303 @@ def bwd_chunked_alloc(q, k, v, out, dout, C: int, g: int = 1, stream=None):
                                   _dev(dvv, "dv"), B, H, T, d, dv, C, g, code,
                                   _stream(stream, q.device)), "kata_bwd_chunked")
     return dq, dk, dvv
+
+
+# ---- mixer operators ------------------------------------------------------------
+# Activations are token-major and may be views with any strides over their outer
+# dimensions; parameters and states are contiguous (fp32, a convolution's state in
+# the activations' type).  Outputs are allocated where they are not given.
+
+def _on_stream(call):
+    """A call with stream=s runs as on s: the kernels there, and what torch
+    allocates for them from s's memory.  The device of the first tensor is made the
+    current one meanwhile, if it is not."""
+    @functools.wraps(call)
+    def run(first, *args, stream=None, **kw):
+        import torch
+        if not first.is_cuda:
+            raise ValueError("expected device tensors")
+        if stream is not None:
+            if stream.device != first.device:
+                raise ValueError(f"stream of {stream.device}, tensors of {first.device}")
+            with torch.cuda.stream(stream):
+                return call(first, *args, **kw)
+        if first.device.index != torch.cuda.current_device():
+            with torch.cuda.device(first.device):
+                return call(first, *args, **kw)
+        return call(first, *args, **kw)
+    return run
+
+
+def _tensor(t, name, like, shape, dtype, strided=False):
+    """The address of a tensor of this shape and type on like's device."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if strided:
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}'s innermost dimension must be contiguous")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _optional(t, name, like, shape, dtype, strided=False):
+    return None if t is None else _tensor(t, name, like, shape, dtype, strided)
+
+
+def _workspace(given, nbytes, like):
+    import torch
+    if given is None or given.numel() < nbytes:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=like.device)
+    _tensor(given, "workspace", like, given.shape, torch.uint8)
+    return given
+
+
+def _dims(t, n, what):
+    if t.dim() != n:
+        raise ValueError(f"expected {what}, got {tuple(t.shape)}")
+    return t.shape
+
+
+@_on_stream
+def conv_fwd(x, w, bias=None, act: int = CONV_SILU, state=None, lengths=None, y=None,
+             state_out=None, final_state: bool = False):
+    """Causal depthwise convolution (kata_conv_fwd): x [B,T,D], w [D,W], bias [D]; returns y
+    [B,T,D], or (y, state_out [B,W-1,D]) with final_state or a state_out.  state: the rows
+    before x; lengths: int32 [B]."""
+    import torch
+    B, T, D = _dims(x, 3, "x [B,T,D]")
+    W = _dims(w, 2, "w [D,W]")[1]
+    code, f32 = _dtype_code(x), torch.float32
+    if y is None:
+        y = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
+    if state_out is None and final_state:
+        state_out = torch.empty((B, W - 1, D), dtype=x.dtype, device=x.device)
+    rows = (B, W - 1, D)
+    _check(lib().kata_conv_fwd(
+        _tensor(x, "x", x, (B, T, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
+        _optional(bias, "bias", x, (D,), f32), _optional(state, "state", x, rows, x.dtype),
+        _optional(lengths, "lengths", x, (B,), torch.int32),
+        _tensor(y, "y", x, (B, T, D), x.dtype, True),
+        _optional(state_out, "state_out", x, rows, x.dtype), B, T, D, W, x.stride(0), x.stride(1),
+        y.stride(0), y.stride(1), act, code, _stream(None, x.device)), "kata_conv_fwd")
+    return y if state_out is None else (y, state_out)
+
+
+@_on_stream
+def conv_step(state, x, w, bias=None, act: int = CONV_SILU, y=None):
+    """One token of every sequence (kata_conv_step): x [B,D] -> y [B,D]; state [B,W-1,D] is
+    moved on in place."""
+    import torch
+    B, D = _dims(x, 2, "x [B,D]")
+    W = _dims(w, 2, "w [D,W]")[1]
+    code, f32 = _dtype_code(x), torch.float32
+    if y is None:
+        y = torch.empty((B, D), dtype=x.dtype, device=x.device)
+    _check(lib().kata_conv_step(
+        _tensor(state, "state", x, (B, W - 1, D), x.dtype),
+        _tensor(x, "x", x, (B, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
+        _optional(bias, "bias", x, (D,), f32), _tensor(y, "y", x, (B, D), x.dtype, True), B, D, W,
+        x.stride(0), y.stride(0), act, code, _stream(None, x.device)), "kata_conv_step")
+    return y
+
+
+@_on_stream
+def conv_bwd(x, w, bias, dy, act: int = CONV_SILU, dx=None, workspace=None):
+    """Gradients (dx, dw, dbias) of conv_fwd without state and lengths
+    (kata_conv_bwd_ws); dbias is None where bias is."""
+    import torch
+    B, T, D = _dims(x, 3, "x [B,T,D]")
+    W = _dims(w, 2, "w [D,W]")[1]
+    code, f32 = _dtype_code(x), torch.float32
+    if dx is None:
+        dx = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
+    dw = torch.empty((D, W), dtype=f32, device=x.device)
+    db = None if bias is None else torch.empty((D,), dtype=f32, device=x.device)
+    nbytes = int(lib().kata_conv_bwd_workspace_bytes(B, T, D, W, code))
+    workspace = _workspace(workspace, nbytes, x)
+    _check(lib().kata_conv_bwd_ws(
+        _tensor(x, "x", x, (B, T, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
+        _optional(bias, "bias", x, (D,), f32), _tensor(dy, "dy", x, (B, T, D), x.dtype, True),
+        _tensor(dx, "dx", x, (B, T, D), x.dtype, True), dw.data_ptr(),
+        None if db is None else db.data_ptr(), B, T, D, W, x.stride(0), x.stride(1), dy.stride(0),
+        dy.stride(1), dx.stride(0), dx.stride(1), act, code, workspace.data_ptr(),
+        workspace.numel(), _stream(None, x.device)), "kata_conv_bwd_ws")
+    return dx, dw, db
+
+
+def rope_frequencies(r: int, base: float = 10000.0, device="cuda"):
+    """The fp64 frequencies base^(-2i/r), i < r/2, of a rotation of r coordinates."""
+    import torch
+    i = torch.arange(r // 2, dtype=torch.float64, device=device)
+    return base ** (-2.0 * i / max(r, 1))
+
+
+def _norm_sides(q, k, freq):
+    B, T, Hq, d = _dims(q, 4, "q [B,T,Hq,d]")
+    Hk = 0
+    if k is not None:
+        Hk = _dims(k, 4, "k [B,T,Hk,d]")[2]
+    return B, T, Hq, Hk, d, 0 if freq is None else 2 * freq.shape[0]
+
+
+def _strides3(t):
+    return (0, 0, 0) if t is None else t.stride()[:3]
+
+
+@_on_stream
+def qk_norm_fwd(q, k=None, wq=None, wk=None, freq=None, pos=None, norm: int = NORM_RMS,
+                eps: float = 1e-6, pairs: bool = False, yq=None, yk=None):
+    """Norms of query and key heads with the position rotation (kata_qk_norm_fwd): q
+    [B,T,Hq,d], k [B,T,Hk,d] (or None), weights [d], freq fp64 [r/2], pos int32 [B,T]
+    (default 0..T-1); returns (yq [B,Hq,T,d], yk [B,Hk,T,d] or None)."""
+    import torch
+    B, T, Hq, Hk, d, r = _norm_sides(q, k, freq)
+    code, f32 = _dtype_code(q), torch.float32
+    if yq is None:
+        yq = torch.empty((B, Hq, T, d), dtype=q.dtype, device=q.device)
+    if yk is None and k is not None:
+        yk = torch.empty((B, Hk, T, d), dtype=q.dtype, device=q.device)
+    _check(lib().kata_qk_norm_fwd(
+        _tensor(q, "q", q, (B, T, Hq, d), q.dtype, True),
+        _optional(k, "k", q, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", q, (d,), f32),
+        _optional(wk, "wk", q, (d,), f32), _optional(pos, "pos", q, (B, T), torch.int32),
+        _optional(freq if r else None, "freq", q, (r // 2,), torch.float64),
+        _tensor(yq, "yq", q, (B, Hq, T, d), q.dtype),
+        _optional(yk, "yk", q, (B, Hk, T, d), q.dtype), B, T, Hq, Hk, d, r, *_strides3(q),
+        *_strides3(k), norm, eps, int(pairs), code, _stream(None, q.device)), "kata_qk_norm_fwd")
+    return yq, yk
+
+
+@_on_stream
+def qk_norm_bwd(q, k=None, wq=None, wk=None, freq=None, dq=None, dk=None, pos=None,
+                norm: int = NORM_RMS, eps: float = 1e-6, pairs: bool = False, dxq=None, dxk=None,
+                workspace=None):
+    """Gradients (dxq, dxk, dwq, dwk) of qk_norm_fwd from dq [B,Hq,T,d] and dk [B,Hk,T,d] (fp32
+    or q's type), via kata_qk_norm_bwd_ws; None where the input is."""
+    import torch
+    B, T, Hq, Hk, d, r = _norm_sides(q, k, freq)
+    code, f32 = _dtype_code(q), torch.float32
+    if dxq is None:
+        dxq = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
+    if dxk is None and k is not None:
+        dxk = torch.empty((B, T, Hk, d), dtype=q.dtype, device=q.device)
+    dwq = None if wq is None else torch.empty((d,), dtype=f32, device=q.device)
+    dwk = None if wk is None else torch.empty((d,), dtype=f32, device=q.device)
+    nbytes = int(lib().kata_qk_norm_bwd_workspace_bytes(B, T, Hq, Hk, d, code))
+    workspace = _workspace(workspace, nbytes, q)
+    _check(lib().kata_qk_norm_bwd_ws(
+        _tensor(q, "q", q, (B, T, Hq, d), q.dtype, True),
+        _optional(k, "k", q, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", q, (d,), f32),
+        _optional(wk, "wk", q, (d,), f32), _optional(pos, "pos", q, (B, T), torch.int32),
+        _optional(freq if r else None, "freq", q, (r // 2,), torch.float64),
+        _tensor(dq, "dq", q, (B, Hq, T, d), dq.dtype),
+        _optional(dk, "dk", q, (B, Hk, T, d), dq.dtype),
+        _tensor(dxq, "dxq", q, (B, T, Hq, d), q.dtype, True),
+        _optional(dxk, "dxk", q, (B, T, Hk, d), q.dtype, True),
+        None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(), B, T, Hq,
+        Hk, d, r, *_strides3(q), *_strides3(k), *_strides3(dxq), *_strides3(dxk), norm, eps,
+        int(pairs), code, _dtype_code(dq), workspace.data_ptr(), workspace.numel(),
+        _stream(None, q.device)), "kata_qk_norm_bwd_ws")
+    return dxq, dxk, dwq, dwk
+
+
+_SsmStrides = ctypes.c_longlong * 15  # kata_ssm_strides_t
+
+
+def _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, tokens):
+    """Sizes, and the addresses of the inputs in the order of the entry points; tokens: whether
+    the activations have a token dimension."""
+    import torch
+    n = 4 if tokens else 3
+    lead, (H, P) = x.shape[:-2], _dims(x, n, "x [B,T,H,P]" if tokens else "x [B,H,P]")[-2:]
+    G, N = _dims(Bm, n, "Bm [B,T,G,N]" if tokens else "Bm [B,G,N]")[-2:]
+    f32 = torch.float32
+    if dt.dim() != n - 1:
+        raise ValueError(f"dt must be {tuple(lead) + (H,)}, got {tuple(dt.shape)}")
+    args = (_tensor(x, "x", x, x.shape, x.dtype, True),
+            _tensor(dt.unsqueeze(-1), "dt", x, (*lead, H, 1), x.dtype, True),
+            _tensor(A, "A", x, (H,), f32), _tensor(Bm, "Bm", x, (*lead, G, N), x.dtype, True),
+            _tensor(Cm, "Cm", x, (*lead, G, N), x.dtype, True), _optional(D, "D", x, (H,), f32),
+            _optional(dt_bias, "dt_bias", x, (H,), f32))
+    return lead[0], lead[1] if tokens else 1, H, G, N, P, args
+
+
+def _ssm_strides(x, dt, Bm, Cm, y):
+    if x.dim() == 3:  # one token
+        s = (x.stride(0), 0, x.stride(1), dt.stride(0), 0, dt.stride(1), Bm.stride(0), 0,
+             Bm.stride(1), Cm.stride(0), 0, Cm.stride(1), y.stride(0), 0, y.stride(1))
+    else:
+        s = x.stride()[:3] + dt.stride() + Bm.stride()[:3] + Cm.stride()[:3] + y.stride()[:3]
+    return _SsmStrides(*s)
+
+
+def ssm_workspace_bytes(B, T, H, G, N, P, dtype_code, backward=False) -> int:
+    return int(lib().kata_ssm_workspace_bytes(B, T, H, G, N, P, dtype_code, int(backward)))
+
+
+@_on_stream
+def ssm_fwd(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus: bool = True, state=None,
+            lengths=None, y=None, state_out=None, final_state: bool = False, workspace=None):
+    """Selective scan (kata_ssm_fwd_ws): x [B,T,H,P], dt [B,T,H], A [H], Bm and Cm [B,T,G,N], D
+    and dt_bias [H]; returns y [B,T,H,P], or (y, state_out [B,H,N,P] fp32) with final_state
+    or a state_out.  state: the one before the first token; lengths: int32 [B]."""
+    import torch
+    B, T, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, True)
+    code, f32 = _dtype_code(x), torch.float32
+    if y is None:
+        y = torch.empty((B, T, H, P), dtype=x.dtype, device=x.device)
+    if state_out is None and final_state:
+        state_out = torch.empty((B, H, N, P), dtype=f32, device=x.device)
+    workspace = _workspace(workspace, ssm_workspace_bytes(B, T, H, G, N, P, code), x)
+    _check(lib().kata_ssm_fwd_ws(
+        *args, _optional(state, "state", x, (B, H, N, P), f32),
+        _optional(lengths, "lengths", x, (B,), torch.int32),
+        _tensor(y, "y", x, (B, T, H, P), x.dtype, True),
+        _optional(state_out, "state_out", x, (B, H, N, P), f32), B, T, H, G, N, P,
+        _ssm_strides(x, dt, Bm, Cm, y), int(softplus), code, workspace.data_ptr(),
+        workspace.numel(), _stream(None, x.device)), "kata_ssm_fwd_ws")
+    return y if state_out is None else (y, state_out)
+
+
+@_on_stream
+def ssm_step(S, x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus: bool = True, y=None):
+    """One token of every sequence (kata_ssm_step): x [B,H,P], dt [B,H], Bm and Cm [B,G,N] -> y
+    [B,H,P]; S [B,H,N,P] fp32 is updated in place."""
+    import torch
+    B, _, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, False)
+    code = _dtype_code(x)
+    if y is None:
+        y = torch.empty((B, H, P), dtype=x.dtype, device=x.device)
+    _check(lib().kata_ssm_step(
+        _tensor(S, "S", x, (B, H, N, P), torch.float32), *args,
+        _tensor(y, "y", x, (B, H, P), x.dtype, True), B, H, G, N, P,
+        _ssm_strides(x, dt, Bm, Cm, y), int(softplus), code, _stream(None, x.device)),
+        "kata_ssm_step")
+    return y
+
+
+@_on_stream
+def ssm_bwd(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus: bool = True, workspace=None):
+    """Gradients (dx, ddt, dA, dBm, dCm, dD, dt_dbias) of ssm_fwd from a zero state without
+    lengths (kata_ssm_bwd_ws); None where D or dt_bias is."""
+    import torch
+    B, T, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, True)
+    code, f32 = _dtype_code(x), torch.float32
+    dx, ddt = (torch.empty(s, dtype=x.dtype, device=x.device) for s in ((B, T, H, P), (B, T, H)))
+    dB, dC = (torch.empty((B, T, G, N), dtype=x.dtype, device=x.device) for _ in range(2))
+    dA = torch.empty((H,), dtype=f32, device=x.device)
+    dD = None if D is None else torch.empty((H,), dtype=f32, device=x.device)
+    db = None if dt_bias is None else torch.empty((H,), dtype=f32, device=x.device)
+    workspace = _workspace(workspace, ssm_workspace_bytes(B, T, H, G, N, P, code, True), x)
+    _check(lib().kata_ssm_bwd_ws(
+        *args, _tensor(dy, "dy", x, (B, T, H, P), x.dtype, True), dx.data_ptr(), ddt.data_ptr(),
+        dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), None if dD is None else dD.data_ptr(),
+        None if db is None else db.data_ptr(), B, T, H, G, N, P,
+        _ssm_strides(x, dt, Bm, Cm, dy), int(softplus), code, workspace.data_ptr(),
+        workspace.numel(), _stream(None, x.device)), "kata_ssm_bwd_ws")
+    return dx, ddt, dA, dB, dC, dD, db

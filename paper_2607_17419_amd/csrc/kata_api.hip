@@ -790,3 +790,5 @@ kata_status_t kata_bwd_chunked(const void* q, const void* k, const void* v, cons
 }
 
 }  // extern "C"
+
+#include "kata_mixer_api.hpp"

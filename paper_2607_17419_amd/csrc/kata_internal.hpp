@@ -135,6 +135,63 @@ hipError_t launch_bwd(const void* q, const void* k, const void* v, const float* 
                       int BH, int T, int d, int dv, int C, int g, void* ws, hipStream_t st,
                       hipEvent_t* ev);
 
+// ---- mixer operators (kata_conv.hpp, kata_qknorm.hpp, kata_ssm.hpp) ------------
+// Strides are in elements; a tensor's innermost dimension is contiguous.
+struct ConvShape {
+  int B, T, D, silu;
+  long long xb, xt, yb, yt, gb, gt;  // strides of x, y (forward) or dx (backward), and dy
+};
+hipError_t launch_conv_fwd(const void* x, const float* w, const float* bias, const void* state,
+                           const int* lengths, void* y, void* state_out, const ConvShape& s, int W,
+                           bool bf16, hipStream_t st);
+hipError_t launch_conv_step(void* state, const void* x, const float* w, const float* bias, void* y,
+                            const ConvShape& s, int W, bool bf16, hipStream_t st);
+size_t conv_bwd_workspace_bytes(int B, int T, int D, int W);
+hipError_t launch_conv_bwd(const void* x, const float* w, const float* bias, const void* dy,
+                           void* dx, float* dw, float* db, void* ws, const ConvShape& s, int W,
+                           bool bf16, hipStream_t st);
+
+constexpr int kNormNone = 0, kNormRms = 1, kNormL2 = 2;  // kata_norm_t
+struct NormSide {  // queries or keys
+  long long xb, xt, xh;  // strides of x (of dx in the backward)
+  int H;
+};
+struct NormArgs {
+  NormSide side[2];
+  int B, T, d, r, norm, pairs;  // norm: kNormNone, kNormRms, kNormL2
+  float eps;
+  int split;  // heads (queries then keys) of one workgroup
+};
+hipError_t launch_qk_norm_fwd(const void* q, const void* k, const float* wq, const float* wk,
+                              const int* pos, const double* freq, void* yq, void* yk,
+                              const NormArgs& n, bool bf16, hipStream_t st);
+size_t norm_bwd_workspace_bytes(int B, int T, int d);
+hipError_t launch_qk_norm_bwd(const void* q, const void* k, const float* wq, const float* wk,
+                              const int* pos, const double* freq, const void* dyq, const void* dyk,
+                              void* dxq, void* dxk, float* dwq, float* dwk, void* ws,
+                              const NormArgs& n, const NormSide& dq, const NormSide& dk, bool bf16,
+                              bool dy_bf16, hipStream_t st);
+
+struct SsmArgs {
+  const void *x, *dt, *Bm, *Cm, *dy;
+  const float *A, *D, *bias, *S_in;
+  const int* lengths;
+  void* y;       // forward: y
+  float* S_out;  // nullable
+  int B, T, H, G, N, P, softplus;
+  long long xb, xt, xh, db, dt_t, dh, bb, bt, bg, cb, ct, cg, yb, yt, yh;
+  int vec_x, vec_b, vec_c;  // rows are made of aligned 16-byte pieces
+  int spans, span_chunks;   // a head's chunks are split into spans
+  float* rec;               // [BH][spans - 1][N][P]: states between spans
+  double* rec_log;          // [BH][spans - 1]: log2 of a span's decay
+};
+size_t ssm_workspace_bytes(int B, int T, int H, int G, int N, int P, bool bf16, bool backward);
+int ssm_chunk_of(bool bf16);
+hipError_t launch_ssm_fwd(SsmArgs a, void* ws, bool bf16, hipStream_t st);
+hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, void* dCm,
+                          float* dD, float* dbias, void* ws, bool bf16, hipStream_t st);
+hipError_t launch_ssm_step(float* S, const SsmArgs& a, bool bf16, hipStream_t st);
+
 inline hipError_t record(hipEvent_t* ev, int i, hipStream_t st) {
   return ev ? hipEventRecord(ev[i], st) : hipSuccess;
 }

@@ -1,0 +1,119 @@
+// kata_rows.hpp -- what the mixer operators (kata_conv.hpp, kata_qknorm.hpp,
+// kata_ssm.hpp) share: short vectors of elements as fp32, and the sum of
+// per-workgroup partial sums.
+#pragma once
+
+#include "kata_internal.hpp"
+
+namespace kata {
+
+// V consecutive elements as fp32; the address is aligned to V elements.
+template <int V>
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(p + i);
+      v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = p[i];
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void load_vec(const bf16_t* p, float (&v)[V]) {
+  if constexpr (V == 8) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = bf16lo_f32(w[i]), v[2 * i + 1] = bf16hi_f32(w[i]);
+  } else if constexpr (V == 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    v[0] = bf16lo_f32(u.x), v[1] = bf16hi_f32(u.x), v[2] = bf16lo_f32(u.y), v[3] = bf16hi_f32(u.y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = to_f32(p[i]);
+  }
+}
+
+__device__ __forceinline__ void store_f32(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_f32(bf16_t* p, float x) {
+  p->bits = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+}
+
+// The same elements back, each rounded once to its type.
+template <int V>
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4)
+      *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = v[i];
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void store_vec(bf16_t* p, const float (&v)[V]) {
+  if constexpr (V == 8) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                   pack_bf16x2(v[6], v[7]));
+  } else if constexpr (V == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) store_f32(p + i, v[i]);
+  }
+}
+
+// Logistic function: v_rcp_f32 is within 1 ulp, and 1 + e^-x of +inf gives 0.
+__device__ __forceinline__ float sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.f + expf(-x));
+}
+
+// Sums of per-workgroup partial sums: part[n][cols] fp32 is summed over n in
+// fp64 in a fixed order, so that results do not depend on the order in which
+// workgroups ran; column c goes to out[0], out[1] or out[2] with their widths
+// one after the other (a null one is dropped).
+struct SumOutputs {
+  float* out[3];
+  int width[3];
+};
+constexpr int kSumCols = 16, kSumRows = 16;  // a workgroup: 16 columns, 16 shares of n each
+
+__global__ __launch_bounds__(kSumCols* kSumRows) void sum_partials(const float* part, int n,
+                                                                   int cols, SumOutputs o) {
+  __shared__ double s[kSumRows][kSumCols];
+  const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
+  int c = blockIdx.x * kSumCols + x;
+  double acc = 0.0;
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = y; i < n; i += kSumRows) acc += part[static_cast<size_t>(i) * cols + c];
+  }
+  s[y][x] = acc;
+  __syncthreads();
+  if (y != 0 || c >= cols) return;
+#pragma unroll
+  for (int i = 1; i < kSumRows; ++i) acc += s[i][x];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (c < o.width[k]) {
+      if (o.out[k]) o.out[k][c] = static_cast<float>(acc);
+      return;
+    }
+    c -= o.width[k];
+  }
+}
+
+inline hipError_t launch_sum_partials(const float* part, int n, int cols, const SumOutputs& o,
+                                      hipStream_t st) {
+  sum_partials<<<(cols + kSumCols - 1) / kSumCols, kSumCols * kSumRows, 0, st>>>(part, n, cols, o);
+  return hipGetLastError();
+}
+
+}  // namespace kata

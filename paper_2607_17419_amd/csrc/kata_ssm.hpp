@@ -1,0 +1,1043 @@
+// kata_ssm.hpp -- the selective state space scan: per head a state S [N][P] with
+// a scalar decay and a step that depend on the token,
+//
+//   step_t = softplus(dt_t + bias),  S_t = exp(step_t A) S_{t-1} + step_t B_t x_t^T,
+//   y_t = C_t^T S_t + D x_t,
+//
+// B and C being shared by the H / G heads of a group.  In a chunk of L tokens,
+// with l_t the sum of step A over its tokens up to t, S the state before it and
+// R the gradient of the state after it,
+//
+//   W_ts  = (C_t . B_s) exp(l_t - l_s) step_s      (s <= t, else 0)
+//   y_t   = sum_s W_ts x_s + exp(l_t) C_t^T S + D x_t
+//   S'    = exp(l_L) S + sum_s exp(l_L - l_s) step_s B_s x_s^T
+//   R'    = exp(l_L) R + sum_t exp(l_t) C_t dy_t^T
+//   M_ts  = dy_t . x_s
+//   dx_s  = sum_t W_ts dy_t + exp(l_L - l_s) step_s R^T B_s + D dy_s
+//   dC_t  = sum_s M_ts exp(l_t - l_s) step_s B_s + exp(l_t) S dy_t
+//   dB_s  = sum_t M_ts exp(l_t - l_s) step_s C_t + exp(l_L - l_s) step_s R x_s
+//
+// and, for the gradient e_t of log a_t = step_t A, the sum of W_rs M_rs over
+// s < t <= r and of the state terms whose path crosses token t.  All products
+// are 16 x 16 tiles on the matrix cores: bf16 tensors on the bf16 ones with fp32
+// accumulation, fp32 tensors on the fp32 ones.
+#pragma once
+
+#include "kata_rows.hpp"
+
+namespace kata {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---- tiles --------------------------------------------------------------------
+// Operands travel as "halves": four consecutive k of one row, lane (c, g) =
+// (lane % 16, lane / 16) holding row c, k = 4 g .. 4 g + 3 of a K of 16.  A tile of
+// products D[m][n] comes back with lane (c, g) holding column n = c, rows
+// m = 4 g .. 4 g + 3: rounded, it is again a half, of row n with k = m, so that
+// states and weights pass from one product into the next without moving.
+template <typename E> struct SsmHalf;
+template <> struct SsmHalf<bf16_t> { typedef uint2 type; };
+template <> struct SsmHalf<float> { typedef float4 type; };
+template <typename E> using ssm_half = typename SsmHalf<E>::type;
+
+__device__ __forceinline__ f32x4 mac2(uint2 a0, uint2 a1, uint2 b0, uint2 b1, f32x4 acc) {
+  const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y));
+  const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(b0.x, b0.y, b1.x, b1.y));
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mac2(float4 a0, float4 a1, float4 b0, float4 b1, f32x4 acc) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.x, b0.x, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.y, b0.y, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.z, b0.z, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.w, b0.w, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.x, b1.x, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.y, b1.y, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.z, b1.z, acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a1.w, b1.w, acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x4 half_f32(uint2 h) {
+  return f32x4{bf16lo_f32(h.x), bf16hi_f32(h.x), bf16lo_f32(h.y), bf16hi_f32(h.y)};
+}
+__device__ __forceinline__ f32x4 half_f32(float4 h) { return f32x4{h.x, h.y, h.z, h.w}; }
+
+template <typename E>
+__device__ __forceinline__ ssm_half<E> to_half(f32x4 v) {
+  if constexpr (sizeof(E) == 2) return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else return make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// fp32 values as operands without loss of their leading 16 bits: bf16 as a sum of
+// two (within 2^-18), fp32 as they are.
+template <typename E>
+struct SsmSplit {
+  ssm_half<E> hi, lo;
+  __device__ __forceinline__ explicit SsmSplit(f32x4 v) {
+    hi = to_half<E>(v);
+    if constexpr (sizeof(E) == 2) lo = to_half<E>(v - half_f32(hi));
+  }
+};
+
+// Half of row r0 + c of a tile, k = k0 + 4 g ...
+template <typename E>
+__device__ __forceinline__ ssm_half<E> row_half(const E* tile, int stride, int r0, int k0) {
+  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  return *reinterpret_cast<const ssm_half<E>*>(tile + (r0 + c) * stride + k0 + 4 * g);
+}
+
+// Half of column c0 + c, k running over rows k0 + 4 g ...  bf16: one transposing
+// read (lane j of 16 receives in slot s element j % 4 of the 8-byte piece that
+// lane 4 s + j / 4 addresses).
+__device__ __forceinline__ uint2 col_half(const bf16_t* tile, int stride, int c0, int k0) {
+  typedef short i16x4 __attribute__((ext_vector_type(4)));
+  const int j = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  const bf16_t* p = tile + (k0 + 4 * g + (j >> 2)) * stride + c0 + 4 * (j & 3);
+  const i16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) i16x4*)(const_cast<bf16_t*>(p)));
+  return __builtin_bit_cast(uint2, r);
+}
+__device__ __forceinline__ float4 col_half(const float* tile, int stride, int c0, int k0) {
+  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  const float* p = tile + (k0 + 4 * g) * stride + c0 + c;
+  return make_float4(p[0], p[stride], p[2 * stride], p[3 * stride]);
+}
+
+// Rows of a tile are padded by 16 bytes: the 16 rows of a half then start 4 banks
+// apart, and every read of halves takes each bank the same number of times.
+template <typename E>
+constexpr int ssm_pad(int cols) { return cols + 16 / static_cast<int>(sizeof(E)); }
+
+constexpr int kSsmP = 64;  // columns of the state that a workgroup holds
+// Tokens of a chunk: the in-chunk products grow with it, the states' traffic in
+// the backward shrinks; fp32 tiles take twice the LDS.
+template <typename E> constexpr int ssm_chunk() { return sizeof(E) == 2 ? 64 : 32; }
+
+// Rows r < valid_rows, columns < cols of a token-major tensor into a tile, zeros
+// beyond them (rows past a sequence's end are never read).
+template <typename E, int COLS>
+__device__ __forceinline__ void stage_rows(E* dst, const E* src, long long row_stride, int rows,
+                                           int valid_rows, int cols, bool vec) {
+  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = COLS / V;
+  for (int i = threadIdx.x; i < rows * PER; i += 256) {
+    const int r = i / PER, c = (i % PER) * V;
+    union { uint4 u; E e[V]; } v;
+    v.u = make_uint4(0, 0, 0, 0);
+    if (r < valid_rows && c < cols) {
+      const E* p = src + r * row_stride + c;
+      if (vec && c + V <= cols) {
+        v.u = *reinterpret_cast<const uint4*>(p);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (c + j < cols) v.e[j] = p[j];
+      }
+    }
+    *reinterpret_cast<uint4*>(dst + r * ssm_pad<E>(COLS) + c) = v.u;
+  }
+}
+
+// ---- steps and decays of a chunk -------------------------------------------------
+
+struct SsmChunkLog {  // LDS; l in units of log 2, as hi + lo
+  float hi[64], lo[64], step[64], gate[64];
+};
+
+// One wave (lane = token): step, its derivative by dt (gate), and the running sum l of
+// step A, summed in fp64: differences of l over a chunk keep 2^-48 of the largest,
+// and exp(l_t - l_s) is right where a strong decay stands before weak ones.
+template <typename E, int L>
+__device__ __forceinline__ void ssm_logs(const SsmArgs& a, SsmChunkLog& o, int b, int h, int t0,
+                                         int len) {
+  const int lane = threadIdx.x & 63, t = t0 + lane;
+  float step = 0.f, gate = 0.f;
+  if (lane < L && t < len) {
+    const E* dt = static_cast<const E*>(a.dt) + b * a.db + h * a.dh + t * a.dt_t;
+    const float z = to_f32(*dt) + (a.bias ? a.bias[h] : 0.f);
+    step = z, gate = 1.f;
+    if (a.softplus) {
+      step = z > 20.f ? z : log1pf(expf(z));
+      gate = sigmoid(z);
+    }
+  }
+  double l = static_cast<double>(step) * (static_cast<double>(a.A[h]) * 1.4426950408889634074);
+  // 2^-2000 and 2^2000 are 0 and inf in fp32: bounded, sums and their differences stay finite
+  l = l < -2000.0 ? -2000.0 : (l > 2000.0 ? 2000.0 : l);  // (NaN stays)
+  if (!(lane < L && t < len)) l = 0.0;
+#pragma unroll
+  for (int o2 = 1; o2 < 64; o2 <<= 1) {
+    const double up = __shfl_up(l, o2);
+    if (lane >= o2) l += up;
+  }
+  if (lane < L) {
+    const float hi = static_cast<float>(l);
+    o.hi[lane] = hi;
+    o.lo[lane] = isfinite(hi) ? static_cast<float>(l - hi) : 0.f;
+    o.step[lane] = step;
+    o.gate[lane] = gate;
+  }
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// exp(l_t - l_s)
+__device__ __forceinline__ float ssm_decay(const SsmChunkLog& g, int t, int s) {
+  return exp2_fast((g.hi[t] - g.hi[s]) + (g.lo[t] - g.lo[s]));
+}
+__device__ __forceinline__ float ssm_since(const SsmChunkLog& g, int t) {
+  return exp2_fast(g.hi[t] + g.lo[t]);
+}
+
+// A chunk's lower-triangular 16 x 16 tiles (row tile tt >= column tile ss), numbered.
+__device__ __forceinline__ void ssm_tri(int id, int& tt, int& ss) {
+  tt = 0;
+  while (id > tt) id -= ++tt;
+  ss = id;
+}
+
+// ---- forward -------------------------------------------------------------------
+// A workgroup carries the state of one head (64 of its columns) over the chunks of
+// a span, as accumulators: wave w holds columns 16 w ...  Per chunk, the waves share
+// the tiles of W through LDS, then each forms its columns of y and of the new state.
+template <typename E, int NP>
+struct __attribute__((aligned(16))) SsmOutLds {
+  static constexpr int L = ssm_chunk<E>();
+  E c[L * ssm_pad<E>(NP)], b[L * ssm_pad<E>(NP)], x[L * ssm_pad<E>(kSsmP)],
+      w[L * ssm_pad<E>(L)];
+  SsmChunkLog log;
+};
+
+// The state's columns of this wave as accumulator tiles, from or to [N][P] fp32.
+template <int NP>
+__device__ __forceinline__ void ssm_load_state(const float* S, int N, int P, int p,
+                                               f32x4 (&h)[NP / 16]) {
+  const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int j = 0; j < NP / 16; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = 16 * j + 4 * g + i;
+      h[j][i] = (S && n < N && p < P) ? S[static_cast<size_t>(n) * P + p] : 0.f;
+    }
+}
+template <int NP>
+__device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
+                                                const f32x4 (&h)[NP / 16]) {
+  const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int j = 0; j < NP / 16; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = 16 * j + 4 * g + i;
+      if (n < N && p < P) S[static_cast<size_t>(n) * P + p] = h[j][i];
+    }
+}
+
+// h <- exp(l_L) h + sum_s B_s (scale_s v_s)^T over the chunk's tokens; keys and v are
+// LDS tiles, f the scale of token s.  bf16: the scaled values enter as hi + lo, so
+// that the fp32 state keeps 2^-18 of every term.
+template <typename E, int NP, int L, typename F>
+__device__ __forceinline__ void ssm_state_update(const E* keys, const E* v, int p0, float decay,
+                                                 F f, f32x4 (&h)[NP / 16]) {
+  const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
+#pragma unroll
+  for (int s0 = 0; s0 < L; s0 += 32) {
+    f32x4 v0 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0));
+    f32x4 v1 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0 + 16));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v0[i] *= f(s0 + 4 * g + i);
+      v1[i] *= f(s0 + 16 + 4 * g + i);
+    }
+    const SsmSplit<E> a(v0), b(v1);
+#pragma unroll
+    for (int j = 0; j < NP / 16; ++j) {
+      const auto k0 = col_half(keys, ssm_pad<E>(NP), 16 * j, s0);
+      const auto k1 = col_half(keys, ssm_pad<E>(NP), 16 * j, s0 + 16);
+      h[j] = mac2(k0, k1, a.hi, b.hi, h[j]);
+      if constexpr (sizeof(E) == 2) h[j] = mac2(k0, k1, a.lo, b.lo, h[j]);
+    }
+  }
+}
+
+// Workgroup -> batch, span, block of columns, head; heads of one batch and span run
+// next to each other, so that their group's B and C rows are read once from HBM.
+struct SsmPlace {
+  int b, span, pb, h;
+  __device__ __forceinline__ SsmPlace(const SsmArgs& a, int spans) {
+    const int blocks = (a.P + kSsmP - 1) / kSsmP;
+    unsigned id = blockIdx.x;
+    h = id % a.H, id /= a.H;
+    pb = id % blocks, id /= blocks;
+    span = id % spans;
+    b = id / spans;
+  }
+};
+
+template <typename E, int NP>
+__global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
+  constexpr int L = ssm_chunk<E>();
+  constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
+  __shared__ SsmOutLds<E, NP> m;
+  const SsmPlace at(a, a.spans);
+  const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
+  const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
+  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int span_len = a.span_chunks * L;
+  const int first = at.span * span_len, last = min(first + span_len, len);
+  const float D = a.D ? a.D[h] : 0.f;
+  const size_t NPs = static_cast<size_t>(a.N) * a.P;
+  f32x4 st[NP / 16];
+  const float* from = at.span ? a.rec + (static_cast<size_t>(bh) * (a.spans - 1) + at.span - 1) * NPs
+                              : (a.S_in ? a.S_in + bh * NPs : nullptr);
+  ssm_load_state<NP>(from, a.N, a.P, p, st);
+  const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc;
+  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
+  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
+  E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + p;
+  for (int i = threadIdx.x; i < L * SL; i += 256) store_f32(m.w + i, 0.f);
+  for (int t0 = first; t0 < last; t0 += L) {
+    const int rows = min(L, last - t0);
+    __syncthreads();
+    stage_rows<E, NP>(m.c, Cm + t0 * a.ct, a.ct, L, rows, a.N, a.vec_c);
+    stage_rows<E, NP>(m.b, Bm + t0 * a.bt, a.bt, L, rows, a.N, a.vec_b);
+    stage_rows<E, kSsmP>(m.x, x + t0 * a.xt, a.xt, L, rows, a.P - pc, a.vec_x);
+    if (wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, last);
+    __syncthreads();
+    // W, tile by tile: rows s, columns t of the accumulator are row t of the operand
+    for (int id = wave; id < (L / 16) * (L / 16 + 1) / 2; id += 4) {
+      int tt, ss;
+      ssm_tri(id, tt, ss);
+      f32x4 acc = {};
+#pragma unroll
+      for (int k = 0; k < NP; k += 32)
+        acc = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
+                   row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), acc);
+      const int t = 16 * tt + c;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 16 * ss + 4 * g + i;
+        acc[i] = s <= t ? acc[i] * ssm_decay(m.log, t, s) * m.log.step[s] : 0.f;
+      }
+      *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + 16 * ss + 4 * g) = to_half<E>(acc);
+    }
+    __syncthreads();
+    ssm_half<E> sh[NP / 16], xf[L / 16];
+#pragma unroll
+    for (int j = 0; j < NP / 16; ++j) sh[j] = to_half<E>(st[j]);
+#pragma unroll
+    for (int j = 0; j < L / 16; ++j) xf[j] = col_half(m.x, SP, p0, 16 * j);
+#pragma unroll
+    for (int tt = 0; tt < L / 16; ++tt) {
+      f32x4 acc = {}, in = {};
+#pragma unroll
+      for (int j = 0; j < NP / 16; j += 2)
+        acc = mac2(row_half(m.c, SN, 16 * tt, 16 * j), row_half(m.c, SN, 16 * tt, 16 * j + 16),
+                   sh[j], sh[j + 1], acc);
+#pragma unroll
+      for (int j = 0; j <= tt; j += 2)
+        in = mac2(row_half(m.w, SL, 16 * tt, 16 * j), row_half(m.w, SL, 16 * tt, 16 * j + 16),
+                  xf[j], xf[j + 1], in);
+      // A non-finite x_s times the zero weight of an earlier token is NaN: such sums
+      // are formed again over s <= t alone.
+      if (__any(!(fabsf(in[0]) < INFINITY && fabsf(in[1]) < INFINITY && fabsf(in[2]) < INFINITY &&
+                  fabsf(in[3]) < INFINITY))) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = 16 * tt + 4 * g + i;
+          float sum = 0.f;
+          for (int s = 0; s <= t; ++s)
+            sum = fmaf(to_f32(m.w[t * SL + s]), to_f32(m.x[s * SP + p0 + c]), sum);
+          if (!(fabsf(in[i]) < INFINITY)) in[i] = sum;
+        }
+      }
+      const f32x4 xr = half_f32(xf[tt]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 16 * tt + 4 * g + i;
+        const float out = fmaf(ssm_since(m.log, t), acc[i], fmaf(D, xr[i], in[i]));
+        if (t < rows && p < a.P) store_f32(y + (t0 + t) * a.yt, out);
+      }
+    }
+    ssm_state_update<E, NP, L>(
+        m.b, m.x, p0, ssm_since(m.log, L - 1),
+        [&](int s) { return ssm_decay(m.log, L - 1, s) * m.log.step[s]; }, st);
+  }
+  if (a.S_out && at.span == a.spans - 1)
+    ssm_store_state<NP>(a.S_out + bh * NPs, a.N, a.P, p, st);
+}
+
+// ---- states of spans and chunks --------------------------------------------------
+// REV = false: S over keys B and values x; true: R over keys C and values dy, from a
+// span's last chunk to its first.  CHUNKS = false: a span's own contribution and its
+// decay, to rec; true: from the span's state in rec, every chunk's state before its
+// tokens are added (S at the chunk's start, R at its end), to `chunks`: operand planes
+// (bf16 hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.
+template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1; }
+
+template <typename E, int NP>
+struct __attribute__((aligned(16))) SsmStateLds {
+  static constexpr int L = ssm_chunk<E>();
+  E k[L * ssm_pad<E>(NP)], v[L * ssm_pad<E>(kSsmP)];
+  SsmChunkLog log;
+};
+
+template <typename E, int NP, bool REV, bool CHUNKS>
+__global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
+  constexpr int L = ssm_chunk<E>();
+  __shared__ SsmStateLds<E, NP> m;
+  // without CHUNKS the forward's last and the reverse's first span go nowhere
+  SsmPlace at(a, CHUNKS ? a.spans : a.spans - 1);
+  const int slot = at.span;  // rec's, without CHUNKS
+  if (!CHUNKS && REV) ++at.span;
+  const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
+  const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
+  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int span_len = a.span_chunks * L;
+  const int first = at.span * span_len, last = min(first + span_len, len);
+  const size_t NPs = static_cast<size_t>(a.N) * a.P;
+  const int gaps = a.spans - 1;
+  f32x4 st[NP / 16];
+  const float* from = nullptr;
+  if (CHUNKS && !REV && at.span > 0) from = a.rec + (static_cast<size_t>(bh) * gaps + at.span - 1) * NPs;
+  if (CHUNKS && REV && at.span < gaps) from = a.rec + (static_cast<size_t>(bh) * gaps + at.span) * NPs;
+  ssm_load_state<NP>(from, a.N, a.P, p, st);
+  const E* v = REV ? static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + pc
+                   : static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc;
+  const E* k = REV ? static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg
+                   : static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
+  const long long vt = REV ? a.yt : a.xt, kt = REV ? a.ct : a.bt;
+  const int n = last > first ? (last - first + L - 1) / L : 0;
+  double log_sum = 0.0;
+  for (int i = 0; i < n; ++i) {
+    const int t0 = first + (REV ? n - 1 - i : i) * L, rows = min(L, last - t0);
+    if constexpr (CHUNKS) {
+      const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
+      E* rec = chunks + ((static_cast<size_t>(bh) * blocks + at.pb) * NC + t0 / L) *
+                            (ssm_planes<E>() * kSsmP * NP);
+#pragma unroll
+      for (int j = 0; j < NP / 16; ++j) {
+        const SsmSplit<E> s(st[j]);
+        E* q = rec + (p0 + c) * NP + 16 * j + 4 * g;
+        *reinterpret_cast<ssm_half<E>*>(q) = s.hi;
+        if constexpr (sizeof(E) == 2) *reinterpret_cast<ssm_half<E>*>(q + kSsmP * NP) = s.lo;
+      }
+      if (i == n - 1) break;  // the state past the span's end is the next span's
+    }
+    __syncthreads();
+    stage_rows<E, NP>(m.k, k + t0 * kt, kt, L, rows, a.N, REV ? a.vec_c : a.vec_b);
+    stage_rows<E, kSsmP>(m.v, v + t0 * vt, vt, L, rows, a.P - pc, a.vec_x);
+    if (wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, last);
+    __syncthreads();
+    log_sum += static_cast<double>(m.log.hi[L - 1]) + m.log.lo[L - 1];
+    ssm_state_update<E, NP, L>(
+        m.k, m.v, p0, ssm_since(m.log, L - 1),
+        [&](int s) {
+          return REV ? ssm_since(m.log, s) : ssm_decay(m.log, L - 1, s) * m.log.step[s];
+        },
+        st);
+  }
+  if constexpr (!CHUNKS) {
+    ssm_store_state<NP>(a.rec + (static_cast<size_t>(bh) * gaps + slot) * NPs, a.N, a.P, p, st);
+    if (threadIdx.x == 0 && at.pb == 0) a.rec_log[static_cast<size_t>(bh) * gaps + slot] = log_sum;
+  }
+}
+
+// rec: a span's own contribution becomes the state that enters the next span (REV:
+// the one before), in the same slot.
+template <bool REV>
+__global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
+  const int NPs = a.N * a.P, gaps = a.spans - 1;
+  const int e = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y;
+  if (e >= NPs) return;
+  float s = !REV && a.S_in ? a.S_in[static_cast<size_t>(bh) * NPs + e] : 0.f;
+  float* rec = a.rec + static_cast<size_t>(bh) * gaps * NPs + e;
+  const double* log = a.rec_log + static_cast<size_t>(bh) * gaps;
+#pragma unroll 4
+  for (int i = 0; i < gaps; ++i) {
+    const int j = REV ? gaps - 1 - i : i;
+    float* q = rec + static_cast<size_t>(j) * NPs;
+    s = fmaf(exp2_fast(static_cast<float>(log[j])), s, *q);
+    *q = s;
+  }
+}
+
+// ---- gradients ------------------------------------------------------------------
+// A workgroup takes one chunk of one group and a block of its heads in turn: dB and
+// dC of the group stay in accumulators over the heads (wave w: columns n of tiles
+// w, w + 4), C B^T is formed once.  part: dA, dD, dbias of the chunk, [B * NC][3][H].
+struct SsmGrads {
+  void *dx, *ddt, *dBm, *dCm;
+  float *pB, *pC;  // with several head blocks: their sums, [blocks][B][T][G][N] fp32
+  float* part;
+  const void *fwd, *rev;  // chunk records
+  int head_block, blocks;
+};
+
+template <typename E, int NP>
+struct __attribute__((aligned(16))) SsmGradLds {
+  static constexpr int L = ssm_chunk<E>();
+  E c[L * ssm_pad<E>(NP)], b[L * ssm_pad<E>(NP)];
+  E x[L * ssm_pad<E>(kSsmP)], dy[L * ssm_pad<E>(kSsmP)];
+  E st[ssm_planes<E>() * kSsmP * ssm_pad<E>(NP)];
+  E w[L * ssm_pad<E>(L)], mw[L * ssm_pad<E>(L)];
+  SsmChunkLog log;
+  float row[4][64], col[4][64], diag[64];  // pair sums by tile of the other index
+  float q[4][64], k[4][64];                // state terms by wave
+  float dot[4], dd[4];
+};
+
+// A record's planes into the padded tile.
+template <typename E, int NP>
+__device__ __forceinline__ void ssm_stage_record(E* dst, const E* rec) {
+  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
+  for (int i = threadIdx.x; i < ssm_planes<E>() * kSsmP * PER; i += 256)
+    *reinterpret_cast<uint4*>(dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V) =
+        *reinterpret_cast<const uint4*>(rec + static_cast<size_t>(i) * V);
+}
+
+// The same, adding up the product of the record there (its own pieces) with the new one.
+template <typename E, int NP>
+__device__ __forceinline__ float ssm_swap_record(E* dst, const E* rec) {
+  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
+  constexpr int plane = kSsmP * ssm_pad<E>(NP);
+  float dot = 0.f;
+  for (int i = threadIdx.x; i < kSsmP * PER; i += 256) {
+    E* q = dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V;
+    const E* r = rec + static_cast<size_t>(i) * V;
+    float u[V], w[V];
+    load_vec<V>(q, u);
+    load_vec<V>(r, w);
+    if constexpr (sizeof(E) == 2) {
+      float ul[V], wl[V];
+      load_vec<V>(q + plane, ul);
+      load_vec<V>(r + kSsmP * NP, wl);
+#pragma unroll
+      for (int j = 0; j < V; ++j) dot = fmaf(u[j] + ul[j], w[j] + wl[j], dot);
+      *reinterpret_cast<uint4*>(q + plane) = *reinterpret_cast<const uint4*>(r + kSsmP * NP);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) dot = fmaf(u[j], w[j], dot);
+    }
+    *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(r);
+  }
+  return dot;
+}
+
+__device__ __forceinline__ float sum_lanes(float v, int from, int to) {
+  for (int o = from; o < to; o <<= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+template <typename E, int NP>
+__global__ __launch_bounds__(256) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
+  constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, NTW = (NT + 3) / 4;
+  constexpr int TRI = LT * (LT + 1) / 2, TW = (TRI + 3) / 4;
+  constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
+  constexpr int kRecord = ssm_planes<E>() * kSsmP * NP, kPlane = kSsmP * SN;
+  __shared__ SsmGradLds<E, NP> m;
+  const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
+  unsigned id = blockIdx.x;
+  const int hb = id % o.blocks;
+  id /= o.blocks;
+  const int grp = id % a.G;
+  id /= a.G;
+  const int chunk = id % NC, b = id / NC;
+  const int per = a.H / a.G, t0 = chunk * L, rows = min(L, a.T - t0);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt;
+  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct;
+  stage_rows<E, NP>(m.b, Bm, a.bt, L, rows, a.N, a.vec_b);
+  stage_rows<E, NP>(m.c, Cm, a.ct, L, rows, a.N, a.vec_c);
+  for (int i = threadIdx.x; i < L * SL; i += 256) store_f32(m.w + i, 0.f), store_f32(m.mw + i, 0.f);
+  __syncthreads();
+  f32x4 cb[TW];  // C B^T: rows s, columns t, tiles wave, wave + 4, ...
+  f32x4 dC[NTW][LT] = {}, dB[NTW][LT] = {};
+#pragma unroll
+  for (int j = 0; j < TW; ++j) {
+    cb[j] = f32x4{};
+    if (wave + 4 * j < TRI) {
+      int tt, ss;
+      ssm_tri(wave + 4 * j, tt, ss);
+#pragma unroll
+      for (int k = 0; k < NP; k += 32)
+        cb[j] = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
+                     row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), cb[j]);
+    }
+  }
+  const int h_end = min((hb + 1) * o.head_block, per);
+  for (int hg = hb * o.head_block; hg < h_end; ++hg) {
+    const int h = grp * per + hg, bh = b * a.H + h;
+    const float D = a.D ? a.D[h] : 0.f;
+    f32x4 mm[TW] = {};
+    float qs[LT][4] = {}, ks[LT][4] = {}, dot = 0.f, dd = 0.f;
+    for (int pb = 0; pb < blocks; ++pb) {
+      const int pc = pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
+      const size_t rec = ((static_cast<size_t>(bh) * blocks + pb) * NC + chunk) * kRecord;
+      __syncthreads();
+      stage_rows<E, kSsmP>(m.x, static_cast<const E*>(a.x) + b * a.xb + h * a.xh + t0 * a.xt + pc,
+                           a.xt, L, rows, a.P - pc, a.vec_x);
+      stage_rows<E, kSsmP>(m.dy, static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc,
+                           a.yt, L, rows, a.P - pc, a.vec_x);
+      ssm_stage_record<E, NP>(m.st, static_cast<const E*>(o.fwd) + rec);
+      if (pb == 0 && wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, a.T);
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < TW; ++j) {
+        if (wave + 4 * j >= TRI) continue;
+        int tt, ss;
+        ssm_tri(wave + 4 * j, tt, ss);
+        if (pb == 0) {  // W
+          const int t = 16 * tt + c;
+          f32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int s = 16 * ss + 4 * g + i;
+            w[i] = s <= t ? cb[j][i] * ssm_decay(m.log, t, s) * m.log.step[s] : 0.f;
+          }
+          *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + 16 * ss + 4 * g) = to_half<E>(w);
+        }
+#pragma unroll
+        for (int k = 0; k < kSsmP; k += 32)  // M^T: rows s, columns t
+          mm[j] = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
+                       row_half(m.dy, SP, 16 * tt, k), row_half(m.dy, SP, 16 * tt, k + 16), mm[j]);
+      }
+      // exp(l_t) S dy_t, and its product with C_t
+#pragma unroll
+      for (int j = 0; j < NTW; ++j) {
+        const int n0 = 16 * (wave + 4 * j);
+        if (n0 >= NP) continue;
+#pragma unroll
+        for (int tt = 0; tt < LT; ++tt) {
+          f32x4 acc = {};
+#pragma unroll
+          for (int k = 0; k < kSsmP; k += 32) {
+            const auto a0 = row_half(m.dy, SP, 16 * tt, k), a1 = row_half(m.dy, SP, 16 * tt, k + 16);
+            acc = mac2(a0, a1, col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), acc);
+            if constexpr (sizeof(E) == 2)
+              acc = mac2(a0, a1, col_half(m.st + kPlane, SN, n0, k),
+                         col_half(m.st + kPlane, SN, n0, k + 16), acc);
+          }
+          const f32x4 cr = half_f32(col_half(m.c, SN, n0, 16 * tt));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = ssm_since(m.log, 16 * tt + 4 * g + i) * acc[i];
+            qs[tt][i] = fmaf(cr[i], v, qs[tt][i]);
+            dC[j][tt][i] += v;
+          }
+        }
+      }
+      __syncthreads();
+      dot += ssm_swap_record<E, NP>(m.st, static_cast<const E*>(o.rev) + rec);
+      __syncthreads();
+      // exp(l_L - l_s) step_s R x_s: dB alone reads it, so R's leading bf16 is enough
+#pragma unroll
+      for (int j = 0; j < NTW; ++j) {
+        const int n0 = 16 * (wave + 4 * j);
+        if (n0 >= NP) continue;
+#pragma unroll
+        for (int ss = 0; ss < LT; ++ss) {
+          f32x4 acc = {};
+#pragma unroll
+          for (int k = 0; k < kSsmP; k += 32)
+            acc = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
+                       col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), acc);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int s = 16 * ss + 4 * g + i;
+            dB[j][ss][i] = fmaf(ssm_decay(m.log, L - 1, s) * m.log.step[s], acc[i], dB[j][ss][i]);
+          }
+        }
+      }
+      // dx, this wave's 16 columns
+#pragma unroll
+      for (int ss = 0; ss < LT; ++ss) {
+        f32x4 acc = {};
+#pragma unroll
+        for (int k = 0; k < NP; k += 32) {
+          const auto a0 = row_half(m.b, SN, 16 * ss, k), a1 = row_half(m.b, SN, 16 * ss, k + 16);
+          acc = mac2(a0, a1, row_half(m.st, SN, p0, k), row_half(m.st, SN, p0, k + 16), acc);
+          if constexpr (sizeof(E) == 2)
+            acc = mac2(a0, a1, row_half(m.st + kPlane, SN, p0, k),
+                       row_half(m.st + kPlane, SN, p0, k + 16), acc);
+        }
+        const f32x4 xr = half_f32(col_half(m.x, SP, p0, 16 * ss));
+        const f32x4 yr = half_f32(col_half(m.dy, SP, p0, 16 * ss));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int s = 16 * ss + 4 * g + i;
+          const float v = ssm_decay(m.log, L - 1, s) * acc[i];
+          ks[ss][i] = fmaf(xr[i], v, ks[ss][i]);
+          acc[i] = m.log.step[s] * v;
+          dd = fmaf(xr[i], yr[i], dd);
+        }
+#pragma unroll
+        for (int r = (ss / 2) * 32; r < L; r += 32)
+          acc = mac2(col_half(m.w, SL, 16 * ss, r), col_half(m.w, SL, 16 * ss, r + 16),
+                     col_half(m.dy, SP, p0, r), col_half(m.dy, SP, p0, r + 16), acc);
+        E* dx = static_cast<E*>(o.dx) + ((static_cast<size_t>(b) * a.T + t0) * a.H + h) * a.P + p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int s = 16 * ss + 4 * g + i;
+          if (s < rows && p < a.P)
+            store_f32(dx + static_cast<size_t>(s) * a.H * a.P, fmaf(D, yr[i], acc[i]));
+        }
+      }
+    }
+    // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
+    // over s < t with step_s (row), over t > s (col), s = t
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+      if (wave + 4 * j >= TRI) continue;
+      int tt, ss;
+      ssm_tri(wave + 4 * j, tt, ss);
+      const int t = 16 * tt + c;
+      f32x4 w;
+      float row = 0.f, col[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 16 * ss + 4 * g + i;
+        const float f = s <= t ? mm[j][i] * ssm_decay(m.log, t, s) : 0.f;
+        const float pair = s < t ? f * cb[j][i] : 0.f;
+        w[i] = f * m.log.step[s];
+        row = fmaf(pair, m.log.step[s], row);
+        col[i] = pair;
+        if (s == t) m.diag[s] = f * cb[j][i];
+      }
+      *reinterpret_cast<ssm_half<E>*>(m.mw + t * SL + 16 * ss + 4 * g) = to_half<E>(w);
+      row = sum_lanes(row, 16, 64);
+      if (g == 0) m.row[ss][t] = row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = sum_lanes(col[i], 1, 16);
+        if (c == 0) m.col[tt][16 * ss + 4 * g + i] = v;
+      }
+    }
+#pragma unroll
+    for (int tt = 0; tt < LT; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float q = sum_lanes(qs[tt][i], 1, 16), k = sum_lanes(ks[tt][i], 1, 16);
+        if (c == 0) m.q[wave][16 * tt + 4 * g + i] = q, m.k[wave][16 * tt + 4 * g + i] = k;
+      }
+    dot = sum_lanes(dot, 1, 64), dd = sum_lanes(dd, 1, 64);
+    if (lane == 0) m.dot[wave] = dot, m.dd[wave] = dd;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NTW; ++j) {
+      const int n0 = 16 * (wave + 4 * j);
+      if (n0 >= NP) continue;
+#pragma unroll
+      for (int tt = 0; tt < LT; ++tt) {
+#pragma unroll
+        for (int k = 0; k <= 16 * tt; k += 32)
+          dC[j][tt] = mac2(row_half(m.mw, SL, 16 * tt, k), row_half(m.mw, SL, 16 * tt, k + 16),
+                           col_half(m.b, SN, n0, k), col_half(m.b, SN, n0, k + 16), dC[j][tt]);
+#pragma unroll
+        for (int r = (tt / 2) * 32; r < L; r += 32)
+          dB[j][tt] = mac2(col_half(m.mw, SL, 16 * tt, r), col_half(m.mw, SL, 16 * tt, r + 16),
+                           col_half(m.c, SN, n0, r), col_half(m.c, SN, n0, r + 16), dB[j][tt]);
+      }
+    }
+    if (wave == 0) {
+      // e_t = sum_{u >= t} (q_u + row_u - step_u col_u) + sum_{s < t} step_s k_s + the
+      // state that passes through; in fp64, since the sums over u cancel
+      const int t = min(lane, L - 1);
+      const float step = m.log.step[t];
+      float row = 0.f, col = 0.f;
+#pragma unroll
+      for (int j = 0; j < LT; ++j) {
+        if (16 * j <= t) row += m.row[j][t];
+        if (j >= t / 16) col += m.col[j][t];
+      }
+      const float q = m.q[0][t] + m.q[1][t] + (m.q[2][t] + m.q[3][t]);
+      const float k = m.k[0][t] + m.k[1][t] + (m.k[2][t] + m.k[3][t]);
+      const bool in = lane < rows;
+      double tail = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
+      const double own = in ? static_cast<double>(step) * k : 0.0;
+      double head = own;
+#pragma unroll
+      for (int o2 = 1; o2 < 64; o2 <<= 1) {
+        const double dn = __shfl_down(tail, o2), up = __shfl_up(head, o2);
+        if (lane + o2 < 64) tail += dn;
+        if (lane >= o2) head += up;
+      }
+      const double through = static_cast<double>(ssm_since(m.log, L - 1)) *
+                             (static_cast<double>(m.dot[0]) + m.dot[1] + m.dot[2] + m.dot[3]);
+      const float e = static_cast<float>(tail + (head - own) + through);
+      const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
+      if (in)
+        store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
+                  ddt);
+      const float dA = sum_lanes(in ? e * step : 0.f, 1, 64);
+      const float db = sum_lanes(in ? ddt : 0.f, 1, 64);
+      if (lane == 0) {
+        float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
+        part[0] = dA;
+        part[a.H] = m.dd[0] + m.dd[1] + (m.dd[2] + m.dd[3]);
+        part[2 * a.H] = db;
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NTW; ++j) {
+    const int n = 16 * (wave + 4 * j) + c;
+    if (n >= a.N) continue;
+#pragma unroll
+    for (int tt = 0; tt < LT; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 16 * tt + 4 * g + i;
+        if (t >= rows) continue;
+        const size_t at = ((static_cast<size_t>(b) * a.T + t0 + t) * a.G + grp) * a.N + n;
+        if (o.blocks > 1) {
+          const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
+          o.pB[hb * all + at] = dB[j][tt][i];
+          o.pC[hb * all + at] = dC[j][tt][i];
+        } else {
+          store_f32(static_cast<E*>(o.dBm) + at, dB[j][tt][i]);
+          store_f32(static_cast<E*>(o.dCm) + at, dC[j][tt][i]);
+        }
+      }
+  }
+}
+
+// dB and dC from the sums of the head blocks.
+template <typename E>
+__global__ __launch_bounds__(256) void ssm_join_heads(SsmGrads o, size_t all) {
+  const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= all) return;
+  float b = 0.f, c = 0.f;
+  for (int k = 0; k < o.blocks; ++k) b += o.pB[k * all + i], c += o.pC[k * all + i];
+  store_f32(static_cast<E*>(o.dBm) + i, b);
+  store_f32(static_cast<E*>(o.dCm) + i, c);
+}
+
+// ---- one token --------------------------------------------------------------------
+// One workgroup per head: the state is read and written once (HBM bound), a thread
+// holding V columns of every 256 / (columns / V)-th row; y is joined over the rows
+// in LDS.
+template <typename E, int V>
+__global__ __launch_bounds__(256) void ssm_step_kernel(float* S, SsmArgs a) {
+  __shared__ float red[256 * V];
+  const int b = blockIdx.x / a.H, h = blockIdx.x % a.H, grp = h / (a.H / a.G);
+  const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh;
+  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
+  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
+  const float z = to_f32(*(static_cast<const E*>(a.dt) + b * a.db + h * a.dh)) +
+                  (a.bias ? a.bias[h] : 0.f);
+  const float step = a.softplus ? (z > 20.f ? z : log1pf(expf(z))) : z;
+  const float decay = expf(step * a.A[h]);
+  const int cols = a.P / V, lanes = 256 / cols;  // rows at once; P / V <= 256
+  const int r0 = threadIdx.x / cols, pc = (threadIdx.x % cols) * V;
+  float* s = S + static_cast<size_t>(blockIdx.x) * a.N * a.P + pc;
+  float y[V] = {}, xv[V];
+  if (r0 < lanes) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) xv[i] = to_f32(x[pc + i]) * step;
+#pragma unroll 4
+    for (int n = r0; n < a.N; n += lanes) {
+      float v[V];
+      load_vec<V>(s + static_cast<size_t>(n) * a.P, v);
+      const float bn = to_f32(Bm[n]), cn = to_f32(Cm[n]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        v[i] = fmaf(decay, v[i], bn * xv[i]);
+        y[i] = fmaf(cn, v[i], y[i]);
+      }
+      store_vec<V>(s + static_cast<size_t>(n) * a.P, v);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) red[r0 * a.P + pc + i] = y[i];
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < a.P; p += 256) {
+    float sum = 0.f;
+    for (int r = 0; r < lanes; ++r) sum += red[r * a.P + p];
+    if (a.D) sum = fmaf(a.D[h], to_f32(x[p]), sum);
+    store_f32(static_cast<E*>(a.y) + b * a.yb + h * a.yh + p, sum);
+  }
+}
+
+// ---- launches ---------------------------------------------------------------------
+
+inline int ssm_np(int N) { return N <= 32 ? 32 : (N <= 64 ? 64 : 128); }
+int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chunk<float>(); }
+
+// Spans of a head: one workgroup each, so that the heads of a call with few of them
+// still stand on every CU; a span's own state costs one more pass over x and B, and
+// is not made shorter than four chunks.
+inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
+  const int NC = (T + L - 1) / L;
+  int n = (512 + BHP - 1) / BHP;
+  if (n > NC / 4) n = NC / 4;
+  if (n < 1) n = 1;
+  span_chunks = (NC + n - 1) / n;
+  spans = (NC + span_chunks - 1) / span_chunks;
+}
+
+inline size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+
+struct SsmWorkspace {
+  size_t rec, log, fwd, rev, part, pB, pC, bytes;
+  int spans, span_chunks, head_block, blocks;
+};
+
+inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool bf16,
+                                  bool backward) {
+  SsmWorkspace w = {};
+  const int L = ssm_chunk_of(bf16), NC = (T + L - 1) / L, blocks = (P + kSsmP - 1) / kSsmP;
+  ssm_spans(B * H * blocks, T, L, w.spans, w.span_chunks);
+  size_t at = 0;
+  const auto take = [&at](size_t bytes) {
+    const size_t here = at;
+    at += up256(bytes);
+    return here;
+  };
+  const size_t gaps = static_cast<size_t>(B) * H * (w.spans - 1);
+  w.rec = take(gaps * N * P * sizeof(float));
+  w.log = take(gaps * sizeof(double));
+  w.blocks = 1, w.head_block = H / G;
+  if (backward) {
+    const size_t rec = static_cast<size_t>(kSsmP) * ssm_np(N) * 4;  // bf16: two planes
+    const size_t all = static_cast<size_t>(B) * H * blocks * NC * rec;
+    w.fwd = take(all);
+    w.rev = take(all);
+    w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(float));
+    // Heads of a group are split while there are fewer than about four workgroups per
+    // CU; each split adds fp32 sums of dB and dC to write and read.
+    const long long wgs = static_cast<long long>(B) * G * NC;
+    long long split = (1024 + wgs - 1) / wgs;
+    if (split > H / G) split = H / G;
+    w.head_block = static_cast<int>((H / G + split - 1) / split);
+    w.blocks = (H / G + w.head_block - 1) / w.head_block;
+    if (w.blocks > 1) {
+      const size_t sums = static_cast<size_t>(w.blocks) * B * T * G * N * sizeof(float);
+      w.pB = take(sums);
+      w.pC = take(sums);
+    }
+  }
+  w.bytes = at ? at : 256;
+  return w;
+}
+
+#define KATA_TRY(CALL)                     \
+  do {                                     \
+    const hipError_t e_ = (CALL);          \
+    if (e_ != hipSuccess) return e_;       \
+  } while (0)
+
+template <typename E, int NP, bool REV>
+hipError_t ssm_between_spans(const SsmArgs& a, hipStream_t st) {
+  if (a.spans < 2) return hipSuccess;
+  const int blocks = (a.P + kSsmP - 1) / kSsmP;
+  auto kernel = ssm_state_kernel<E, NP, REV, false>;
+  kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1), 256, 0, st>>>(a, nullptr);
+  KATA_TRY(hipGetLastError());
+  ssm_span_scan<REV><<<dim3((a.N * a.P + 255) / 256, a.B * a.H), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename E, int NP>
+hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
+  KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
+  const int blocks = (a.P + kSsmP - 1) / kSsmP;
+  auto kernel = ssm_out_kernel<E, NP>;
+  kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename E, int NP>
+hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* fwd, E* rev, float* dA, float* dD,
+                      float* dbias, hipStream_t st) {
+  const int blocks = (a.P + kSsmP - 1) / kSsmP, L = ssm_chunk<E>(), NC = (a.T + L - 1) / L;
+  const unsigned grid = static_cast<unsigned>(a.B) * a.H * blocks * a.spans;
+  auto f = ssm_state_kernel<E, NP, false, true>;
+  auto r = ssm_state_kernel<E, NP, true, true>;
+  auto d = ssm_grad_kernel<E, NP>;
+  KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
+  f<<<grid, 256, 0, st>>>(a, fwd);
+  KATA_TRY(hipGetLastError());
+  KATA_TRY((ssm_between_spans<E, NP, true>(a, st)));
+  r<<<grid, 256, 0, st>>>(a, rev);
+  KATA_TRY(hipGetLastError());
+  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, 256, 0, st>>>(a, o);
+  KATA_TRY(hipGetLastError());
+  if (o.blocks > 1) {
+    const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
+    ssm_join_heads<E><<<static_cast<unsigned>((all + 255) / 256), 256, 0, st>>>(o, all);
+    KATA_TRY(hipGetLastError());
+  }
+  return launch_sum_partials(o.part, a.B * NC, 3 * a.H, {{dA, dD, dbias}, {a.H, a.H, a.H}}, st);
+}
+
+#define KATA_SSM_NP(CALL)                \
+  switch (ssm_np(a.N)) {                 \
+    case 32: return CALL(32);            \
+    case 64: return CALL(64);            \
+    default: return CALL(128);           \
+  }
+
+size_t ssm_workspace_bytes(int B, int T, int H, int G, int N, int P, bool bf16, bool backward) {
+  return ssm_workspace(B, T, H, G, N, P, bf16, backward).bytes;
+}
+
+hipError_t launch_ssm_fwd(SsmArgs a, void* ws, bool bf16, hipStream_t st) {
+  const SsmWorkspace w = ssm_workspace(a.B, a.T, a.H, a.G, a.N, a.P, bf16, false);
+  char* base = static_cast<char*>(ws);
+  a.spans = w.spans, a.span_chunks = w.span_chunks;
+  a.rec = reinterpret_cast<float*>(base + w.rec);
+  a.rec_log = reinterpret_cast<double*>(base + w.log);
+  if (bf16) {
+#define KATA_CALL(K) ssm_fwd_np<bf16_t, K>(a, st)
+    KATA_SSM_NP(KATA_CALL)
+#undef KATA_CALL
+  }
+#define KATA_CALL(K) ssm_fwd_np<float, K>(a, st)
+  KATA_SSM_NP(KATA_CALL)
+#undef KATA_CALL
+}
+
+hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, void* dCm,
+                          float* dD, float* dbias, void* ws, bool bf16, hipStream_t st) {
+  const SsmWorkspace w = ssm_workspace(a.B, a.T, a.H, a.G, a.N, a.P, bf16, true);
+  char* base = static_cast<char*>(ws);
+  a.spans = w.spans, a.span_chunks = w.span_chunks;
+  a.rec = reinterpret_cast<float*>(base + w.rec);
+  a.rec_log = reinterpret_cast<double*>(base + w.log);
+  const SsmGrads o = {dx, ddt, dBm, dCm, reinterpret_cast<float*>(base + w.pB),
+                      reinterpret_cast<float*>(base + w.pC),
+                      reinterpret_cast<float*>(base + w.part), base + w.fwd, base + w.rev,
+                      w.head_block, w.blocks};
+  if (bf16) {
+#define KATA_CALL(K)                                                                         \
+  ssm_bwd_np<bf16_t, K>(a, o, reinterpret_cast<bf16_t*>(base + w.fwd),                       \
+                        reinterpret_cast<bf16_t*>(base + w.rev), dA, dD, dbias, st)
+    KATA_SSM_NP(KATA_CALL)
+#undef KATA_CALL
+  }
+#define KATA_CALL(K)                                                                       \
+  ssm_bwd_np<float, K>(a, o, reinterpret_cast<float*>(base + w.fwd),                       \
+                       reinterpret_cast<float*>(base + w.rev), dA, dD, dbias, st)
+  KATA_SSM_NP(KATA_CALL)
+#undef KATA_CALL
+}
+#undef KATA_SSM_NP
+
+hipError_t launch_ssm_step(float* S, const SsmArgs& a, bool bf16, hipStream_t st) {
+  const unsigned grid = static_cast<unsigned>(a.B) * a.H;
+  const bool vec = a.P % 4 == 0;
+  if (bf16) {
+    if (vec) ssm_step_kernel<bf16_t, 4><<<grid, 256, 0, st>>>(S, a);
+    else ssm_step_kernel<bf16_t, 1><<<grid, 256, 0, st>>>(S, a);
+  } else {
+    if (vec) ssm_step_kernel<float, 4><<<grid, 256, 0, st>>>(S, a);
+    else ssm_step_kernel<float, 1><<<grid, 256, 0, st>>>(S, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace kata
