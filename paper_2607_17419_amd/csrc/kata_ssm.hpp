@@ -112,47 +112,62 @@ constexpr int kSsmP = 64;  // columns of the state that a workgroup holds
 // the backward shrinks; fp32 tiles take twice the LDS.
 template <typename E> constexpr int ssm_chunk() { return sizeof(E) == 2 ? 64 : 32; }
 
-// Rows r < valid_rows, columns < cols of a token-major tensor into a tile, zeros
-// beyond them (rows past a sequence's end are never read).
-template <typename E, int COLS>
-__device__ __forceinline__ void stage_rows(E* dst, const E* src, long long row_stride, int rows,
-                                           int valid_rows, int cols, bool vec) {
-  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = COLS / V;
-  for (int i = threadIdx.x; i < rows * PER; i += 256) {
-    const int r = i / PER, c = (i % PER) * V;
-    union { uint4 u; E e[V]; } v;
-    v.u = make_uint4(0, 0, 0, 0);
-    if (r < valid_rows && c < cols) {
-      const E* p = src + r * row_stride + c;
-      if (vec && c + V <= cols) {
-        v.u = *reinterpret_cast<const uint4*>(p);
-      } else {
+// A token-major tensor's rows on their way into a tile: K pieces of 16 bytes per
+// thread, loaded a chunk ahead of their use.  Rows at or past `valid` and columns at or
+// past `cols` become zeros (their loads are moved to the last valid row and column 0, so
+// that every thread loads without a branch, and rows past a sequence's end are never
+// read).  vec: rows are whole aligned pieces; otherwise elements are read one by one.
+template <typename E, int ROWS, int COLS, int THREADS>
+struct SsmRows {
+  static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = COLS / V;
+  static constexpr int K = (ROWS * PER + THREADS - 1) / THREADS;
+  uint4 r[K];
+  __device__ __forceinline__ void load(const E* src, long long stride, int valid, int cols,
+                                       bool vec) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (c + j < cols) v.e[j] = p[j];
+    for (int j = 0; j < K; ++j) {
+      const int i = threadIdx.x + j * THREADS, row = i / PER, c = (i % PER) * V;
+      const E* p = src + min(row, valid - 1) * stride;
+      if (vec) {
+        r[j] = *reinterpret_cast<const uint4*>(p + (c < cols ? c : 0));
+      } else {
+        union { uint4 u; E e[V]; } v;
+        v.u = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < V; ++k)
+          if (c + k < cols) v.e[k] = p[c + k];
+        r[j] = v.u;
       }
     }
-    *reinterpret_cast<uint4*>(dst + r * ssm_pad<E>(COLS) + c) = v.u;
   }
-}
-
-// ---- steps and decays of a chunk -------------------------------------------------
-
-struct SsmChunkLog {  // LDS; l in units of log 2, as hi + lo
-  float hi[64], lo[64], step[64], gate[64];
+  __device__ __forceinline__ void store(E* dst, int valid, int cols) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int i = threadIdx.x + j * THREADS, row = i / PER, c = (i % PER) * V;
+      if (ROWS * PER % THREADS && i >= ROWS * PER) continue;
+      *reinterpret_cast<uint4*>(dst + row * ssm_pad<E>(COLS) + c) =
+          row < valid && c < cols ? r[j] : make_uint4(0, 0, 0, 0);
+    }
+  }
 };
 
-// One wave (lane = token): step, its derivative by dt (gate), and the running sum l of
-// step A, summed in fp64: differences of l over a chunk keep 2^-48 of the largest,
-// and exp(l_t - l_s) is right where a strong decay stands before weak ones.
+// ---- steps and decays of a chunk -------------------------------------------------
+// A first kernel forms them once for all others: per token {hi, lo, step, gate} with the
+// running sum l = hi + lo of step A over the chunk in units of log 2 (summed in fp64:
+// differences of l keep 2^-48 of the largest, and exp(l_t - l_s) is right where a strong
+// decay stands before weak ones), and gate the derivative of step by dt.
 template <typename E, int L>
-__device__ __forceinline__ void ssm_logs(const SsmArgs& a, SsmChunkLog& o, int b, int h, int t0,
-                                         int len) {
-  const int lane = threadIdx.x & 63, t = t0 + lane;
+__global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
+  const int per = (a.H + 3) / 4;
+  const int h = (blockIdx.x % per) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int chunk = (blockIdx.x / per) % NC, b = blockIdx.x / per / NC;
+  if (h >= a.H) return;
+  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+  const int t = chunk * L + lane;
+  const bool live = lane < L && t < len;
   float step = 0.f, gate = 0.f;
-  if (lane < L && t < len) {
-    const E* dt = static_cast<const E*>(a.dt) + b * a.db + h * a.dh + t * a.dt_t;
-    const float z = to_f32(*dt) + (a.bias ? a.bias[h] : 0.f);
+  if (live) {
+    const float z = to_f32(static_cast<const E*>(a.dt)[b * a.db + h * a.dh + t * a.dt_t]) +
+                    (a.bias ? a.bias[h] : 0.f);
     step = z, gate = 1.f;
     if (a.softplus) {
       step = z > 20.f ? z : log1pf(expf(z));
@@ -162,42 +177,68 @@ __device__ __forceinline__ void ssm_logs(const SsmArgs& a, SsmChunkLog& o, int b
   double l = static_cast<double>(step) * (static_cast<double>(a.A[h]) * 1.4426950408889634074);
   // 2^-2000 and 2^2000 are 0 and inf in fp32: bounded, sums and their differences stay finite
   l = l < -2000.0 ? -2000.0 : (l > 2000.0 ? 2000.0 : l);  // (NaN stays)
-  if (!(lane < L && t < len)) l = 0.0;
+  if (!live) l = 0.0;
 #pragma unroll
-  for (int o2 = 1; o2 < 64; o2 <<= 1) {
-    const double up = __shfl_up(l, o2);
-    if (lane >= o2) l += up;
+  for (int o = 1; o < L; o <<= 1) {
+    const double up = __shfl_up(l, o);
+    if (lane >= o) l += up;
   }
-  if (lane < L) {
-    const float hi = static_cast<float>(l);
-    o.hi[lane] = hi;
-    o.lo[lane] = isfinite(hi) ? static_cast<float>(l - hi) : 0.f;
-    o.step[lane] = step;
-    o.gate[lane] = gate;
-  }
+  if (lane >= L) return;
+  const float hi = static_cast<float>(l);
+  a.logs[(static_cast<size_t>(b * a.H + h) * NC + chunk) * L + lane] =
+      make_float4(hi, isfinite(hi) ? static_cast<float>(l - hi) : 0.f, step, gate);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// exp(l_t - l_s)
-__device__ __forceinline__ float ssm_decay(const SsmChunkLog& g, int t, int s) {
-  return exp2_fast((g.hi[t] - g.hi[s]) + (g.lo[t] - g.lo[s]));
-}
-__device__ __forceinline__ float ssm_since(const SsmChunkLog& g, int t) {
-  return exp2_fast(g.hi[t] + g.lo[t]);
+// A chunk's logs in LDS, with exp(l_t) (since) and exp(l_L - l_t) (left); all = exp(l_L).
+struct __attribute__((aligned(16))) SsmChunkLog {
+  float hi[64], lo[64], step[64], gate[64], since[64], left[64];
+  float all, log;  // log: l_L, rounded
+
+  // By one whole wave; lanes past the chunk hold a copy of its last token.
+  template <int L>
+  __device__ __forceinline__ void store(float4 v) {
+    const int lane = threadIdx.x & 63;
+    const float eh = __shfl(v.x, L - 1), el = __shfl(v.y, L - 1);
+    if (lane == 0) all = exp2_fast(eh + el), log = eh + el;
+    if (lane >= L) return;
+    hi[lane] = v.x, lo[lane] = v.y, step[lane] = v.z, gate[lane] = v.w;
+    since[lane] = exp2_fast(v.x + v.y);
+    left[lane] = exp2_fast((eh - v.x) + (el - v.y));
+  }
+  __device__ __forceinline__ f32x4 four(const float* p, int i) const {
+    return *reinterpret_cast<const f32x4*>(p + i);
+  }
+  // exp(l_t - l_s) of token t and four tokens s0 ..
+  __device__ __forceinline__ f32x4 decay(int t, int s0) const {
+    const f32x4 d = (hi[t] - four(hi, s0)) + (lo[t] - four(lo, s0));
+    return f32x4{exp2_fast(d[0]), exp2_fast(d[1]), exp2_fast(d[2]), exp2_fast(d[3])};
+  }
+};
+
+template <int L>
+__device__ __forceinline__ const float4* ssm_log_row(const SsmArgs& a, int bh, int NC) {
+  return a.logs + static_cast<size_t>(bh) * NC * L + min(static_cast<int>(threadIdx.x & 63), L - 1);
 }
 
 // A chunk's lower-triangular 16 x 16 tiles (row tile tt >= column tile ss), numbered.
 __device__ __forceinline__ void ssm_tri(int id, int& tt, int& ss) {
-  tt = 0;
-  while (id > tt) id -= ++tt;
-  ss = id;
+  tt = id >= 6 ? 3 : (id >= 3 ? 2 : (id >= 1 ? 1 : 0));
+  ss = id - tt * (tt + 1) / 2;
+}
+
+// Workgroups go to the 8 XCDs in turn: numbered so that neighbours share an XCD's L2.
+__device__ __forceinline__ unsigned ssm_xcd_order() {
+  const unsigned n = gridDim.x, x = blockIdx.x & 7, q = n >> 3, r = n & 7;
+  return x * q + min(x, r) + (blockIdx.x >> 3);
 }
 
 // ---- forward -------------------------------------------------------------------
 // A workgroup carries the state of one head (64 of its columns) over the chunks of
 // a span, as accumulators: wave w holds columns 16 w ...  Per chunk, the waves share
-// the tiles of W through LDS, then each forms its columns of y and of the new state.
+// the tiles of W through LDS, then each forms its columns of y and of the new state,
+// while the next chunk's rows are on their way.
 template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmOutLds {
   static constexpr int L = ssm_chunk<E>();
@@ -233,7 +274,7 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 }
 
 // h <- exp(l_L) h + sum_s B_s (scale_s v_s)^T over the chunk's tokens; keys and v are
-// LDS tiles, f the scale of token s.  bf16: the scaled values enter as hi + lo, so
+// LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so
 // that the fp32 state keeps 2^-18 of every term.
 template <typename E, int NP, int L, typename F>
 __device__ __forceinline__ void ssm_state_update(const E* keys, const E* v, int p0, float decay,
@@ -243,13 +284,8 @@ __device__ __forceinline__ void ssm_state_update(const E* keys, const E* v, int 
   for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
 #pragma unroll
   for (int s0 = 0; s0 < L; s0 += 32) {
-    f32x4 v0 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0));
-    f32x4 v1 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0 + 16));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v0[i] *= f(s0 + 4 * g + i);
-      v1[i] *= f(s0 + 16 + 4 * g + i);
-    }
+    const f32x4 v0 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0)) * f(s0 + 4 * g);
+    const f32x4 v1 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0 + 16)) * f(s0 + 16 + 4 * g);
     const SsmSplit<E> a(v0), b(v1);
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) {
@@ -262,12 +298,12 @@ __device__ __forceinline__ void ssm_state_update(const E* keys, const E* v, int 
 }
 
 // Workgroup -> batch, span, block of columns, head; heads of one batch and span run
-// next to each other, so that their group's B and C rows are read once from HBM.
+// next to each other, so that their group's B and C rows come from HBM once.
 struct SsmPlace {
   int b, span, pb, h;
   __device__ __forceinline__ SsmPlace(const SsmArgs& a, int spans) {
     const int blocks = (a.P + kSsmP - 1) / kSsmP;
-    unsigned id = blockIdx.x;
+    unsigned id = ssm_xcd_order();
     h = id % a.H, id /= a.H;
     pb = id % blocks, id /= blocks;
     span = id % spans;
@@ -275,15 +311,29 @@ struct SsmPlace {
   }
 };
 
+// Four neighbouring results of a row, the first at column p of P.
+template <typename E>
+__device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P, bool vec) {
+  if (vec) {
+    if (p < P) *reinterpret_cast<ssm_half<E>*>(dst) = to_half<E>(v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < P) store_f32(dst + i, v[i]);
+  }
+}
+
 template <typename E, int NP>
 __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
   constexpr int L = ssm_chunk<E>();
   constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
+  constexpr int TRI = (L / 16) * (L / 16 + 1) / 2;
   __shared__ SsmOutLds<E, NP> m;
   const SsmPlace at(a, a.spans);
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
+  const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c, py = pc + p0 + 4 * g;
+  const int NC = (a.T + L - 1) / L;
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int span_len = a.span_chunks * L;
   const int first = at.span * span_len, last = min(first + span_len, len);
@@ -296,18 +346,34 @@ __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
   const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc;
   const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
   const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
-  E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + p;
+  E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + py;
+  const float4* logs = ssm_log_row<L>(a, bh, NC);
+  SsmRows<E, L, NP, 256> rc, rb;
+  SsmRows<E, L, kSsmP, 256> rx;
+  float4 rl;
+  const auto fetch = [&](int t0) {
+    const int rows = min(L, last - t0);
+    rc.load(Cm + t0 * a.ct, a.ct, rows, a.N, a.vec_c);
+    rb.load(Bm + t0 * a.bt, a.bt, rows, a.N, a.vec_b);
+    rx.load(x + t0 * a.xt, a.xt, rows, a.P - pc, a.vec_x);
+    if (wave == 0) rl = logs[t0];
+  };
+  if (first < last) fetch(first);
   for (int i = threadIdx.x; i < L * SL; i += 256) store_f32(m.w + i, 0.f);
   for (int t0 = first; t0 < last; t0 += L) {
     const int rows = min(L, last - t0);
-    __syncthreads();
-    stage_rows<E, NP>(m.c, Cm + t0 * a.ct, a.ct, L, rows, a.N, a.vec_c);
-    stage_rows<E, NP>(m.b, Bm + t0 * a.bt, a.bt, L, rows, a.N, a.vec_b);
-    stage_rows<E, kSsmP>(m.x, x + t0 * a.xt, a.xt, L, rows, a.P - pc, a.vec_x);
-    if (wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, last);
-    __syncthreads();
+    lds_barrier();
+    rc.store(m.c, rows, a.N);
+    rb.store(m.b, rows, a.N);
+    rx.store(m.x, rows, a.P - pc);
+    if (wave == 0) m.log.template store<L>(rl);
+    lds_barrier();
+    if (t0 + L < last) fetch(t0 + L);
     // W, tile by tile: rows s, columns t of the accumulator are row t of the operand
-    for (int id = wave; id < (L / 16) * (L / 16 + 1) / 2; id += 4) {
+#pragma unroll
+    for (int j = 0; j < (TRI + 3) / 4; ++j) {
+      const int id = wave + 4 * j;
+      if (id >= TRI) break;
       int tt, ss;
       ssm_tri(id, tt, ss);
       f32x4 acc = {};
@@ -315,15 +381,14 @@ __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
       for (int k = 0; k < NP; k += 32)
         acc = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
                    row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), acc);
-      const int t = 16 * tt + c;
+      const int t = 16 * tt + c, s = 16 * ss + 4 * g;
+      acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = 16 * ss + 4 * g + i;
-        acc[i] = s <= t ? acc[i] * ssm_decay(m.log, t, s) * m.log.step[s] : 0.f;
-      }
-      *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + 16 * ss + 4 * g) = to_half<E>(acc);
+      for (int i = 0; i < 4; ++i) acc[i] = s + i <= t ? acc[i] : 0.f;
+      *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + s) = to_half<E>(acc);
     }
-    __syncthreads();
+    lds_barrier();
+    // y, rows p, columns t
     ssm_half<E> sh[NP / 16], xf[L / 16];
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) sh[j] = to_half<E>(st[j]);
@@ -334,36 +399,32 @@ __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
       f32x4 acc = {}, in = {};
 #pragma unroll
       for (int j = 0; j < NP / 16; j += 2)
-        acc = mac2(row_half(m.c, SN, 16 * tt, 16 * j), row_half(m.c, SN, 16 * tt, 16 * j + 16),
-                   sh[j], sh[j + 1], acc);
+        acc = mac2(sh[j], sh[j + 1], row_half(m.c, SN, 16 * tt, 16 * j),
+                   row_half(m.c, SN, 16 * tt, 16 * j + 16), acc);
 #pragma unroll
       for (int j = 0; j <= tt; j += 2)
-        in = mac2(row_half(m.w, SL, 16 * tt, 16 * j), row_half(m.w, SL, 16 * tt, 16 * j + 16),
-                  xf[j], xf[j + 1], in);
+        in = mac2(xf[j], xf[j + 1], row_half(m.w, SL, 16 * tt, 16 * j),
+                  row_half(m.w, SL, 16 * tt, 16 * j + 16), in);
+      const int t = 16 * tt + c;
       // A non-finite x_s times the zero weight of an earlier token is NaN: such sums
       // are formed again over s <= t alone.
-      if (__any(!(fabsf(in[0]) < INFINITY && fabsf(in[1]) < INFINITY && fabsf(in[2]) < INFINITY &&
-                  fabsf(in[3]) < INFINITY))) {
+      const float size = fmaxf(fmaxf(fabsf(in[0]), fabsf(in[1])), fmaxf(fabsf(in[2]), fabsf(in[3])));
+      const float check = (in[0] + in[1]) + (in[2] + in[3]);
+      if (__any(!(size < INFINITY) || check != check)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int t = 16 * tt + 4 * g + i;
           float sum = 0.f;
           for (int s = 0; s <= t; ++s)
-            sum = fmaf(to_f32(m.w[t * SL + s]), to_f32(m.x[s * SP + p0 + c]), sum);
+            sum = fmaf(to_f32(m.w[t * SL + s]), to_f32(m.x[s * SP + p0 + 4 * g + i]), sum);
           if (!(fabsf(in[i]) < INFINITY)) in[i] = sum;
         }
       }
-      const f32x4 xr = half_f32(xf[tt]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = 16 * tt + 4 * g + i;
-        const float out = fmaf(ssm_since(m.log, t), acc[i], fmaf(D, xr[i], in[i]));
-        if (t < rows && p < a.P) store_f32(y + (t0 + t) * a.yt, out);
-      }
+      const f32x4 out = m.log.since[t] * acc + (D * half_f32(row_half(m.x, SP, 16 * tt, p0)) + in);
+      if (t < rows) ssm_store4<E>(y + (t0 + t) * a.yt, out, py, a.P, a.vec_y);
     }
     ssm_state_update<E, NP, L>(
-        m.b, m.x, p0, ssm_since(m.log, L - 1),
-        [&](int s) { return ssm_decay(m.log, L - 1, s) * m.log.step[s]; }, st);
+        m.b, m.x, p0, m.log.all,
+        [&](int s) { return m.log.four(m.log.left, s) * m.log.four(m.log.step, s); }, st);
   }
   if (a.S_out && at.span == a.spans - 1)
     ssm_store_state<NP>(a.S_out + bh * NPs, a.N, a.P, p, st);
@@ -395,6 +456,7 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
   const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
+  const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int span_len = a.span_chunks * L;
   const int first = at.span * span_len, last = min(first + span_len, len);
@@ -410,12 +472,24 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   const E* k = REV ? static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg
                    : static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
   const long long vt = REV ? a.yt : a.xt, kt = REV ? a.ct : a.bt;
+  const float4* logs = ssm_log_row<L>(a, bh, NC);
   const int n = last > first ? (last - first + L - 1) / L : 0;
+  const int steps = CHUNKS ? n - 1 : n;  // the state past the span's end is the next span's
+  SsmRows<E, L, NP, 256> rk;
+  SsmRows<E, L, kSsmP, 256> rv;
+  float4 rl;
+  const auto start = [&](int i) { return first + (REV ? n - 1 - i : i) * L; };
+  const auto fetch = [&](int t0) {
+    const int rows = min(L, last - t0);
+    rk.load(k + t0 * kt, kt, rows, a.N, REV ? a.vec_c : a.vec_b);
+    rv.load(v + t0 * vt, vt, rows, a.P - pc, a.vec_x);
+    if (wave == 0) rl = logs[t0];
+  };
+  if (steps > 0) fetch(start(0));
   double log_sum = 0.0;
   for (int i = 0; i < n; ++i) {
-    const int t0 = first + (REV ? n - 1 - i : i) * L, rows = min(L, last - t0);
+    const int t0 = start(i), rows = min(L, last - t0);
     if constexpr (CHUNKS) {
-      const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
       E* rec = chunks + ((static_cast<size_t>(bh) * blocks + at.pb) * NC + t0 / L) *
                             (ssm_planes<E>() * kSsmP * NP);
 #pragma unroll
@@ -425,18 +499,20 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
         *reinterpret_cast<ssm_half<E>*>(q) = s.hi;
         if constexpr (sizeof(E) == 2) *reinterpret_cast<ssm_half<E>*>(q + kSsmP * NP) = s.lo;
       }
-      if (i == n - 1) break;  // the state past the span's end is the next span's
+      if (i >= steps) break;
     }
-    __syncthreads();
-    stage_rows<E, NP>(m.k, k + t0 * kt, kt, L, rows, a.N, REV ? a.vec_c : a.vec_b);
-    stage_rows<E, kSsmP>(m.v, v + t0 * vt, vt, L, rows, a.P - pc, a.vec_x);
-    if (wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, last);
-    __syncthreads();
-    log_sum += static_cast<double>(m.log.hi[L - 1]) + m.log.lo[L - 1];
+    lds_barrier();
+    rk.store(m.k, rows, a.N);
+    rv.store(m.v, rows, a.P - pc);
+    if (wave == 0) m.log.template store<L>(rl);
+    lds_barrier();
+    if (i + 1 < steps) fetch(start(i + 1));
+    if (!CHUNKS) log_sum += m.log.log;
     ssm_state_update<E, NP, L>(
-        m.k, m.v, p0, ssm_since(m.log, L - 1),
+        m.k, m.v, p0, m.log.all,
         [&](int s) {
-          return REV ? ssm_since(m.log, s) : ssm_decay(m.log, L - 1, s) * m.log.step[s];
+          return REV ? m.log.four(m.log.since, s)
+                     : m.log.four(m.log.left, s) * m.log.four(m.log.step, s);
         },
         st);
   }
@@ -456,19 +532,32 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
   float s = !REV && a.S_in ? a.S_in[static_cast<size_t>(bh) * NPs + e] : 0.f;
   float* rec = a.rec + static_cast<size_t>(bh) * gaps * NPs + e;
   const double* log = a.rec_log + static_cast<size_t>(bh) * gaps;
-#pragma unroll 4
-  for (int i = 0; i < gaps; ++i) {
-    const int j = REV ? gaps - 1 - i : i;
-    float* q = rec + static_cast<size_t>(j) * NPs;
-    s = fmaf(exp2_fast(static_cast<float>(log[j])), s, *q);
-    *q = s;
+  constexpr int U = 8;  // records in flight
+  for (int i = 0; i < gaps; i += U) {
+    float v[U], d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(i + u, gaps - 1), j = REV ? gaps - 1 - k : k;
+      v[u] = rec[static_cast<size_t>(j) * NPs];
+      d[u] = exp2_fast(static_cast<float>(log[j]));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u >= gaps) break;
+      const int j = REV ? gaps - 1 - (i + u) : i + u;
+      s = fmaf(d[u], s, v[u]);
+      rec[static_cast<size_t>(j) * NPs] = s;
+    }
   }
 }
 
 // ---- gradients ------------------------------------------------------------------
-// A workgroup takes one chunk of one group and a block of its heads in turn: dB and
-// dC of the group stay in accumulators over the heads (wave w: columns n of tiles
-// w, w + 4), C B^T is formed once.  part: dA, dD, dbias of the chunk, [B * NC][3][H].
+// A workgroup of eight waves takes one chunk of one group and a block of its heads in
+// turn: dB and dC of the group stay in accumulators over the heads, C B^T is formed
+// once, and the next head's rows and records are on their way while one is worked on.
+// Results stand with features (n, p) along an accumulator's rows and tokens along its
+// columns, so that a lane holds four neighbouring features of one token.
+// part: dA, dD, dbias of the chunk, [B * NC][3][H].
 struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
   float *pB, *pC;  // with several head blocks: their sums, [blocks][B][T][G][N] fp32
@@ -486,61 +575,79 @@ struct __attribute__((aligned(16))) SsmGradLds {
   E w[L * ssm_pad<E>(L)], mw[L * ssm_pad<E>(L)];
   SsmChunkLog log;
   float row[4][64], col[4][64], diag[64];  // pair sums by tile of the other index
-  float q[4][64], k[4][64];                // state terms by wave
-  float dot[4], dd[4];
+  float q[NP / 16][64], k[kSsmP / 16][64];  // state terms by tile of n, of p
+  float dot[8], dd[8];
 };
 
-// A record's planes into the padded tile.
+// The pieces of a chunk record that a thread moves: the same ones of every plane.
 template <typename E, int NP>
-__device__ __forceinline__ void ssm_stage_record(E* dst, const E* rec) {
-  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
-  for (int i = threadIdx.x; i < ssm_planes<E>() * kSsmP * PER; i += 256)
-    *reinterpret_cast<uint4*>(dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V) =
-        *reinterpret_cast<const uint4*>(rec + static_cast<size_t>(i) * V);
-}
-
-// The same, adding up the product of the record there (its own pieces) with the new one.
-template <typename E, int NP>
-__device__ __forceinline__ float ssm_swap_record(E* dst, const E* rec) {
-  constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
-  constexpr int plane = kSsmP * ssm_pad<E>(NP);
-  float dot = 0.f;
-  for (int i = threadIdx.x; i < kSsmP * PER; i += 256) {
-    E* q = dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V;
-    const E* r = rec + static_cast<size_t>(i) * V;
-    float u[V], w[V];
-    load_vec<V>(q, u);
-    load_vec<V>(r, w);
-    if constexpr (sizeof(E) == 2) {
-      float ul[V], wl[V];
-      load_vec<V>(q + plane, ul);
-      load_vec<V>(r + kSsmP * NP, wl);
+struct SsmRecord {
+  static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V, N = kSsmP * PER;
+  static constexpr int K = (N + 511) / 512, PL = ssm_planes<E>();
+  uint4 r[PL][K];
+  __device__ __forceinline__ void load(const E* rec) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) dot = fmaf(u[j] + ul[j], w[j] + wl[j], dot);
-      *reinterpret_cast<uint4*>(q + plane) = *reinterpret_cast<const uint4*>(r + kSsmP * NP);
-    } else {
+    for (int q = 0; q < PL; ++q)
 #pragma unroll
-      for (int j = 0; j < V; ++j) dot = fmaf(u[j], w[j], dot);
-    }
-    *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(r);
+      for (int j = 0; j < K; ++j)
+        r[q][j] = *reinterpret_cast<const uint4*>(
+            rec + q * kSsmP * NP + min(static_cast<int>(threadIdx.x) + j * 512, N - 1) * V);
   }
-  return dot;
-}
+  __device__ __forceinline__ void store(E* dst) const {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int i = threadIdx.x + j * 512;
+      if (N % 512 && i >= N) continue;
+      E* p = dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V;
+#pragma unroll
+      for (int q = 0; q < PL; ++q) *reinterpret_cast<uint4*>(p + q * kSsmP * ssm_pad<E>(NP)) = r[q][j];
+    }
+  }
+  // The sum of products of this record's values with another's.
+  __device__ __forceinline__ float dot(const SsmRecord& o) const {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      if (N % 512 && threadIdx.x + j * 512 >= N) continue;
+      float u[V], w[V];
+      load_vec<V>(reinterpret_cast<const E*>(&r[0][j]), u);
+      load_vec<V>(reinterpret_cast<const E*>(&o.r[0][j]), w);
+      if constexpr (PL == 2) {
+        float ul[V], wl[V];
+        load_vec<V>(reinterpret_cast<const E*>(&r[1][j]), ul);
+        load_vec<V>(reinterpret_cast<const E*>(&o.r[1][j]), wl);
+#pragma unroll
+        for (int i = 0; i < V; ++i) u[i] += ul[i], w[i] += wl[i];
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum = fmaf(u[i], w[i], sum);
+    }
+    return sum;
+  }
+};
 
 __device__ __forceinline__ float sum_lanes(float v, int from, int to) {
-  for (int o = from; o < to; o <<= 1) v += __shfl_xor(v, o);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+    if (o >= from && o < to) v += __shfl_xor(v, o);
   return v;
 }
 
+__device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
+  return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
+}
+
 template <typename E, int NP>
-__global__ __launch_bounds__(256) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
-  constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, NTW = (NT + 3) / 4;
-  constexpr int TRI = LT * (LT + 1) / 2, TW = (TRI + 3) / 4;
+__global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
+  constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, PT = kSsmP / 16;
+  constexpr int TRI = LT * (LT + 1) / 2, TW = (TRI + 7) / 8;
+  // wave -> a tile of n with every NG-th tile of tokens, a tile of p with every second
+  constexpr int NG = 8 / NT, TN = (LT + NG - 1) / NG, TP = LT / 2;
   constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
   constexpr int kRecord = ssm_planes<E>() * kSsmP * NP, kPlane = kSsmP * SN;
   __shared__ SsmGradLds<E, NP> m;
   const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
-  unsigned id = blockIdx.x;
+  unsigned id = ssm_xcd_order();
   const int hb = id % o.blocks;
   id /= o.blocks;
   const int grp = id % a.G;
@@ -548,198 +655,201 @@ __global__ __launch_bounds__(256) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   const int chunk = id % NC, b = id / NC;
   const int per = a.H / a.G, t0 = chunk * L, rows = min(L, a.T - t0);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt;
-  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct;
-  stage_rows<E, NP>(m.b, Bm, a.bt, L, rows, a.N, a.vec_b);
-  stage_rows<E, NP>(m.c, Cm, a.ct, L, rows, a.N, a.vec_c);
-  for (int i = threadIdx.x; i < L * SL; i += 256) store_f32(m.w + i, 0.f), store_f32(m.mw + i, 0.f);
-  __syncthreads();
-  f32x4 cb[TW];  // C B^T: rows s, columns t, tiles wave, wave + 4, ...
-  f32x4 dC[NTW][LT] = {}, dB[NTW][LT] = {};
+  const int n0 = 16 * (wave % NT), p0 = 16 * (wave % PT);
+  const int h0 = grp * per + hb * o.head_block;
+  const int turns = (min((hb + 1) * o.head_block, per) - hb * o.head_block) * blocks;
+  SsmRows<E, L, kSsmP, 512> rx, ry;
+  SsmRecord<E, NP> rs, rr;
+  float4 rl;
+  const auto fetch = [&](int turn) {
+    const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP, bh = b * a.H + h;
+    rx.load(static_cast<const E*>(a.x) + b * a.xb + h * a.xh + t0 * a.xt + pc, a.xt, rows,
+            a.P - pc, a.vec_x);
+    ry.load(static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc, a.yt, rows,
+            a.P - pc, a.vec_x);
+    const size_t rec = ((static_cast<size_t>(bh) * blocks + pb) * NC + chunk) * kRecord;
+    rs.load(static_cast<const E*>(o.fwd) + rec);
+    rr.load(static_cast<const E*>(o.rev) + rec);
+    if (wave == 0) rl = ssm_log_row<L>(a, bh, NC)[t0];
+  };
+  {
+    SsmRows<E, L, NP, 512> rb, rc;
+    rb.load(static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt, a.bt, rows, a.N, a.vec_b);
+    rc.load(static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct, a.ct, rows, a.N, a.vec_c);
+    fetch(0);
+    rb.store(m.b, rows, a.N);
+    rc.store(m.c, rows, a.N);
+  }
+  for (int i = threadIdx.x; i < L * SL; i += 512) store_f32(m.w + i, 0.f), store_f32(m.mw + i, 0.f);
+  lds_barrier();
+  f32x4 cb[TW];  // C B^T: rows s, columns t, tiles wave, wave + 8
+  f32x4 dC[TN] = {}, dB[TN] = {};
 #pragma unroll
   for (int j = 0; j < TW; ++j) {
     cb[j] = f32x4{};
-    if (wave + 4 * j < TRI) {
+    if (wave + 8 * j < TRI) {
       int tt, ss;
-      ssm_tri(wave + 4 * j, tt, ss);
+      ssm_tri(wave + 8 * j, tt, ss);
 #pragma unroll
       for (int k = 0; k < NP; k += 32)
         cb[j] = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
                      row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), cb[j]);
     }
   }
-  const int h_end = min((hb + 1) * o.head_block, per);
-  for (int hg = hb * o.head_block; hg < h_end; ++hg) {
-    const int h = grp * per + hg, bh = b * a.H + h;
+  f32x4 mm[TW];
+  float qs[TN], ks[TP], dot = 0.f, dd = 0.f;
+  for (int turn = 0; turn < turns; ++turn) {
+    const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP;
     const float D = a.D ? a.D[h] : 0.f;
-    f32x4 mm[TW] = {};
-    float qs[LT][4] = {}, ks[LT][4] = {}, dot = 0.f, dd = 0.f;
-    for (int pb = 0; pb < blocks; ++pb) {
-      const int pc = pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
-      const size_t rec = ((static_cast<size_t>(bh) * blocks + pb) * NC + chunk) * kRecord;
-      __syncthreads();
-      stage_rows<E, kSsmP>(m.x, static_cast<const E*>(a.x) + b * a.xb + h * a.xh + t0 * a.xt + pc,
-                           a.xt, L, rows, a.P - pc, a.vec_x);
-      stage_rows<E, kSsmP>(m.dy, static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc,
-                           a.yt, L, rows, a.P - pc, a.vec_x);
-      ssm_stage_record<E, NP>(m.st, static_cast<const E*>(o.fwd) + rec);
-      if (pb == 0 && wave == 0) ssm_logs<E, L>(a, m.log, b, h, t0, a.T);
-      __syncthreads();
+    if (pb == 0) {
 #pragma unroll
-      for (int j = 0; j < TW; ++j) {
-        if (wave + 4 * j >= TRI) continue;
-        int tt, ss;
-        ssm_tri(wave + 4 * j, tt, ss);
-        if (pb == 0) {  // W
-          const int t = 16 * tt + c;
-          f32x4 w;
+      for (int j = 0; j < TW; ++j) mm[j] = f32x4{};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int s = 16 * ss + 4 * g + i;
-            w[i] = s <= t ? cb[j][i] * ssm_decay(m.log, t, s) * m.log.step[s] : 0.f;
-          }
-          *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + 16 * ss + 4 * g) = to_half<E>(w);
-        }
+      for (int j = 0; j < TN; ++j) qs[j] = 0.f;
 #pragma unroll
-        for (int k = 0; k < kSsmP; k += 32)  // M^T: rows s, columns t
-          mm[j] = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
-                       row_half(m.dy, SP, 16 * tt, k), row_half(m.dy, SP, 16 * tt, k + 16), mm[j]);
-      }
-      // exp(l_t) S dy_t, and its product with C_t
-#pragma unroll
-      for (int j = 0; j < NTW; ++j) {
-        const int n0 = 16 * (wave + 4 * j);
-        if (n0 >= NP) continue;
-#pragma unroll
-        for (int tt = 0; tt < LT; ++tt) {
-          f32x4 acc = {};
-#pragma unroll
-          for (int k = 0; k < kSsmP; k += 32) {
-            const auto a0 = row_half(m.dy, SP, 16 * tt, k), a1 = row_half(m.dy, SP, 16 * tt, k + 16);
-            acc = mac2(a0, a1, col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), acc);
-            if constexpr (sizeof(E) == 2)
-              acc = mac2(a0, a1, col_half(m.st + kPlane, SN, n0, k),
-                         col_half(m.st + kPlane, SN, n0, k + 16), acc);
-          }
-          const f32x4 cr = half_f32(col_half(m.c, SN, n0, 16 * tt));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = ssm_since(m.log, 16 * tt + 4 * g + i) * acc[i];
-            qs[tt][i] = fmaf(cr[i], v, qs[tt][i]);
-            dC[j][tt][i] += v;
-          }
-        }
-      }
-      __syncthreads();
-      dot += ssm_swap_record<E, NP>(m.st, static_cast<const E*>(o.rev) + rec);
-      __syncthreads();
-      // exp(l_L - l_s) step_s R x_s: dB alone reads it, so R's leading bf16 is enough
-#pragma unroll
-      for (int j = 0; j < NTW; ++j) {
-        const int n0 = 16 * (wave + 4 * j);
-        if (n0 >= NP) continue;
-#pragma unroll
-        for (int ss = 0; ss < LT; ++ss) {
-          f32x4 acc = {};
-#pragma unroll
-          for (int k = 0; k < kSsmP; k += 32)
-            acc = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
-                       col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), acc);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int s = 16 * ss + 4 * g + i;
-            dB[j][ss][i] = fmaf(ssm_decay(m.log, L - 1, s) * m.log.step[s], acc[i], dB[j][ss][i]);
-          }
-        }
-      }
-      // dx, this wave's 16 columns
-#pragma unroll
-      for (int ss = 0; ss < LT; ++ss) {
-        f32x4 acc = {};
-#pragma unroll
-        for (int k = 0; k < NP; k += 32) {
-          const auto a0 = row_half(m.b, SN, 16 * ss, k), a1 = row_half(m.b, SN, 16 * ss, k + 16);
-          acc = mac2(a0, a1, row_half(m.st, SN, p0, k), row_half(m.st, SN, p0, k + 16), acc);
-          if constexpr (sizeof(E) == 2)
-            acc = mac2(a0, a1, row_half(m.st + kPlane, SN, p0, k),
-                       row_half(m.st + kPlane, SN, p0, k + 16), acc);
-        }
-        const f32x4 xr = half_f32(col_half(m.x, SP, p0, 16 * ss));
-        const f32x4 yr = half_f32(col_half(m.dy, SP, p0, 16 * ss));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int s = 16 * ss + 4 * g + i;
-          const float v = ssm_decay(m.log, L - 1, s) * acc[i];
-          ks[ss][i] = fmaf(xr[i], v, ks[ss][i]);
-          acc[i] = m.log.step[s] * v;
-          dd = fmaf(xr[i], yr[i], dd);
-        }
-#pragma unroll
-        for (int r = (ss / 2) * 32; r < L; r += 32)
-          acc = mac2(col_half(m.w, SL, 16 * ss, r), col_half(m.w, SL, 16 * ss, r + 16),
-                     col_half(m.dy, SP, p0, r), col_half(m.dy, SP, p0, r + 16), acc);
-        E* dx = static_cast<E*>(o.dx) + ((static_cast<size_t>(b) * a.T + t0) * a.H + h) * a.P + p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int s = 16 * ss + 4 * g + i;
-          if (s < rows && p < a.P)
-            store_f32(dx + static_cast<size_t>(s) * a.H * a.P, fmaf(D, yr[i], acc[i]));
-        }
-      }
+      for (int j = 0; j < TP; ++j) ks[j] = 0.f;
+      dot = dd = 0.f;
     }
+    // x, dy and st were last read before the barrier that ended the head (or block) before
+    if (blocks > 1) lds_barrier();
+    rx.store(m.x, rows, a.P - pc);
+    ry.store(m.dy, rows, a.P - pc);
+    rs.store(m.st);
+    if (wave == 0 && pb == 0) m.log.template store<L>(rl);
+    dot += rs.dot(rr);
+    lds_barrier();
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+      if (wave + 8 * j >= TRI) break;
+      int tt, ss;
+      ssm_tri(wave + 8 * j, tt, ss);
+      if (pb == 0) {  // W
+        const int t = 16 * tt + c, s = 16 * ss + 4 * g;
+        f32x4 w = cb[j] * m.log.decay(t, s) * m.log.four(m.log.step, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = s + i <= t ? w[i] : 0.f;
+        *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + s) = to_half<E>(w);
+      }
+#pragma unroll
+      for (int k = 0; k < kSsmP; k += 32)  // M^T: rows s, columns t
+        mm[j] = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
+                     row_half(m.dy, SP, 16 * tt, k), row_half(m.dy, SP, 16 * tt, k + 16), mm[j]);
+    }
+    // exp(l_t) S dy_t, and its product with C_t
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int tt = wave / NT + NG * j;
+      if (tt >= LT) break;
+      f32x4 acc = {};
+#pragma unroll
+      for (int k = 0; k < kSsmP; k += 32) {
+        const auto y0 = row_half(m.dy, SP, 16 * tt, k), y1 = row_half(m.dy, SP, 16 * tt, k + 16);
+        acc = mac2(col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), y0, y1, acc);
+        if constexpr (sizeof(E) == 2)
+          acc = mac2(col_half(m.st + kPlane, SN, n0, k), col_half(m.st + kPlane, SN, n0, k + 16), y0,
+                     y1, acc);
+      }
+      acc *= m.log.since[16 * tt + c];
+      qs[j] += dot4(half_f32(row_half(m.c, SN, 16 * tt, n0)), acc);
+      dC[j] += acc;
+    }
+    lds_barrier();
+    rr.store(m.st);
+    if (turn + 1 < turns) fetch(turn + 1);
+    lds_barrier();
+    // exp(l_L - l_s) step_s R x_s: dB alone reads it, so R's leading bf16 is enough
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int ss = wave / NT + NG * j;
+      if (ss >= LT) break;
+      f32x4 acc = {};
+#pragma unroll
+      for (int k = 0; k < kSsmP; k += 32)
+        acc = mac2(col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16),
+                   row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16), acc);
+      dB[j] += (m.log.left[16 * ss + c] * m.log.step[16 * ss + c]) * acc;
+    }
+    // dx, sixteen of its columns
+#pragma unroll
+    for (int j = 0; j < TP; ++j) {
+      const int ss = wave / PT + 2 * j, s = 16 * ss + c, p = pc + p0 + 4 * g;
+      f32x4 acc = {};
+#pragma unroll
+      for (int k = 0; k < NP; k += 32) {
+        const auto b0 = row_half(m.b, SN, 16 * ss, k), b1 = row_half(m.b, SN, 16 * ss, k + 16);
+        acc = mac2(row_half(m.st, SN, p0, k), row_half(m.st, SN, p0, k + 16), b0, b1, acc);
+        if constexpr (sizeof(E) == 2)
+          acc = mac2(row_half(m.st + kPlane, SN, p0, k), row_half(m.st + kPlane, SN, p0, k + 16), b0,
+                     b1, acc);
+      }
+      const f32x4 xr = half_f32(row_half(m.x, SP, 16 * ss, p0));
+      const f32x4 yr = half_f32(row_half(m.dy, SP, 16 * ss, p0));
+      acc *= m.log.left[s];
+      ks[j] += dot4(xr, acc);
+      dd += dot4(xr, yr);
+      acc *= m.log.step[s];
+#pragma unroll
+      for (int r = 0; r < L; r += 32)
+        if (r + 16 >= 16 * ss)  // W_rs of the tiles r >= s
+          acc = mac2(col_half(m.dy, SP, p0, r), col_half(m.dy, SP, p0, r + 16),
+                     col_half(m.w, SL, 16 * ss, r), col_half(m.w, SL, 16 * ss, r + 16), acc);
+      if (s < rows)
+        ssm_store4<E>(static_cast<E*>(o.dx) +
+                          ((static_cast<size_t>(b) * a.T + t0 + s) * a.H + h) * a.P + p,
+                      acc + D * yr, p, a.P, a.vec_g);
+    }
+    if (pb + 1 < blocks) continue;
     // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
     // over s < t with step_s (row), over t > s (col), s = t
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
-      if (wave + 4 * j >= TRI) continue;
+      if (wave + 8 * j >= TRI) break;
       int tt, ss;
-      ssm_tri(wave + 4 * j, tt, ss);
-      const int t = 16 * tt + c;
-      f32x4 w;
-      float row = 0.f, col[4];
+      ssm_tri(wave + 8 * j, tt, ss);
+      const int t = 16 * tt + c, s = 16 * ss + 4 * g;
+      f32x4 f = mm[j] * m.log.decay(t, s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = 16 * ss + 4 * g + i;
-        const float f = s <= t ? mm[j][i] * ssm_decay(m.log, t, s) : 0.f;
-        const float pair = s < t ? f * cb[j][i] : 0.f;
-        w[i] = f * m.log.step[s];
-        row = fmaf(pair, m.log.step[s], row);
-        col[i] = pair;
-        if (s == t) m.diag[s] = f * cb[j][i];
-      }
-      *reinterpret_cast<ssm_half<E>*>(m.mw + t * SL + 16 * ss + 4 * g) = to_half<E>(w);
-      row = sum_lanes(row, 16, 64);
+      for (int i = 0; i < 4; ++i) f[i] = s + i <= t ? f[i] : 0.f;
+      f32x4 pair = f * cb[j];
+      const f32x4 step = m.log.four(m.log.step, s);
+      *reinterpret_cast<ssm_half<E>*>(m.mw + t * SL + s) = to_half<E>(f * step);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (s + i == t) m.diag[t] = pair[i], pair[i] = 0.f;
+      const float row = sum_lanes(dot4(pair, step), 16, 64);
       if (g == 0) m.row[ss][t] = row;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float v = sum_lanes(col[i], 1, 16);
-        if (c == 0) m.col[tt][16 * ss + 4 * g + i] = v;
+        const float v = sum_lanes(pair[i], 1, 16);
+        if (c == 0) m.col[tt][s + i] = v;
       }
     }
 #pragma unroll
-    for (int tt = 0; tt < LT; ++tt)
+    for (int j = 0; j < TN; ++j) {
+      const int tt = wave / NT + NG * j;
+      const float q = sum_lanes(qs[j], 16, 64);
+      if (g == 0 && tt < LT) m.q[n0 / 16][16 * tt + c] = q;
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float q = sum_lanes(qs[tt][i], 1, 16), k = sum_lanes(ks[tt][i], 1, 16);
-        if (c == 0) m.q[wave][16 * tt + 4 * g + i] = q, m.k[wave][16 * tt + 4 * g + i] = k;
-      }
+    for (int j = 0; j < TP; ++j) {
+      const float k = sum_lanes(ks[j], 16, 64);
+      if (g == 0) m.k[p0 / 16][16 * (wave / PT + 2 * j) + c] = k;
+    }
     dot = sum_lanes(dot, 1, 64), dd = sum_lanes(dd, 1, 64);
     if (lane == 0) m.dot[wave] = dot, m.dd[wave] = dd;
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
-    for (int j = 0; j < NTW; ++j) {
-      const int n0 = 16 * (wave + 4 * j);
-      if (n0 >= NP) continue;
+    for (int j = 0; j < TN; ++j) {
+      const int tt = wave / NT + NG * j;
+      if (tt >= LT) break;
 #pragma unroll
-      for (int tt = 0; tt < LT; ++tt) {
-#pragma unroll
-        for (int k = 0; k <= 16 * tt; k += 32)
-          dC[j][tt] = mac2(row_half(m.mw, SL, 16 * tt, k), row_half(m.mw, SL, 16 * tt, k + 16),
-                           col_half(m.b, SN, n0, k), col_half(m.b, SN, n0, k + 16), dC[j][tt]);
-#pragma unroll
-        for (int r = (tt / 2) * 32; r < L; r += 32)
-          dB[j][tt] = mac2(col_half(m.mw, SL, 16 * tt, r), col_half(m.mw, SL, 16 * tt, r + 16),
-                           col_half(m.c, SN, n0, r), col_half(m.c, SN, n0, r + 16), dB[j][tt]);
+      for (int k = 0; k < L; k += 32) {
+        if (k <= 16 * tt)
+          dC[j] = mac2(col_half(m.b, SN, n0, k), col_half(m.b, SN, n0, k + 16),
+                       row_half(m.mw, SL, 16 * tt, k), row_half(m.mw, SL, 16 * tt, k + 16), dC[j]);
+        if (k + 16 >= 16 * tt)
+          dB[j] = mac2(col_half(m.c, SN, n0, k), col_half(m.c, SN, n0, k + 16),
+                       col_half(m.mw, SL, 16 * tt, k), col_half(m.mw, SL, 16 * tt, k + 16), dB[j]);
       }
     }
     if (wave == 0) {
@@ -747,27 +857,31 @@ __global__ __launch_bounds__(256) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
       // state that passes through; in fp64, since the sums over u cancel
       const int t = min(lane, L - 1);
       const float step = m.log.step[t];
-      float row = 0.f, col = 0.f;
+      float row = 0.f, col = 0.f, q = 0.f, k = 0.f;
 #pragma unroll
       for (int j = 0; j < LT; ++j) {
         if (16 * j <= t) row += m.row[j][t];
         if (j >= t / 16) col += m.col[j][t];
       }
-      const float q = m.q[0][t] + m.q[1][t] + (m.q[2][t] + m.q[3][t]);
-      const float k = m.k[0][t] + m.k[1][t] + (m.k[2][t] + m.k[3][t]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) q += m.q[j][t];
+#pragma unroll
+      for (int j = 0; j < PT; ++j) k += m.k[j][t];
       const bool in = lane < rows;
       double tail = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
       const double own = in ? static_cast<double>(step) * k : 0.0;
       double head = own;
 #pragma unroll
-      for (int o2 = 1; o2 < 64; o2 <<= 1) {
+      for (int o2 = 1; o2 < L; o2 <<= 1) {
         const double dn = __shfl_down(tail, o2), up = __shfl_up(head, o2);
         if (lane + o2 < 64) tail += dn;
         if (lane >= o2) head += up;
       }
-      const double through = static_cast<double>(ssm_since(m.log, L - 1)) *
-                             (static_cast<double>(m.dot[0]) + m.dot[1] + m.dot[2] + m.dot[3]);
-      const float e = static_cast<float>(tail + (head - own) + through);
+      float through = 0.f, xy = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) through += m.dot[j], xy += m.dd[j];
+      const float e = static_cast<float>(tail + (head - own) +
+                                         static_cast<double>(m.log.all) * through);
       const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
       if (in)
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
@@ -777,31 +891,24 @@ __global__ __launch_bounds__(256) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
       if (lane == 0) {
         float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
         part[0] = dA;
-        part[a.H] = m.dd[0] + m.dd[1] + (m.dd[2] + m.dd[3]);
+        part[a.H] = xy;
         part[2 * a.H] = db;
       }
     }
   }
 #pragma unroll
-  for (int j = 0; j < NTW; ++j) {
-    const int n = 16 * (wave + 4 * j) + c;
-    if (n >= a.N) continue;
-#pragma unroll
-    for (int tt = 0; tt < LT; ++tt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = 16 * tt + 4 * g + i;
-        if (t >= rows) continue;
-        const size_t at = ((static_cast<size_t>(b) * a.T + t0 + t) * a.G + grp) * a.N + n;
-        if (o.blocks > 1) {
-          const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
-          o.pB[hb * all + at] = dB[j][tt][i];
-          o.pC[hb * all + at] = dC[j][tt][i];
-        } else {
-          store_f32(static_cast<E*>(o.dBm) + at, dB[j][tt][i]);
-          store_f32(static_cast<E*>(o.dCm) + at, dC[j][tt][i]);
-        }
-      }
+  for (int j = 0; j < TN; ++j) {
+    const int t = 16 * (wave / NT + NG * j) + c, n = n0 + 4 * g;
+    if (t >= rows) break;
+    const size_t at = ((static_cast<size_t>(b) * a.T + t0 + t) * a.G + grp) * a.N + n;
+    if (o.blocks > 1) {
+      const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
+      ssm_store4<float>(o.pB + hb * all + at, dB[j], n, a.N, a.N % 4 == 0);
+      ssm_store4<float>(o.pC + hb * all + at, dC[j], n, a.N, a.N % 4 == 0);
+    } else {
+      ssm_store4<E>(static_cast<E*>(o.dBm) + at, dB[j], n, a.N, a.vec_gb);
+      ssm_store4<E>(static_cast<E*>(o.dCm) + at, dC[j], n, a.N, a.vec_gb);
+    }
   }
 }
 
@@ -882,7 +989,7 @@ inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
 inline size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
 struct SsmWorkspace {
-  size_t rec, log, fwd, rev, part, pB, pC, bytes;
+  size_t logs, rec, log, fwd, rev, part, pB, pC, bytes;
   int spans, span_chunks, head_block, blocks;
 };
 
@@ -897,6 +1004,7 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     at += up256(bytes);
     return here;
   };
+  w.logs = take(static_cast<size_t>(B) * H * NC * L * sizeof(float4));
   const size_t gaps = static_cast<size_t>(B) * H * (w.spans - 1);
   w.rec = take(gaps * N * P * sizeof(float));
   w.log = take(gaps * sizeof(double));
@@ -941,8 +1049,17 @@ hipError_t ssm_between_spans(const SsmArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <typename E>
+hipError_t ssm_logs(const SsmArgs& a, hipStream_t st) {
+  constexpr int L = ssm_chunk<E>();
+  const int NC = (a.T + L - 1) / L;
+  ssm_logs_kernel<E, L><<<static_cast<unsigned>(a.B) * NC * ((a.H + 3) / 4), 256, 0, st>>>(a, NC);
+  return hipGetLastError();
+}
+
 template <typename E, int NP>
 hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
+  KATA_TRY(ssm_logs<E>(a, st));
   KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
   auto kernel = ssm_out_kernel<E, NP>;
@@ -958,13 +1075,14 @@ hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* fwd, E* rev, float
   auto f = ssm_state_kernel<E, NP, false, true>;
   auto r = ssm_state_kernel<E, NP, true, true>;
   auto d = ssm_grad_kernel<E, NP>;
+  KATA_TRY(ssm_logs<E>(a, st));
   KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
   f<<<grid, 256, 0, st>>>(a, fwd);
   KATA_TRY(hipGetLastError());
   KATA_TRY((ssm_between_spans<E, NP, true>(a, st)));
   r<<<grid, 256, 0, st>>>(a, rev);
   KATA_TRY(hipGetLastError());
-  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, 256, 0, st>>>(a, o);
+  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, 512, 0, st>>>(a, o);
   KATA_TRY(hipGetLastError());
   if (o.blocks > 1) {
     const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
@@ -989,6 +1107,7 @@ hipError_t launch_ssm_fwd(SsmArgs a, void* ws, bool bf16, hipStream_t st) {
   const SsmWorkspace w = ssm_workspace(a.B, a.T, a.H, a.G, a.N, a.P, bf16, false);
   char* base = static_cast<char*>(ws);
   a.spans = w.spans, a.span_chunks = w.span_chunks;
+  a.logs = reinterpret_cast<float4*>(base + w.logs);
   a.rec = reinterpret_cast<float*>(base + w.rec);
   a.rec_log = reinterpret_cast<double*>(base + w.log);
   if (bf16) {
@@ -1006,6 +1125,7 @@ hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, 
   const SsmWorkspace w = ssm_workspace(a.B, a.T, a.H, a.G, a.N, a.P, bf16, true);
   char* base = static_cast<char*>(ws);
   a.spans = w.spans, a.span_chunks = w.span_chunks;
+  a.logs = reinterpret_cast<float4*>(base + w.logs);
   a.rec = reinterpret_cast<float*>(base + w.rec);
   a.rec_log = reinterpret_cast<double*>(base + w.log);
   const SsmGrads o = {dx, ddt, dBm, dCm, reinterpret_cast<float*>(base + w.pB),
