@@ -180,8 +180,7 @@ struct SsmArgs {
   float* S_out;  // nullable
   int B, T, H, G, N, P, softplus;
   long long xb, xt, xh, db, dt_t, dh, bb, bt, bg, cb, ct, cg, yb, yt, yh;
-  int vec_x, vec_b, vec_c;  // inputs (x with dy): rows are whole aligned 16-byte pieces
-  int vec_y, vec_g, vec_gb;  // y, dx, dB and dC: four elements at a time are aligned
+  int vec;                  // all rows are whole aligned 16-byte pieces, outputs' of four elements
   int spans, span_chunks;   // a head's chunks are split into spans
   float4* logs;             // [BH][chunks][tokens]: see ssm_logs_kernel
   float* rec;               // [BH][spans - 1][N][P]: states between spans

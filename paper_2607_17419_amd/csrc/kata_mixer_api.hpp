@@ -149,7 +149,7 @@ bool ssm_tensors(kata::SsmArgs& a, const void* x, const void* dt, const float* A
   const int piece = dtype == KATA_BF16 ? 8 : 4;
   const auto pieces = [piece](const void* p, int cols, long long u, long long v, long long w) {
     return aligned_to(p, 16) && cols % piece == 0 && u % piece == 0 && v % piece == 0 &&
-           w % piece == 0;
+           w % piece == 0 && v <= 1 << 24;  // a chunk's rows within 32-bit offsets
   };
   a = {};
   a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.D = D, a.bias = bias, a.dy = dy, a.y = y;
@@ -159,12 +159,8 @@ bool ssm_tensors(kata::SsmArgs& a, const void* x, const void* dt, const float* A
   a.bb = s.b_batch, a.bt = s.b_token, a.bg = s.b_group;
   a.cb = s.c_batch, a.ct = s.c_token, a.cg = s.c_group;
   a.yb = s.y_batch, a.yt = s.y_token, a.yh = s.y_head;
-  a.vec_x = pieces(x, P, a.xb, a.xt, a.xh);
-  if (dy) a.vec_x = a.vec_x && pieces(dy, P, a.yb, a.yt, a.yh);
-  a.vec_b = pieces(Bm, N, a.bb, a.bt, a.bg);
-  a.vec_c = pieces(Cm, N, a.cb, a.ct, a.cg);
-  const unsigned four = dtype == KATA_BF16 ? 8 : 16;
-  a.vec_y = P % 4 == 0 && aligned_to(y, four) && a.yb % 4 == 0 && a.yt % 4 == 0 && a.yh % 4 == 0;
+  a.vec = pieces(x, P, a.xb, a.xt, a.xh) && pieces(Bm, N, a.bb, a.bt, a.bg) &&
+          pieces(Cm, N, a.cb, a.ct, a.cg) && pieces(y ? y : dy, P, a.yb, a.yt, a.yh);
   return true;
 }
 
@@ -355,9 +351,7 @@ kata_status_t kata_ssm_bwd_ws(const void* x, const void* dt, const float* A, con
   if (!aligned_to(dA, 4) || !aligned_to(dD, 4) || !aligned_to(dt_dbias, 4))
     return KATA_ERR_INVALID_ARG;
   const bool bf16 = dtype == KATA_BF16;
-  const unsigned four = bf16 ? 8 : 16;
-  a.vec_g = P % 4 == 0 && aligned_to(dx, four);
-  a.vec_gb = N % 4 == 0 && aligned_to(dBm, four) && aligned_to(dCm, four);
+  a.vec = a.vec && aligned16(dx) && aligned16(dBm) && aligned16(dCm);
   if (!ws_ok(workspace, workspace_bytes, kata::ssm_workspace_bytes(B, T, H, G, N, P, bf16, true)))
     return KATA_ERR_INVALID_ARG;
   return from_hip(kata::launch_ssm_bwd(a, dx, ddt, dA, dBm, dCm, dD, dt_dbias, workspace, bf16,

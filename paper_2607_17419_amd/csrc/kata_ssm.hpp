@@ -23,6 +23,8 @@
 // accumulation, fp32 tensors on the fp32 ones.
 #pragma once
 
+#include <type_traits>
+
 #include "kata_rows.hpp"
 
 namespace kata {
@@ -78,34 +80,72 @@ struct SsmSplit {
   }
 };
 
-// Half of row r0 + c of a tile, k = k0 + 4 g ...
-template <typename E>
-__device__ __forceinline__ ssm_half<E> row_half(const E* tile, int stride, int r0, int k0) {
-  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  return *reinterpret_cast<const ssm_half<E>*>(tile + (r0 + c) * stride + k0 + 4 * g);
-}
+// Tiles in LDS.  fp32: rows padded by 16 bytes.  bf16: rows unpadded, the 16-byte piece q of
+// row r standing at q ^ swizzle(r): with the bits of r that decide which rows share their
+// banks, reversed, the 16 rows of a row half fall on distinct banks, and so do the eight
+// rows (two pieces of each) of a transposing read.
+template <typename E, int COLS>
+struct SsmTile {
+  static constexpr bool kSwizzled = sizeof(E) == 2;
+  static constexpr int stride = COLS + (kSwizzled ? 0 : 4);
+  static constexpr int size(int rows) { return rows * stride; }
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (COLS >= 128) return (r & 1) * 8 + (r >> 1 & 1) * 4 + (r >> 2 & 1) * 2 + (r >> 3 & 1);
+    else if constexpr (COLS == 64) return (r >> 1 & 1) * 4 + (r >> 2 & 1) * 2 + (r >> 3 & 1);
+    else return (r >> 2 & 1) * 2 + (r >> 3 & 1);
+  }
+  static __device__ __forceinline__ int at(int r, int col) {
+    if constexpr (kSwizzled) return r * stride + ((col >> 3 ^ swizzle(r)) << 3) + (col & 7);
+    else return r * stride + col;
+  }
+  // A lane's offsets within a tile (fresh: see SsmSelf).
+  struct Lane {
+    int r, c;
+    __device__ __forceinline__ Lane() {
+      const int j = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+      r = at(j, 4 * g);
+      c = kSwizzled ? at(4 * g + (j >> 2), 4 * (j & 3)) : at(4 * g, j);
+    }
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(r), "+v"(c)); }
+    // Half of row r0 + lane's c, k = k0 + 4 g ...;  r0, k0 multiples of 16.
+    __device__ __forceinline__ ssm_half<E> row(const E* tile, int r0, int k0) const {
+      const int o = kSwizzled ? r ^ k0 : r + k0;
+      return *reinterpret_cast<const ssm_half<E>*>(tile + r0 * stride + o);
+    }
+    // Half of column c0 + lane's c, k running over rows k0 + 4 g ...  bf16: one transposing
+    // read (lane j of 16 receives in slot s element j % 4 of the 8-byte piece that lane
+    // 4 s + j / 4 addresses).
+    __device__ __forceinline__ ssm_half<E> col(const E* tile, int c0, int k0) const {
+      if constexpr (kSwizzled) {
+        typedef short i16x4 __attribute__((ext_vector_type(4)));
+        const E* p = tile + k0 * stride + (c ^ c0);
+        const i16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4*)(const_cast<E*>(p)));
+        return __builtin_bit_cast(uint2, v);
+      } else {
+        const E* p = tile + k0 * stride + c0 + c;
+        return make_float4(p[0], p[stride], p[2 * stride], p[3 * stride]);
+      }
+    }
+  };
+};
 
-// Half of column c0 + c, k running over rows k0 + 4 g ...  bf16: one transposing
-// read (lane j of 16 receives in slot s element j % 4 of the 8-byte piece that
-// lane 4 s + j / 4 addresses).
-__device__ __forceinline__ uint2 col_half(const bf16_t* tile, int stride, int c0, int k0) {
-  typedef short i16x4 __attribute__((ext_vector_type(4)));
-  const int j = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const bf16_t* p = tile + (k0 + 4 * g + (j >> 2)) * stride + c0 + 4 * (j & 3);
-  const i16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) i16x4*)(const_cast<bf16_t*>(p)));
-  return __builtin_bit_cast(uint2, r);
-}
-__device__ __forceinline__ float4 col_half(const float* tile, int stride, int c0, int k0) {
-  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const float* p = tile + (k0 + 4 * g) * stride + c0 + c;
-  return make_float4(p[0], p[stride], p[2 * stride], p[3 * stride]);
-}
-
-// Rows of a tile are padded by 16 bytes: the 16 rows of a half then start 4 banks
-// apart, and every read of halves takes each bank the same number of times.
-template <typename E>
-constexpr int ssm_pad(int cols) { return cols + 16 / static_cast<int>(sizeof(E)); }
+// A thread's place: its wave (a scalar, so that what depends on it alone costs no vector
+// register), lane = 16 g + c.  fresh(), called in every turn of a loop, hides from the compiler
+// that they stay the same: it would otherwise form the addresses of all operands ahead of
+// the loop, some 200 of them, and spill accumulators to keep them.
+struct SsmSelf {
+  int thread, wave, lane, c, g;
+  __device__ __forceinline__ SsmSelf() : thread(threadIdx.x) { place(); }
+  __device__ __forceinline__ void fresh() {
+    asm volatile("" : "+v"(thread));
+    place();
+  }
+  __device__ __forceinline__ void place() {
+    wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    lane = thread & 63, c = lane & 15, g = lane >> 4;
+  }
+};
 
 constexpr int kSsmP = 64;  // columns of the state that a workgroup holds
 // Tokens of a chunk: the in-chunk products grow with it, the states' traffic in
@@ -114,39 +154,56 @@ template <typename E> constexpr int ssm_chunk() { return sizeof(E) == 2 ? 64 : 3
 
 // A token-major tensor's rows on their way into a tile: K pieces of 16 bytes per
 // thread, loaded a chunk ahead of their use.  Rows at or past `valid` and columns at or
-// past `cols` become zeros (their loads are moved to the last valid row and column 0, so
-// that every thread loads without a branch, and rows past a sequence's end are never
-// read).  vec: rows are whole aligned pieces; otherwise elements are read one by one.
-template <typename E, int ROWS, int COLS, int THREADS>
+// past `cols` become zeros (their loads are moved to row 0, column 0, so that every
+// thread loads without a branch, and rows past a sequence's end are never read).  VEC:
+// rows are whole aligned pieces within 32-bit offsets; otherwise elements one by one.
+template <typename E, int ROWS, int COLS, int THREADS, bool VEC>
 struct SsmRows {
   static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = COLS / V;
-  static constexpr int K = (ROWS * PER + THREADS - 1) / THREADS;
+  static constexpr int K = ROWS * PER / THREADS, kStep = THREADS / PER;  // rows between pieces
+  static_assert(ROWS * PER % THREADS == 0, "every thread moves whole pieces");
   uint4 r[K];
-  __device__ __forceinline__ void load(const E* src, long long stride, int valid, int cols,
-                                       bool vec) {
+  unsigned off;  // bytes, of the first piece
+  static __device__ __forceinline__ int row() { return threadIdx.x / PER; }
+  static __device__ __forceinline__ int column() { return threadIdx.x % PER * V; }
+  __device__ __forceinline__ explicit SsmRows(long long stride)
+      : off((row() * static_cast<unsigned>(stride) + column()) * static_cast<unsigned>(sizeof(E))) {}
+  __device__ __forceinline__ void load(const E* src, long long stride, int valid, int cols) {
+    if constexpr (VEC) {
+      if (valid == ROWS && cols >= COLS) {  // the same for all threads
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      const int i = threadIdx.x + j * THREADS, row = i / PER, c = (i % PER) * V;
-      const E* p = src + min(row, valid - 1) * stride;
-      if (vec) {
-        r[j] = *reinterpret_cast<const uint4*>(p + (c < cols ? c : 0));
+        for (int j = 0; j < K; ++j)
+          r[j] = *reinterpret_cast<const uint4*>(
+              reinterpret_cast<const char*>(src + j * kStep * stride) + off);
       } else {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          const bool in = row() + j * kStep < valid && column() < cols;
+          const uint4 v = *reinterpret_cast<const uint4*>(
+              reinterpret_cast<const char*>(src) +
+              (in ? off + j * kStep * static_cast<unsigned>(stride) *
+                          static_cast<unsigned>(sizeof(E)) : 0u));
+          r[j] = in ? v : make_uint4(0, 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
         union { uint4 u; E e[V]; } v;
         v.u = make_uint4(0, 0, 0, 0);
+        const int at = row() + j * kStep;
+        const E* p = src + at * stride + column();
         for (int k = 0; k < V; ++k)
-          if (c + k < cols) v.e[k] = p[c + k];
+          if (at < valid && column() + k < cols) v.e[k] = p[k];
         r[j] = v.u;
       }
     }
   }
-  __device__ __forceinline__ void store(E* dst, int valid, int cols) const {
+  __device__ __forceinline__ void store(E* dst) const {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      const int i = threadIdx.x + j * THREADS, row = i / PER, c = (i % PER) * V;
-      if (ROWS * PER % THREADS && i >= ROWS * PER) continue;
-      *reinterpret_cast<uint4*>(dst + row * ssm_pad<E>(COLS) + c) =
-          row < valid && c < cols ? r[j] : make_uint4(0, 0, 0, 0);
-    }
+    for (int j = 0; j < K; ++j)
+      *reinterpret_cast<uint4*>(dst + SsmTile<E, COLS>::at(row(), column()) +
+                                j * kStep * SsmTile<E, COLS>::stride) = r[j];
   }
 };
 
@@ -189,11 +246,16 @@ __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
       make_float4(hi, isfinite(hi) ? static_cast<float>(l - hi) : 0.f, step, gate);
 }
 
+// Ends a stretch that the scheduler may reorder: operand reads of later stretches are not
+// moved up, where they would hold registers that the accumulators need.
+__device__ __forceinline__ void ssm_stretch() { __builtin_amdgcn_sched_barrier(0); }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A chunk's logs in LDS, with exp(l_t) (since) and exp(l_L - l_t) (left); all = exp(l_L).
 struct __attribute__((aligned(16))) SsmChunkLog {
-  float hi[64], lo[64], step[64], gate[64], since[64], left[64];
+  // push: left times step
+  float hi[64], lo[64], step[64], gate[64], since[64], left[64], push[64];
   float all, log;  // log: l_L, rounded
 
   // By one whole wave; lanes past the chunk hold a copy of its last token.
@@ -205,7 +267,9 @@ struct __attribute__((aligned(16))) SsmChunkLog {
     if (lane >= L) return;
     hi[lane] = v.x, lo[lane] = v.y, step[lane] = v.z, gate[lane] = v.w;
     since[lane] = exp2_fast(v.x + v.y);
-    left[lane] = exp2_fast((eh - v.x) + (el - v.y));
+    const float rest = exp2_fast((eh - v.x) + (el - v.y));
+    left[lane] = rest;
+    push[lane] = rest * v.z;
   }
   __device__ __forceinline__ f32x4 four(const float* p, int i) const {
     return *reinterpret_cast<const f32x4*>(p + i);
@@ -242,8 +306,8 @@ __device__ __forceinline__ unsigned ssm_xcd_order() {
 template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmOutLds {
   static constexpr int L = ssm_chunk<E>();
-  E c[L * ssm_pad<E>(NP)], b[L * ssm_pad<E>(NP)], x[L * ssm_pad<E>(kSsmP)],
-      w[L * ssm_pad<E>(L)];
+  E c[SsmTile<E, NP>::size(L)], b[SsmTile<E, NP>::size(L)], x[SsmTile<E, kSsmP>::size(L)],
+      w[SsmTile<E, L>::size(L)];
   SsmChunkLog log;
 };
 
@@ -277,23 +341,26 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 // LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so
 // that the fp32 state keeps 2^-18 of every term.
 template <typename E, int NP, int L, typename F>
-__device__ __forceinline__ void ssm_state_update(const E* keys, const E* v, int p0, float decay,
+__device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::Lane& kt,
+                                                 const typename SsmTile<E, kSsmP>::Lane& vt,
+                                                 const E* keys, const E* v, int p0, float decay,
                                                  F f, f32x4 (&h)[NP / 16]) {
   const int g = (threadIdx.x >> 4) & 3;
 #pragma unroll
   for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
 #pragma unroll
   for (int s0 = 0; s0 < L; s0 += 32) {
-    const f32x4 v0 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0)) * f(s0 + 4 * g);
-    const f32x4 v1 = half_f32(col_half(v, ssm_pad<E>(kSsmP), p0, s0 + 16)) * f(s0 + 16 + 4 * g);
+    const f32x4 v0 = half_f32(vt.col(v, p0, s0)) * f(s0 + 4 * g);
+    const f32x4 v1 = half_f32(vt.col(v, p0, s0 + 16)) * f(s0 + 16 + 4 * g);
     const SsmSplit<E> a(v0), b(v1);
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) {
-      const auto k0 = col_half(keys, ssm_pad<E>(NP), 16 * j, s0);
-      const auto k1 = col_half(keys, ssm_pad<E>(NP), 16 * j, s0 + 16);
+      const auto k0 = kt.col(keys, 16 * j, s0);
+      const auto k1 = kt.col(keys, 16 * j, s0 + 16);
       h[j] = mac2(k0, k1, a.hi, b.hi, h[j]);
       if constexpr (sizeof(E) == 2) h[j] = mac2(k0, k1, a.lo, b.lo, h[j]);
     }
+    ssm_stretch();
   }
 }
 
@@ -312,9 +379,9 @@ struct SsmPlace {
 };
 
 // Four neighbouring results of a row, the first at column p of P.
-template <typename E>
-__device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P, bool vec) {
-  if (vec) {
+template <bool VEC, typename E>
+__device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P) {
+  if constexpr (VEC) {
     if (p < P) *reinterpret_cast<ssm_half<E>*>(dst) = to_half<E>(v);
   } else {
 #pragma unroll
@@ -323,16 +390,22 @@ __device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P, bool v
   }
 }
 
-template <typename E, int NP>
-__global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
+template <typename E, int NP, bool VEC>
+__global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs a) {
   constexpr int L = ssm_chunk<E>();
-  constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
+  typedef SsmTile<E, NP> KT;
+  typedef SsmTile<E, kSsmP> VT;
+  typedef SsmTile<E, L> WT;
   constexpr int TRI = (L / 16) * (L / 16 + 1) / 2;
   __shared__ SsmOutLds<E, NP> m;
+  typename KT::Lane kt;
+  typename VT::Lane vt;
+  typename WT::Lane wt;
   const SsmPlace at(a, a.spans);
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
-  const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c, py = pc + p0 + 4 * g;
+  SsmSelf me;
+  const int &wave = me.wave, &c = me.c, &g = me.g;
+  const int pc = at.pb * kSsmP;
   const int NC = (a.T + L - 1) / L;
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int span_len = a.span_chunks * L;
@@ -342,33 +415,36 @@ __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
   f32x4 st[NP / 16];
   const float* from = at.span ? a.rec + (static_cast<size_t>(bh) * (a.spans - 1) + at.span - 1) * NPs
                               : (a.S_in ? a.S_in + bh * NPs : nullptr);
-  ssm_load_state<NP>(from, a.N, a.P, p, st);
-  const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc;
-  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
-  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
-  E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + py;
-  const float4* logs = ssm_log_row<L>(a, bh, NC);
-  SsmRows<E, L, NP, 256> rc, rb;
-  SsmRows<E, L, kSsmP, 256> rx;
+  ssm_load_state<NP>(from, a.N, a.P, pc + 16 * wave + c, st);
+  // the rows of the next chunk to fetch, and of y
+  const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc + first * a.xt;
+  const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + first * a.bt;
+  const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + first * a.ct;
+  const float4* logs = ssm_log_row<L>(a, bh, NC) + first;
+  E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + pc + first * a.yt;
+  SsmRows<E, L, NP, 256, VEC> rc(a.ct), rb(a.bt);
+  SsmRows<E, L, kSsmP, 256, VEC> rx(a.xt);
   float4 rl;
   const auto fetch = [&](int t0) {
     const int rows = min(L, last - t0);
-    rc.load(Cm + t0 * a.ct, a.ct, rows, a.N, a.vec_c);
-    rb.load(Bm + t0 * a.bt, a.bt, rows, a.N, a.vec_b);
-    rx.load(x + t0 * a.xt, a.xt, rows, a.P - pc, a.vec_x);
-    if (wave == 0) rl = logs[t0];
+    rc.load(Cm, a.ct, rows, a.N);
+    rb.load(Bm, a.bt, rows, a.N);
+    rx.load(x, a.xt, rows, a.P - pc);
+    if (wave == 0) rl = *logs;
+    Cm += L * a.ct, Bm += L * a.bt, x += L * a.xt, logs += L;
   };
   if (first < last) fetch(first);
-  for (int i = threadIdx.x; i < L * SL; i += 256) store_f32(m.w + i, 0.f);
+  for (int i = threadIdx.x; i < WT::size(L); i += 256) store_f32(m.w + i, 0.f);
   for (int t0 = first; t0 < last; t0 += L) {
     const int rows = min(L, last - t0);
     lds_barrier();
-    rc.store(m.c, rows, a.N);
-    rb.store(m.b, rows, a.N);
-    rx.store(m.x, rows, a.P - pc);
+    rc.store(m.c);
+    rb.store(m.b);
+    rx.store(m.x);
     if (wave == 0) m.log.template store<L>(rl);
     lds_barrier();
     if (t0 + L < last) fetch(t0 + L);
+    kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
     // W, tile by tile: rows s, columns t of the accumulator are row t of the operand
 #pragma unroll
     for (int j = 0; j < (TRI + 3) / 4; ++j) {
@@ -379,55 +455,81 @@ __global__ __launch_bounds__(256) void ssm_out_kernel(SsmArgs a) {
       f32x4 acc = {};
 #pragma unroll
       for (int k = 0; k < NP; k += 32)
-        acc = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
-                   row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), acc);
+        acc = mac2(kt.row(m.b, 16 * ss, k), kt.row(m.b, 16 * ss, k + 16),
+                   kt.row(m.c, 16 * tt, k), kt.row(m.c, 16 * tt, k + 16), acc);
       const int t = 16 * tt + c, s = 16 * ss + 4 * g;
       acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
+      if (tt == ss) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = s + i <= t ? acc[i] : 0.f;
-      *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + s) = to_half<E>(acc);
+        for (int i = 0; i < 4; ++i) acc[i] = 4 * g + i <= c ? acc[i] : 0.f;
+      }
+      *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(acc);
     }
     lds_barrier();
     // y, rows p, columns t
+    me.fresh();
+    const int p0 = 16 * wave, py = pc + p0 + 4 * g;
+    const unsigned yoff =
+        (c * static_cast<unsigned>(a.yt) + p0 + 4 * g) * static_cast<unsigned>(sizeof(E));
     ssm_half<E> sh[NP / 16], xf[L / 16];
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) sh[j] = to_half<E>(st[j]);
 #pragma unroll
-    for (int j = 0; j < L / 16; ++j) xf[j] = col_half(m.x, SP, p0, 16 * j);
+    for (int j = 0; j < L / 16; ++j) xf[j] = vt.col(m.x, p0, 16 * j);
+    f32x4 in[L / 16];
+    float bad = 0.f;
 #pragma unroll
     for (int tt = 0; tt < L / 16; ++tt) {
-      f32x4 acc = {}, in = {};
-#pragma unroll
-      for (int j = 0; j < NP / 16; j += 2)
-        acc = mac2(sh[j], sh[j + 1], row_half(m.c, SN, 16 * tt, 16 * j),
-                   row_half(m.c, SN, 16 * tt, 16 * j + 16), acc);
+      in[tt] = f32x4{};
 #pragma unroll
       for (int j = 0; j <= tt; j += 2)
-        in = mac2(xf[j], xf[j + 1], row_half(m.w, SL, 16 * tt, 16 * j),
-                  row_half(m.w, SL, 16 * tt, 16 * j + 16), in);
-      const int t = 16 * tt + c;
-      // A non-finite x_s times the zero weight of an earlier token is NaN: such sums
-      // are formed again over s <= t alone.
-      const float size = fmaxf(fmaxf(fabsf(in[0]), fabsf(in[1])), fmaxf(fabsf(in[2]), fabsf(in[3])));
-      const float check = (in[0] + in[1]) + (in[2] + in[3]);
-      if (__any(!(size < INFINITY) || check != check)) {
+        in[tt] = mac2(xf[j], xf[j + 1], wt.row(m.w, 16 * tt, 16 * j),
+                      wt.row(m.w, 16 * tt, 16 * j + 16), in[tt]);
+      bad = fmaf(in[tt][0], 0.f, fmaf(in[tt][1], 0.f, fmaf(in[tt][2], 0.f, fmaf(in[tt][3], 0.f, bad))));
+    }
+    ssm_stretch();
+    // A non-finite x_s times the zero weight of an earlier token is NaN: such sums are
+    // formed again over s <= t alone.
+    if (__any(bad != bad)) {
+      f32x4 sum[L / 16] = {};
+#pragma nounroll
+      for (int s = 0; s < L; ++s) {
+        const f32x4 v = half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float sum = 0.f;
-          for (int s = 0; s <= t; ++s)
-            sum = fmaf(to_f32(m.w[t * SL + s]), to_f32(m.x[s * SP + p0 + 4 * g + i]), sum);
-          if (!(fabsf(in[i]) < INFINITY)) in[i] = sum;
-        }
+        for (int tt = 0; tt < L / 16; ++tt)
+          if (s <= 16 * tt + c) sum[tt] += to_f32(m.w[WT::at(16 * tt + c, s)]) * v;
       }
-      const f32x4 out = m.log.since[t] * acc + (D * half_f32(row_half(m.x, SP, 16 * tt, p0)) + in);
-      if (t < rows) ssm_store4<E>(y + (t0 + t) * a.yt, out, py, a.P, a.vec_y);
+#pragma unroll
+      for (int tt = 0; tt < L / 16; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(fabsf(in[tt][i]) < INFINITY)) in[tt][i] = sum[tt][i];
+    }
+#pragma unroll
+    for (int tt = 0; tt < L / 16; ++tt) {
+      f32x4 acc = {};
+#pragma unroll
+      for (int j = 0; j < NP / 16; j += 2)
+        acc = mac2(sh[j], sh[j + 1], kt.row(m.c, 16 * tt, 16 * j),
+                   kt.row(m.c, 16 * tt, 16 * j + 16), acc);
+      const int t = 16 * tt + c;
+      const f32x4 out = m.log.since[t] * acc + (D * half_f32(vt.row(m.x, 16 * tt, p0)) + in[tt]);
+      if (t < rows) {
+        E* row = y + 16 * tt * a.yt;
+        if constexpr (VEC)
+          ssm_store4<true>(reinterpret_cast<E*>(reinterpret_cast<char*>(row) + yoff), out, py, a.P);
+        else
+          ssm_store4<false>(row + c * a.yt + p0 + 4 * g, out, py, a.P);
+      }
+      ssm_stretch();
     }
     ssm_state_update<E, NP, L>(
-        m.b, m.x, p0, m.log.all,
-        [&](int s) { return m.log.four(m.log.left, s) * m.log.four(m.log.step, s); }, st);
+        kt, vt, m.b, m.x, p0, m.log.all,
+        [&](int s) { return m.log.four(m.log.push, s); }, st);
+    y += L * a.yt;
   }
   if (a.S_out && at.span == a.spans - 1)
-    ssm_store_state<NP>(a.S_out + bh * NPs, a.N, a.P, p, st);
+    ssm_store_state<NP>(a.S_out + bh * NPs, a.N, a.P, pc + 16 * wave + c, st);
 }
 
 // ---- states of spans and chunks --------------------------------------------------
@@ -441,20 +543,23 @@ template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1
 template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmStateLds {
   static constexpr int L = ssm_chunk<E>();
-  E k[L * ssm_pad<E>(NP)], v[L * ssm_pad<E>(kSsmP)];
+  E k[SsmTile<E, NP>::size(L)], v[SsmTile<E, kSsmP>::size(L)];
   SsmChunkLog log;
 };
 
-template <typename E, int NP, bool REV, bool CHUNKS>
+template <typename E, int NP, bool REV, bool CHUNKS, bool VEC>
 __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   constexpr int L = ssm_chunk<E>();
   __shared__ SsmStateLds<E, NP> m;
+  typename SsmTile<E, NP>::Lane kl;
+  typename SsmTile<E, kSsmP>::Lane vl;
   // without CHUNKS the forward's last and the reverse's first span go nowhere
   SsmPlace at(a, CHUNKS ? a.spans : a.spans - 1);
   const int slot = at.span;  // rec's, without CHUNKS
   if (!CHUNKS && REV) ++at.span;
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
-  const int wave = threadIdx.x >> 6, c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  SsmSelf me;
+  const int &wave = me.wave, &c = me.c, &g = me.g;
   const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
   const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
@@ -475,20 +580,20 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   const float4* logs = ssm_log_row<L>(a, bh, NC);
   const int n = last > first ? (last - first + L - 1) / L : 0;
   const int steps = CHUNKS ? n - 1 : n;  // the state past the span's end is the next span's
-  SsmRows<E, L, NP, 256> rk;
-  SsmRows<E, L, kSsmP, 256> rv;
+  SsmRows<E, L, NP, 256, VEC> rk(kt);
+  SsmRows<E, L, kSsmP, 256, VEC> rv(vt);
   float4 rl;
   const auto start = [&](int i) { return first + (REV ? n - 1 - i : i) * L; };
   const auto fetch = [&](int t0) {
     const int rows = min(L, last - t0);
-    rk.load(k + t0 * kt, kt, rows, a.N, REV ? a.vec_c : a.vec_b);
-    rv.load(v + t0 * vt, vt, rows, a.P - pc, a.vec_x);
+    rk.load(k + t0 * kt, kt, rows, a.N);
+    rv.load(v + t0 * vt, vt, rows, a.P - pc);
     if (wave == 0) rl = logs[t0];
   };
   if (steps > 0) fetch(start(0));
   double log_sum = 0.0;
   for (int i = 0; i < n; ++i) {
-    const int t0 = start(i), rows = min(L, last - t0);
+    const int t0 = start(i);
     if constexpr (CHUNKS) {
       E* rec = chunks + ((static_cast<size_t>(bh) * blocks + at.pb) * NC + t0 / L) *
                             (ssm_planes<E>() * kSsmP * NP);
@@ -502,17 +607,17 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
       if (i >= steps) break;
     }
     lds_barrier();
-    rk.store(m.k, rows, a.N);
-    rv.store(m.v, rows, a.P - pc);
+    rk.store(m.k);
+    rv.store(m.v);
     if (wave == 0) m.log.template store<L>(rl);
     lds_barrier();
     if (i + 1 < steps) fetch(start(i + 1));
+    kl.fresh(), vl.fresh(), me.fresh();
     if (!CHUNKS) log_sum += m.log.log;
     ssm_state_update<E, NP, L>(
-        m.k, m.v, p0, m.log.all,
+        kl, vl, m.k, m.v, p0, m.log.all,
         [&](int s) {
-          return REV ? m.log.four(m.log.since, s)
-                     : m.log.four(m.log.left, s) * m.log.four(m.log.step, s);
+          return m.log.four(REV ? m.log.since : m.log.push, s);
         },
         st);
   }
@@ -552,11 +657,14 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
 }
 
 // ---- gradients ------------------------------------------------------------------
-// A workgroup of eight waves takes one chunk of one group and a block of its heads in
-// turn: dB and dC of the group stay in accumulators over the heads, C B^T is formed
-// once, and the next head's rows and records are on their way while one is worked on.
-// Results stand with features (n, p) along an accumulator's rows and tokens along its
-// columns, so that a lane holds four neighbouring features of one token.
+// A workgroup takes one chunk of one group and a block of its heads in turn: dB and dC
+// of the group stay in accumulators over the heads, C B^T is formed once, and the next
+// head's rows and records are on their way while one is worked on.  Results stand with
+// features (n, p) along an accumulator's rows and tokens along its columns, so that a
+// lane holds four neighbouring features of one token; a wave forms 2 x 2 tiles where
+// there are as many, each operand read serving two products.  Four waves, so that two
+// workgroups share a CU and one works through the other's barriers; eight at N > 64,
+// whose records leave LDS for one workgroup.
 // part: dA, dD, dbias of the chunk, [B * NC][3][H].
 struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
@@ -566,41 +674,43 @@ struct SsmGrads {
   int head_block, blocks;
 };
 
+constexpr int ssm_grad_threads(int NP) { return NP > 64 ? 512 : 256; }
+
 template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmGradLds {
-  static constexpr int L = ssm_chunk<E>();
-  E c[L * ssm_pad<E>(NP)], b[L * ssm_pad<E>(NP)];
-  E x[L * ssm_pad<E>(kSsmP)], dy[L * ssm_pad<E>(kSsmP)];
-  E st[ssm_planes<E>() * kSsmP * ssm_pad<E>(NP)];
-  E w[L * ssm_pad<E>(L)], mw[L * ssm_pad<E>(L)];
+  static constexpr int L = ssm_chunk<E>(), kWaves = ssm_grad_threads(NP) / 64;
+  E c[SsmTile<E, NP>::size(L)], b[SsmTile<E, NP>::size(L)];
+  E x[SsmTile<E, kSsmP>::size(L)], dy[SsmTile<E, kSsmP>::size(L)];
+  E st[ssm_planes<E>() * SsmTile<E, NP>::size(kSsmP)];
+  E w[SsmTile<E, L>::size(L)], mw[SsmTile<E, L>::size(L)];
   SsmChunkLog log;
-  float row[4][64], col[4][64], diag[64];  // pair sums by tile of the other index
+  float row[4][64], col[4][64], diag[64];   // pair sums by tile of the other index
   float q[NP / 16][64], k[kSsmP / 16][64];  // state terms by tile of n, of p
-  float dot[8], dd[8];
+  float dot[kWaves], dd[kWaves];
 };
 
 // The pieces of a chunk record that a thread moves: the same ones of every plane.
-template <typename E, int NP>
+template <typename E, int NP, int THREADS>
 struct SsmRecord {
   static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V, N = kSsmP * PER;
-  static constexpr int K = (N + 511) / 512, PL = ssm_planes<E>();
+  static constexpr int K = (N + THREADS - 1) / THREADS, PL = ssm_planes<E>();
+  static_assert(N % THREADS == 0, "every thread moves whole pieces");
   uint4 r[PL][K];
   __device__ __forceinline__ void load(const E* rec) {
 #pragma unroll
     for (int q = 0; q < PL; ++q)
 #pragma unroll
       for (int j = 0; j < K; ++j)
-        r[q][j] = *reinterpret_cast<const uint4*>(
-            rec + q * kSsmP * NP + min(static_cast<int>(threadIdx.x) + j * 512, N - 1) * V);
+        r[q][j] = *reinterpret_cast<const uint4*>(rec + q * kSsmP * NP + (threadIdx.x + j * THREADS) * V);
   }
   __device__ __forceinline__ void store(E* dst) const {
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      const int i = threadIdx.x + j * 512;
-      if (N % 512 && i >= N) continue;
-      E* p = dst + (i / PER) * ssm_pad<E>(NP) + (i % PER) * V;
+      const int i = threadIdx.x + j * THREADS;
+      E* p = dst + SsmTile<E, NP>::at(i / PER, i % PER * V);
 #pragma unroll
-      for (int q = 0; q < PL; ++q) *reinterpret_cast<uint4*>(p + q * kSsmP * ssm_pad<E>(NP)) = r[q][j];
+      for (int q = 0; q < PL; ++q)
+        *reinterpret_cast<uint4*>(p + q * SsmTile<E, NP>::size(kSsmP)) = r[q][j];
     }
   }
   // The sum of products of this record's values with another's.
@@ -608,7 +718,6 @@ struct SsmRecord {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      if (N % 512 && threadIdx.x + j * 512 >= N) continue;
       float u[V], w[V];
       load_vec<V>(reinterpret_cast<const E*>(&r[0][j]), u);
       load_vec<V>(reinterpret_cast<const E*>(&o.r[0][j]), w);
@@ -626,26 +735,45 @@ struct SsmRecord {
   }
 };
 
-__device__ __forceinline__ float sum_lanes(float v, int from, int to) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-    if (o >= from && o < to) v += __shfl_xor(v, o);
+// Sums over the 16 lanes c of a row of lanes (DPP), over the four rows g, over all.
+__device__ __forceinline__ float sum_c(float v) {
+  const auto move = [](float x, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x),
+                                                              decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  v += move(v, std::integral_constant<int, 0xB1>{});   // lane ^ 1
+  v += move(v, std::integral_constant<int, 0x4E>{});   // lane ^ 2
+  v += move(v, std::integral_constant<int, 0x141>{});  // 7 - lane of 8
+  v += move(v, std::integral_constant<int, 0x140>{});  // 15 - lane of 16
   return v;
 }
+__device__ __forceinline__ float sum_g(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+__device__ __forceinline__ float sum_wave(float v) { return sum_g(sum_c(v)); }
 
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
 }
 
-template <typename E, int NP>
-__global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
+template <typename E, int NP, bool VEC>
+__global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, PT = kSsmP / 16;
-  constexpr int TRI = LT * (LT + 1) / 2, TW = (TRI + 7) / 8;
-  // wave -> a tile of n with every NG-th tile of tokens, a tile of p with every second
-  constexpr int NG = 8 / NT, TN = (LT + NG - 1) / NG, TP = LT / 2;
-  constexpr int SN = ssm_pad<E>(NP), SP = ssm_pad<E>(kSsmP), SL = ssm_pad<E>(L);
-  constexpr int kRecord = ssm_planes<E>() * kSsmP * NP, kPlane = kSsmP * SN;
+  constexpr int THREADS = ssm_grad_threads(NP), WV = THREADS / 64;
+  constexpr int TRI = LT * (LT + 1) / 2, TW = (TRI + WV - 1) / WV;
+  // dB, dC: waves stand WN x NG over tiles of n and tokens, each with NN x TN tiles;
+  // dx: WP x WS, PP x TP tiles of p and tokens
+  constexpr int NG = LT == 4 && NT == 2 ? 4 : 2, WN = WV / NG, NN = NT / WN, TN = LT / NG;
+  constexpr int WS = WV / 2 < LT ? WV / 2 : LT, WP = WV / WS, PP = PT / WP, TP = LT / WS;
+  typedef SsmTile<E, NP> KT;
+  typedef SsmTile<E, kSsmP> VT;
+  typedef SsmTile<E, L> WT;
+  constexpr int kRecord = ssm_planes<E>() * kSsmP * NP, kPlane = KT::size(kSsmP);
   __shared__ SsmGradLds<E, NP> m;
+  typename KT::Lane kt;
+  typename VT::Lane vt;
+  typename WT::Lane wt;
   const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
   unsigned id = ssm_xcd_order();
   const int hb = id % o.blocks;
@@ -654,46 +782,46 @@ __global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   id /= a.G;
   const int chunk = id % NC, b = id / NC;
   const int per = a.H / a.G, t0 = chunk * L, rows = min(L, a.T - t0);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int n0 = 16 * (wave % NT), p0 = 16 * (wave % PT);
+  SsmSelf me;
+  const int &wave = me.wave, &lane = me.lane, &c = me.c, &g = me.g;
   const int h0 = grp * per + hb * o.head_block;
   const int turns = (min((hb + 1) * o.head_block, per) - hb * o.head_block) * blocks;
-  SsmRows<E, L, kSsmP, 512> rx, ry;
-  SsmRecord<E, NP> rs, rr;
+  SsmRows<E, L, kSsmP, THREADS, VEC> rx(a.xt), ry(a.yt);
+  SsmRecord<E, NP, THREADS> rs, rr;
   float4 rl;
   const auto fetch = [&](int turn) {
     const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP, bh = b * a.H + h;
     rx.load(static_cast<const E*>(a.x) + b * a.xb + h * a.xh + t0 * a.xt + pc, a.xt, rows,
-            a.P - pc, a.vec_x);
+            a.P - pc);
     ry.load(static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc, a.yt, rows,
-            a.P - pc, a.vec_x);
+            a.P - pc);
     const size_t rec = ((static_cast<size_t>(bh) * blocks + pb) * NC + chunk) * kRecord;
     rs.load(static_cast<const E*>(o.fwd) + rec);
     rr.load(static_cast<const E*>(o.rev) + rec);
     if (wave == 0) rl = ssm_log_row<L>(a, bh, NC)[t0];
   };
   {
-    SsmRows<E, L, NP, 512> rb, rc;
-    rb.load(static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt, a.bt, rows, a.N, a.vec_b);
-    rc.load(static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct, a.ct, rows, a.N, a.vec_c);
+    SsmRows<E, L, NP, THREADS, VEC> rb(a.bt), rc(a.ct);
+    rb.load(static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt, a.bt, rows, a.N);
+    rc.load(static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct, a.ct, rows, a.N);
     fetch(0);
-    rb.store(m.b, rows, a.N);
-    rc.store(m.c, rows, a.N);
+    rb.store(m.b);
+    rc.store(m.c);
   }
-  for (int i = threadIdx.x; i < L * SL; i += 512) store_f32(m.w + i, 0.f), store_f32(m.mw + i, 0.f);
+  for (int i = threadIdx.x; i < WT::size(L); i += THREADS) store_f32(m.w + i, 0.f), store_f32(m.mw + i, 0.f);
   lds_barrier();
-  f32x4 cb[TW];  // C B^T: rows s, columns t, tiles wave, wave + 8
-  f32x4 dC[TN] = {}, dB[TN] = {};
+  f32x4 cb[TW];  // C B^T: rows s, columns t, tiles wave, wave + WV, ...
+  f32x4 dC[NN][TN] = {}, dB[NN][TN] = {};
 #pragma unroll
   for (int j = 0; j < TW; ++j) {
     cb[j] = f32x4{};
-    if (wave + 8 * j < TRI) {
+    if (wave + WV * j < TRI) {
       int tt, ss;
-      ssm_tri(wave + 8 * j, tt, ss);
+      ssm_tri(wave + WV * j, tt, ss);
 #pragma unroll
       for (int k = 0; k < NP; k += 32)
-        cb[j] = mac2(row_half(m.b, SN, 16 * ss, k), row_half(m.b, SN, 16 * ss, k + 16),
-                     row_half(m.c, SN, 16 * tt, k), row_half(m.c, SN, 16 * tt, k + 16), cb[j]);
+        cb[j] = mac2(kt.row(m.b, 16 * ss, k), kt.row(m.b, 16 * ss, k + 16),
+                     kt.row(m.c, 16 * tt, k), kt.row(m.c, 16 * tt, k + 16), cb[j]);
     }
   }
   f32x4 mm[TW];
@@ -710,146 +838,228 @@ __global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
       for (int j = 0; j < TP; ++j) ks[j] = 0.f;
       dot = dd = 0.f;
     }
-    // x, dy and st were last read before the barrier that ended the head (or block) before
+    // x, dy and st were last read before the barrier that ended the head before; within a
+    // head its blocks have none there
     if (blocks > 1) lds_barrier();
-    rx.store(m.x, rows, a.P - pc);
-    ry.store(m.dy, rows, a.P - pc);
+    rx.store(m.x);
+    ry.store(m.dy);
     rs.store(m.st);
     if (wave == 0 && pb == 0) m.log.template store<L>(rl);
     dot += rs.dot(rr);
     lds_barrier();
+    kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
-      if (wave + 8 * j >= TRI) break;
+      if (wave + WV * j >= TRI) break;
       int tt, ss;
-      ssm_tri(wave + 8 * j, tt, ss);
+      ssm_tri(wave + WV * j, tt, ss);
       if (pb == 0) {  // W
         const int t = 16 * tt + c, s = 16 * ss + 4 * g;
         f32x4 w = cb[j] * m.log.decay(t, s) * m.log.four(m.log.step, s);
+        if (tt == ss) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = s + i <= t ? w[i] : 0.f;
-        *reinterpret_cast<ssm_half<E>*>(m.w + t * SL + s) = to_half<E>(w);
+          for (int i = 0; i < 4; ++i) w[i] = 4 * g + i <= c ? w[i] : 0.f;
+        }
+        *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
 #pragma unroll
       for (int k = 0; k < kSsmP; k += 32)  // M^T: rows s, columns t
-        mm[j] = mac2(row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16),
-                     row_half(m.dy, SP, 16 * tt, k), row_half(m.dy, SP, 16 * tt, k + 16), mm[j]);
+        mm[j] = mac2(vt.row(m.x, 16 * ss, k), vt.row(m.x, 16 * ss, k + 16),
+                     vt.row(m.dy, 16 * tt, k), vt.row(m.dy, 16 * tt, k + 16), mm[j]);
     }
+    ssm_stretch();
     // exp(l_t) S dy_t, and its product with C_t
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int tt = wave / NT + NG * j;
-      if (tt >= LT) break;
-      f32x4 acc = {};
+    int n0 = 16 * NN * (wave % WN), tn = wave / WN;  // tiles of tokens tn, tn + NG
+    {
+      f32x4 acc[NN][TN] = {};
 #pragma unroll
       for (int k = 0; k < kSsmP; k += 32) {
-        const auto y0 = row_half(m.dy, SP, 16 * tt, k), y1 = row_half(m.dy, SP, 16 * tt, k + 16);
-        acc = mac2(col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16), y0, y1, acc);
-        if constexpr (sizeof(E) == 2)
-          acc = mac2(col_half(m.st + kPlane, SN, n0, k), col_half(m.st + kPlane, SN, n0, k + 16), y0,
-                     y1, acc);
+        ssm_half<E> y[TN][2];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          y[j][0] = vt.row(m.dy, 16 * (tn + NG * j), k), y[j][1] = vt.row(m.dy, 16 * (tn + NG * j), k + 16);
+#pragma unroll
+        for (int i = 0; i < NN; ++i)
+#pragma unroll
+          for (int q = 0; q < ssm_planes<E>(); ++q) {
+            const auto s0 = kt.col(m.st + q * kPlane, n0 + 16 * i, k);
+            const auto s1 = kt.col(m.st + q * kPlane, n0 + 16 * i, k + 16);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mac2(s0, s1, y[j][0], y[j][1], acc[i][j]);
+          }
       }
-      acc *= m.log.since[16 * tt + c];
-      qs[j] += dot4(half_f32(row_half(m.c, SN, 16 * tt, n0)), acc);
-      dC[j] += acc;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int tt = tn + NG * j;
+        const float since = m.log.since[16 * tt + c];
+#pragma unroll
+        for (int i = 0; i < NN; ++i) {
+          acc[i][j] *= since;
+          qs[j] += dot4(half_f32(kt.row(m.c, 16 * tt, n0 + 16 * i)), acc[i][j]);
+          dC[i][j] += acc[i][j];
+        }
+      }
     }
     lds_barrier();
     rr.store(m.st);
     if (turn + 1 < turns) fetch(turn + 1);
     lds_barrier();
     // exp(l_L - l_s) step_s R x_s: dB alone reads it, so R's leading bf16 is enough
+    kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
+    n0 = 16 * NN * (wave % WN), tn = wave / WN;
+    {
+      f32x4 acc[NN][TN] = {};
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int ss = wave / NT + NG * j;
-      if (ss >= LT) break;
-      f32x4 acc = {};
+      for (int k = 0; k < kSsmP; k += 32) {
+        ssm_half<E> x[TN][2];
 #pragma unroll
-      for (int k = 0; k < kSsmP; k += 32)
-        acc = mac2(col_half(m.st, SN, n0, k), col_half(m.st, SN, n0, k + 16),
-                   row_half(m.x, SP, 16 * ss, k), row_half(m.x, SP, 16 * ss, k + 16), acc);
-      dB[j] += (m.log.left[16 * ss + c] * m.log.step[16 * ss + c]) * acc;
+        for (int j = 0; j < TN; ++j)
+          x[j][0] = vt.row(m.x, 16 * (tn + NG * j), k), x[j][1] = vt.row(m.x, 16 * (tn + NG * j), k + 16);
+#pragma unroll
+        for (int i = 0; i < NN; ++i) {
+          const auto r0 = kt.col(m.st, n0 + 16 * i, k), r1 = kt.col(m.st, n0 + 16 * i, k + 16);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = mac2(r0, r1, x[j][0], x[j][1], acc[i][j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const float push = m.log.push[16 * (tn + NG * j) + c];
+#pragma unroll
+        for (int i = 0; i < NN; ++i) dB[i][j] += push * acc[i][j];
+      }
     }
-    // dx, sixteen of its columns
-#pragma unroll
-    for (int j = 0; j < TP; ++j) {
-      const int ss = wave / PT + 2 * j, s = 16 * ss + c, p = pc + p0 + 4 * g;
-      f32x4 acc = {};
+    ssm_stretch();
+    const int p0 = 16 * PP * (wave % WP), tp = wave / WP;  // tp, tp + WS
+    {
+      f32x4 acc[PP][TP] = {};
 #pragma unroll
       for (int k = 0; k < NP; k += 32) {
-        const auto b0 = row_half(m.b, SN, 16 * ss, k), b1 = row_half(m.b, SN, 16 * ss, k + 16);
-        acc = mac2(row_half(m.st, SN, p0, k), row_half(m.st, SN, p0, k + 16), b0, b1, acc);
-        if constexpr (sizeof(E) == 2)
-          acc = mac2(row_half(m.st + kPlane, SN, p0, k), row_half(m.st + kPlane, SN, p0, k + 16), b0,
-                     b1, acc);
-      }
-      const f32x4 xr = half_f32(row_half(m.x, SP, 16 * ss, p0));
-      const f32x4 yr = half_f32(row_half(m.dy, SP, 16 * ss, p0));
-      acc *= m.log.left[s];
-      ks[j] += dot4(xr, acc);
-      dd += dot4(xr, yr);
-      acc *= m.log.step[s];
+        ssm_half<E> v[TP][2];
 #pragma unroll
-      for (int r = 0; r < L; r += 32)
-        if (r + 16 >= 16 * ss)  // W_rs of the tiles r >= s
-          acc = mac2(col_half(m.dy, SP, p0, r), col_half(m.dy, SP, p0, r + 16),
-                     col_half(m.w, SL, 16 * ss, r), col_half(m.w, SL, 16 * ss, r + 16), acc);
-      if (s < rows)
-        ssm_store4<E>(static_cast<E*>(o.dx) +
-                          ((static_cast<size_t>(b) * a.T + t0 + s) * a.H + h) * a.P + p,
-                      acc + D * yr, p, a.P, a.vec_g);
+        for (int j = 0; j < TP; ++j)
+          v[j][0] = kt.row(m.b, 16 * (tp + WS * j), k), v[j][1] = kt.row(m.b, 16 * (tp + WS * j), k + 16);
+#pragma unroll
+        for (int i = 0; i < PP; ++i)
+#pragma unroll
+          for (int q = 0; q < ssm_planes<E>(); ++q) {
+            const auto r0 = kt.row(m.st + q * kPlane, p0 + 16 * i, k);
+            const auto r1 = kt.row(m.st + q * kPlane, p0 + 16 * i, k + 16);
+#pragma unroll
+            for (int j = 0; j < TP; ++j) acc[i][j] = mac2(r0, r1, v[j][0], v[j][1], acc[i][j]);
+          }
+      }
+      ssm_stretch();
+      f32x4 skip[PP][TP];  // D dy
+#pragma unroll
+      for (int j = 0; j < TP; ++j) {
+        const int ss = tp + WS * j;
+        const float left = m.log.left[16 * ss + c], step = m.log.step[16 * ss + c];
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+          const f32x4 xr = half_f32(vt.row(m.x, 16 * ss, p0 + 16 * i));
+          const f32x4 yr = half_f32(vt.row(m.dy, 16 * ss, p0 + 16 * i));
+          acc[i][j] *= left;
+          ks[j] += dot4(xr, acc[i][j]);
+          dd += dot4(xr, yr);
+          acc[i][j] *= step;
+          skip[i][j] = D * yr;
+        }
+      }
+      ssm_stretch();
+#pragma unroll
+      for (int r = 0; r < L; r += 32) {
+        ssm_half<E> y[PP][2];
+#pragma unroll
+        for (int i = 0; i < PP; ++i)
+          y[i][0] = vt.col(m.dy, p0 + 16 * i, r), y[i][1] = vt.col(m.dy, p0 + 16 * i, r + 16);
+#pragma unroll
+        for (int j = 0; j < TP; ++j) {
+          const int ss = tp + WS * j;
+          if (r + 16 < 16 * ss) continue;  // W_rs of the tiles r >= s
+          const auto w0 = wt.col(m.w, 16 * ss, r), w1 = wt.col(m.w, 16 * ss, r + 16);
+#pragma unroll
+          for (int i = 0; i < PP; ++i) acc[i][j] = mac2(y[i][0], y[i][1], w0, w1, acc[i][j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < TP; ++j) {
+        const int s = 16 * (tp + WS * j) + c;
+        E* row = static_cast<E*>(o.dx) + ((static_cast<size_t>(b) * a.T + t0 + s) * a.H + h) * a.P;
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+          const int p = pc + p0 + 16 * i + 4 * g;
+          if (s < rows) ssm_store4<VEC>(row + p, acc[i][j] + skip[i][j], p, a.P);
+        }
+      }
     }
+    ssm_stretch();
     if (pb + 1 < blocks) continue;
+    me.fresh();
     // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
     // over s < t with step_s (row), over t > s (col), s = t
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
-      if (wave + 8 * j >= TRI) break;
+      if (wave + WV * j >= TRI) break;
       int tt, ss;
-      ssm_tri(wave + 8 * j, tt, ss);
+      ssm_tri(wave + WV * j, tt, ss);
       const int t = 16 * tt + c, s = 16 * ss + 4 * g;
       f32x4 f = mm[j] * m.log.decay(t, s);
+      if (tt == ss) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = s + i <= t ? f[i] : 0.f;
+        for (int i = 0; i < 4; ++i) f[i] = 4 * g + i <= c ? f[i] : 0.f;
+      }
       f32x4 pair = f * cb[j];
       const f32x4 step = m.log.four(m.log.step, s);
-      *reinterpret_cast<ssm_half<E>*>(m.mw + t * SL + s) = to_half<E>(f * step);
+      *reinterpret_cast<ssm_half<E>*>(m.mw + WT::at(t, s)) = to_half<E>(f * step);
+      if (tt == ss) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (s + i == t) m.diag[t] = pair[i], pair[i] = 0.f;
-      const float row = sum_lanes(dot4(pair, step), 16, 64);
-      if (g == 0) m.row[ss][t] = row;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = sum_lanes(pair[i], 1, 16);
-        if (c == 0) m.col[tt][s + i] = v;
+        for (int i = 0; i < 4; ++i)
+          if (4 * g + i == c) m.diag[t] = pair[i], pair[i] = 0.f;
       }
+      const float row = sum_g(dot4(pair, step));
+      if (g == 0) m.row[ss][t] = row;
+      f32x4 col;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) col[i] = sum_c(pair[i]);
+      if (c == 0) *reinterpret_cast<f32x4*>(&m.col[tt][s]) = col;
     }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int tt = wave / NT + NG * j;
-      const float q = sum_lanes(qs[j], 16, 64);
-      if (g == 0 && tt < LT) m.q[n0 / 16][16 * tt + c] = q;
+      const float q = sum_g(qs[j]);
+      if (g == 0) m.q[wave % WN][16 * (tn + NG * j) + c] = q;
     }
 #pragma unroll
     for (int j = 0; j < TP; ++j) {
-      const float k = sum_lanes(ks[j], 16, 64);
-      if (g == 0) m.k[p0 / 16][16 * (wave / PT + 2 * j) + c] = k;
+      const float k = sum_g(ks[j]);
+      if (g == 0) m.k[wave % WP][16 * (tp + WS * j) + c] = k;
     }
-    dot = sum_lanes(dot, 1, 64), dd = sum_lanes(dd, 1, 64);
+    dot = sum_wave(dot), dd = sum_wave(dd);
     if (lane == 0) m.dot[wave] = dot, m.dd[wave] = dd;
     lds_barrier();
+    kt.fresh(), wt.fresh(), me.fresh();
+    n0 = 16 * NN * (wave % WN), tn = wave / WN;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int tt = wave / NT + NG * j;
-      if (tt >= LT) break;
+    for (int k = 0; k < L; k += 32) {
+      ssm_half<E> kb[NN][2], kc[NN][2];
 #pragma unroll
-      for (int k = 0; k < L; k += 32) {
-        if (k <= 16 * tt)
-          dC[j] = mac2(col_half(m.b, SN, n0, k), col_half(m.b, SN, n0, k + 16),
-                       row_half(m.mw, SL, 16 * tt, k), row_half(m.mw, SL, 16 * tt, k + 16), dC[j]);
-        if (k + 16 >= 16 * tt)
-          dB[j] = mac2(col_half(m.c, SN, n0, k), col_half(m.c, SN, n0, k + 16),
-                       col_half(m.mw, SL, 16 * tt, k), col_half(m.mw, SL, 16 * tt, k + 16), dB[j]);
+      for (int i = 0; i < NN; ++i) {
+        kb[i][0] = kt.col(m.b, n0 + 16 * i, k), kb[i][1] = kt.col(m.b, n0 + 16 * i, k + 16);
+        kc[i][0] = kt.col(m.c, n0 + 16 * i, k), kc[i][1] = kt.col(m.c, n0 + 16 * i, k + 16);
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int tt = tn + NG * j;
+        if (k <= 16 * tt) {
+          const auto w0 = wt.row(m.mw, 16 * tt, k), w1 = wt.row(m.mw, 16 * tt, k + 16);
+#pragma unroll
+          for (int i = 0; i < NN; ++i) dC[i][j] = mac2(kb[i][0], kb[i][1], w0, w1, dC[i][j]);
+        }
+        if (k + 16 >= 16 * tt) {
+          const auto w0 = wt.col(m.mw, 16 * tt, k), w1 = wt.col(m.mw, 16 * tt, k + 16);
+#pragma unroll
+          for (int i = 0; i < NN; ++i) dB[i][j] = mac2(kc[i][0], kc[i][1], w0, w1, dB[i][j]);
+        }
       }
     }
     if (wave == 0) {
@@ -864,9 +1074,9 @@ __global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
         if (j >= t / 16) col += m.col[j][t];
       }
 #pragma unroll
-      for (int j = 0; j < NT; ++j) q += m.q[j][t];
+      for (int j = 0; j < WN; ++j) q += m.q[j][t];
 #pragma unroll
-      for (int j = 0; j < PT; ++j) k += m.k[j][t];
+      for (int j = 0; j < WP; ++j) k += m.k[j][t];
       const bool in = lane < rows;
       double tail = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
       const double own = in ? static_cast<double>(step) * k : 0.0;
@@ -879,15 +1089,14 @@ __global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
       }
       float through = 0.f, xy = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) through += m.dot[j], xy += m.dd[j];
+      for (int j = 0; j < WV; ++j) through += m.dot[j], xy += m.dd[j];
       const float e = static_cast<float>(tail + (head - own) +
                                          static_cast<double>(m.log.all) * through);
       const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
       if (in)
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
                   ddt);
-      const float dA = sum_lanes(in ? e * step : 0.f, 1, 64);
-      const float db = sum_lanes(in ? ddt : 0.f, 1, 64);
+      const float dA = sum_wave(in ? e * step : 0.f), db = sum_wave(in ? ddt : 0.f);
       if (lane == 0) {
         float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
         part[0] = dA;
@@ -896,18 +1105,23 @@ __global__ __launch_bounds__(512) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
       }
     }
   }
+  const int n0 = 16 * NN * (wave % WN), tn = wave / WN;
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
-    const int t = 16 * (wave / NT + NG * j) + c, n = n0 + 4 * g;
+    const int t = 16 * (tn + NG * j) + c;
     if (t >= rows) break;
-    const size_t at = ((static_cast<size_t>(b) * a.T + t0 + t) * a.G + grp) * a.N + n;
-    if (o.blocks > 1) {
-      const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
-      ssm_store4<float>(o.pB + hb * all + at, dB[j], n, a.N, a.N % 4 == 0);
-      ssm_store4<float>(o.pC + hb * all + at, dC[j], n, a.N, a.N % 4 == 0);
-    } else {
-      ssm_store4<E>(static_cast<E*>(o.dBm) + at, dB[j], n, a.N, a.vec_gb);
-      ssm_store4<E>(static_cast<E*>(o.dCm) + at, dC[j], n, a.N, a.vec_gb);
+    const size_t at = ((static_cast<size_t>(b) * a.T + t0 + t) * a.G + grp) * a.N;
+    const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
+#pragma unroll
+    for (int i = 0; i < NN; ++i) {
+      const int n = n0 + 16 * i + 4 * g;
+      if (o.blocks > 1) {
+        ssm_store4<VEC>(o.pB + hb * all + at + n, dB[i][j], n, a.N);
+        ssm_store4<VEC>(o.pC + hb * all + at + n, dC[i][j], n, a.N);
+      } else {
+        ssm_store4<VEC>(static_cast<E*>(o.dBm) + at + n, dB[i][j], n, a.N);
+        ssm_store4<VEC>(static_cast<E*>(o.dCm) + at + n, dC[i][j], n, a.N);
+      }
     }
   }
 }
@@ -979,7 +1193,7 @@ int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chunk<floa
 // is not made shorter than four chunks.
 inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
   const int NC = (T + L - 1) / L;
-  int n = (512 + BHP - 1) / BHP;
+  int n = (1024 + BHP - 1) / BHP;
   if (n > NC / 4) n = NC / 4;
   if (n < 1) n = 1;
   span_chunks = (NC + n - 1) / n;
@@ -1038,11 +1252,11 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     if (e_ != hipSuccess) return e_;       \
   } while (0)
 
-template <typename E, int NP, bool REV>
+template <typename E, int NP, bool VEC, bool REV>
 hipError_t ssm_between_spans(const SsmArgs& a, hipStream_t st) {
   if (a.spans < 2) return hipSuccess;
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
-  auto kernel = ssm_state_kernel<E, NP, REV, false>;
+  auto kernel = ssm_state_kernel<E, NP, REV, false, VEC>;
   kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1), 256, 0, st>>>(a, nullptr);
   KATA_TRY(hipGetLastError());
   ssm_span_scan<REV><<<dim3((a.N * a.P + 255) / 256, a.B * a.H), 256, 0, st>>>(a);
@@ -1057,32 +1271,33 @@ hipError_t ssm_logs(const SsmArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename E, int NP>
+template <typename E, int NP, bool VEC>
 hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
+  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, st)));
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
-  auto kernel = ssm_out_kernel<E, NP>;
+  auto kernel = ssm_out_kernel<E, NP, VEC>;
   kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
-template <typename E, int NP>
+template <typename E, int NP, bool VEC>
 hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* fwd, E* rev, float* dA, float* dD,
                       float* dbias, hipStream_t st) {
   const int blocks = (a.P + kSsmP - 1) / kSsmP, L = ssm_chunk<E>(), NC = (a.T + L - 1) / L;
   const unsigned grid = static_cast<unsigned>(a.B) * a.H * blocks * a.spans;
-  auto f = ssm_state_kernel<E, NP, false, true>;
-  auto r = ssm_state_kernel<E, NP, true, true>;
-  auto d = ssm_grad_kernel<E, NP>;
+  auto f = ssm_state_kernel<E, NP, false, true, VEC>;
+  auto r = ssm_state_kernel<E, NP, true, true, VEC>;
+  auto d = ssm_grad_kernel<E, NP, VEC>;
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, false>(a, st)));
+  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, st)));
   f<<<grid, 256, 0, st>>>(a, fwd);
   KATA_TRY(hipGetLastError());
-  KATA_TRY((ssm_between_spans<E, NP, true>(a, st)));
+  KATA_TRY((ssm_between_spans<E, NP, VEC, true>(a, st)));
   r<<<grid, 256, 0, st>>>(a, rev);
   KATA_TRY(hipGetLastError());
-  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, 512, 0, st>>>(a, o);
+  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, ssm_grad_threads(NP), 0,
+      st>>>(a, o);
   KATA_TRY(hipGetLastError());
   if (o.blocks > 1) {
     const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
@@ -1111,11 +1326,11 @@ hipError_t launch_ssm_fwd(SsmArgs a, void* ws, bool bf16, hipStream_t st) {
   a.rec = reinterpret_cast<float*>(base + w.rec);
   a.rec_log = reinterpret_cast<double*>(base + w.log);
   if (bf16) {
-#define KATA_CALL(K) ssm_fwd_np<bf16_t, K>(a, st)
+#define KATA_CALL(K) (a.vec ? ssm_fwd_np<bf16_t, K, true>(a, st) : ssm_fwd_np<bf16_t, K, false>(a, st))
     KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
   }
-#define KATA_CALL(K) ssm_fwd_np<float, K>(a, st)
+#define KATA_CALL(K) (a.vec ? ssm_fwd_np<float, K, true>(a, st) : ssm_fwd_np<float, K, false>(a, st))
   KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
 }
@@ -1133,15 +1348,17 @@ hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, 
                       reinterpret_cast<float*>(base + w.part), base + w.fwd, base + w.rev,
                       w.head_block, w.blocks};
   if (bf16) {
-#define KATA_CALL(K)                                                                         \
-  ssm_bwd_np<bf16_t, K>(a, o, reinterpret_cast<bf16_t*>(base + w.fwd),                       \
-                        reinterpret_cast<bf16_t*>(base + w.rev), dA, dD, dbias, st)
+    bf16_t *f = reinterpret_cast<bf16_t*>(base + w.fwd), *r = reinterpret_cast<bf16_t*>(base + w.rev);
+#define KATA_CALL(K)                                                           \
+  (a.vec ? ssm_bwd_np<bf16_t, K, true>(a, o, f, r, dA, dD, dbias, st)          \
+         : ssm_bwd_np<bf16_t, K, false>(a, o, f, r, dA, dD, dbias, st))
     KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
   }
-#define KATA_CALL(K)                                                                       \
-  ssm_bwd_np<float, K>(a, o, reinterpret_cast<float*>(base + w.fwd),                       \
-                       reinterpret_cast<float*>(base + w.rev), dA, dD, dbias, st)
+  float *f = reinterpret_cast<float*>(base + w.fwd), *r = reinterpret_cast<float*>(base + w.rev);
+#define KATA_CALL(K)                                                          \
+  (a.vec ? ssm_bwd_np<float, K, true>(a, o, f, r, dA, dD, dbias, st)          \
+         : ssm_bwd_np<float, K, false>(a, o, f, r, dA, dD, dbias, st))
   KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
 }
