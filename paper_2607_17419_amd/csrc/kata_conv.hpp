@@ -76,22 +76,35 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(const E* __restrict__ x,
   for (int j = 0; j < W - 1; ++j) conv_row<E, W, V>(x, state, s, b, t0 - (W - 1) + j, c, past[j]);
   const E* xp = x + b * s.xb + c;
   E* yp = y + b * s.yb + c;
-#pragma unroll 4
-  for (int t = t0; t < t1; ++t) {
-    load_vec<V>(xp + t * s.xt, past[W - 1]);
-    float out[V];
+  // four tokens at a time, the next four on their way (past the end: the last one again)
+  RawVec<E, V> next[4];
+  const auto fetch = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float p = bv[i];
+    for (int k = 0; k < 4; ++k) next[k] = load_raw<E, V>(xp + min(t + k, t1 - 1) * s.xt);
+  };
+  fetch(t0);
+  for (int t = t0; t < t1; t += 4) {
+    RawVec<E, V> now[4];
 #pragma unroll
-      for (int j = 0; j < W; ++j) p = fmaf(wv[j][i], past[j][i], p);
-      out[i] = s.silu ? p * sigmoid(p) : p;
+    for (int k = 0; k < 4; ++k) now[k] = next[k];
+    if (t + 4 < t1) fetch(t + 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      raw_f32<E, V>(now[k], past[W - 1]);
+      float out[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float p = bv[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j) p = fmaf(wv[j][i], past[j][i], p);
+        out[i] = s.silu ? p * sigmoid(p) : p;
+      }
+      if (t + k < t1) store_vec<V>(yp + (t + k) * s.yt, out);
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) past[j][i] = past[j + 1][i];
     }
-    store_vec<V>(yp + t * s.yt, out);
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-      for (int i = 0; i < V; ++i) past[j][i] = past[j + 1][i];
   }
 }
 
@@ -161,43 +174,60 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(const E* __restrict__ x,
 #pragma unroll
       for (int j = 0; j < W - 1; ++j)
         conv_row<E, W, V>(x, static_cast<const E*>(nullptr), s, b, t0 - (W - 1) + j, c, past[j]);
-#pragma unroll 4
-      for (int u = t0; u < t1 + W - 1; ++u) {
-        float gy[V];
-        if (u < s.T) {
-          load_vec<V>(xp + u * s.xt, past[W - 1]);
-          load_vec<V>(gp + u * s.gt, gy);
-        } else {
+      // four tokens at a time, the next four on their way (past the end: the last one again,
+      // with a dpre of zero)
+      RawVec<E, V> nx[4], ng[4];
+      const auto fetch = [&](int u) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) past[W - 1][i] = gy[i] = 0.f;
+        for (int k = 0; k < 4; ++k) {
+          const int at = min(u + k, s.T - 1);
+          nx[k] = load_raw<E, V>(xp + at * s.xt);
+          ng[k] = load_raw<E, V>(gp + at * s.gt);
         }
-        float out[V];
+      };
+      const int end = t1 + W - 1;
+      fetch(t0);
+      for (int u0 = t0; u0 < end; u0 += 4) {
+        RawVec<E, V> rx[4], rg[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          if (s.silu) {
-            float p = bv[i];
+        for (int k = 0; k < 4; ++k) rx[k] = nx[k], rg[k] = ng[k];
+        if (u0 + 4 < end) fetch(u0 + 4);
 #pragma unroll
-            for (int j = 0; j < W; ++j) p = fmaf(wv[j][i], past[j][i], p);
-            const float sg = sigmoid(p);
-            gy[i] *= sg * fmaf(p, 1.f - sg, 1.f);
+        for (int k = 0; k < 4; ++k) {
+          const int u = u0 + k;
+          float gy[V], out[V];
+          raw_f32<E, V>(rx[k], past[W - 1]);
+          raw_f32<E, V>(rg[k], gy);
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            if (s.silu) {
+              float p = bv[i];
+#pragma unroll
+              for (int j = 0; j < W; ++j) p = fmaf(wv[j][i], past[j][i], p);
+              const float sg = sigmoid(p);
+              gy[i] *= sg * fmaf(p, 1.f - sg, 1.f);
+            }
+            if (u >= s.T) gy[i] = 0.f;
+            g[W - 1][i] = gy[i];
+            float a = 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) a = fmaf(wv[j][i], g[W - 1 - j][i], a);
+            out[i] = a;
           }
-          if (u >= s.T) gy[i] = 0.f;
-          g[W - 1][i] = gy[i];
           if (u < t1) {
-            db[i] += gy[i];
 #pragma unroll
-            for (int j = 0; j < W; ++j) dw[j][i] = fmaf(gy[i], past[j][i], dw[j][i]);
+            for (int i = 0; i < V; ++i) {
+              db[i] += gy[i];
+#pragma unroll
+              for (int j = 0; j < W; ++j) dw[j][i] = fmaf(gy[i], past[j][i], dw[j][i]);
+            }
           }
-          float a = 0.f;
+          if (u - (W - 1) >= t0 && u < end) store_vec<V>(dp + (u - (W - 1)) * s.yt, out);
 #pragma unroll
-          for (int j = 0; j < W; ++j) a = fmaf(wv[j][i], g[W - 1 - j][i], a);
-          out[i] = a;
+          for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) past[j][i] = past[j + 1][i], g[j][i] = g[j + 1][i];
         }
-        if (u - (W - 1) >= t0) store_vec<V>(dp + (u - (W - 1)) * s.yt, out);
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-          for (int i = 0; i < V; ++i) past[j][i] = past[j + 1][i], g[j][i] = g[j + 1][i];
       }
     }
   }

@@ -101,12 +101,34 @@ __device__ __forceinline__ void norm_angles(const double* freq, int rh, int u0, 
   }
 }
 
-template <int LANES>
-__device__ __forceinline__ float norm_group_sum(float x) {
+// A lane's coordinates of a head's row as they stand in memory; VEC as in norm_load.
+template <bool VEC, typename E>
+struct NormRow {
+  RawVec<E, 4> u, v;
+  __device__ __forceinline__ void load(const E* p, const int (&e0)[4], const int (&e1)[4], int d,
+                                       bool paired) {
+    if constexpr (VEC) {
+      u = load_raw<E, 4>(p + e0[0]);
+      v = load_raw<E, 4>(p + (paired ? e0[0] + 4 : e1[0]));
+    } else {
 #pragma unroll
-  for (int o = LANES >> 1; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
+      for (int i = 0; i < 4; ++i) {
+        u.e[i] = e0[i] < d ? p[e0[i]] : E{};
+        v.e[i] = e1[i] < d ? p[e1[i]] : E{};
+      }
+    }
+  }
+  __device__ __forceinline__ void get(bool paired, float (&a)[4], float (&b)[4]) const {
+    float x[4], y[4];
+    raw_f32<E, 4>(u, x);
+    raw_f32<E, 4>(v, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = VEC && paired ? (i < 2 ? x[2 * i] : y[2 * i - 4]) : x[i];
+      b[i] = VEC && paired ? (i < 2 ? x[2 * i + 1] : y[2 * i - 3]) : y[i];
+    }
+  }
+};
 
 template <int LANES, bool VEC, typename E>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(const E* __restrict__ q,
@@ -130,41 +152,58 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(const E* __restrict__ 
   const NormSlots slots{n.d, n.r, n.pairs};
 #pragma unroll
   for (int i = 0; i < 4; ++i) slots.at(u0 + i, e0[i], e1[i]);
-  float co[4], si[4];
-  norm_angles(freq, rh, u0, pos ? pos[token] : t, co, si);
-  const int H = n.side[0].H + n.side[1].H, h0 = blockIdx.y * n.split;
   const float scale = n.norm == kNormRms ? 1.f / static_cast<float>(n.d) : 1.f;
-  for (int hh = h0; hh < min(h0 + n.split, H); ++hh) {
-    const bool key = hh >= n.side[0].H;
+  const int h0 = blockIdx.y * n.split, h1 = min(h0 + n.split, n.side[0].H + n.side[1].H);
+  float co[4], si[4];
+  bool angles = false;
+#pragma unroll
+  for (int key = 0; key < 2; ++key) {
     const NormSide& s = n.side[key];
-    const int h = key ? hh - n.side[0].H : hh;
+    const int from = max(h0 - (key ? n.side[0].H : 0), 0), to = min(h1 - (key ? n.side[0].H : 0), s.H);
+    if (from >= to) continue;
+    const E* x = (key ? k : q) + b * s.xb + t * s.xt;
+    E* y = (key ? yk : yq) + (static_cast<long long>(b) * s.H * n.T + t) * n.d;
     const float* w = key ? wk : wq;
-    const E* x = (key ? k : q) + b * s.xb + t * s.xt + h * s.xh;
-    E* y = (key ? yk : yq) + ((static_cast<long long>(b) * s.H + h) * n.T + t) * n.d;
-    float a[4] = {}, c[4] = {};
-    if (live) norm_load<VEC>(x, e0, e1, n.d, paired, a, c);
-    if (n.norm != kNormNone) {
-      float ss = 0.f;
+    // four heads at a time, the next four on their way (past the last: it again)
+    NormRow<VEC, E> next[4];
+    const auto fetch = [&](int h) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(c[i], c[i], ss));
-      const float inv = 1.f / sqrtf(fmaf(norm_group_sum<LANES>(ss), scale, n.eps));
+      for (int i = 0; i < 4; ++i) next[i].load(x + min(h + i, to - 1) * s.xh, e0, e1, n.d, paired);
+    };
+    if (live) fetch(from);
+    if (!angles) norm_angles(freq, rh, u0, pos ? pos[token] : t, co, si);
+    angles = true;
+    float wa[4] = {1.f, 1.f, 1.f, 1.f}, wc[4] = {1.f, 1.f, 1.f, 1.f};
+    if (w && live) norm_load<false>(w, e0, e1, n.d, false, wa, wc);
+    for (int h = from; h < to; h += 4) {
+      NormRow<VEC, E> now[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] *= inv, c[i] *= inv;
+      for (int i = 0; i < 4; ++i) now[i] = next[i];
+      if (live && h + 4 < to) fetch(h + 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (h + j >= to) break;  // the same for all lanes
+        float a[4] = {}, c[4] = {};
+        if (live) now[j].get(paired, a, c);
+        if (n.norm != kNormNone) {
+          float ss = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(c[i], c[i], ss));
+          const float inv = __builtin_amdgcn_rsqf(fmaf(sum_group<LANES>(ss), scale, n.eps));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[i] *= inv, c[i] *= inv;
+        }
+        if (!live) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i] *= wa[i], c[i] *= wc[i];
+          const float ta = fmaf(a[i], co[i], -c[i] * si[i]);
+          c[i] = fmaf(a[i], si[i], c[i] * co[i]);
+          a[i] = ta;
+        }
+        norm_store<VEC>(y + static_cast<long long>(h + j) * n.T * n.d, e0, e1, n.d, paired, a, c);
+      }
     }
-    if (!live) continue;
-    if (w) {
-      float wa[4], wc[4];
-      norm_load<false>(w, e0, e1, n.d, false, wa, wc);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] *= wa[i], c[i] *= wc[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float ta = fmaf(a[i], co[i], -c[i] * si[i]);
-      c[i] = fmaf(a[i], si[i], c[i] * co[i]);
-      a[i] = ta;
-    }
-    norm_store<VEC>(y, e0, e1, n.d, paired, a, c);
   }
 }
 
@@ -225,7 +264,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
           float ss = 0.f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(c[i], c[i], ss));
-          inv = 1.f / sqrtf(fmaf(norm_group_sum<LANES>(ss), scale, n.eps));
+          inv = __builtin_amdgcn_rsqf(fmaf(sum_group<LANES>(ss), scale, n.eps));
         }
         float dot = 0.f;
 #pragma unroll
@@ -237,7 +276,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
           dot = fmaf(ga[i], a[i], fmaf(gc[i], c[i], dot));
         }
         if (n.norm != kNormNone) {
-          dot = norm_group_sum<LANES>(dot) * scale;
+          dot = sum_group<LANES>(dot) * scale;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             ga[i] = inv * fmaf(-a[i], dot, ga[i]);

@@ -70,9 +70,56 @@ __device__ __forceinline__ void store_vec(bf16_t* p, const float (&v)[V]) {
   }
 }
 
-// Logistic function: v_rcp_f32 is within 1 ulp, and 1 + e^-x of +inf gives 0.
+// Logistic function from the hardware's exp2 and reciprocal (each within 1 ulp; the
+// product x log2 e adds |x| 2^-24 to the exponential's relative error, which counts only
+// where the result is near 0 or 1 and x (1 - sigmoid) small).  1 + inf gives 0.
 __device__ __forceinline__ float sigmoid(float x) {
-  return __builtin_amdgcn_rcpf(1.f + expf(-x));
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * x));
+}
+
+// V elements as they stand in memory, loaded some time before they are used.
+template <typename E, int V>
+struct RawVec {
+  E e[V];
+};
+template <typename E, int V>
+__device__ __forceinline__ RawVec<E, V> load_raw(const E* p) {
+  RawVec<E, V> r;
+  if constexpr (V * sizeof(E) == 16) r = __builtin_bit_cast(RawVec<E, V>, *reinterpret_cast<const uint4*>(p));
+  else if constexpr (V * sizeof(E) == 8) r = __builtin_bit_cast(RawVec<E, V>, *reinterpret_cast<const uint2*>(p));
+  else
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.e[i] = p[i];
+  return r;
+}
+template <typename E, int V>
+__device__ __forceinline__ void raw_f32(const RawVec<E, V>& r, float (&v)[V]) {
+  if constexpr (sizeof(E) == 2 && V % 2 == 0) {
+    struct Words { uint32_t w[V / 2]; };
+    const Words u = __builtin_bit_cast(Words, r);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) v[2 * i] = bf16lo_f32(u.w[i]), v[2 * i + 1] = bf16hi_f32(u.w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = to_f32(r.e[i]);
+  }
+}
+
+// Sum over groups of LANES (a power of two) neighbouring lanes, in every lane; within
+// rows of 16 lanes by DPP moves.
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+template <int LANES>
+__device__ __forceinline__ float sum_group(float x) {
+  if constexpr (LANES >= 2) x += dpp_move<0xB1>(x);    // lane ^ 1
+  if constexpr (LANES >= 4) x += dpp_move<0x4E>(x);    // lane ^ 2
+  if constexpr (LANES >= 8) x += dpp_move<0x141>(x);   // 7 - lane of 8
+  if constexpr (LANES >= 16) x += dpp_move<0x140>(x);  // 15 - lane of 16
+  if constexpr (LANES >= 32) x += __shfl_xor(x, 16);
+  if constexpr (LANES >= 64) x += __shfl_xor(x, 32);
+  return x;
 }
 
 // Sums of per-workgroup partial sums: part[n][cols] fp32 is summed over n in

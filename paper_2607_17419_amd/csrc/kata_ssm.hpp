@@ -23,8 +23,6 @@
 // accumulation, fp32 tensors on the fp32 ones.
 #pragma once
 
-#include <type_traits>
-
 #include "kata_rows.hpp"
 
 namespace kata {
@@ -445,7 +443,8 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
     lds_barrier();
     if (t0 + L < last) fetch(t0 + L);
     kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
-    // W, tile by tile: rows s, columns t of the accumulator are row t of the operand
+    // W, tile by tile, with D on its diagonal: rows s, columns t of the accumulator are row t
+    // of the operand
 #pragma unroll
     for (int j = 0; j < (TRI + 3) / 4; ++j) {
       const int id = wave + 4 * j;
@@ -461,71 +460,58 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
       acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
       if (tt == ss) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = 4 * g + i <= c ? acc[i] : 0.f;
+        for (int i = 0; i < 4; ++i)
+          acc[i] = 4 * g + i <= c ? acc[i] + (4 * g + i == c ? D : 0.f) : 0.f;
       }
       *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(acc);
     }
     lds_barrier();
-    // y, rows p, columns t
     me.fresh();
     const int p0 = 16 * wave, py = pc + p0 + 4 * g;
-    const unsigned yoff =
-        (c * static_cast<unsigned>(a.yt) + p0 + 4 * g) * static_cast<unsigned>(sizeof(E));
-    ssm_half<E> sh[NP / 16], xf[L / 16];
+    ssm_half<E> sh[NP / 16];
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) sh[j] = to_half<E>(st[j]);
+    ssm_state_update<E, NP, L>(
+        kt, vt, m.b, m.x, p0, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
+    // y, rows p, columns t
+    ssm_half<E> xf[L / 16];
 #pragma unroll
     for (int j = 0; j < L / 16; ++j) xf[j] = vt.col(m.x, p0, 16 * j);
-    f32x4 in[L / 16];
-    float bad = 0.f;
+    // A non-finite x_s times the zero weight of an earlier token is NaN.  It has made the
+    // state's column non-finite too, which one row of it tells: the sums are then formed
+    // over s <= t alone.
+    const bool bad = __any(!(fabsf(st[0][0]) < INFINITY));
+    const unsigned yoff =
+        (c * static_cast<unsigned>(a.yt) + p0 + 4 * g) * static_cast<unsigned>(sizeof(E));
 #pragma unroll
     for (int tt = 0; tt < L / 16; ++tt) {
-      in[tt] = f32x4{};
-#pragma unroll
-      for (int j = 0; j <= tt; j += 2)
-        in[tt] = mac2(xf[j], xf[j + 1], wt.row(m.w, 16 * tt, 16 * j),
-                      wt.row(m.w, 16 * tt, 16 * j + 16), in[tt]);
-      bad = fmaf(in[tt][0], 0.f, fmaf(in[tt][1], 0.f, fmaf(in[tt][2], 0.f, fmaf(in[tt][3], 0.f, bad))));
-    }
-    ssm_stretch();
-    // A non-finite x_s times the zero weight of an earlier token is NaN: such sums are
-    // formed again over s <= t alone.
-    if (__any(bad != bad)) {
-      f32x4 sum[L / 16] = {};
-#pragma nounroll
-      for (int s = 0; s < L; ++s) {
-        const f32x4 v = half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
-#pragma unroll
-        for (int tt = 0; tt < L / 16; ++tt)
-          if (s <= 16 * tt + c) sum[tt] += to_f32(m.w[WT::at(16 * tt + c, s)]) * v;
-      }
-#pragma unroll
-      for (int tt = 0; tt < L / 16; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(fabsf(in[tt][i]) < INFINITY)) in[tt][i] = sum[tt][i];
-    }
-#pragma unroll
-    for (int tt = 0; tt < L / 16; ++tt) {
+      const int t = 16 * tt + c;
       f32x4 acc = {};
 #pragma unroll
       for (int j = 0; j < NP / 16; j += 2)
         acc = mac2(sh[j], sh[j + 1], kt.row(m.c, 16 * tt, 16 * j),
                    kt.row(m.c, 16 * tt, 16 * j + 16), acc);
-      const int t = 16 * tt + c;
-      const f32x4 out = m.log.since[t] * acc + (D * half_f32(vt.row(m.x, 16 * tt, p0)) + in[tt]);
+      acc *= m.log.since[t];
+      if (bad) {
+#pragma nounroll
+        for (int s = 0; s <= t; ++s)
+          acc += to_f32(m.w[WT::at(t, s)]) *
+                 half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
+      } else {
+#pragma unroll
+        for (int j = 0; j <= tt; j += 2)
+          acc = mac2(xf[j], xf[j + 1], wt.row(m.w, 16 * tt, 16 * j),
+                     wt.row(m.w, 16 * tt, 16 * j + 16), acc);
+      }
       if (t < rows) {
         E* row = y + 16 * tt * a.yt;
         if constexpr (VEC)
-          ssm_store4<true>(reinterpret_cast<E*>(reinterpret_cast<char*>(row) + yoff), out, py, a.P);
+          ssm_store4<true>(reinterpret_cast<E*>(reinterpret_cast<char*>(row) + yoff), acc, py, a.P);
         else
-          ssm_store4<false>(row + c * a.yt + p0 + 4 * g, out, py, a.P);
+          ssm_store4<false>(row + c * a.yt + p0 + 4 * g, acc, py, a.P);
       }
       ssm_stretch();
     }
-    ssm_state_update<E, NP, L>(
-        kt, vt, m.b, m.x, p0, m.log.all,
-        [&](int s) { return m.log.four(m.log.push, s); }, st);
     y += L * a.yt;
   }
   if (a.S_out && at.span == a.spans - 1)
@@ -735,23 +721,13 @@ struct SsmRecord {
   }
 };
 
-// Sums over the 16 lanes c of a row of lanes (DPP), over the four rows g, over all.
-__device__ __forceinline__ float sum_c(float v) {
-  const auto move = [](float x, auto ctrl) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x),
-                                                              decltype(ctrl)::value, 0xF, 0xF, true));
-  };
-  v += move(v, std::integral_constant<int, 0xB1>{});   // lane ^ 1
-  v += move(v, std::integral_constant<int, 0x4E>{});   // lane ^ 2
-  v += move(v, std::integral_constant<int, 0x141>{});  // 7 - lane of 8
-  v += move(v, std::integral_constant<int, 0x140>{});  // 15 - lane of 16
-  return v;
-}
+// Sums over the 16 lanes c of a g, over the four g, over all.
+__device__ __forceinline__ float sum_c(float v) { return sum_group<16>(v); }
 __device__ __forceinline__ float sum_g(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
-__device__ __forceinline__ float sum_wave(float v) { return sum_g(sum_c(v)); }
+__device__ __forceinline__ float sum_wave(float v) { return sum_group<64>(v); }
 
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
