@@ -670,9 +670,10 @@ struct __attribute__((aligned(16))) SsmGradLds {
   E st[ssm_planes<E>() * SsmTile<E, NP>::size(kSsmP)];
   E w[SsmTile<E, L>::size(L)], mw[SsmTile<E, L>::size(L)];
   SsmChunkLog log;
-  float row[4][64], col[4][64], diag[64];   // pair sums by tile of the other index
+  float row[4][64], col[4][64];             // pair sums by tile of the other index
+  float diag[64], trace[64];                // of (C B^T) M exp(l_t - l_s), of M
   float q[NP / 16][64], k[kSsmP / 16][64];  // state terms by tile of n, of p
-  float dot[kWaves], dd[kWaves];
+  float dot[kWaves];
 };
 
 // The pieces of a chunk record that a thread moves: the same ones of every plane.
@@ -699,23 +700,26 @@ struct SsmRecord {
         *reinterpret_cast<uint4*>(p + q * SsmTile<E, NP>::size(kSsmP)) = r[q][j];
     }
   }
-  // The sum of products of this record's values with another's.
+  // The sum of products of this record's values with another's; bf16 planes: of hi hi,
+  // hi lo and lo hi (lo lo is below 2^-16 of it).
   __device__ __forceinline__ float dot(const SsmRecord& o) const {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      float u[V], w[V];
-      load_vec<V>(reinterpret_cast<const E*>(&r[0][j]), u);
-      load_vec<V>(reinterpret_cast<const E*>(&o.r[0][j]), w);
       if constexpr (PL == 2) {
-        float ul[V], wl[V];
-        load_vec<V>(reinterpret_cast<const E*>(&r[1][j]), ul);
-        load_vec<V>(reinterpret_cast<const E*>(&o.r[1][j]), wl);
+        struct Words { bf16x2 w[4]; };
+        const Words a = __builtin_bit_cast(Words, r[0][j]), al = __builtin_bit_cast(Words, r[1][j]);
+        const Words b = __builtin_bit_cast(Words, o.r[0][j]), bl = __builtin_bit_cast(Words, o.r[1][j]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) u[i] += ul[i], w[i] += wl[i];
+        for (int i = 0; i < 4; ++i) {
+          sum = __builtin_amdgcn_fdot2_f32_bf16(a.w[i], b.w[i], sum, false);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(a.w[i], bl.w[i], sum, false);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(al.w[i], b.w[i], sum, false);
+        }
+      } else {
+        const float4 a = __builtin_bit_cast(float4, r[0][j]), b = __builtin_bit_cast(float4, o.r[0][j]);
+        sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, sum))));
       }
-#pragma unroll
-      for (int i = 0; i < V; ++i) sum = fmaf(u[i], w[i], sum);
     }
     return sum;
   }
@@ -800,8 +804,8 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
                      kt.row(m.c, 16 * tt, k), kt.row(m.c, 16 * tt, k + 16), cb[j]);
     }
   }
-  f32x4 mm[TW];
-  float qs[TN], ks[TP], dot = 0.f, dd = 0.f;
+  f32x4 mm[TW], dec[TW];  // M, exp(l_t - l_s) with zeros at s > t
+  float qs[TN], ks[TP], dot = 0.f;
   for (int turn = 0; turn < turns; ++turn) {
     const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP;
     const float D = a.D ? a.D[h] : 0.f;
@@ -812,7 +816,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       for (int j = 0; j < TN; ++j) qs[j] = 0.f;
 #pragma unroll
       for (int j = 0; j < TP; ++j) ks[j] = 0.f;
-      dot = dd = 0.f;
+      dot = 0.f;
     }
     // x, dy and st were last read before the barrier that ended the head before; within a
     // head its blocks have none there
@@ -829,12 +833,18 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       if (wave + WV * j >= TRI) break;
       int tt, ss;
       ssm_tri(wave + WV * j, tt, ss);
-      if (pb == 0) {  // W
+      if (pb == 0) {  // W, with D on its diagonal
         const int t = 16 * tt + c, s = 16 * ss + 4 * g;
-        f32x4 w = cb[j] * m.log.decay(t, s) * m.log.four(m.log.step, s);
+        dec[j] = m.log.decay(t, s);
         if (tt == ss) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = 4 * g + i <= c ? w[i] : 0.f;
+          for (int i = 0; i < 4; ++i) dec[j][i] = 4 * g + i <= c ? dec[j][i] : 0.f;
+        }
+        f32x4 w = cb[j] * dec[j] * m.log.four(m.log.step, s);
+        if (tt == ss) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = 4 * g + i <= c ? w[i] + (4 * g + i == c ? D : 0.f) : 0.f;
         }
         *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
@@ -870,9 +880,8 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         const float since = m.log.since[16 * tt + c];
 #pragma unroll
         for (int i = 0; i < NN; ++i) {
-          acc[i][j] *= since;
-          qs[j] += dot4(half_f32(kt.row(m.c, 16 * tt, n0 + 16 * i)), acc[i][j]);
-          dC[i][j] += acc[i][j];
+          qs[j] = fmaf(since, dot4(half_f32(kt.row(m.c, 16 * tt, n0 + 16 * i)), acc[i][j]), qs[j]);
+          dC[i][j] += since * acc[i][j];
         }
       }
     }
@@ -926,20 +935,14 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
           }
       }
       ssm_stretch();
-      f32x4 skip[PP][TP];  // D dy
 #pragma unroll
       for (int j = 0; j < TP; ++j) {
         const int ss = tp + WS * j;
-        const float left = m.log.left[16 * ss + c], step = m.log.step[16 * ss + c];
+        const float left = m.log.left[16 * ss + c], push = m.log.push[16 * ss + c];
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
-          const f32x4 xr = half_f32(vt.row(m.x, 16 * ss, p0 + 16 * i));
-          const f32x4 yr = half_f32(vt.row(m.dy, 16 * ss, p0 + 16 * i));
-          acc[i][j] *= left;
-          ks[j] += dot4(xr, acc[i][j]);
-          dd += dot4(xr, yr);
-          acc[i][j] *= step;
-          skip[i][j] = D * yr;
+          ks[j] = fmaf(left, dot4(half_f32(vt.row(m.x, 16 * ss, p0 + 16 * i)), acc[i][j]), ks[j]);
+          acc[i][j] *= push;
         }
       }
       ssm_stretch();
@@ -965,7 +968,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
           const int p = pc + p0 + 16 * i + 4 * g;
-          if (s < rows) ssm_store4<VEC>(row + p, acc[i][j] + skip[i][j], p, a.P);
+          if (s < rows) ssm_store4<VEC>(row + p, acc[i][j], p, a.P);
         }
       }
     }
@@ -980,18 +983,14 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       int tt, ss;
       ssm_tri(wave + WV * j, tt, ss);
       const int t = 16 * tt + c, s = 16 * ss + 4 * g;
-      f32x4 f = mm[j] * m.log.decay(t, s);
-      if (tt == ss) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = 4 * g + i <= c ? f[i] : 0.f;
-      }
+      const f32x4 f = mm[j] * dec[j];
       f32x4 pair = f * cb[j];
       const f32x4 step = m.log.four(m.log.step, s);
       *reinterpret_cast<ssm_half<E>*>(m.mw + WT::at(t, s)) = to_half<E>(f * step);
       if (tt == ss) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (4 * g + i == c) m.diag[t] = pair[i], pair[i] = 0.f;
+          if (4 * g + i == c) m.diag[t] = pair[i], m.trace[t] = mm[j][i], pair[i] = 0.f;
       }
       const float row = sum_g(dot4(pair, step));
       if (g == 0) m.row[ss][t] = row;
@@ -1010,8 +1009,8 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       const float k = sum_g(ks[j]);
       if (g == 0) m.k[wave % WP][16 * (tp + WS * j) + c] = k;
     }
-    dot = sum_wave(dot), dd = sum_wave(dd);
-    if (lane == 0) m.dot[wave] = dot, m.dd[wave] = dd;
+    dot = sum_wave(dot);
+    if (lane == 0) m.dot[wave] = dot;
     lds_barrier();
     kt.fresh(), wt.fresh(), me.fresh();
     n0 = 16 * NN * (wave % WN), tn = wave / WN;
@@ -1063,9 +1062,9 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         if (lane + o2 < 64) tail += dn;
         if (lane >= o2) head += up;
       }
-      float through = 0.f, xy = 0.f;
+      float through = 0.f;
 #pragma unroll
-      for (int j = 0; j < WV; ++j) through += m.dot[j], xy += m.dd[j];
+      for (int j = 0; j < WV; ++j) through += m.dot[j];
       const float e = static_cast<float>(tail + (head - own) +
                                          static_cast<double>(m.log.all) * through);
       const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
@@ -1073,10 +1072,11 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
                   ddt);
       const float dA = sum_wave(in ? e * step : 0.f), db = sum_wave(in ? ddt : 0.f);
+      const float dD = sum_wave(in ? m.trace[t] : 0.f);
       if (lane == 0) {
         float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
         part[0] = dA;
-        part[a.H] = xy;
+        part[a.H] = dD;
         part[2 * a.H] = db;
       }
     }
@@ -1205,10 +1205,10 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     w.fwd = take(all);
     w.rev = take(all);
     w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(float));
-    // Heads of a group are split while there are fewer than about four workgroups per
-    // CU; each split adds fp32 sums of dB and dC to write and read.
+    // Heads of a group are split while there are fewer workgroups than two per CU (what
+    // LDS holds); each split adds fp32 sums of dB and dC to write and read.
     const long long wgs = static_cast<long long>(B) * G * NC;
-    long long split = (1024 + wgs - 1) / wgs;
+    long long split = (512 + wgs - 1) / wgs;
     if (split > H / G) split = H / G;
     w.head_block = static_cast<int>((H / G + split - 1) / split);
     w.blocks = (H / G + w.head_block - 1) / w.head_block;
