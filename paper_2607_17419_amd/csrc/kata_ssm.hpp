@@ -206,6 +206,32 @@ struct SsmRows {
 };
 
 // ---- steps and decays of a chunk -------------------------------------------------
+// Ends a stretch that the scheduler may reorder: operand reads of later stretches are not
+// moved up, where they would hold registers that the accumulators need.
+__device__ __forceinline__ void ssm_stretch() { __builtin_amdgcn_sched_barrier(0); }
+
+// Inclusive sums over a wave's lanes in fp64: within rows of 16 lanes by DPP shifts, then
+// the last lane of a row to the next row, of the first two rows to the last two.
+struct Halves64 {
+  int lo, hi;
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double x) {
+  const auto move = [](int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); };
+  const Halves64 h = __builtin_bit_cast(Halves64, x);
+  return x + __builtin_bit_cast(double, Halves64{move(h.lo), move(h.hi)});
+}
+__device__ __forceinline__ double scan_wave(double x) {
+  x = dpp_add<0x111, 0xF>(x);
+  x = dpp_add<0x112, 0xF>(x);
+  x = dpp_add<0x114, 0xF>(x);
+  x = dpp_add<0x118, 0xF>(x);
+  x = dpp_add<0x142, 0xA>(x);
+  return dpp_add<0x143, 0xC>(x);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // A first kernel forms them once for all others: per token {hi, lo, step, gate} with the
 // running sum l = hi + lo of step A over the chunk in units of log 2 (summed in fp64:
 // differences of l keep 2^-48 of the largest, and exp(l_t - l_s) is right where a strong
@@ -233,22 +259,12 @@ __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   // 2^-2000 and 2^2000 are 0 and inf in fp32: bounded, sums and their differences stay finite
   l = l < -2000.0 ? -2000.0 : (l > 2000.0 ? 2000.0 : l);  // (NaN stays)
   if (!live) l = 0.0;
-#pragma unroll
-  for (int o = 1; o < L; o <<= 1) {
-    const double up = __shfl_up(l, o);
-    if (lane >= o) l += up;
-  }
+  l = scan_wave(l);
   if (lane >= L) return;
   const float hi = static_cast<float>(l);
   a.logs[(static_cast<size_t>(b * a.H + h) * NC + chunk) * L + lane] =
       make_float4(hi, isfinite(hi) ? static_cast<float>(l - hi) : 0.f, step, gate);
 }
-
-// Ends a stretch that the scheduler may reorder: operand reads of later stretches are not
-// moved up, where they would hold registers that the accumulators need.
-__device__ __forceinline__ void ssm_stretch() { __builtin_amdgcn_sched_barrier(0); }
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A chunk's logs in LDS, with exp(l_t) (since) and exp(l_L - l_t) (left); all = exp(l_L).
 struct __attribute__((aligned(16))) SsmChunkLog {
@@ -366,9 +382,8 @@ __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::
 // next to each other, so that their group's B and C rows come from HBM once.
 struct SsmPlace {
   int b, span, pb, h;
-  __device__ __forceinline__ SsmPlace(const SsmArgs& a, int spans) {
+  __device__ __forceinline__ SsmPlace(const SsmArgs& a, int spans, unsigned id) {
     const int blocks = (a.P + kSsmP - 1) / kSsmP;
-    unsigned id = ssm_xcd_order();
     h = id % a.H, id /= a.H;
     pb = id % blocks, id /= blocks;
     span = id % spans;
@@ -399,7 +414,7 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
   typename KT::Lane kt;
   typename VT::Lane vt;
   typename WT::Lane wt;
-  const SsmPlace at(a, a.spans);
+  const SsmPlace at(a, a.spans, ssm_xcd_order());
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   SsmSelf me;
   const int &wave = me.wave, &c = me.c, &g = me.g;
@@ -519,11 +534,12 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
 }
 
 // ---- states of spans and chunks --------------------------------------------------
-// REV = false: S over keys B and values x; true: R over keys C and values dy, from a
-// span's last chunk to its first.  CHUNKS = false: a span's own contribution and its
-// decay, to rec; true: from the span's state in rec, every chunk's state before its
-// tokens are added (S at the chunk's start, R at its end), to `chunks`: operand planes
-// (bf16 hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.
+// Forward: S over keys B and values x; reverse: R over keys C and values dy, from a
+// span's last chunk to its first; a launch does the first `dirs` of the two, half of its
+// workgroups each.  CHUNKS = false: a span's own contribution and its decay, to rec;
+// true: from the span's state in rec, every chunk's state before its tokens are added (S
+// at the chunk's start, R at its end), to `chunks` (R's behind S's): operand planes (bf16
+// hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.
 template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1; }
 
 template <typename E, int NP>
@@ -533,16 +549,19 @@ struct __attribute__((aligned(16))) SsmStateLds {
   SsmChunkLog log;
 };
 
-template <typename E, int NP, bool REV, bool CHUNKS, bool VEC>
-__global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
+template <typename E, int NP, bool CHUNKS, bool VEC>
+__global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, int dirs) {
   constexpr int L = ssm_chunk<E>();
   __shared__ SsmStateLds<E, NP> m;
   typename SsmTile<E, NP>::Lane kl;
   typename SsmTile<E, kSsmP>::Lane vl;
   // without CHUNKS the forward's last and the reverse's first span go nowhere
-  SsmPlace at(a, CHUNKS ? a.spans : a.spans - 1);
+  unsigned id = ssm_xcd_order();
+  const bool rev = id >= gridDim.x / dirs;
+  if (rev) id -= gridDim.x / dirs;
+  SsmPlace at(a, CHUNKS ? a.spans : a.spans - 1, id);
   const int slot = at.span;  // rec's, without CHUNKS
-  if (!CHUNKS && REV) ++at.span;
+  if (!CHUNKS && rev) ++at.span;
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   SsmSelf me;
   const int &wave = me.wave, &c = me.c, &g = me.g;
@@ -555,21 +574,21 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   const int gaps = a.spans - 1;
   f32x4 st[NP / 16];
   const float* from = nullptr;
-  if (CHUNKS && !REV && at.span > 0) from = a.rec + (static_cast<size_t>(bh) * gaps + at.span - 1) * NPs;
-  if (CHUNKS && REV && at.span < gaps) from = a.rec + (static_cast<size_t>(bh) * gaps + at.span) * NPs;
+  const size_t recs = (rev ? static_cast<size_t>(a.B) * a.H * gaps : 0) + static_cast<size_t>(bh) * gaps;
+  if (CHUNKS && (rev ? at.span < gaps : at.span > 0)) from = a.rec + (recs + at.span - !rev) * NPs;
   ssm_load_state<NP>(from, a.N, a.P, p, st);
-  const E* v = REV ? static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + pc
+  const E* v = rev ? static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + pc
                    : static_cast<const E*>(a.x) + b * a.xb + h * a.xh + pc;
-  const E* k = REV ? static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg
+  const E* k = rev ? static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg
                    : static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
-  const long long vt = REV ? a.yt : a.xt, kt = REV ? a.ct : a.bt;
+  const long long vt = rev ? a.yt : a.xt, kt = rev ? a.ct : a.bt;
   const float4* logs = ssm_log_row<L>(a, bh, NC);
   const int n = last > first ? (last - first + L - 1) / L : 0;
   const int steps = CHUNKS ? n - 1 : n;  // the state past the span's end is the next span's
   SsmRows<E, L, NP, 256, VEC> rk(kt);
   SsmRows<E, L, kSsmP, 256, VEC> rv(vt);
   float4 rl;
-  const auto start = [&](int i) { return first + (REV ? n - 1 - i : i) * L; };
+  const auto start = [&](int i) { return first + (rev ? n - 1 - i : i) * L; };
   const auto fetch = [&](int t0) {
     const int rows = min(L, last - t0);
     rk.load(k + t0 * kt, kt, rows, a.N);
@@ -581,7 +600,7 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
   for (int i = 0; i < n; ++i) {
     const int t0 = start(i);
     if constexpr (CHUNKS) {
-      E* rec = chunks + ((static_cast<size_t>(bh) * blocks + at.pb) * NC + t0 / L) *
+      E* rec = chunks + ((static_cast<size_t>(bh + (rev ? a.B * a.H : 0)) * blocks + at.pb) * NC + t0 / L) *
                             (ssm_planes<E>() * kSsmP * NP);
 #pragma unroll
       for (int j = 0; j < NP / 16; ++j) {
@@ -602,40 +621,38 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks) {
     if (!CHUNKS) log_sum += m.log.log;
     ssm_state_update<E, NP, L>(
         kl, vl, m.k, m.v, p0, m.log.all,
-        [&](int s) {
-          return m.log.four(REV ? m.log.since : m.log.push, s);
-        },
-        st);
+        [&](int s) { return m.log.four(rev ? m.log.since : m.log.push, s); }, st);
   }
   if constexpr (!CHUNKS) {
-    ssm_store_state<NP>(a.rec + (static_cast<size_t>(bh) * gaps + slot) * NPs, a.N, a.P, p, st);
-    if (threadIdx.x == 0 && at.pb == 0) a.rec_log[static_cast<size_t>(bh) * gaps + slot] = log_sum;
+    ssm_store_state<NP>(a.rec + (recs + slot) * NPs, a.N, a.P, p, st);
+    if (threadIdx.x == 0 && at.pb == 0) a.rec_log[recs + slot] = log_sum;
   }
 }
 
-// rec: a span's own contribution becomes the state that enters the next span (REV:
-// the one before), in the same slot.
-template <bool REV>
+// rec: a span's own contribution becomes the state that enters the next span (reverse:
+// the one before), in the same slot.  Grid: elements, heads, directions.
 __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
   const int NPs = a.N * a.P, gaps = a.spans - 1;
   const int e = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y;
+  const bool rev = blockIdx.z;
   if (e >= NPs) return;
-  float s = !REV && a.S_in ? a.S_in[static_cast<size_t>(bh) * NPs + e] : 0.f;
-  float* rec = a.rec + static_cast<size_t>(bh) * gaps * NPs + e;
-  const double* log = a.rec_log + static_cast<size_t>(bh) * gaps;
+  float s = !rev && a.S_in ? a.S_in[static_cast<size_t>(bh) * NPs + e] : 0.f;
+  const size_t recs = (static_cast<size_t>(rev) * a.B * a.H + bh) * gaps;
+  float* rec = a.rec + recs * NPs + e;
+  const double* log = a.rec_log + recs;
   constexpr int U = 8;  // records in flight
   for (int i = 0; i < gaps; i += U) {
     float v[U], d[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = min(i + u, gaps - 1), j = REV ? gaps - 1 - k : k;
+      const int k = min(i + u, gaps - 1), j = rev ? gaps - 1 - k : k;
       v[u] = rec[static_cast<size_t>(j) * NPs];
       d[u] = exp2_fast(static_cast<float>(log[j]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u >= gaps) break;
-      const int j = REV ? gaps - 1 - (i + u) : i + u;
+      const int j = rev ? gaps - 1 - (i + u) : i + u;
       s = fmaf(d[u], s, v[u]);
       rec[static_cast<size_t>(j) * NPs] = s;
     }
@@ -1053,19 +1070,17 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
       for (int j = 0; j < WP; ++j) k += m.k[j][t];
       const bool in = lane < rows;
-      double tail = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
-      const double own = in ? static_cast<double>(step) * k : 0.0;
-      double head = own;
-#pragma unroll
-      for (int o2 = 1; o2 < L; o2 <<= 1) {
-        const double dn = __shfl_down(tail, o2), up = __shfl_up(head, o2);
-        if (lane + o2 < 64) tail += dn;
-        if (lane >= o2) head += up;
-      }
+      const double after = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
+      const double before = in ? static_cast<double>(step) * k : 0.0;
+      // sum_{u >= t} after + sum_{s < t} before, from one running sum of their difference
+      const double diff = scan_wave(before - after), all = scan_wave(after);
+      const Halves64 last = __builtin_bit_cast(Halves64, all);
+      const double total = __builtin_bit_cast(
+          double, Halves64{__builtin_amdgcn_readlane(last.lo, 63), __builtin_amdgcn_readlane(last.hi, 63)});
       float through = 0.f;
 #pragma unroll
       for (int j = 0; j < WV; ++j) through += m.dot[j];
-      const float e = static_cast<float>(tail + (head - own) +
+      const float e = static_cast<float>(total + (diff - (before - after)) +
                                          static_cast<double>(m.log.all) * through);
       const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
       if (in)
@@ -1196,14 +1211,15 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
   };
   w.logs = take(static_cast<size_t>(B) * H * NC * L * sizeof(float4));
   const size_t gaps = static_cast<size_t>(B) * H * (w.spans - 1);
-  w.rec = take(gaps * N * P * sizeof(float));
-  w.log = take(gaps * sizeof(double));
+  const int dirs = backward ? 2 : 1;
+  w.rec = take(dirs * gaps * N * P * sizeof(float));
+  w.log = take(dirs * gaps * sizeof(double));
   w.blocks = 1, w.head_block = H / G;
   if (backward) {
     const size_t rec = static_cast<size_t>(kSsmP) * ssm_np(N) * 4;  // bf16: two planes
     const size_t all = static_cast<size_t>(B) * H * blocks * NC * rec;
-    w.fwd = take(all);
-    w.rev = take(all);
+    w.fwd = take(2 * all);
+    w.rev = w.fwd + all;
     w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(float));
     // Heads of a group are split while there are fewer workgroups than two per CU (what
     // LDS holds); each split adds fp32 sums of dB and dC to write and read.
@@ -1228,14 +1244,15 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     if (e_ != hipSuccess) return e_;       \
   } while (0)
 
-template <typename E, int NP, bool VEC, bool REV>
-hipError_t ssm_between_spans(const SsmArgs& a, hipStream_t st) {
+// The states between spans, forward (and reverse: dirs = 2).
+template <typename E, int NP, bool VEC>
+hipError_t ssm_between_spans(const SsmArgs& a, int dirs, hipStream_t st) {
   if (a.spans < 2) return hipSuccess;
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
-  auto kernel = ssm_state_kernel<E, NP, REV, false, VEC>;
-  kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1), 256, 0, st>>>(a, nullptr);
+  ssm_state_kernel<E, NP, false, VEC>
+      <<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1) * dirs, 256, 0, st>>>(a, nullptr, dirs);
   KATA_TRY(hipGetLastError());
-  ssm_span_scan<REV><<<dim3((a.N * a.P + 255) / 256, a.B * a.H), 256, 0, st>>>(a);
+  ssm_span_scan<<<dim3((a.N * a.P + 255) / 256, a.B * a.H, dirs), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -1250,7 +1267,7 @@ hipError_t ssm_logs(const SsmArgs& a, hipStream_t st) {
 template <typename E, int NP, bool VEC>
 hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, st)));
+  KATA_TRY((ssm_between_spans<E, NP, VEC>(a, 1, st)));
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
   auto kernel = ssm_out_kernel<E, NP, VEC>;
   kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans, 256, 0, st>>>(a);
@@ -1258,20 +1275,15 @@ hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
 }
 
 template <typename E, int NP, bool VEC>
-hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* fwd, E* rev, float* dA, float* dD,
+hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* chunks, float* dA, float* dD,
                       float* dbias, hipStream_t st) {
   const int blocks = (a.P + kSsmP - 1) / kSsmP, L = ssm_chunk<E>(), NC = (a.T + L - 1) / L;
-  const unsigned grid = static_cast<unsigned>(a.B) * a.H * blocks * a.spans;
-  auto f = ssm_state_kernel<E, NP, false, true, VEC>;
-  auto r = ssm_state_kernel<E, NP, true, true, VEC>;
-  auto d = ssm_grad_kernel<E, NP, VEC>;
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, st)));
-  f<<<grid, 256, 0, st>>>(a, fwd);
+  KATA_TRY((ssm_between_spans<E, NP, VEC>(a, 2, st)));
+  ssm_state_kernel<E, NP, true, VEC>
+      <<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans * 2, 256, 0, st>>>(a, chunks, 2);
   KATA_TRY(hipGetLastError());
-  KATA_TRY((ssm_between_spans<E, NP, VEC, true>(a, st)));
-  r<<<grid, 256, 0, st>>>(a, rev);
-  KATA_TRY(hipGetLastError());
+  auto d = ssm_grad_kernel<E, NP, VEC>;
   d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, ssm_grad_threads(NP), 0,
       st>>>(a, o);
   KATA_TRY(hipGetLastError());
@@ -1324,17 +1336,17 @@ hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, 
                       reinterpret_cast<float*>(base + w.part), base + w.fwd, base + w.rev,
                       w.head_block, w.blocks};
   if (bf16) {
-    bf16_t *f = reinterpret_cast<bf16_t*>(base + w.fwd), *r = reinterpret_cast<bf16_t*>(base + w.rev);
-#define KATA_CALL(K)                                                           \
-  (a.vec ? ssm_bwd_np<bf16_t, K, true>(a, o, f, r, dA, dD, dbias, st)          \
-         : ssm_bwd_np<bf16_t, K, false>(a, o, f, r, dA, dD, dbias, st))
+    bf16_t* chunks = reinterpret_cast<bf16_t*>(base + w.fwd);
+#define KATA_CALL(K)                                                        \
+  (a.vec ? ssm_bwd_np<bf16_t, K, true>(a, o, chunks, dA, dD, dbias, st)     \
+         : ssm_bwd_np<bf16_t, K, false>(a, o, chunks, dA, dD, dbias, st))
     KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
   }
-  float *f = reinterpret_cast<float*>(base + w.fwd), *r = reinterpret_cast<float*>(base + w.rev);
-#define KATA_CALL(K)                                                          \
-  (a.vec ? ssm_bwd_np<float, K, true>(a, o, f, r, dA, dD, dbias, st)          \
-         : ssm_bwd_np<float, K, false>(a, o, f, r, dA, dD, dbias, st))
+  float* chunks = reinterpret_cast<float*>(base + w.fwd);
+#define KATA_CALL(K)                                                       \
+  (a.vec ? ssm_bwd_np<float, K, true>(a, o, chunks, dA, dD, dbias, st)     \
+         : ssm_bwd_np<float, K, false>(a, o, chunks, dA, dD, dbias, st))
   KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
 }
