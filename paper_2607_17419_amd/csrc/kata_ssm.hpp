@@ -542,17 +542,18 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
 // hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.
 template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1; }
 
-template <typename E, int NP>
+template <typename E, int NP, bool CHUNKS>
 struct __attribute__((aligned(16))) SsmStateLds {
   static constexpr int L = ssm_chunk<E>();
   E k[SsmTile<E, NP>::size(L)], v[SsmTile<E, kSsmP>::size(L)];
+  E out[CHUNKS ? SsmTile<E, NP>::size(kSsmP) : 8];  // 16 rows of a record's plane per wave
   SsmChunkLog log;
 };
 
 template <typename E, int NP, bool CHUNKS, bool VEC>
 __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, int dirs) {
   constexpr int L = ssm_chunk<E>();
-  __shared__ SsmStateLds<E, NP> m;
+  __shared__ SsmStateLds<E, NP, CHUNKS> m;
   typename SsmTile<E, NP>::Lane kl;
   typename SsmTile<E, kSsmP>::Lane vl;
   // without CHUNKS the forward's last and the reverse's first span go nowhere
@@ -602,12 +603,28 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
     if constexpr (CHUNKS) {
       E* rec = chunks + ((static_cast<size_t>(bh + (rev ? a.B * a.H : 0)) * blocks + at.pb) * NC + t0 / L) *
                             (ssm_planes<E>() * kSsmP * NP);
+      // a wave's 16 rows of a plane are one piece of memory: turned in LDS (by this wave for
+      // itself), so that stores are whole lines
+      constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
+      typedef SsmTile<E, NP> KT;
+      E* mine = m.out + p0 * KT::stride;
 #pragma unroll
-      for (int j = 0; j < NP / 16; ++j) {
-        const SsmSplit<E> s(st[j]);
-        E* q = rec + (p0 + c) * NP + 16 * j + 4 * g;
-        *reinterpret_cast<ssm_half<E>*>(q) = s.hi;
-        if constexpr (sizeof(E) == 2) *reinterpret_cast<ssm_half<E>*>(q + kSsmP * NP) = s.lo;
+      for (int q = 0; q < ssm_planes<E>(); ++q) {
+#pragma unroll
+        for (int j = 0; j < NP / 16; ++j) {
+          const SsmSplit<E> s(st[j]);
+          ssm_half<E> h = s.hi;
+          if constexpr (sizeof(E) == 2) h = q ? s.lo : s.hi;
+          *reinterpret_cast<ssm_half<E>*>(mine + KT::at(c, 16 * j + 4 * g)) = h;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 16 * PER / 64; ++j) {
+          const int at = me.lane + 64 * j;
+          *reinterpret_cast<uint4*>(rec + q * kSsmP * NP + p0 * NP + at * V) =
+              *reinterpret_cast<const uint4*>(mine + KT::at(at / PER, at % PER * V));
+        }
+        __builtin_amdgcn_wave_barrier();
       }
       if (i >= steps) break;
     }
