@@ -152,38 +152,35 @@ template <typename E> constexpr int ssm_chunk() { return sizeof(E) == 2 ? 64 : 3
 
 // A token-major tensor's rows on their way into a tile: K pieces of 16 bytes per
 // thread, loaded a chunk ahead of their use.  Rows at or past `valid` and columns at or
-// past `cols` become zeros (their loads are moved to row 0, column 0, so that every
-// thread loads without a branch, and rows past a sequence's end are never read).  VEC:
-// rows are whole aligned pieces within 32-bit offsets; otherwise elements one by one.
+// past `cols` become zeros and are never read.  VEC (rows are whole aligned pieces, further
+// apart than their width and within 2^31 bytes): by buffer loads, whose bounds give the
+// zeros, one address register for all pieces and no branch; a branch between loads makes the
+// compiler wait for those before it, which cost three memory latencies per chunk.
+// Otherwise elements one by one.
 template <typename E, int ROWS, int COLS, int THREADS, bool VEC>
 struct SsmRows {
   static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = COLS / V;
   static constexpr int K = ROWS * PER / THREADS, kStep = THREADS / PER;  // rows between pieces
   static_assert(ROWS * PER % THREADS == 0, "every thread moves whole pieces");
   uint4 r[K];
-  unsigned off;  // bytes, of the first piece
-  static __device__ __forceinline__ int row() { return threadIdx.x / PER; }
-  static __device__ __forceinline__ int column() { return threadIdx.x % PER * V; }
-  __device__ __forceinline__ explicit SsmRows(long long stride)
-      : off((row() * static_cast<unsigned>(stride) + column()) * static_cast<unsigned>(sizeof(E))) {}
+  const SsmSelf& me;  // addresses are formed anew from its thread number
+  __device__ __forceinline__ int row() const { return me.thread / PER; }
+  __device__ __forceinline__ int column() const { return me.thread % PER * V; }
+  __device__ __forceinline__ explicit SsmRows(const SsmSelf& self) : me(self) {}
   __device__ __forceinline__ void load(const E* src, long long stride, int valid, int cols) {
     if constexpr (VEC) {
-      if (valid == ROWS && cols >= COLS) {  // the same for all threads
+      const int bytes = ((valid - 1) * static_cast<int>(stride) + min(cols, COLS)) *
+                        static_cast<int>(sizeof(E));
+      const auto buffer =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(src), 0, bytes, 0x00020000);
+      const unsigned step = kStep * static_cast<unsigned>(stride) * static_cast<unsigned>(sizeof(E));
+      const unsigned at = column() < cols ? (row() * static_cast<unsigned>(stride) + column()) *
+                                                static_cast<unsigned>(sizeof(E))
+                                          : 0x80000000u;  // out of bounds with any step
 #pragma unroll
-        for (int j = 0; j < K; ++j)
-          r[j] = *reinterpret_cast<const uint4*>(
-              reinterpret_cast<const char*>(src + j * kStep * stride) + off);
-      } else {
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-          const bool in = row() + j * kStep < valid && column() < cols;
-          const uint4 v = *reinterpret_cast<const uint4*>(
-              reinterpret_cast<const char*>(src) +
-              (in ? off + j * kStep * static_cast<unsigned>(stride) *
-                          static_cast<unsigned>(sizeof(E)) : 0u));
-          r[j] = in ? v : make_uint4(0, 0, 0, 0);
-        }
-      }
+      for (int j = 0; j < K; ++j)
+        r[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
+                                             buffer, static_cast<int>(at + j * step), 0, 0));
     } else {
 #pragma unroll
       for (int j = 0; j < K; ++j) {
@@ -195,6 +192,24 @@ struct SsmRows {
           if (at < valid && column() + k < cols) v.e[k] = p[k];
         r[j] = v.u;
       }
+    }
+  }
+  // Whether one of the pieces has a value that is not finite: an exponent of all ones.
+  __device__ __forceinline__ bool non_finite() const {
+    if constexpr (sizeof(E) == 2) {
+      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 most = {};
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        for (uint32_t w : {r[j].x, r[j].y, r[j].z, r[j].w})
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
+      return max(most.x, most.y) >= 0x7F80;
+    } else {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        for (uint32_t w : {r[j].x, r[j].y, r[j].z, r[j].w}) most = max(most, w & 0x7FFFFFFFu);
+      return most >= 0x7F800000u;
     }
   }
   __device__ __forceinline__ void store(E* dst) const {
@@ -313,16 +328,23 @@ __device__ __forceinline__ unsigned ssm_xcd_order() {
 }
 
 // ---- forward -------------------------------------------------------------------
-// A workgroup carries the state of one head (64 of its columns) over the chunks of
-// a span, as accumulators: wave w holds columns 16 w ...  Per chunk, the waves share
-// the tiles of W through LDS, then each forms its columns of y and of the new state,
-// while the next chunk's rows are on their way.
+// A workgroup carries the state of one head (64 of its columns) over the chunks of a
+// span, as accumulators: wave w holds columns 16 w ...  Per chunk a wave forms the
+// weights of 16 tokens, which as accumulators are already the operand that they are
+// needed as, and with them and all columns' states (shared through LDS as operands, a
+// chunk behind the accumulators) these tokens' y; then the new state of its columns.
+// The next chunk's rows are on their way meanwhile.  y is turned in LDS into whole lines.
+constexpr int ssm_most(int a, int b) { return a > b ? a : b; }
+
 template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmOutLds {
   static constexpr int L = ssm_chunk<E>();
-  E c[SsmTile<E, NP>::size(L)], b[SsmTile<E, NP>::size(L)], x[SsmTile<E, kSsmP>::size(L)],
-      w[SsmTile<E, L>::size(L)];
+  // a wave's part of st: 16 columns' states, or 16 rows of y
+  static constexpr int kPart = SsmTile<E, ssm_most(NP, kSsmP)>::size(16);
+  E c[SsmTile<E, NP>::size(L)], b[SsmTile<E, NP>::size(L)], x[SsmTile<E, kSsmP>::size(L)];
+  E st[4 * kPart];
   SsmChunkLog log;
+  int bad;  // the last chunk whose x has non-finite values
 };
 
 // The state's columns of this wave as accumulator tiles, from or to [N][P] fp32.
@@ -391,6 +413,29 @@ struct SsmPlace {
   }
 };
 
+// A 16-byte piece of a row, the first element at column p of P.
+template <bool VEC, typename E>
+__device__ __forceinline__ void ssm_store_piece(E* dst, uint4 v, int p, int P) {
+  if constexpr (VEC) {
+    if (p < P) *reinterpret_cast<uint4*>(dst) = v;
+  } else {
+    constexpr int V = 16 / static_cast<int>(sizeof(E));
+    const RawVec<E, V> e = *reinterpret_cast<const RawVec<E, V>*>(&v);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (p + i < P) dst[i] = e.e[i];
+  }
+}
+
+// Non-finite values replaced by zeros.
+template <typename E>
+__device__ __forceinline__ ssm_half<E> ssm_finite(ssm_half<E> h) {
+  f32x4 v = half_f32(h);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < INFINITY ? v[i] : 0.f;
+  return to_half<E>(v);
+}
+
 // Four neighbouring results of a row, the first at column p of P.
 template <bool VEC, typename E>
 __device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P) {
@@ -405,15 +450,16 @@ __device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P) {
 
 template <typename E, int NP, bool VEC>
 __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs a) {
-  constexpr int L = ssm_chunk<E>();
+  constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16;
+  constexpr int PW = LT == 4 ? 4 : 2;  // tiles of columns of which a wave forms y
   typedef SsmTile<E, NP> KT;
   typedef SsmTile<E, kSsmP> VT;
-  typedef SsmTile<E, L> WT;
-  constexpr int TRI = (L / 16) * (L / 16 + 1) / 2;
-  __shared__ SsmOutLds<E, NP> m;
+  typedef SsmTile<E, 16 * PW> YT;
+  typedef SsmOutLds<E, NP> Lds;
+  static_assert(YT::size(16) <= Lds::kPart && KT::size(16) <= Lds::kPart, "a wave's part");
+  __shared__ Lds m;
   typename KT::Lane kt;
   typename VT::Lane vt;
-  typename WT::Lane wt;
   const SsmPlace at(a, a.spans, ssm_xcd_order());
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   SsmSelf me;
@@ -425,7 +471,7 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
   const int first = at.span * span_len, last = min(first + span_len, len);
   const float D = a.D ? a.D[h] : 0.f;
   const size_t NPs = static_cast<size_t>(a.N) * a.P;
-  f32x4 st[NP / 16];
+  f32x4 st[NT];
   const float* from = at.span ? a.rec + (static_cast<size_t>(bh) * (a.spans - 1) + at.span - 1) * NPs
                               : (a.S_in ? a.S_in + bh * NPs : nullptr);
   ssm_load_state<NP>(from, a.N, a.P, pc + 16 * wave + c, st);
@@ -435,8 +481,8 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
   const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + first * a.ct;
   const float4* logs = ssm_log_row<L>(a, bh, NC) + first;
   E* y = static_cast<E*>(a.y) + b * a.yb + h * a.yh + pc + first * a.yt;
-  SsmRows<E, L, NP, 256, VEC> rc(a.ct), rb(a.bt);
-  SsmRows<E, L, kSsmP, 256, VEC> rx(a.xt);
+  SsmRows<E, L, NP, 256, VEC> rc(me), rb(me);
+  SsmRows<E, L, kSsmP, 256, VEC> rx(me);
   float4 rl;
   const auto fetch = [&](int t0) {
     const int rows = min(L, last - t0);
@@ -446,88 +492,106 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
     if (wave == 0) rl = *logs;
     Cm += L * a.ct, Bm += L * a.bt, x += L * a.xt, logs += L;
   };
-  if (first < last) fetch(first);
-  for (int i = threadIdx.x; i < WT::size(L); i += 256) store_f32(m.w + i, 0.f);
-  for (int t0 = first; t0 < last; t0 += L) {
-    const int rows = min(L, last - t0);
-    lds_barrier();
+  // a chunk's rows, and the state before it, into LDS
+  const auto stage = [&](int t0) {
     rc.store(m.c);
     rb.store(m.b);
     rx.store(m.x);
     if (wave == 0) m.log.template store<L>(rl);
+    if (rx.non_finite()) m.bad = t0;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+      *reinterpret_cast<ssm_half<E>*>(m.st + wave * Lds::kPart + KT::at(c, 16 * j + 4 * g)) =
+          to_half<E>(st[j]);
+  };
+  if (threadIdx.x == 0) m.bad = -1;
+  lds_barrier();
+  if (first < last) fetch(first), stage(first);
+  for (int t0 = first; t0 < last; t0 += L) {
+    const int rows = min(L, last - t0);
     lds_barrier();
     if (t0 + L < last) fetch(t0 + L);
-    kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
-    // W, tile by tile, with D on its diagonal: rows s, columns t of the accumulator are row t
-    // of the operand
+    kt.fresh(), vt.fresh(), me.fresh();
+    // the tile of tokens, turned with the workgroup: later tiles have more weights to form
+    const int tt = (wave + blockIdx.x) % LT, q0 = LT == 4 ? 0 : PW * (wave / LT);
+    const int t = 16 * tt + c;
+    ssm_half<E> cr[NT], w[LT];
 #pragma unroll
-    for (int j = 0; j < (TRI + 3) / 4; ++j) {
-      const int id = wave + 4 * j;
-      if (id >= TRI) break;
-      int tt, ss;
-      ssm_tri(id, tt, ss);
+    for (int k = 0; k < NT; ++k) cr[k] = kt.row(m.c, 16 * tt, 16 * k);
+#pragma unroll
+    for (int ss = 0; ss < LT; ++ss) {
+      w[ss] = ssm_half<E>{};
+      if (ss > tt) continue;
+      // C B^T, rows s, columns t: as a half, row t of W; D on the diagonal
       f32x4 acc = {};
 #pragma unroll
-      for (int k = 0; k < NP; k += 32)
-        acc = mac2(kt.row(m.b, 16 * ss, k), kt.row(m.b, 16 * ss, k + 16),
-                   kt.row(m.c, 16 * tt, k), kt.row(m.c, 16 * tt, k + 16), acc);
-      const int t = 16 * tt + c, s = 16 * ss + 4 * g;
+      for (int k = 0; k < NT; k += 2)
+        acc = mac2(kt.row(m.b, 16 * ss, 16 * k), kt.row(m.b, 16 * ss, 16 * k + 16), cr[k], cr[k + 1], acc);
+      const int s = 16 * ss + 4 * g;
       acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
       if (tt == ss) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           acc[i] = 4 * g + i <= c ? acc[i] + (4 * g + i == c ? D : 0.f) : 0.f;
       }
-      *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(acc);
+      w[ss] = to_half<E>(acc);
     }
-    lds_barrier();
-    me.fresh();
-    const int p0 = 16 * wave, py = pc + p0 + 4 * g;
-    ssm_half<E> sh[NP / 16];
-#pragma unroll
-    for (int j = 0; j < NP / 16; ++j) sh[j] = to_half<E>(st[j]);
-    ssm_state_update<E, NP, L>(
-        kt, vt, m.b, m.x, p0, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
+    ssm_stretch();
     // y, rows p, columns t
-    ssm_half<E> xf[L / 16];
+    const float since = m.log.since[t];
+    const bool bad = m.bad == t0;
+    ssm_half<E> out[PW];
 #pragma unroll
-    for (int j = 0; j < L / 16; ++j) xf[j] = vt.col(m.x, p0, 16 * j);
-    // A non-finite x_s times the zero weight of an earlier token is NaN.  It has made the
-    // state's column non-finite too, which one row of it tells: the sums are then formed
-    // over s <= t alone.
-    const bool bad = __any(!(fabsf(st[0][0]) < INFINITY));
-    const unsigned yoff =
-        (c * static_cast<unsigned>(a.yt) + p0 + 4 * g) * static_cast<unsigned>(sizeof(E));
-#pragma unroll
-    for (int tt = 0; tt < L / 16; ++tt) {
-      const int t = 16 * tt + c;
+    for (int j = 0; j < PW; ++j) {
+      const int p0 = 16 * (q0 + j);
+      const E* sp = m.st + (q0 + j) * Lds::kPart;
       f32x4 acc = {};
 #pragma unroll
-      for (int j = 0; j < NP / 16; j += 2)
-        acc = mac2(sh[j], sh[j + 1], kt.row(m.c, 16 * tt, 16 * j),
-                   kt.row(m.c, 16 * tt, 16 * j + 16), acc);
-      acc *= m.log.since[t];
-      if (bad) {
-#pragma nounroll
-        for (int s = 0; s <= t; ++s)
-          acc += to_f32(m.w[WT::at(t, s)]) *
-                 half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
-      } else {
+      for (int k = 0; k < NT; k += 2)
+        acc = mac2(kt.row(sp, 0, 16 * k), kt.row(sp, 0, 16 * k + 16), cr[k], cr[k + 1], acc);
+      acc *= since;
 #pragma unroll
-        for (int j = 0; j <= tt; j += 2)
-          acc = mac2(xf[j], xf[j + 1], wt.row(m.w, 16 * tt, 16 * j),
-                     wt.row(m.w, 16 * tt, 16 * j + 16), acc);
+      for (int ss = 0; ss < LT; ss += 2) {
+        if (ss > tt) continue;
+        auto x0 = vt.col(m.x, p0, 16 * ss), x1 = vt.col(m.x, p0, 16 * ss + 16);
+        if (bad) x0 = ssm_finite<E>(x0), x1 = ssm_finite<E>(x1);
+        acc = mac2(x0, x1, w[ss], w[ss + 1], acc);
       }
-      if (t < rows) {
-        E* row = y + 16 * tt * a.yt;
-        if constexpr (VEC)
-          ssm_store4<true>(reinterpret_cast<E*>(reinterpret_cast<char*>(row) + yoff), acc, py, a.P);
-        else
-          ssm_store4<false>(row + c * a.yt + p0 + 4 * g, acc, py, a.P);
+      // A non-finite x_s times the zero weight of an earlier token would be NaN: left out
+      // of the products, it makes the tokens from s on NaN here.
+      if (bad) {
+        bool seen[4] = {};
+#pragma nounroll
+        for (int s = 0; s <= t; ++s) {
+          const f32x4 v = half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) seen[i] |= !(fabsf(v[i]) < INFINITY);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = seen[i] ? NAN : acc[i];
       }
-      ssm_stretch();
+      out[j] = to_half<E>(acc);
     }
+    ssm_stretch();
+    ssm_state_update<E, NP, L>(
+        kt, vt, m.b, m.x, 16 * wave, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
+    lds_barrier();
+    // a wave's 16 rows of y, turned in its own part of st
+    E* mine = m.st + wave * Lds::kPart;
+#pragma unroll
+    for (int j = 0; j < PW; ++j)
+      *reinterpret_cast<ssm_half<E>*>(mine + YT::at(c, 16 * j + 4 * g)) = out[j];
+    __builtin_amdgcn_wave_barrier();
+    constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = 16 * PW / V;
+#pragma unroll
+    for (int j = 0; j < 16 * PER / 64; ++j) {
+      const int i = me.lane + 64 * j, r = 16 * tt + i / PER, col = i % PER * V;
+      const uint4 v = *reinterpret_cast<const uint4*>(mine + YT::at(i / PER, col));
+      if (r < rows) ssm_store_piece<VEC>(y + r * a.yt + 16 * q0 + col, v, pc + 16 * q0 + col, a.P);
+    }
+    __builtin_amdgcn_wave_barrier();
     y += L * a.yt;
+    if (t0 + L < last) stage(t0 + L);
   }
   if (a.S_out && at.span == a.spans - 1)
     ssm_store_state<NP>(a.S_out + bh * NPs, a.N, a.P, pc + 16 * wave + c, st);
@@ -586,8 +650,8 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
   const float4* logs = ssm_log_row<L>(a, bh, NC);
   const int n = last > first ? (last - first + L - 1) / L : 0;
   const int steps = CHUNKS ? n - 1 : n;  // the state past the span's end is the next span's
-  SsmRows<E, L, NP, 256, VEC> rk(kt);
-  SsmRows<E, L, kSsmP, 256, VEC> rv(vt);
+  SsmRows<E, L, NP, 256, VEC> rk(me);
+  SsmRows<E, L, kSsmP, 256, VEC> rv(me);
   float4 rl;
   const auto start = [&](int i) { return first + (rev ? n - 1 - i : i) * L; };
   const auto fetch = [&](int t0) {
@@ -717,21 +781,34 @@ struct SsmRecord {
   static constexpr int K = (N + THREADS - 1) / THREADS, PL = ssm_planes<E>();
   static_assert(N % THREADS == 0, "every thread moves whole pieces");
   uint4 r[PL][K];
+  const SsmSelf& me;
+  __device__ __forceinline__ explicit SsmRecord(const SsmSelf& self) : me(self) {}
   __device__ __forceinline__ void load(const E* rec) {
 #pragma unroll
     for (int q = 0; q < PL; ++q)
 #pragma unroll
       for (int j = 0; j < K; ++j)
-        r[q][j] = *reinterpret_cast<const uint4*>(rec + q * kSsmP * NP + (threadIdx.x + j * THREADS) * V);
+        r[q][j] = *reinterpret_cast<const uint4*>(rec + q * kSsmP * NP + (me.thread + j * THREADS) * V);
   }
   __device__ __forceinline__ void store(E* dst) const {
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      const int i = threadIdx.x + j * THREADS;
+      const int i = me.thread + j * THREADS;
       E* p = dst + SsmTile<E, NP>::at(i / PER, i % PER * V);
 #pragma unroll
       for (int q = 0; q < PL; ++q)
         *reinterpret_cast<uint4*>(p + q * SsmTile<E, NP>::size(kSsmP)) = r[q][j];
+    }
+  }
+  // This thread's pieces back.
+  __device__ __forceinline__ void read(const E* src) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int i = me.thread + j * THREADS;
+      const E* p = src + SsmTile<E, NP>::at(i / PER, i % PER * V);
+#pragma unroll
+      for (int q = 0; q < PL; ++q)
+        r[q][j] = *reinterpret_cast<const uint4*>(p + q * SsmTile<E, NP>::size(kSsmP));
     }
   }
   // The sum of products of this record's values with another's; bf16 planes: of hi hi,
@@ -771,7 +848,8 @@ __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
 }
 
-template <typename E, int NP, bool VEC>
+// ONE: P <= 64, a head is one block of columns
+template <typename E, int NP, bool VEC, bool ONE>
 __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, PT = kSsmP / 16;
   constexpr int THREADS = ssm_grad_threads(NP), WV = THREADS / 64;
@@ -788,7 +866,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
   typename KT::Lane kt;
   typename VT::Lane vt;
   typename WT::Lane wt;
-  const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
+  const int NC = (a.T + L - 1) / L, blocks = ONE ? 1 : (a.P + kSsmP - 1) / kSsmP;
   unsigned id = ssm_xcd_order();
   const int hb = id % o.blocks;
   id /= o.blocks;
@@ -800,25 +878,28 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
   const int &wave = me.wave, &lane = me.lane, &c = me.c, &g = me.g;
   const int h0 = grp * per + hb * o.head_block;
   const int turns = (min((hb + 1) * o.head_block, per) - hb * o.head_block) * blocks;
-  SsmRows<E, L, kSsmP, THREADS, VEC> rx(a.xt), ry(a.yt);
-  SsmRecord<E, NP, THREADS> rs, rr;
+  SsmRows<E, L, kSsmP, THREADS, VEC> rx(me), ry(me);
+  SsmRecord<E, NP, THREADS> rs(me), rr(me);
   float4 rl;
+  const auto record = [&](int turn) {
+    return ((static_cast<size_t>(b * a.H + h0 + turn / blocks) * blocks + turn % blocks) * NC + chunk) *
+           kRecord;
+  };
   const auto fetch = [&](int turn) {
     const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP, bh = b * a.H + h;
     rx.load(static_cast<const E*>(a.x) + b * a.xb + h * a.xh + t0 * a.xt + pc, a.xt, rows,
             a.P - pc);
     ry.load(static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc, a.yt, rows,
             a.P - pc);
-    const size_t rec = ((static_cast<size_t>(bh) * blocks + pb) * NC + chunk) * kRecord;
-    rs.load(static_cast<const E*>(o.fwd) + rec);
-    rr.load(static_cast<const E*>(o.rev) + rec);
+    rs.load(static_cast<const E*>(o.fwd) + record(turn));
     if (wave == 0) rl = ssm_log_row<L>(a, bh, NC)[t0];
   };
   {
-    SsmRows<E, L, NP, THREADS, VEC> rb(a.bt), rc(a.ct);
+    SsmRows<E, L, NP, THREADS, VEC> rb(me), rc(me);
     rb.load(static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt, a.bt, rows, a.N);
     rc.load(static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct, a.ct, rows, a.N);
     fetch(0);
+    rr.load(static_cast<const E*>(o.rev) + record(0));
     rb.store(m.b);
     rc.store(m.c);
   }
@@ -838,7 +919,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
                      kt.row(m.c, 16 * tt, k), kt.row(m.c, 16 * tt, k + 16), cb[j]);
     }
   }
-  f32x4 mm[TW], dec[TW];  // M, exp(l_t - l_s) with zeros at s > t
+  f32x4 mm[TW];  // M: rows s, columns t
   float qs[TN], ks[TP], dot = 0.f;
   for (int turn = 0; turn < turns; ++turn) {
     const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP;
@@ -852,14 +933,11 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       for (int j = 0; j < TP; ++j) ks[j] = 0.f;
       dot = 0.f;
     }
-    // x, dy and st were last read before the barrier that ended the head before; within a
-    // head its blocks have none there
-    if (blocks > 1) lds_barrier();
+    // x, dy and st were last read before the barrier that ended the turn before
     rx.store(m.x);
     ry.store(m.dy);
     rs.store(m.st);
     if (wave == 0 && pb == 0) m.log.template store<L>(rl);
-    dot += rs.dot(rr);
     lds_barrier();
     kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
 #pragma unroll
@@ -867,14 +945,22 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       if (wave + WV * j >= TRI) break;
       int tt, ss;
       ssm_tri(wave + WV * j, tt, ss);
-      if (pb == 0) {  // W, with D on its diagonal
-        const int t = 16 * tt + c, s = 16 * ss + 4 * g;
-        dec[j] = m.log.decay(t, s);
-        if (tt == ss) {
+      const int t = 16 * tt + c, s = 16 * ss + 4 * g;
+      f32x4 acc = ONE ? f32x4{} : mm[j];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) dec[j][i] = 4 * g + i <= c ? dec[j][i] : 0.f;
-        }
-        f32x4 w = cb[j] * dec[j] * m.log.four(m.log.step, s);
+      for (int k = 0; k < kSsmP; k += 32)
+        acc = mac2(vt.row(m.x, 16 * ss, k), vt.row(m.x, 16 * ss, k + 16),
+                   vt.row(m.dy, 16 * tt, k), vt.row(m.dy, 16 * tt, k + 16), acc);
+      if (!ONE) mm[j] = acc;
+      if (pb != 0 && pb + 1 != blocks) continue;
+      f32x4 dec = m.log.decay(t, s);
+      const f32x4 step = m.log.four(m.log.step, s);
+      if (tt == ss) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dec[i] = 4 * g + i <= c ? dec[i] : 0.f;
+      }
+      if (pb == 0) {  // W, with D on its diagonal
+        f32x4 w = cb[j] * dec * step;
         if (tt == ss) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -882,10 +968,23 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         }
         *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
+      if (pb + 1 != blocks) continue;
+      // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
+      // over s < t with step_s (row), over t > s (col), s = t
+      const f32x4 f = acc * dec;
+      f32x4 pair = f * cb[j];
+      *reinterpret_cast<ssm_half<E>*>(m.mw + WT::at(t, s)) = to_half<E>(f * step);
+      if (tt == ss) {
 #pragma unroll
-      for (int k = 0; k < kSsmP; k += 32)  // M^T: rows s, columns t
-        mm[j] = mac2(vt.row(m.x, 16 * ss, k), vt.row(m.x, 16 * ss, k + 16),
-                     vt.row(m.dy, 16 * tt, k), vt.row(m.dy, 16 * tt, k + 16), mm[j]);
+        for (int i = 0; i < 4; ++i)
+          if (4 * g + i == c) m.diag[t] = pair[i], m.trace[t] = acc[i], pair[i] = 0.f;
+      }
+      const float row = sum_g(dot4(pair, step));
+      if (g == 0) m.row[ss][t] = row;
+      f32x4 col;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) col[i] = sum_c(pair[i]);
+      if (c == 0) *reinterpret_cast<f32x4*>(&m.col[tt][s]) = col;
     }
     ssm_stretch();
     // exp(l_t) S dy_t, and its product with C_t
@@ -920,7 +1019,10 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       }
     }
     lds_barrier();
+    rs.read(m.st);  // again, its registers having served others meanwhile
+    dot += rs.dot(rr);
     rr.store(m.st);
+    ssm_stretch();
     if (turn + 1 < turns) fetch(turn + 1);
     lds_barrier();
     // exp(l_L - l_s) step_s R x_s: dB alone reads it, so R's leading bf16 is enough
@@ -1007,32 +1109,12 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       }
     }
     ssm_stretch();
-    if (pb + 1 < blocks) continue;
-    me.fresh();
-    // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
-    // over s < t with step_s (row), over t > s (col), s = t
-#pragma unroll
-    for (int j = 0; j < TW; ++j) {
-      if (wave + WV * j >= TRI) break;
-      int tt, ss;
-      ssm_tri(wave + WV * j, tt, ss);
-      const int t = 16 * tt + c, s = 16 * ss + 4 * g;
-      const f32x4 f = mm[j] * dec[j];
-      f32x4 pair = f * cb[j];
-      const f32x4 step = m.log.four(m.log.step, s);
-      *reinterpret_cast<ssm_half<E>*>(m.mw + WT::at(t, s)) = to_half<E>(f * step);
-      if (tt == ss) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (4 * g + i == c) m.diag[t] = pair[i], m.trace[t] = mm[j][i], pair[i] = 0.f;
-      }
-      const float row = sum_g(dot4(pair, step));
-      if (g == 0) m.row[ss][t] = row;
-      f32x4 col;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) col[i] = sum_c(pair[i]);
-      if (c == 0) *reinterpret_cast<f32x4*>(&m.col[tt][s]) = col;
+    if (pb + 1 < blocks) {
+      lds_barrier();
+      rr.load(static_cast<const E*>(o.rev) + record(turn + 1));
+      continue;
     }
+    me.fresh();
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const float q = sum_g(qs[j]);
@@ -1048,6 +1130,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     lds_barrier();
     kt.fresh(), wt.fresh(), me.fresh();
     n0 = 16 * NN * (wave % WN), tn = wave / WN;
+    if (turn + 1 < turns) rr.load(static_cast<const E*>(o.rev) + record(turn + 1));
 #pragma unroll
     for (int k = 0; k < L; k += 32) {
       ssm_half<E> kb[NN][2], kc[NN][2];
@@ -1300,9 +1383,10 @@ hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* chunks, float* dA,
   ssm_state_kernel<E, NP, true, VEC>
       <<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans * 2, 256, 0, st>>>(a, chunks, 2);
   KATA_TRY(hipGetLastError());
-  auto d = ssm_grad_kernel<E, NP, VEC>;
-  d<<<static_cast<unsigned>(a.B) * NC * a.G * o.blocks, ssm_grad_threads(NP), 0,
-      st>>>(a, o);
+  const unsigned grid = static_cast<unsigned>(a.B) * NC * a.G * o.blocks;
+  constexpr int threads = ssm_grad_threads(NP);
+  if (VEC && blocks == 1) ssm_grad_kernel<E, NP, VEC, VEC><<<grid, threads, 0, st>>>(a, o);
+  else ssm_grad_kernel<E, NP, VEC, false><<<grid, threads, 0, st>>>(a, o);
   KATA_TRY(hipGetLastError());
   if (o.blocks > 1) {
     const size_t all = static_cast<size_t>(a.B) * a.T * a.G * a.N;
