@@ -682,33 +682,38 @@ def _on_stream(call):
     @functools.wraps(call)
     def run(first, *args, stream=None, **kw):
         import torch
-        if not first.is_cuda:
+        device = first.get_device()
+        if device < 0:
             raise ValueError("expected device tensors")
-        if stream is not None:
-            if stream.device != first.device:
-                raise ValueError(f"stream of {stream.device}, tensors of {first.device}")
-            with torch.cuda.stream(stream):
+        if stream is None:
+            if device == torch._C._cuda_getDevice():
                 return call(first, *args, **kw)
-        if first.device.index != torch.cuda.current_device():
             with torch.cuda.device(first.device):
                 return call(first, *args, **kw)
-        return call(first, *args, **kw)
+        if stream.device != first.device:
+            raise ValueError(f"stream of {stream.device}, tensors of {first.device}")
+        with torch.cuda.stream(stream):
+            return call(first, *args, **kw)
     return run
 
 
+_ANY = "any"  # strides over the innermost dimension too
+
+
 def _tensor(t, name, like, shape, dtype, strided=False):
-    """The address of a tensor of this shape and type on like's device."""
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.device != like.device:
+    """The address of a tensor of this shape (a tuple) and type on like's device.  Few steps: of
+    a single token's call these checks are half of the host's time."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != like.get_device():
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if strided:
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if not t.is_contiguous():
+        if not strided:
+            raise ValueError(f"{name} must be contiguous")
+        if strided is not _ANY and shape[-1] > 1 and t.stride(-1) != 1:
             raise ValueError(f"{name}'s innermost dimension must be contiguous")
-    elif not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
@@ -725,9 +730,10 @@ def _workspace(given, nbytes, like):
 
 
 def _dims(t, n, what):
-    if t.dim() != n:
-        raise ValueError(f"expected {what}, got {tuple(t.shape)}")
-    return t.shape
+    s = t.shape
+    if len(s) != n:
+        raise ValueError(f"expected {what}, got {tuple(s)}")
+    return s
 
 
 @_on_stream
@@ -884,10 +890,8 @@ def _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, tokens):
     lead, (H, P) = x.shape[:-2], _dims(x, n, "x [B,T,H,P]" if tokens else "x [B,H,P]")[-2:]
     G, N = _dims(Bm, n, "Bm [B,T,G,N]" if tokens else "Bm [B,G,N]")[-2:]
     f32 = torch.float32
-    if dt.dim() != n - 1:
-        raise ValueError(f"dt must be {tuple(lead) + (H,)}, got {tuple(dt.shape)}")
     args = (_tensor(x, "x", x, x.shape, x.dtype, True),
-            _tensor(dt.unsqueeze(-1), "dt", x, (*lead, H, 1), x.dtype, True),
+            _tensor(dt, "dt", x, (*lead, H), x.dtype, _ANY),
             _tensor(A, "A", x, (H,), f32), _tensor(Bm, "Bm", x, (*lead, G, N), x.dtype, True),
             _tensor(Cm, "Cm", x, (*lead, G, N), x.dtype, True), _optional(D, "D", x, (H,), f32),
             _optional(dt_bias, "dt_bias", x, (H,), f32))

@@ -264,11 +264,8 @@ __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   if (live) {
     const float z = to_f32(static_cast<const E*>(a.dt)[b * a.db + h * a.dh + t * a.dt_t]) +
                     (a.bias ? a.bias[h] : 0.f);
-    step = z, gate = 1.f;
-    if (a.softplus) {
-      step = z > 20.f ? z : log1pf(expf(z));
-      gate = sigmoid(z);
-    }
+    step = a.softplus ? softplus(z) : z;
+    gate = a.softplus ? sigmoid(z) : 1.f;
   }
   double l = static_cast<double>(step) * (static_cast<double>(a.A[h]) * 1.4426950408889634074);
   // 2^-2000 and 2^2000 are 0 and inf in fp32: bounded, sums and their differences stay finite
@@ -516,6 +513,10 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
     const int tt = (wave + blockIdx.x) % LT, q0 = LT == 4 ? 0 : PW * (wave / LT);
     const int t = 16 * tt + c;
     ssm_half<E> cr[NT], w[LT];
+    bool above[4];  // the diagonal
+    float skip[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c, skip[i] = 4 * g + i == c ? D : 0.f;
 #pragma unroll
     for (int k = 0; k < NT; ++k) cr[k] = kt.row(m.c, 16 * tt, 16 * k);
 #pragma unroll
@@ -531,47 +532,49 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
       acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
       if (tt == ss) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          acc[i] = 4 * g + i <= c ? acc[i] + (4 * g + i == c ? D : 0.f) : 0.f;
+        for (int i = 0; i < 4; ++i) acc[i] = above[i] ? 0.f : acc[i] + skip[i];
       }
       w[ss] = to_half<E>(acc);
     }
     ssm_stretch();
     // y, rows p, columns t
     const float since = m.log.since[t];
-    const bool bad = m.bad == t0;
     ssm_half<E> out[PW];
+    const auto columns = [&](auto finite) {
 #pragma unroll
-    for (int j = 0; j < PW; ++j) {
-      const int p0 = 16 * (q0 + j);
-      const E* sp = m.st + (q0 + j) * Lds::kPart;
-      f32x4 acc = {};
+      for (int j = 0; j < PW; ++j) {
+        const int p0 = 16 * (q0 + j);
+        const E* sp = m.st + (q0 + j) * Lds::kPart;
+        f32x4 acc = {};
 #pragma unroll
-      for (int k = 0; k < NT; k += 2)
-        acc = mac2(kt.row(sp, 0, 16 * k), kt.row(sp, 0, 16 * k + 16), cr[k], cr[k + 1], acc);
-      acc *= since;
+        for (int k = 0; k < NT; k += 2)
+          acc = mac2(kt.row(sp, 0, 16 * k), kt.row(sp, 0, 16 * k + 16), cr[k], cr[k + 1], acc);
+        acc *= since;
 #pragma unroll
-      for (int ss = 0; ss < LT; ss += 2) {
-        if (ss > tt) continue;
-        auto x0 = vt.col(m.x, p0, 16 * ss), x1 = vt.col(m.x, p0, 16 * ss + 16);
-        if (bad) x0 = ssm_finite<E>(x0), x1 = ssm_finite<E>(x1);
-        acc = mac2(x0, x1, w[ss], w[ss + 1], acc);
-      }
-      // A non-finite x_s times the zero weight of an earlier token would be NaN: left out
-      // of the products, it makes the tokens from s on NaN here.
-      if (bad) {
-        bool seen[4] = {};
-#pragma nounroll
-        for (int s = 0; s <= t; ++s) {
-          const f32x4 v = half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) seen[i] |= !(fabsf(v[i]) < INFINITY);
+        for (int ss = 0; ss < LT; ss += 2) {
+          if (ss > tt) continue;
+          auto x0 = vt.col(m.x, p0, 16 * ss), x1 = vt.col(m.x, p0, 16 * ss + 16);
+          if (!finite) x0 = ssm_finite<E>(x0), x1 = ssm_finite<E>(x1);
+          acc = mac2(x0, x1, w[ss], w[ss + 1], acc);
         }
+        if (!finite) {
+          bool seen[4] = {};
+#pragma nounroll
+          for (int s = 0; s <= t; ++s) {
+            const f32x4 v = half_f32(*reinterpret_cast<const ssm_half<E>*>(m.x + VT::at(s, p0 + 4 * g)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = seen[i] ? NAN : acc[i];
+            for (int i = 0; i < 4; ++i) seen[i] |= !(fabsf(v[i]) < INFINITY);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = seen[i] ? NAN : acc[i];
+        }
+        out[j] = to_half<E>(acc);
       }
-      out[j] = to_half<E>(acc);
-    }
+    };
+    // A non-finite x_s times the zero weight of an earlier token would be NaN: left out of
+    // the products, it makes the tokens from s on NaN.
+    if (__builtin_amdgcn_readfirstlane(m.bad) != t0) columns(std::true_type{});
+    else columns(std::false_type{});
     ssm_stretch();
     ssm_state_update<E, NP, L>(
         kt, vt, m.b, m.x, 16 * wave, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
@@ -1241,7 +1244,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(float* S, SsmArgs a) {
   const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
   const float z = to_f32(*(static_cast<const E*>(a.dt) + b * a.db + h * a.dh)) +
                   (a.bias ? a.bias[h] : 0.f);
-  const float step = a.softplus ? (z > 20.f ? z : log1pf(expf(z))) : z;
+  const float step = a.softplus ? softplus(z) : z;
   const float decay = expf(step * a.A[h]);
   const int cols = a.P / V, lanes = 256 / cols;  // rows at once; P / V <= 256
   const int r0 = threadIdx.x / cols, pc = (threadIdx.x % cols) * V;
