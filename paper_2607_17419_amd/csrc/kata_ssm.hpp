@@ -770,7 +770,7 @@ struct __attribute__((aligned(16))) SsmGradLds {
   E x[SsmTile<E, kSsmP>::size(L)], dy[SsmTile<E, kSsmP>::size(L)];
   E st[ssm_planes<E>() * SsmTile<E, NP>::size(kSsmP)];
   E w[SsmTile<E, L>::size(L)], mw[SsmTile<E, L>::size(L)];
-  SsmChunkLog log;
+  SsmChunkLog log[2];                       // of this head and the next
   float row[4][64], col[4][64];             // pair sums by tile of the other index
   float diag[64], trace[64];                // of (C B^T) M exp(l_t - l_s), of M
   float q[NP / 16][64], k[kSsmP / 16][64];  // state terms by tile of n, of p
@@ -927,6 +927,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
   for (int turn = 0; turn < turns; ++turn) {
     const int h = h0 + turn / blocks, pb = turn % blocks, pc = pb * kSsmP;
     const float D = a.D ? a.D[h] : 0.f;
+    SsmChunkLog& lg = m.log[turn / blocks & 1];
     if (pb == 0) {
 #pragma unroll
       for (int j = 0; j < TW; ++j) mm[j] = f32x4{};
@@ -940,9 +941,13 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     rx.store(m.x);
     ry.store(m.dy);
     rs.store(m.st);
-    if (wave == 0 && pb == 0) m.log.template store<L>(rl);
+    if (wave == 0 && pb == 0) lg.template store<L>(rl);
     lds_barrier();
     kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
+    bool above[4];  // the diagonal
+    float skip[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c, skip[i] = 4 * g + i == c ? D : 0.f;
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
       if (wave + WV * j >= TRI) break;
@@ -956,18 +961,17 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
                    vt.row(m.dy, 16 * tt, k), vt.row(m.dy, 16 * tt, k + 16), acc);
       if (!ONE) mm[j] = acc;
       if (pb != 0 && pb + 1 != blocks) continue;
-      f32x4 dec = m.log.decay(t, s);
-      const f32x4 step = m.log.four(m.log.step, s);
+      f32x4 dec = lg.decay(t, s);
+      const f32x4 step = lg.four(lg.step, s);
       if (tt == ss) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dec[i] = 4 * g + i <= c ? dec[i] : 0.f;
+        for (int i = 0; i < 4; ++i) dec[i] = above[i] ? 0.f : dec[i];
       }
       if (pb == 0) {  // W, with D on its diagonal
         f32x4 w = cb[j] * dec * step;
         if (tt == ss) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = 4 * g + i <= c ? w[i] + (4 * g + i == c ? D : 0.f) : 0.f;
+          for (int i = 0; i < 4; ++i) w[i] = above[i] ? 0.f : w[i] + skip[i];
         }
         *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
@@ -1013,7 +1017,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const int tt = tn + NG * j;
-        const float since = m.log.since[16 * tt + c];
+        const float since = lg.since[16 * tt + c];
 #pragma unroll
         for (int i = 0; i < NN; ++i) {
           qs[j] = fmaf(since, dot4(half_f32(kt.row(m.c, 16 * tt, n0 + 16 * i)), acc[i][j]), qs[j]);
@@ -1048,7 +1052,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       }
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const float push = m.log.push[16 * (tn + NG * j) + c];
+        const float push = lg.push[16 * (tn + NG * j) + c];
 #pragma unroll
         for (int i = 0; i < NN; ++i) dB[i][j] += push * acc[i][j];
       }
@@ -1077,7 +1081,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
       for (int j = 0; j < TP; ++j) {
         const int ss = tp + WS * j;
-        const float left = m.log.left[16 * ss + c], push = m.log.push[16 * ss + c];
+        const float left = lg.left[16 * ss + c], push = lg.push[16 * ss + c];
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
           ks[j] = fmaf(left, dot4(half_f32(vt.row(m.x, 16 * ss, p0 + 16 * i)), acc[i][j]), ks[j]);
@@ -1157,11 +1161,12 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         }
       }
     }
-    if (wave == 0) {
+    // the waves take turns at what one wave does
+    if (wave == turn % WV) {
       // e_t = sum_{u >= t} (q_u + row_u - step_u col_u) + sum_{s < t} step_s k_s + the
       // state that passes through; in fp64, since the sums over u cancel
       const int t = min(lane, L - 1);
-      const float step = m.log.step[t];
+      const float step = lg.step[t];
       float row = 0.f, col = 0.f, q = 0.f, k = 0.f;
 #pragma unroll
       for (int j = 0; j < LT; ++j) {
@@ -1184,8 +1189,8 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
       for (int j = 0; j < WV; ++j) through += m.dot[j];
       const float e = static_cast<float>(total + (diff - (before - after)) +
-                                         static_cast<double>(m.log.all) * through);
-      const float ddt = (m.diag[t] + col + k + e * a.A[h]) * m.log.gate[t];
+                                         static_cast<double>(lg.all) * through);
+      const float ddt = (m.diag[t] + col + k + e * a.A[h]) * lg.gate[t];
       if (in)
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
                   ddt);
