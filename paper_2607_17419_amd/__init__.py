@@ -700,15 +700,15 @@ def _on_stream(call):
 _ANY = "any"  # strides over the innermost dimension too
 
 
-def _tensor(t, name, like, shape, dtype, strided=False):
-    """The address of a tensor of this shape (a tuple) and type on like's device.  Few steps: of
-    a single token's call these checks are half of the host's time."""
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != like.get_device():
+def _tensor(t, name, device, shape, dtype, strided=False):
+    """The address of a tensor of this shape (a tuple) and type on the device of this number.
+    Few steps: of a single token's call these checks are half of the host's time."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
         if t.shape != shape:
             raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
         if t.dtype is not dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+        raise ValueError(f"{name} is on {t.device}, not on device {device}")
     if not t.is_contiguous():
         if not strided:
             raise ValueError(f"{name} must be contiguous")
@@ -717,15 +717,15 @@ def _tensor(t, name, like, shape, dtype, strided=False):
     return t.data_ptr()
 
 
-def _optional(t, name, like, shape, dtype, strided=False):
-    return None if t is None else _tensor(t, name, like, shape, dtype, strided)
+def _optional(t, name, device, shape, dtype, strided=False):
+    return None if t is None else _tensor(t, name, device, shape, dtype, strided)
 
 
 def _workspace(given, nbytes, like):
     import torch
     if given is None or given.numel() < nbytes:
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=like.device)
-    _tensor(given, "workspace", like, given.shape, torch.uint8)
+    _tensor(given, "workspace", like.get_device(), given.shape, torch.uint8)
     return given
 
 
@@ -745,18 +745,18 @@ def conv_fwd(x, w, bias=None, act: int = CONV_SILU, state=None, lengths=None, y=
     import torch
     B, T, D = _dims(x, 3, "x [B,T,D]")
     W = _dims(w, 2, "w [D,W]")[1]
-    code, f32 = _dtype_code(x), torch.float32
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
     if y is None:
         y = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
     if state_out is None and final_state:
         state_out = torch.empty((B, W - 1, D), dtype=x.dtype, device=x.device)
     rows = (B, W - 1, D)
     _check(lib().kata_conv_fwd(
-        _tensor(x, "x", x, (B, T, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
-        _optional(bias, "bias", x, (D,), f32), _optional(state, "state", x, rows, x.dtype),
-        _optional(lengths, "lengths", x, (B,), torch.int32),
-        _tensor(y, "y", x, (B, T, D), x.dtype, True),
-        _optional(state_out, "state_out", x, rows, x.dtype), B, T, D, W, x.stride(0), x.stride(1),
+        _tensor(x, "x", dev, (B, T, D), x.dtype, True), _tensor(w, "w", dev, (D, W), f32),
+        _optional(bias, "bias", dev, (D,), f32), _optional(state, "state", dev, rows, x.dtype),
+        _optional(lengths, "lengths", dev, (B,), torch.int32),
+        _tensor(y, "y", dev, (B, T, D), x.dtype, True),
+        _optional(state_out, "state_out", dev, rows, x.dtype), B, T, D, W, x.stride(0), x.stride(1),
         y.stride(0), y.stride(1), act, code, _stream(None, x.device)), "kata_conv_fwd")
     return y if state_out is None else (y, state_out)
 
@@ -768,13 +768,13 @@ def conv_step(state, x, w, bias=None, act: int = CONV_SILU, y=None):
     import torch
     B, D = _dims(x, 2, "x [B,D]")
     W = _dims(w, 2, "w [D,W]")[1]
-    code, f32 = _dtype_code(x), torch.float32
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
     if y is None:
         y = torch.empty((B, D), dtype=x.dtype, device=x.device)
     _check(lib().kata_conv_step(
-        _tensor(state, "state", x, (B, W - 1, D), x.dtype),
-        _tensor(x, "x", x, (B, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
-        _optional(bias, "bias", x, (D,), f32), _tensor(y, "y", x, (B, D), x.dtype, True), B, D, W,
+        _tensor(state, "state", dev, (B, W - 1, D), x.dtype),
+        _tensor(x, "x", dev, (B, D), x.dtype, True), _tensor(w, "w", dev, (D, W), f32),
+        _optional(bias, "bias", dev, (D,), f32), _tensor(y, "y", dev, (B, D), x.dtype, True), B, D, W,
         x.stride(0), y.stride(0), act, code, _stream(None, x.device)), "kata_conv_step")
     return y
 
@@ -786,7 +786,7 @@ def conv_bwd(x, w, bias, dy, act: int = CONV_SILU, dx=None, workspace=None):
     import torch
     B, T, D = _dims(x, 3, "x [B,T,D]")
     W = _dims(w, 2, "w [D,W]")[1]
-    code, f32 = _dtype_code(x), torch.float32
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
     if dx is None:
         dx = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
     dw = torch.empty((D, W), dtype=f32, device=x.device)
@@ -794,9 +794,9 @@ def conv_bwd(x, w, bias, dy, act: int = CONV_SILU, dx=None, workspace=None):
     nbytes = int(lib().kata_conv_bwd_workspace_bytes(B, T, D, W, code))
     workspace = _workspace(workspace, nbytes, x)
     _check(lib().kata_conv_bwd_ws(
-        _tensor(x, "x", x, (B, T, D), x.dtype, True), _tensor(w, "w", x, (D, W), f32),
-        _optional(bias, "bias", x, (D,), f32), _tensor(dy, "dy", x, (B, T, D), x.dtype, True),
-        _tensor(dx, "dx", x, (B, T, D), x.dtype, True), dw.data_ptr(),
+        _tensor(x, "x", dev, (B, T, D), x.dtype, True), _tensor(w, "w", dev, (D, W), f32),
+        _optional(bias, "bias", dev, (D,), f32), _tensor(dy, "dy", dev, (B, T, D), x.dtype, True),
+        _tensor(dx, "dx", dev, (B, T, D), x.dtype, True), dw.data_ptr(),
         None if db is None else db.data_ptr(), B, T, D, W, x.stride(0), x.stride(1), dy.stride(0),
         dy.stride(1), dx.stride(0), dx.stride(1), act, code, workspace.data_ptr(),
         workspace.numel(), _stream(None, x.device)), "kata_conv_bwd_ws")
@@ -830,18 +830,18 @@ def qk_norm_fwd(q, k=None, wq=None, wk=None, freq=None, pos=None, norm: int = NO
     (default 0..T-1); returns (yq [B,Hq,T,d], yk [B,Hk,T,d] or None)."""
     import torch
     B, T, Hq, Hk, d, r = _norm_sides(q, k, freq)
-    code, f32 = _dtype_code(q), torch.float32
+    code, f32, dev = _dtype_code(q), torch.float32, q.get_device()
     if yq is None:
         yq = torch.empty((B, Hq, T, d), dtype=q.dtype, device=q.device)
     if yk is None and k is not None:
         yk = torch.empty((B, Hk, T, d), dtype=q.dtype, device=q.device)
     _check(lib().kata_qk_norm_fwd(
-        _tensor(q, "q", q, (B, T, Hq, d), q.dtype, True),
-        _optional(k, "k", q, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", q, (d,), f32),
-        _optional(wk, "wk", q, (d,), f32), _optional(pos, "pos", q, (B, T), torch.int32),
-        _optional(freq if r else None, "freq", q, (r // 2,), torch.float64),
-        _tensor(yq, "yq", q, (B, Hq, T, d), q.dtype),
-        _optional(yk, "yk", q, (B, Hk, T, d), q.dtype), B, T, Hq, Hk, d, r, *_strides3(q),
+        _tensor(q, "q", dev, (B, T, Hq, d), q.dtype, True),
+        _optional(k, "k", dev, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", dev, (d,), f32),
+        _optional(wk, "wk", dev, (d,), f32), _optional(pos, "pos", dev, (B, T), torch.int32),
+        _optional(freq if r else None, "freq", dev, (r // 2,), torch.float64),
+        _tensor(yq, "yq", dev, (B, Hq, T, d), q.dtype),
+        _optional(yk, "yk", dev, (B, Hk, T, d), q.dtype), B, T, Hq, Hk, d, r, *_strides3(q),
         *_strides3(k), norm, eps, int(pairs), code, _stream(None, q.device)), "kata_qk_norm_fwd")
     return yq, yk
 
@@ -854,7 +854,7 @@ def qk_norm_bwd(q, k=None, wq=None, wk=None, freq=None, dq=None, dk=None, pos=No
     or q's type), via kata_qk_norm_bwd_ws; None where the input is."""
     import torch
     B, T, Hq, Hk, d, r = _norm_sides(q, k, freq)
-    code, f32 = _dtype_code(q), torch.float32
+    code, f32, dev = _dtype_code(q), torch.float32, q.get_device()
     if dxq is None:
         dxq = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
     if dxk is None and k is not None:
@@ -864,14 +864,14 @@ def qk_norm_bwd(q, k=None, wq=None, wk=None, freq=None, dq=None, dk=None, pos=No
     nbytes = int(lib().kata_qk_norm_bwd_workspace_bytes(B, T, Hq, Hk, d, code))
     workspace = _workspace(workspace, nbytes, q)
     _check(lib().kata_qk_norm_bwd_ws(
-        _tensor(q, "q", q, (B, T, Hq, d), q.dtype, True),
-        _optional(k, "k", q, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", q, (d,), f32),
-        _optional(wk, "wk", q, (d,), f32), _optional(pos, "pos", q, (B, T), torch.int32),
-        _optional(freq if r else None, "freq", q, (r // 2,), torch.float64),
-        _tensor(dq, "dq", q, (B, Hq, T, d), dq.dtype),
-        _optional(dk, "dk", q, (B, Hk, T, d), dq.dtype),
-        _tensor(dxq, "dxq", q, (B, T, Hq, d), q.dtype, True),
-        _optional(dxk, "dxk", q, (B, T, Hk, d), q.dtype, True),
+        _tensor(q, "q", dev, (B, T, Hq, d), q.dtype, True),
+        _optional(k, "k", dev, (B, T, Hk, d), q.dtype, True), _optional(wq, "wq", dev, (d,), f32),
+        _optional(wk, "wk", dev, (d,), f32), _optional(pos, "pos", dev, (B, T), torch.int32),
+        _optional(freq if r else None, "freq", dev, (r // 2,), torch.float64),
+        _tensor(dq, "dq", dev, (B, Hq, T, d), dq.dtype),
+        _optional(dk, "dk", dev, (B, Hk, T, d), dq.dtype),
+        _tensor(dxq, "dxq", dev, (B, T, Hq, d), q.dtype, True),
+        _optional(dxk, "dxk", dev, (B, T, Hk, d), q.dtype, True),
         None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(), B, T, Hq,
         Hk, d, r, *_strides3(q), *_strides3(k), *_strides3(dxq), *_strides3(dxk), norm, eps,
         int(pairs), code, _dtype_code(dq), workspace.data_ptr(), workspace.numel(),
@@ -889,19 +889,20 @@ def _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, tokens):
     n = 4 if tokens else 3
     lead, (H, P) = x.shape[:-2], _dims(x, n, "x [B,T,H,P]" if tokens else "x [B,H,P]")[-2:]
     G, N = _dims(Bm, n, "Bm [B,T,G,N]" if tokens else "Bm [B,G,N]")[-2:]
-    f32 = torch.float32
-    args = (_tensor(x, "x", x, x.shape, x.dtype, True),
-            _tensor(dt, "dt", x, (*lead, H), x.dtype, _ANY),
-            _tensor(A, "A", x, (H,), f32), _tensor(Bm, "Bm", x, (*lead, G, N), x.dtype, True),
-            _tensor(Cm, "Cm", x, (*lead, G, N), x.dtype, True), _optional(D, "D", x, (H,), f32),
-            _optional(dt_bias, "dt_bias", x, (H,), f32))
+    f32, dev = torch.float32, x.get_device()
+    args = (_tensor(x, "x", dev, x.shape, x.dtype, True),
+            _tensor(dt, "dt", dev, (*lead, H), x.dtype, _ANY),
+            _tensor(A, "A", dev, (H,), f32), _tensor(Bm, "Bm", dev, (*lead, G, N), x.dtype, True),
+            _tensor(Cm, "Cm", dev, (*lead, G, N), x.dtype, True), _optional(D, "D", dev, (H,), f32),
+            _optional(dt_bias, "dt_bias", dev, (H,), f32))
     return lead[0], lead[1] if tokens else 1, H, G, N, P, args
 
 
 def _ssm_strides(x, dt, Bm, Cm, y):
     if x.dim() == 3:  # one token
-        s = (x.stride(0), 0, x.stride(1), dt.stride(0), 0, dt.stride(1), Bm.stride(0), 0,
-             Bm.stride(1), Cm.stride(0), 0, Cm.stride(1), y.stride(0), 0, y.stride(1))
+        (xb, xh, _), (tb, th), (bb, bg, _), (cb, cg, _), (yb, yh, _) = (
+            x.stride(), dt.stride(), Bm.stride(), Cm.stride(), y.stride())
+        s = (xb, 0, xh, tb, 0, th, bb, 0, bg, cb, 0, cg, yb, 0, yh)
     else:
         s = x.stride()[:3] + dt.stride() + Bm.stride()[:3] + Cm.stride()[:3] + y.stride()[:3]
     return _SsmStrides(*s)
@@ -919,17 +920,17 @@ def ssm_fwd(x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus: bool = True, state
     or a state_out.  state: the one before the first token; lengths: int32 [B]."""
     import torch
     B, T, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, True)
-    code, f32 = _dtype_code(x), torch.float32
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
     if y is None:
         y = torch.empty((B, T, H, P), dtype=x.dtype, device=x.device)
     if state_out is None and final_state:
         state_out = torch.empty((B, H, N, P), dtype=f32, device=x.device)
     workspace = _workspace(workspace, ssm_workspace_bytes(B, T, H, G, N, P, code), x)
     _check(lib().kata_ssm_fwd_ws(
-        *args, _optional(state, "state", x, (B, H, N, P), f32),
-        _optional(lengths, "lengths", x, (B,), torch.int32),
-        _tensor(y, "y", x, (B, T, H, P), x.dtype, True),
-        _optional(state_out, "state_out", x, (B, H, N, P), f32), B, T, H, G, N, P,
+        *args, _optional(state, "state", dev, (B, H, N, P), f32),
+        _optional(lengths, "lengths", dev, (B,), torch.int32),
+        _tensor(y, "y", dev, (B, T, H, P), x.dtype, True),
+        _optional(state_out, "state_out", dev, (B, H, N, P), f32), B, T, H, G, N, P,
         _ssm_strides(x, dt, Bm, Cm, y), int(softplus), code, workspace.data_ptr(),
         workspace.numel(), _stream(None, x.device)), "kata_ssm_fwd_ws")
     return y if state_out is None else (y, state_out)
@@ -941,12 +942,12 @@ def ssm_step(S, x, dt, A, Bm, Cm, D=None, dt_bias=None, softplus: bool = True, y
     [B,H,P]; S [B,H,N,P] fp32 is updated in place."""
     import torch
     B, _, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, False)
-    code = _dtype_code(x)
+    code, dev = _dtype_code(x), x.get_device()
     if y is None:
         y = torch.empty((B, H, P), dtype=x.dtype, device=x.device)
     _check(lib().kata_ssm_step(
-        _tensor(S, "S", x, (B, H, N, P), torch.float32), *args,
-        _tensor(y, "y", x, (B, H, P), x.dtype, True), B, H, G, N, P,
+        _tensor(S, "S", dev, (B, H, N, P), torch.float32), *args,
+        _tensor(y, "y", dev, (B, H, P), x.dtype, True), B, H, G, N, P,
         _ssm_strides(x, dt, Bm, Cm, y), int(softplus), code, _stream(None, x.device)),
         "kata_ssm_step")
     return y
@@ -958,7 +959,7 @@ def ssm_bwd(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus: bool = True, workspace=N
     lengths (kata_ssm_bwd_ws); None where D or dt_bias is."""
     import torch
     B, T, H, G, N, P, args = _ssm_inputs(x, dt, A, Bm, Cm, D, dt_bias, True)
-    code, f32 = _dtype_code(x), torch.float32
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
     dx, ddt = (torch.empty(s, dtype=x.dtype, device=x.device) for s in ((B, T, H, P), (B, T, H)))
     dB, dC = (torch.empty((B, T, G, N), dtype=x.dtype, device=x.device) for _ in range(2))
     dA = torch.empty((H,), dtype=f32, device=x.device)
@@ -966,7 +967,7 @@ def ssm_bwd(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus: bool = True, workspace=N
     db = None if dt_bias is None else torch.empty((H,), dtype=f32, device=x.device)
     workspace = _workspace(workspace, ssm_workspace_bytes(B, T, H, G, N, P, code, True), x)
     _check(lib().kata_ssm_bwd_ws(
-        *args, _tensor(dy, "dy", x, (B, T, H, P), x.dtype, True), dx.data_ptr(), ddt.data_ptr(),
+        *args, _tensor(dy, "dy", dev, (B, T, H, P), x.dtype, True), dx.data_ptr(), ddt.data_ptr(),
         dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), None if dD is None else dD.data_ptr(),
         None if db is None else db.data_ptr(), B, T, H, G, N, P,
         _ssm_strides(x, dt, Bm, Cm, dy), int(softplus), code, workspace.data_ptr(),
