@@ -371,9 +371,12 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 }
 
 // h <- exp(l_L) h + sum_s B_s (scale_s v_s)^T over the chunk's tokens; keys and v are
-// LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so
-// that the fp32 state keeps 2^-18 of every term.
-template <typename E, int NP, int L, typename F>
+// LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so that
+// the fp32 state keeps 2^-18 of every term: enough for what is rounded to bf16 afterwards (y)
+// and for the sums of the gradients; EXACT, for a state that is returned, with a third part,
+// which keeps all of fp32's bits (the error of a state of 2000 tokens falls from 2e-6 to 1e-7;
+// a forward that returns none would take 1.1 times as long with it).
+template <typename E, int NP, int L, bool EXACT, typename F>
 __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::Lane& kt,
                                                  const typename SsmTile<E, kSsmP>::Lane& vt,
                                                  const E* keys, const E* v, int p0, float decay,
@@ -386,12 +389,18 @@ __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::
     const f32x4 v0 = half_f32(vt.col(v, p0, s0)) * f(s0 + 4 * g);
     const f32x4 v1 = half_f32(vt.col(v, p0, s0 + 16)) * f(s0 + 16 + 4 * g);
     const SsmSplit<E> a(v0), b(v1);
+    ssm_half<E> a2, b2;
+    if constexpr (EXACT) {
+      a2 = to_half<E>((v0 - half_f32(a.hi)) - half_f32(a.lo));
+      b2 = to_half<E>((v1 - half_f32(b.hi)) - half_f32(b.lo));
+    }
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) {
       const auto k0 = kt.col(keys, 16 * j, s0);
       const auto k1 = kt.col(keys, 16 * j, s0 + 16);
       h[j] = mac2(k0, k1, a.hi, b.hi, h[j]);
       if constexpr (sizeof(E) == 2) h[j] = mac2(k0, k1, a.lo, b.lo, h[j]);
+      if constexpr (EXACT) h[j] = mac2(k0, k1, a2, b2, h[j]);
     }
     ssm_stretch();
   }
@@ -445,7 +454,7 @@ __device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P) {
   }
 }
 
-template <typename E, int NP, bool VEC>
+template <typename E, int NP, bool VEC, bool EXACT>
 __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs a) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16;
   constexpr int PW = LT == 4 ? 4 : 2;  // tiles of columns of which a wave forms y
@@ -576,7 +585,7 @@ __global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs 
     if (__builtin_amdgcn_readfirstlane(m.bad) != t0) columns(std::true_type{});
     else columns(std::false_type{});
     ssm_stretch();
-    ssm_state_update<E, NP, L>(
+    ssm_state_update<E, NP, L, EXACT>(
         kt, vt, m.b, m.x, 16 * wave, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
     lds_barrier();
     // a wave's 16 rows of y, turned in its own part of st
@@ -617,7 +626,7 @@ struct __attribute__((aligned(16))) SsmStateLds {
   SsmChunkLog log;
 };
 
-template <typename E, int NP, bool CHUNKS, bool VEC>
+template <typename E, int NP, bool CHUNKS, bool VEC, bool EXACT>
 __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, int dirs) {
   constexpr int L = ssm_chunk<E>();
   __shared__ SsmStateLds<E, NP, CHUNKS> m;
@@ -703,7 +712,7 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
     if (i + 1 < steps) fetch(start(i + 1));
     kl.fresh(), vl.fresh(), me.fresh();
     if (!CHUNKS) log_sum += m.log.log;
-    ssm_state_update<E, NP, L>(
+    ssm_state_update<E, NP, L, EXACT>(
         kl, vl, m.k, m.v, p0, m.log.all,
         [&](int s) { return m.log.four(rev ? m.log.since : m.log.push, s); }, st);
   }
@@ -1353,11 +1362,11 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
   } while (0)
 
 // The states between spans, forward (and reverse: dirs = 2).
-template <typename E, int NP, bool VEC>
+template <typename E, int NP, bool VEC, bool EXACT>
 hipError_t ssm_between_spans(const SsmArgs& a, int dirs, hipStream_t st) {
   if (a.spans < 2) return hipSuccess;
   const int blocks = (a.P + kSsmP - 1) / kSsmP;
-  ssm_state_kernel<E, NP, false, VEC>
+  ssm_state_kernel<E, NP, false, VEC, EXACT>
       <<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1) * dirs, 256, 0, st>>>(a, nullptr, dirs);
   KATA_TRY(hipGetLastError());
   ssm_span_scan<<<dim3((a.N * a.P + 255) / 256, a.B * a.H, dirs), 256, 0, st>>>(a);
@@ -1372,14 +1381,19 @@ hipError_t ssm_logs(const SsmArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <typename E, int NP, bool VEC, bool EXACT>
+hipError_t ssm_fwd_exact(const SsmArgs& a, hipStream_t st) {
+  KATA_TRY(ssm_logs<E>(a, st));
+  KATA_TRY((ssm_between_spans<E, NP, VEC, EXACT>(a, 1, st)));
+  const int blocks = (a.P + kSsmP - 1) / kSsmP;
+  ssm_out_kernel<E, NP, VEC, EXACT>
+      <<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
 template <typename E, int NP, bool VEC>
 hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
-  KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, VEC>(a, 1, st)));
-  const int blocks = (a.P + kSsmP - 1) / kSsmP;
-  auto kernel = ssm_out_kernel<E, NP, VEC>;
-  kernel<<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans, 256, 0, st>>>(a);
-  return hipGetLastError();
+  constexpr bool bf16 = sizeof(E) == 2;  // fp32 states need no parts
+  return a.S_out ? ssm_fwd_exact<E, NP, VEC, bf16>(a, st) : ssm_fwd_exact<E, NP, VEC, false>(a, st);
 }
 
 template <typename E, int NP, bool VEC>
@@ -1387,8 +1401,8 @@ hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* chunks, float* dA,
                       float* dbias, hipStream_t st) {
   const int blocks = (a.P + kSsmP - 1) / kSsmP, L = ssm_chunk<E>(), NC = (a.T + L - 1) / L;
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, VEC>(a, 2, st)));
-  ssm_state_kernel<E, NP, true, VEC>
+  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, 2, st)));
+  ssm_state_kernel<E, NP, true, VEC, false>
       <<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans * 2, 256, 0, st>>>(a, chunks, 2);
   KATA_TRY(hipGetLastError());
   const unsigned grid = static_cast<unsigned>(a.B) * NC * a.G * o.blocks;
