@@ -147,9 +147,9 @@ bool ssm_tensors(kata::SsmArgs& a, const void* x, const void* dt, const float* A
   if (!layout_ok({{B, s.c_batch}, {T, s.c_token}, {G, s.c_group}}, N, false)) return false;
   if (!layout_ok({{B, s.y_batch}, {T, s.y_token}, {H, s.y_head}}, P, y != nullptr)) return false;
   const int piece = dtype == KATA_BF16 ? 8 : 4;
-  const auto pieces = [piece, T](const void* p, int cols, long long u, long long v, long long w) {
+  const auto pieces = [piece](const void* p, int cols, long long u, long long v, long long w) {
     return aligned_to(p, 16) && cols % piece == 0 && u % piece == 0 && v % piece == 0 &&
-           w % piece == 0 && v <= 1 << 21 && (T == 1 || v >= cols);
+           w % piece == 0 && v <= 1 << 21 && v >= cols;  // (also of one token: its rows end there)
   };
   a = {};
   a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.D = D, a.bias = bias, a.dy = dy, a.y = y;

@@ -407,6 +407,26 @@ def test_ssm_spans_joined(kata):
 
 # ---- layouts, streams, graphs ---------------------------------------------------------
 
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("T", (1, 70))
+def test_ssm_tokens_broadcast_with_stride_zero(kata, T, dtype):
+    """The same token over and over by a token stride of 0, also where there is but one."""
+    B, H, G, N, P = 2, 2, 1, 32, 64
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, 1, H, G, N, P, dtype, 31)
+    dy = normal(gen, B, 1, H, P, dtype=dtype)
+
+    def again(t):
+        s = list(t.stride())
+        s[1] = 0
+        return t.as_strided((t.shape[0], T, *t.shape[2:]), s)
+    ins = [again(up(t, dtype)) for t in (x, dt, Bm, Cm, dy)]
+    full = [t.clone(memory_format=torch.contiguous_format) for t in ins]
+    rest = (up(D), up(bias))
+    for a, b in zip(*([*kata.ssm_fwd(*t[:2], up(A), *t[2:4], *rest, final_state=True),
+                       *kata.ssm_bwd(*t[:2], up(A), *t[2:4], *rest, t[4])] for t in (ins, full))):
+        assert torch.equal(a, b)
+
+
 def test_other_orders_of_dimensions(kata):
     """Time-major activations and outputs, and heads broadcast with stride 0."""
     B, T, H, G, N, P = 3, 90, 4, 1, 32, 32
