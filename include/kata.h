@@ -435,13 +435,14 @@ KATA_API int kata_bwd_fused_scan(int B, int H, int T, int d, int dv, int C, int 
  *    read nor written; a returned state is the one after its last token (of
  *    no tokens: the given state, or zeros).
  *  - No output may alias or overlap an input, except the states that a step
- *    updates in place; equal base addresses are KATA_ERR_INVALID_ARG.
+ *    updates in place, or another output; equal base addresses are
+ *    KATA_ERR_INVALID_ARG.
  *  - Non-finite inputs reach no output of an earlier token, another sequence or
  *    (where heads are separate) another head; in gradients they may reach
  *    every output of their sequence, and the parameters'.
  *  - Every call enqueues kernel launches only and can be captured into a HIP
  *    graph; results do not depend on the order in which workgroups run.
- *    T <= 2^30; larger T and launches of more than 2^31 - 1 workgroups are
+ *    T <= 2^30; larger T and launches of 2^32 threads or more are
  *    KATA_ERR_UNSUPPORTED.
  */
 

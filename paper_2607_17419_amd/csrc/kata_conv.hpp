@@ -13,8 +13,6 @@
 // twice; channels go along the lanes, so every row of a wave is one piece.
 #pragma once
 
-#include <initializer_list>
-
 #include "kata_rows.hpp"
 
 namespace kata {
@@ -253,10 +251,6 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(const E* __restrict__ x,
 template <typename E>
 constexpr int conv_vec() { return 16 / static_cast<int>(sizeof(E)); }
 
-inline bool conv_aligned(const void* p, int bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0;
-}
-
 template <typename E, int W, int V>
 hipError_t conv_fwd_runs(const E* x, const float* w, const float* bias, const E* state,
                          const int* lengths, E* y, E* state_out, const ConvShape& s,
@@ -269,7 +263,6 @@ hipError_t conv_fwd_runs(const E* x, const float* w, const float* bias, const E*
   const int R = wide ? 16 : 4;
   const int runs = (s.T + R - 1) / R;
   const long long blocks = (static_cast<long long>(groups) * runs * s.B + 255) / 256;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(blocks));
   if (wide)
     conv_fwd_kernel<E, W, V, 16><<<grid, 256, 0, st>>>(x, w, bias, state, lengths, y, state_out, s,
@@ -284,9 +277,7 @@ hipError_t conv_fwd_runs(const E* x, const float* w, const float* bias, const E*
 template <typename E, int V>
 bool conv_vec_ok(const ConvShape& s, std::initializer_list<const void*> p) {
   if (s.D % V || s.xb % V || s.xt % V || s.yb % V || s.yt % V || s.gb % V || s.gt % V) return false;
-  for (const void* q : p)
-    if (q && !conv_aligned(q, V * static_cast<int>(sizeof(E)))) return false;
-  return true;
+  return ptr_aligned(p, V * static_cast<int>(sizeof(E)));
 }
 
 #define KATA_CONV_TAPS(CALL)            \
@@ -316,7 +307,6 @@ hipError_t conv_step_v(E* state, const E* x, const float* w, const float* bias, 
                        const ConvShape& s, hipStream_t st) {
   const int groups = s.D / V;
   const long long blocks = (static_cast<long long>(groups) * s.B + 255) / 256;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   conv_step_kernel<E, W, V><<<static_cast<unsigned>(blocks), 256, 0, st>>>(state, x, w, bias, y, s,
                                                                            groups);
   return hipGetLastError();

@@ -151,6 +151,8 @@ hipError_t launch_conv_bwd(const void* x, const float* w, const float* bias, con
                            void* dx, float* dw, float* db, void* ws, const ConvShape& s, int W,
                            bool bf16, hipStream_t st);
 
+// Lanes of a token: a power of two with four pairs of coordinates in each.
+inline int norm_lanes(int d) { return d <= 16 ? 2 : d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 constexpr int kNormNone = 0, kNormRms = 1, kNormL2 = 2;  // kata_norm_t
 struct NormSide {  // queries or keys
   long long xb, xt, xh;  // strides of x (of dx in the backward)
@@ -187,7 +189,6 @@ struct SsmArgs {
   double* rec_log;          // [BH][spans - 1]: log2 of a span's decay
 };
 size_t ssm_workspace_bytes(int B, int T, int H, int G, int N, int P, bool bf16, bool backward);
-int ssm_chunk_of(bool bf16);
 hipError_t launch_ssm_fwd(SsmArgs a, void* ws, bool bf16, hipStream_t st);
 hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, void* dCm,
                           float* dD, float* dbias, void* ws, bool bf16, hipStream_t st);

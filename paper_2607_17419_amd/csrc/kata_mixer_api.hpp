@@ -5,7 +5,7 @@
 namespace {
 
 constexpr int kMaxTokens = 1 << 30;
-constexpr long long kMaxGrid = 0x7FFFFFFF;
+constexpr long long kMaxThreads = (1LL << 32) - 512;  // of a launch, in whole workgroups
 
 struct Dim {
   long long n, stride;
@@ -56,6 +56,17 @@ bool aligned_to(const void* p, unsigned bytes) {
   return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0;
 }
 bool elem_aligned(const void* p, int dtype) { return aligned_to(p, dtype == KATA_BF16 ? 2 : 4); }
+// Whether no output stands where an input or another output begins.
+bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* in : ins)
+      if (in == *o) return false;
+    for (const void* const* other = outs.begin(); other != o; ++other)
+      if (*other == *o) return false;
+  }
+  return true;
+}
 bool ws_ok(const void* ws, size_t have, size_t need) {
   return ws && aligned_to(ws, 256) && have >= need;
 }
@@ -68,8 +79,8 @@ kata_status_t conv_check(int B, int T, int D, int W, int act, int dtype) {
   if (act != KATA_CONV_NONE && act != KATA_CONV_SILU) return KATA_ERR_INVALID_ARG;
   if (!product_ok(B, T, D, 1)) return KATA_ERR_INVALID_ARG;
   if (W < 2 || W > 4 || D > (1 << 20) || T > kMaxTokens) return KATA_ERR_UNSUPPORTED;
-  // a thread per channel and four tokens at the least
-  if (static_cast<long long>(B) * ((T + 3) / 4) > kMaxGrid / D * 256) return KATA_ERR_UNSUPPORTED;
+  // a thread per channel and 16 tokens at the most (runs of four: of few threads)
+  if (static_cast<long long>(B) * ((T + 15) / 16) > kMaxThreads / D) return KATA_ERR_UNSUPPORTED;
   return KATA_OK;
 }
 
@@ -87,7 +98,7 @@ kata_status_t norm_check(int B, int T, int Hq, int Hk, int d, int r, int norm, f
   if (static_cast<long long>(Hq) + Hk > kGridYZ || d > 256 || T > kMaxTokens)
     return KATA_ERR_UNSUPPORTED;
   if (!product_ok(B, T, Hq + Hk, d)) return KATA_ERR_INVALID_ARG;
-  if (static_cast<long long>(B) * T > kMaxGrid) return KATA_ERR_UNSUPPORTED;
+  if (static_cast<long long>(B) * T > kMaxThreads / kata::norm_lanes(d)) return KATA_ERR_UNSUPPORTED;
   return KATA_OK;
 }
 
@@ -114,14 +125,17 @@ kata::NormArgs norm_args(int B, int T, int Hq, int Hk, int d, int r, const long 
 
 // ---- selective scan ---------------------------------------------------------------
 
-kata_status_t ssm_check(int B, int T, int H, int G, int N, int P, int softplus, int dtype) {
+kata_status_t ssm_check(int B, int T, int H, int G, int N, int P, int softplus, int dtype,
+                        bool backward) {
   if (B < 1 || T < 1 || H < 1 || G < 1 || N < 1 || P < 1 || H % G) return KATA_ERR_INVALID_ARG;
   if (!type_ok(dtype) || (softplus != 0 && softplus != 1)) return KATA_ERR_INVALID_ARG;
   if (!product_ok(B, T, H, N > P ? N : P)) return KATA_ERR_INVALID_ARG;
   if (N > 128 || P > 256 || static_cast<long long>(B) * H > kGridYZ || T > kMaxTokens)
     return KATA_ERR_UNSUPPORTED;
-  // workgroups: heads x blocks of columns x chunks at the most
-  if (static_cast<long long>(B) * H * 4 * (T / 32 + 1) > kMaxGrid) return KATA_ERR_UNSUPPORTED;
+  // per chunk of 32 tokens or more: a wave per head, and in the backward up to eight per group
+  const long long chunks = static_cast<long long>(B) * (T / (dtype == KATA_BF16 ? 64 : 32) + 1);
+  if (chunks > kMaxThreads / ((H + 3) / 4 * 256)) return KATA_ERR_UNSUPPORTED;
+  if (backward && chunks > kMaxThreads / (G * 512LL)) return KATA_ERR_UNSUPPORTED;
   return KATA_OK;
 }
 
@@ -179,8 +193,7 @@ kata_status_t kata_conv_fwd(const void* x, const float* w, const float* bias, co
   for (const void* p : {x, state_in, static_cast<const void*>(y), static_cast<const void*>(state_out)})
     if (!elem_aligned(p, dtype)) return KATA_ERR_INVALID_ARG;
   if (!aligned_to(w, 4) || !aligned_to(bias, 4) || !aligned_to(lengths, 4)) return KATA_ERR_INVALID_ARG;
-  if (x == y || (state_out && (state_out == state_in || state_out == y || state_out == x)))
-    return KATA_ERR_INVALID_ARG;
+  if (!apart({y, state_out}, {x, w, bias, state_in, lengths})) return KATA_ERR_INVALID_ARG;
   if (!layout_ok({{B, x_batch}, {T, x_token}}, D, false) ||
       !layout_ok({{B, y_batch}, {T, y_token}}, D, true))
     return KATA_ERR_INVALID_ARG;
@@ -198,7 +211,7 @@ kata_status_t kata_conv_step(void* state, const void* x, const float* w, const f
   for (const void* p : {x, static_cast<const void*>(state), static_cast<const void*>(y)})
     if (!elem_aligned(p, dtype)) return KATA_ERR_INVALID_ARG;
   if (!aligned_to(w, 4) || !aligned_to(bias, 4)) return KATA_ERR_INVALID_ARG;
-  if (x == y || state == x || state == y) return KATA_ERR_INVALID_ARG;
+  if (!apart({y, state}, {x, w, bias})) return KATA_ERR_INVALID_ARG;
   if (!layout_ok({{B, x_batch}}, D, false) || !layout_ok({{B, y_batch}}, D, true))
     return KATA_ERR_INVALID_ARG;
   const kata::ConvShape s = {B, 1, D, act == KATA_CONV_SILU, x_batch, 0, y_batch, 0, 0, 0};
@@ -223,7 +236,7 @@ kata_status_t kata_conv_bwd_ws(const void* x, const float* w, const float* bias,
     if (!elem_aligned(p, dtype)) return KATA_ERR_INVALID_ARG;
   for (const float* p : {w, bias, static_cast<const float*>(dw), static_cast<const float*>(dbias)})
     if (!aligned_to(p, 4)) return KATA_ERR_INVALID_ARG;
-  if (dx == x || dx == dy) return KATA_ERR_INVALID_ARG;
+  if (!apart({dx, dw, dbias, workspace}, {x, w, bias, dy})) return KATA_ERR_INVALID_ARG;
   if (!layout_ok({{B, x_batch}, {T, x_token}}, D, false) ||
       !layout_ok({{B, dy_batch}, {T, dy_token}}, D, false) ||
       !layout_ok({{B, dx_batch}, {T, dx_token}}, D, true))
@@ -249,7 +262,7 @@ kata_status_t kata_qk_norm_fwd(const void* q, const void* k, const float* wq, co
     return KATA_ERR_INVALID_ARG;
   if (!yq || !elem_aligned(yq, dtype) || (Hk > 0) != (yk != nullptr)) return KATA_ERR_INVALID_ARG;
   if (yk && !elem_aligned(yk, dtype)) return KATA_ERR_INVALID_ARG;
-  if (yq == q || yq == k || yq == yk || (yk && (yk == q || yk == k))) return KATA_ERR_INVALID_ARG;
+  if (!apart({yq, yk}, {q, k, wq, wk, pos, freq})) return KATA_ERR_INVALID_ARG;
   return from_hip(kata::launch_qk_norm_fwd(q, k, wq, wk, pos, freq, yq, yk,
                                            norm_args(B, T, Hq, Hk, d, r, s, norm, eps, pairs),
                                            dtype == KATA_BF16, stream));
@@ -281,9 +294,8 @@ kata_status_t kata_qk_norm_bwd_ws(
   if (!dxq || !elem_aligned(dxq, dtype) || keys != (dxk != nullptr) || !elem_aligned(dxk, dtype))
     return KATA_ERR_INVALID_ARG;
   if (!aligned_to(dwq, 4) || !aligned_to(dwk, 4) || (dwk && !keys)) return KATA_ERR_INVALID_ARG;
-  for (const void* out : {static_cast<const void*>(dxq), static_cast<const void*>(dxk)})
-    if (out && (out == q || out == k || out == dq || out == dk)) return KATA_ERR_INVALID_ARG;
-  if (dxq == dxk) return KATA_ERR_INVALID_ARG;
+  if (!apart({dxq, dxk, dwq, dwk, workspace}, {q, k, wq, wk, pos, freq, dq, dk}))
+    return KATA_ERR_INVALID_ARG;
   if (!layout_ok({{B, dxq_batch}, {T, dxq_token}, {Hq, dxq_head}}, d, true)) return KATA_ERR_INVALID_ARG;
   if (keys && !layout_ok({{B, dxk_batch}, {T, dxk_token}, {Hk, dxk_head}}, d, true))
     return KATA_ERR_INVALID_ARG;
@@ -300,7 +312,7 @@ kata_status_t kata_qk_norm_bwd_ws(
 
 size_t kata_ssm_workspace_bytes(int B, int T, int H, int G, int N, int P, kata_dtype_t dtype,
                                 int backward) {
-  if (ssm_check(B, T, H, G, N, P, 1, raw(dtype)) != KATA_OK) return 0;
+  if (ssm_check(B, T, H, G, N, P, 1, raw(dtype), backward != 0) != KATA_OK) return 0;
   return kata::ssm_workspace_bytes(B, T, H, G, N, P, dtype == KATA_BF16, backward != 0);
 }
 
@@ -310,16 +322,15 @@ kata_status_t kata_ssm_fwd_ws(const void* x, const void* dt, const float* A, con
                               int T, int H, int G, int N, int P, const kata_ssm_strides_t* strides,
                               int softplus, kata_dtype_t dtype, void* workspace,
                               size_t workspace_bytes, hipStream_t stream) {
-  const kata_status_t c = ssm_check(B, T, H, G, N, P, softplus, raw(dtype));
+  const kata_status_t c = ssm_check(B, T, H, G, N, P, softplus, raw(dtype), false);
   if (c != KATA_OK) return c;
   kata::SsmArgs a;
   if (!y || !ssm_tensors(a, x, dt, A, Bm, Cm, D, dt_bias, nullptr, y, B, T, H, G, N, P, strides,
                          softplus, dtype))
     return KATA_ERR_INVALID_ARG;
-  for (const void* p : {x, dt, Bm, Cm})
-    if (p == y) return KATA_ERR_INVALID_ARG;
+  if (!apart({y, S_out, workspace}, {x, dt, A, Bm, Cm, D, dt_bias, S_in, lengths}))
+    return KATA_ERR_INVALID_ARG;
   if (!aligned16(S_in) || !aligned16(S_out) || !aligned_to(lengths, 4)) return KATA_ERR_INVALID_ARG;
-  if (S_out && S_out == S_in) return KATA_ERR_INVALID_ARG;
   const bool bf16 = dtype == KATA_BF16;
   if (!ws_ok(workspace, workspace_bytes,
              kata::ssm_workspace_bytes(B, T, H, G, N, P, bf16, false)))
@@ -334,7 +345,7 @@ kata_status_t kata_ssm_bwd_ws(const void* x, const void* dt, const float* A, con
                               float* dt_dbias, int B, int T, int H, int G, int N, int P,
                               const kata_ssm_strides_t* strides, int softplus, kata_dtype_t dtype,
                               void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  const kata_status_t c = ssm_check(B, T, H, G, N, P, softplus, raw(dtype));
+  const kata_status_t c = ssm_check(B, T, H, G, N, P, softplus, raw(dtype), true);
   if (c != KATA_OK) return c;
   kata::SsmArgs a;
   if (!dy || !ssm_tensors(a, x, dt, A, Bm, Cm, D, dt_bias, dy, nullptr, B, T, H, G, N, P, strides,
@@ -343,10 +354,8 @@ kata_status_t kata_ssm_bwd_ws(const void* x, const void* dt, const float* A, con
   for (const void* out : {static_cast<const void*>(dx), static_cast<const void*>(ddt),
                           static_cast<const void*>(dBm), static_cast<const void*>(dCm)}) {
     if (!out || !elem_aligned(out, dtype)) return KATA_ERR_INVALID_ARG;
-    for (const void* in : {x, dt, Bm, Cm, dy})
-      if (in == out) return KATA_ERR_INVALID_ARG;
   }
-  if (dx == ddt || dx == dBm || dx == dCm || ddt == dBm || ddt == dCm || dBm == dCm)
+  if (!apart({dx, ddt, dA, dBm, dCm, dD, dt_dbias, workspace}, {x, dt, A, Bm, Cm, D, dt_bias, dy}))
     return KATA_ERR_INVALID_ARG;
   if (!aligned_to(dA, 4) || !aligned_to(dD, 4) || !aligned_to(dt_dbias, 4))
     return KATA_ERR_INVALID_ARG;
@@ -362,15 +371,14 @@ kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, const float
                             const void* Cm, const float* D, const float* dt_bias, void* y, int B,
                             int H, int G, int N, int P, const kata_ssm_strides_t* strides,
                             int softplus, kata_dtype_t dtype, hipStream_t stream) {
-  const kata_status_t c = ssm_check(B, 1, H, G, N, P, softplus, raw(dtype));
+  const kata_status_t c = ssm_check(B, 1, H, G, N, P, softplus, raw(dtype), false);
   if (c != KATA_OK) return c;
   kata::SsmArgs a;
   if (!S || !aligned16(S) || !y ||
       !ssm_tensors(a, x, dt, A, Bm, Cm, D, dt_bias, nullptr, y, B, 1, H, G, N, P, strides, softplus,
                    dtype))
     return KATA_ERR_INVALID_ARG;
-  for (const void* p : {x, dt, Bm, Cm, static_cast<const void*>(S)})
-    if (p == y) return KATA_ERR_INVALID_ARG;
+  if (!apart({y, S}, {x, dt, A, Bm, Cm, D, dt_bias})) return KATA_ERR_INVALID_ARG;
   return from_hip(kata::launch_ssm_step(S, a, dtype == KATA_BF16, stream));
 }
 

@@ -17,7 +17,6 @@
 // one near 0 (fp32 angles are off by 0.06 rad at a position of 10^6).
 #pragma once
 
-#include <initializer_list>
 #include <type_traits>
 
 #include "kata_rows.hpp"
@@ -311,9 +310,6 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
 
 // ---- launches ---------------------------------------------------------------
 
-// Lanes of a token: a power of two with four slots in each.
-inline int norm_lanes(int d) { return d <= 16 ? 2 : d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
-
 template <typename F>
 void norm_with_lanes(int d, F f) {
   switch (norm_lanes(d)) {
@@ -334,10 +330,6 @@ inline bool norm_vec_ok(int d, int r, std::initializer_list<long long> strides) 
   return true;
 }
 
-inline bool norm_ptr_ok(const void* p, int bytes) {
-  return !p || (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0;
-}
-
 template <typename E>
 hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* wk, const int* pos,
                          const double* freq, E* yq, E* yk, NormArgs n, hipStream_t st) {
@@ -345,7 +337,6 @@ hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* w
   const long long tokens = static_cast<long long>(n.B) * n.T;
   const int per = 256 / norm_lanes(n.d), H = n.side[0].H + n.side[1].H;
   const long long blocks = (tokens + per - 1) / per;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   // All heads of a token in one lane group share its angles; with few tokens the heads
   // are split until about two workgroups stand on every CU.
   int splits = static_cast<int>((512 + blocks - 1) / blocks);
@@ -354,8 +345,7 @@ hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* w
   const dim3 grid(static_cast<unsigned>(blocks), (H + n.split - 1) / n.split);
   const NormSide &a = n.side[0], &c = n.side[1];
   const bool vec = norm_vec_ok(n.d, n.r, {a.xb, a.xt, a.xh, c.xb, c.xt, c.xh}) &&
-                   norm_ptr_ok(q, bytes) && norm_ptr_ok(k, bytes) && norm_ptr_ok(yq, bytes) &&
-                   norm_ptr_ok(yk, bytes);
+                   ptr_aligned({q, k, yq, yk}, bytes);
   norm_with_lanes(n.d, [&](auto lanes) {
     constexpr int kLanes = decltype(lanes)::value;
     if (vec)
@@ -390,8 +380,7 @@ hipError_t qk_norm_bwd_e(const E* q, const E* k, const float* wq, const float* w
   const NormSide &a = n.side[0], &c = n.side[1];
   const bool vec = norm_vec_ok(n.d, n.r, {a.xb, a.xt, a.xh, c.xb, c.xt, c.xh, dq.xb, dq.xt, dq.xh,
                                           dk.xb, dk.xt, dk.xh}) &&
-                   norm_ptr_ok(q, bytes) && norm_ptr_ok(k, bytes) && norm_ptr_ok(dxq, bytes) &&
-                   norm_ptr_ok(dxk, bytes) && norm_ptr_ok(dyq, ybytes) && norm_ptr_ok(dyk, ybytes);
+                   ptr_aligned({q, k, dxq, dxk}, bytes) && ptr_aligned({dyq, dyk}, ybytes);
   norm_with_lanes(n.d, [&](auto lanes) {
     constexpr int kLanes = decltype(lanes)::value;
     if (vec)

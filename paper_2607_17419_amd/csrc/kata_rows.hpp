@@ -3,9 +3,18 @@
 // per-workgroup partial sums.
 #pragma once
 
+#include <initializer_list>
+
 #include "kata_internal.hpp"
 
 namespace kata {
+
+// Whether all addresses (or null) are multiples of a power of two.
+inline bool ptr_aligned(std::initializer_list<const void*> p, int bytes) {
+  for (const void* q : p)
+    if (reinterpret_cast<uintptr_t>(q) & static_cast<uintptr_t>(bytes - 1)) return false;
+  return true;
+}
 
 // V consecutive elements as fp32; the address is aligned to V elements.
 template <int V>

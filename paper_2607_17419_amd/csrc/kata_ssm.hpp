@@ -455,7 +455,7 @@ __device__ __forceinline__ void ssm_store4(E* dst, f32x4 v, int p, int P) {
 }
 
 template <typename E, int NP, bool VEC, bool EXACT>
-__global__ __launch_bounds__(256, NP <= 64 ? 4 : 2) void ssm_out_kernel(SsmArgs a) {
+__global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void ssm_out_kernel(SsmArgs a) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16;
   constexpr int PW = LT == 4 ? 4 : 2;  // tiles of columns of which a wave forms y
   typedef SsmTile<E, NP> KT;
@@ -1294,7 +1294,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(float* S, SsmArgs a) {
 // ---- launches ---------------------------------------------------------------------
 
 inline int ssm_np(int N) { return N <= 32 ? 32 : (N <= 64 ? 64 : 128); }
-int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chunk<float>(); }
+inline int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chunk<float>(); }
 
 // Spans of a head: one workgroup each, so that the heads of a call with few of them
 // still stand on every CU; a span's own state costs one more pass over x and B, and

@@ -405,7 +405,51 @@ def test_ssm_spans_joined(kata):
     near(S, last, state_tol(smag, N, T, F32), "state")
 
 
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("B,T,H,G,N,P", ((1, 100, 2, 1, 48, 96), (2, 70, 2, 2, 128, 256), (1, 130, 3, 1, 24, 72)))
+def test_ssm_several_blocks_of_columns(kata, B, T, H, G, N, P, dtype):
+    """Heads of more than 64 columns in whole aligned pieces, the last block full or not."""
+    test_ssm_fwd(kata, B, T, H, G, N, P, dtype)
+    test_ssm_bwd(kata, B, T, H, G, N, P, dtype)
+
+
 # ---- layouts, streams, graphs ---------------------------------------------------------
+
+def far(t, dtype, batch, token):
+    """The same values with these strides over batch and token, in a buffer of their extent."""
+    strides = [batch, token, *t.stride()[2:]]
+    end = 1 + sum((n - 1) * s for n, s in zip(t.shape, strides))
+    v = torch.empty(end, dtype=dtype, device=DEV).as_strided(t.shape, strides)
+    return v.copy_(t)
+
+
+@pytest.mark.parametrize("batch,token", ((1 << 32, 0), (64, 1 << 24)))
+def test_offsets_past_32_bits(kata, batch, token):
+    """Sequences 2^32 elements apart, and tokens 2^24 apart whose offsets pass 2^32."""
+    B, T, H, G, N, P = (2, 70, 1, 1, 32, 64) if token == 0 else (1, 300, 1, 1, 32, 64)
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, T, H, G, N, P, BF16, 41)
+    dy = normal(gen, B, T, H, P, dtype=BF16)
+    ins = [up(t, BF16) for t in (x, dt, Bm, Cm, dy)]
+    rest = (up(A), up(D), up(bias))
+    w, wq = up(normal(gen, P, 4, dtype=F32)), up(normal(gen, P, dtype=F32))
+    freq = kata.rope_frequencies(P, device=DEV)
+
+    def calls(x, dt, Bm, Cm, dy, **out):
+        y, S = kata.ssm_fwd(x, dt, rest[0], Bm, Cm, *rest[1:], final_state=True, **out)
+        u, g = x.flatten(2), dy.flatten(2)
+        return [y, S, *kata.ssm_bwd(x, dt, rest[0], Bm, Cm, *rest[1:], dy), kata.conv_fwd(u, w),
+                *kata.conv_bwd(u, w, None, g)[:2], kata.qk_norm_fwd(x, None, wq, None, freq)[0],
+                *kata.qk_norm_bwd(x, None, wq, None, freq, y.transpose(1, 2).contiguous())[::2]]
+    want = calls(*ins)
+    if token == 0:
+        views = [far(t, BF16, batch, t.stride(1)) for t in ins]
+        y = far(torch.zeros_like(ins[0]), BF16, batch, P)
+    else:
+        views = [far(t, BF16, batch, token) for t in ins]
+        y = far(torch.zeros_like(ins[0]), BF16, batch, token)
+    for a, b in zip(calls(*views, y=y), want):
+        assert torch.equal(a, b)
+
 
 @pytest.mark.parametrize("dtype", (BF16, F32))
 @pytest.mark.parametrize("T", (1, 70))

@@ -210,6 +210,47 @@ def test_ssm_strides_reject(field, value):
     assert L.kata_ssm_fwd_ws(*p, 2, 8, 4, 2, 16, 16, arr, 1, 1, WS, 1 << 40, NUL) == 1
 
 
+def test_launches_past_the_grid_are_refused():
+    L = kata.lib()
+    conv = dict(B=1 << 10, T=1 << 20, D=1 << 10, xb=1 << 30, xt=1 << 10, yb=1 << 30, yt=1 << 10)
+    assert _conv_fwd(**conv) == 2
+    assert L.kata_conv_bwd_workspace_bytes(1 << 10, 1 << 20, 1 << 10, 4, 1) == 0
+    norm = dict(B=2, T=1 << 27, Hq=1, Hk=0, k=NUL, yk=NUL, d=256, r=0, freq=NUL,
+                qs=(1 << 35, 256, 256))
+    assert _norm_fwd(**norm) == 2
+    assert L.kata_qk_norm_bwd_workspace_bytes(2, 1 << 27, 1, 0, 256, 1) == 0
+    # a wave per head and chunk, and in the backward eight per group and chunk
+    sizes = [1 << 15, 1 << 15, 1, 1, 16, 16]
+    assert L.kata_ssm_workspace_bytes(*sizes, 1, 1) == 0
+    assert L.kata_ssm_bwd_ws(*_ssm_ptrs(15), *sizes, NUL, 1, 1, WS, 1 << 62, NUL) == 2
+    sizes[1] = 1 << 16
+    assert L.kata_ssm_workspace_bytes(*sizes, 1, 0) == 0
+    assert L.kata_ssm_fwd_ws(*_ssm_ptrs(11), *sizes, NUL, 1, 1, WS, 1 << 62, NUL) == 2
+
+
+def test_outputs_apart_from_each_other_and_all_inputs():
+    L = kata.lib()
+    assert _conv_fwd(s_out=FAKE2) == 1 and _conv_fwd(w=FAKE3, s_out=FAKE3) == 1
+    assert _conv_fwd(lengths=FAKE2) == 1
+    assert _norm_fwd(wq=FAKE3) == 1 and _norm_fwd(pos=FAKE2) == 1
+    p = _ssm_ptrs(15)
+    sizes = [2, 8, 4, 2, 16, 16]
+    need = L.kata_ssm_workspace_bytes(*sizes, 1, 1)
+    for i, bad in ((9, p[2]), (10, p[9]), (10, p[5]), (9, p[8])):
+        args = p[:11] + sizes + [NUL, 1, 1, WS, need, NUL]
+        args[i] = bad
+        assert L.kata_ssm_fwd_ws(*args) == 1, i
+    for i, bad in ((10, p[2]), (13, p[10]), (14, p[8]), (14, p[6]), (24, p[0])):
+        args = p + sizes + [NUL, 1, 1, WS, need, NUL]
+        args[i] = bad
+        assert L.kata_ssm_bwd_ws(*args) == 1, i
+    step = p[:9] + [2, 4, 2, 16, 16, NUL, 1, 1, NUL]
+    for i, bad in ((0, p[3]), (8, p[2]), (8, p[7])):
+        args = list(step)
+        args[i] = bad
+        assert L.kata_ssm_step(*args) == 1, i
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros(2, 8, 16)
     with pytest.raises(ValueError):
