@@ -723,31 +723,34 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
 }
 
 // rec: a span's own contribution becomes the state that enters the next span (reverse:
-// the one before), in the same slot.  Grid: elements, heads, directions.
+// the one before), in the same slot.  Grid: V elements a thread, heads, directions.
+template <int V>
 __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
   const int NPs = a.N * a.P, gaps = a.spans - 1;
-  const int e = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y;
+  const int e = (blockIdx.x * 256 + threadIdx.x) * V, bh = blockIdx.y;
   const bool rev = blockIdx.z;
   if (e >= NPs) return;
-  float s = !rev && a.S_in ? a.S_in[static_cast<size_t>(bh) * NPs + e] : 0.f;
+  float s[V] = {};
+  if (!rev && a.S_in) load_vec<V>(a.S_in + static_cast<size_t>(bh) * NPs + e, s);
   const size_t recs = (static_cast<size_t>(rev) * a.B * a.H + bh) * gaps;
   float* rec = a.rec + recs * NPs + e;
   const double* log = a.rec_log + recs;
   constexpr int U = 8;  // records in flight
   for (int i = 0; i < gaps; i += U) {
-    float v[U], d[U];
+    float v[U][V], d[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = min(i + u, gaps - 1), j = rev ? gaps - 1 - k : k;
-      v[u] = rec[static_cast<size_t>(j) * NPs];
+      load_vec<V>(rec + static_cast<size_t>(j) * NPs, v[u]);
       d[u] = exp2_fast(static_cast<float>(log[j]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u >= gaps) break;
       const int j = rev ? gaps - 1 - (i + u) : i + u;
-      s = fmaf(d[u], s, v[u]);
-      rec[static_cast<size_t>(j) * NPs] = s;
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[k] = fmaf(d[u], s[k], v[u][k]);
+      store_vec<V>(rec + static_cast<size_t>(j) * NPs, s);
     }
   }
 }
@@ -1338,10 +1341,12 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     w.fwd = take(2 * all);
     w.rev = w.fwd + all;
     w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(float));
-    // Heads of a group are split while there are fewer workgroups than two per CU (what
-    // LDS holds); each split adds fp32 sums of dB and dC to write and read.
-    const long long wgs = static_cast<long long>(B) * G * NC;
-    long long split = (512 + wgs - 1) / wgs;
+    // Heads of a group are split while there are fewer workgroups than the 256 CUs hold in
+    // LDS, two each (N > 64: one); each split adds fp32 sums of dB and dC to write and read.
+    // Training steps of B 2, T 2048, H 32, P 64, bf16, with room for 512 and for 256: N 64
+    // 125 and 142 us, N 128 196 and 185 us; 1024: N 128 219 us.
+    const long long wgs = static_cast<long long>(B) * G * NC, room = N > 64 ? 256 : 512;
+    long long split = (room + wgs - 1) / wgs;
     if (split > H / G) split = H / G;
     w.head_block = static_cast<int>((H / G + split - 1) / split);
     w.blocks = (H / G + w.head_block - 1) / w.head_block;
@@ -1369,7 +1374,10 @@ hipError_t ssm_between_spans(const SsmArgs& a, int dirs, hipStream_t st) {
   ssm_state_kernel<E, NP, false, VEC, EXACT>
       <<<static_cast<unsigned>(a.B) * a.H * blocks * (a.spans - 1) * dirs, 256, 0, st>>>(a, nullptr, dirs);
   KATA_TRY(hipGetLastError());
-  ssm_span_scan<<<dim3((a.N * a.P + 255) / 256, a.B * a.H, dirs), 256, 0, st>>>(a);
+  if (a.N * a.P % 4 == 0)
+    ssm_span_scan<4><<<dim3((a.N * a.P / 4 + 255) / 256, a.B * a.H, dirs), 256, 0, st>>>(a);
+  else
+    ssm_span_scan<1><<<dim3((a.N * a.P + 255) / 256, a.B * a.H, dirs), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
