@@ -167,7 +167,7 @@ struct NormArgs {
 hipError_t launch_qk_norm_fwd(const void* q, const void* k, const float* wq, const float* wk,
                               const int* pos, const double* freq, void* yq, void* yk,
                               const NormArgs& n, bool bf16, hipStream_t st);
-size_t norm_bwd_workspace_bytes(int B, int T, int d);
+size_t norm_bwd_workspace_bytes(int B, int T, int H, int d);
 hipError_t launch_qk_norm_bwd(const void* q, const void* k, const float* wq, const float* wk,
                               const int* pos, const double* freq, const void* dyq, const void* dyk,
                               void* dxq, void* dxk, float* dwq, float* dwk, void* ws,

@@ -270,7 +270,7 @@ kata_status_t kata_qk_norm_fwd(const void* q, const void* k, const float* wq, co
 
 size_t kata_qk_norm_bwd_workspace_bytes(int B, int T, int Hq, int Hk, int d, kata_dtype_t dtype) {
   if (norm_check(B, T, Hq, Hk, d, 0, KATA_NORM_NONE, 0.f, 0, raw(dtype)) != KATA_OK) return 0;
-  return kata::norm_bwd_workspace_bytes(B, T, d);
+  return kata::norm_bwd_workspace_bytes(B, T, Hq + Hk, d);
 }
 
 kata_status_t kata_qk_norm_bwd_ws(
@@ -299,7 +299,7 @@ kata_status_t kata_qk_norm_bwd_ws(
   if (!layout_ok({{B, dxq_batch}, {T, dxq_token}, {Hq, dxq_head}}, d, true)) return KATA_ERR_INVALID_ARG;
   if (keys && !layout_ok({{B, dxk_batch}, {T, dxk_token}, {Hk, dxk_head}}, d, true))
     return KATA_ERR_INVALID_ARG;
-  if (!ws_ok(workspace, workspace_bytes, kata::norm_bwd_workspace_bytes(B, T, d)))
+  if (!ws_ok(workspace, workspace_bytes, kata::norm_bwd_workspace_bytes(B, T, Hq + Hk, d)))
     return KATA_ERR_INVALID_ARG;
   const kata::NormSide oq = {dxq_batch, dxq_token, dxq_head, Hq};
   kata::NormSide ok = {};

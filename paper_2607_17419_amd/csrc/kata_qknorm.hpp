@@ -207,9 +207,10 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(const E* __restrict__ 
 }
 
 // Gradients; dx has x's strides' layout of its own (NormArgs ds), dy is
-// head-major fp32 or E.  A workgroup walks tokens; the sums of dw stay in
-// registers until the end, then are joined over the workgroup's token groups
-// in LDS and written as one partial sum per workgroup: wq's d, then wk's.
+// head-major fp32 or E.  A workgroup walks tokens, and of them the heads of its row of the
+// grid; the sums of dw stay in registers until the end, then are joined over the
+// workgroup's token groups in LDS and written as one partial sum per workgroup: wq's d,
+// then wk's.
 template <int LANES, bool VEC, typename E, typename Y>
 __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
     const E* __restrict__ q, const E* __restrict__ k, const float* __restrict__ wq,
@@ -228,6 +229,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
 #pragma unroll
   for (int i = 0; i < 4; ++i) slots.at(u0 + i, e0[i], e1[i]);
   const float scale = n.norm == kNormRms ? 1.f / static_cast<float>(n.d) : 1.f;
+  const int h0 = blockIdx.y * n.split, h1 = min(h0 + n.split, n.side[0].H + n.side[1].H);
   float dwa[2][4] = {}, dwc[2][4] = {};
   for (long long token = static_cast<long long>(blockIdx.x) * groups + group; token < tokens;
        token += static_cast<long long>(gridDim.x) * groups) {
@@ -238,6 +240,8 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
     for (int key = 0; key < 2; ++key) {
       const NormSide& s = n.side[key];
       const NormSide& ds = key ? dk : dq;
+      const int from = max(h0 - (key ? n.side[0].H : 0), 0), to = min(h1 - (key ? n.side[0].H : 0), s.H);
+      if (from >= to) continue;
       const float* w = key ? wk : wq;
       float wa[4], wc[4];
 #pragma unroll
@@ -246,7 +250,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
       const E* x0 = (key ? k : q) + b * s.xb + t * s.xt;
       E* dx0 = (key ? dxk : dxq) + b * ds.xb + t * ds.xt;
       const Y* dy0 = (key ? dyk : dyq) + (static_cast<long long>(b) * s.H * n.T + t) * n.d;
-      for (int h = 0; h < s.H; ++h) {
+      for (int h = from; h < to; ++h) {
         float a[4] = {}, c[4] = {}, ga[4] = {}, gc[4] = {};
         if (live) {
           norm_load<VEC>(x0 + h * s.xh, e0, e1, n.d, paired, a, c);
@@ -304,7 +308,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(
     slots.at(ll * kNormSlots + (v & 3), c0, c1);
     const int e = (v & 4) ? c1 : c0;
     if (ll * kNormSlots + (v & 3) < U && e < n.d)
-      part[static_cast<size_t>(blockIdx.x) * 2 * n.d + (v >> 3) * n.d + e] = acc;
+      part[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * n.d + (v >> 3) * n.d + e] = acc;
   }
 }
 
@@ -330,6 +334,16 @@ inline bool norm_vec_ok(int d, int r, std::initializer_list<long long> strides) 
   return true;
 }
 
+// Heads of a workgroup: all heads of a token in one lane group share its angles; with few
+// tokens the heads are split until about two workgroups stand on every CU.  16 + 16 heads of
+// 64, split and not: 256 tokens forward 4.0 and 12 us, 2000 6.1 and 13 us;
+// backward 100 tokens 6.8 and 22 us, 2000 14 and 29 us.
+inline int norm_split(long long blocks, int H) {
+  const long long splits = (512 + blocks - 1) / blocks;
+  const int n = static_cast<int>(splits < H ? splits : H);
+  return (H + n - 1) / n;
+}
+
 template <typename E>
 hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* wk, const int* pos,
                          const double* freq, E* yq, E* yk, NormArgs n, hipStream_t st) {
@@ -337,11 +351,7 @@ hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* w
   const long long tokens = static_cast<long long>(n.B) * n.T;
   const int per = 256 / norm_lanes(n.d), H = n.side[0].H + n.side[1].H;
   const long long blocks = (tokens + per - 1) / per;
-  // All heads of a token in one lane group share its angles; with few tokens the heads
-  // are split until about two workgroups stand on every CU.
-  int splits = static_cast<int>((512 + blocks - 1) / blocks);
-  if (splits > H) splits = H;
-  n.split = (H + splits - 1) / splits;
+  n.split = norm_split(blocks, H);
   const dim3 grid(static_cast<unsigned>(blocks), (H + n.split - 1) / n.split);
   const NormSide &a = n.side[0], &c = n.side[1];
   const bool vec = norm_vec_ok(n.d, n.r, {a.xb, a.xt, a.xh, c.xb, c.xt, c.xh}) &&
@@ -356,16 +366,19 @@ hipError_t qk_norm_fwd_e(const E* q, const E* k, const float* wq, const float* w
   return hipGetLastError();
 }
 
-// Workgroups of the backward: each writes one partial sum of dw.
+// Workgroups of the backward along the tokens, two per CU at the most and with equal walks;
+// each (of each part of the heads) writes one partial sum of dw.  8 x 4096 tokens, 16 + 16
+// heads of 64: 89 us (512), 99 (768: unequal walks), 141 (256), 90 (1024).
 inline int norm_bwd_blocks(int B, int T, int d) {
   const long long per = 256 / norm_lanes(d);
-  const long long n = (static_cast<long long>(B) * T + per - 1) / per;
-  return static_cast<int>(n < 1024 ? n : 1024);
+  const long long n = (static_cast<long long>(B) * T + per - 1) / per, walk = (n + 511) / 512;
+  return static_cast<int>((n + walk - 1) / walk);
 }
 
-size_t norm_bwd_workspace_bytes(int B, int T, int d) {
-  return (static_cast<size_t>(norm_bwd_blocks(B, T, d)) * 2 * d * sizeof(float) + 255) &
-         ~static_cast<size_t>(255);
+size_t norm_bwd_workspace_bytes(int B, int T, int H, int d) {
+  const int blocks = norm_bwd_blocks(B, T, d), split = norm_split(blocks, H);
+  const size_t parts = static_cast<size_t>(blocks) * ((H + split - 1) / split);
+  return (parts * 2 * d * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
 
 template <typename E, typename Y>
@@ -375,7 +388,9 @@ hipError_t qk_norm_bwd_e(const E* q, const E* k, const float* wq, const float* w
                          const NormSide& dk, hipStream_t st) {
   constexpr int bytes = 4 * static_cast<int>(sizeof(E));
   constexpr int ybytes = 4 * static_cast<int>(sizeof(Y));
-  const int blocks = norm_bwd_blocks(n.B, n.T, n.d);
+  const int blocks = norm_bwd_blocks(n.B, n.T, n.d), H = n.side[0].H + n.side[1].H;
+  n.split = norm_split(blocks, H);
+  const dim3 grid(blocks, (H + n.split - 1) / n.split);
   float* part = dwq || dwk ? static_cast<float*>(ws) : nullptr;
   const NormSide &a = n.side[0], &c = n.side[1];
   const bool vec = norm_vec_ok(n.d, n.r, {a.xb, a.xt, a.xh, c.xb, c.xt, c.xh, dq.xb, dq.xt, dq.xh,
@@ -384,15 +399,15 @@ hipError_t qk_norm_bwd_e(const E* q, const E* k, const float* wq, const float* w
   norm_with_lanes(n.d, [&](auto lanes) {
     constexpr int kLanes = decltype(lanes)::value;
     if (vec)
-      qk_norm_bwd_kernel<kLanes, true, E, Y><<<blocks, 256, 0, st>>>(
+      qk_norm_bwd_kernel<kLanes, true, E, Y><<<grid, 256, 0, st>>>(
           q, k, wq, wk, pos, freq, dyq, dyk, dxq, dxk, part, n, dq, dk);
     else
-      qk_norm_bwd_kernel<kLanes, false, E, Y><<<blocks, 256, 0, st>>>(
+      qk_norm_bwd_kernel<kLanes, false, E, Y><<<grid, 256, 0, st>>>(
           q, k, wq, wk, pos, freq, dyq, dyk, dxq, dxk, part, n, dq, dk);
   });
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !part) return e;
-  return launch_sum_partials(part, blocks, 2 * n.d, {{dwq, dwk, nullptr}, {n.d, n.d, 0}}, st);
+  return launch_sum_partials(part, grid.x * grid.y, 2 * n.d, {{dwq, dwk, nullptr}, {n.d, n.d, 0}}, st);
 }
 
 hipError_t launch_qk_norm_fwd(const void* q, const void* k, const float* wq, const float* wk,
