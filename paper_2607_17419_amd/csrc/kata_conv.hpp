@@ -140,9 +140,17 @@ __global__ __launch_bounds__(256) void conv_step_kernel(E* __restrict__ state,
 // tokens past a run once more for its last dx.  dw and dbias are summed in
 // registers over the runs of a wave, over the four waves in LDS, and written as
 // one partial sum per workgroup, [D*W] then [D], for sum_partials.
-constexpr int kConvBwdRun = 32;
+//
+// Runs of 32 tokens read 3/32 of the rows twice, runs of 8 3/8 of them; the short ones are
+// for calls whose long runs are fewer than a wave for each of the 1024 SIMDs.  D 1152 bf16,
+// runs of 32 and of 8: 100 tokens 17 and 9.1 us, 2000 18 and 12, 6000 (940 waves) 21 and 21,
+// 12000 26 and 30, 32768 49 and 64.
+inline int conv_bwd_run(int B, int T, int D) {
+  const long long waves = (static_cast<long long>(T) + 31) / 32 * B * ((D + 255) / 256);
+  return waves >= 1024 ? 32 : 8;
+}
 
-template <typename E, int W, int V>
+template <typename E, int W, int V, int R>
 __global__ __launch_bounds__(256) void conv_bwd_kernel(const E* __restrict__ x,
                                                        const float* __restrict__ w,
                                                        const float* __restrict__ bias,
@@ -150,7 +158,6 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(const E* __restrict__ x,
                                                        E* __restrict__ dx,
                                                        float* __restrict__ part, ConvShape s,
                                                        int runs) {
-  constexpr int R = kConvBwdRun;
   __shared__ float red[4][64][V * (W + 1)];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = (blockIdx.x * 64 + lane) * V;
@@ -328,14 +335,15 @@ hipError_t conv_step_e(void* state, const void* x, const float* w, const float* 
 
 // Workgroups along the runs: one run per wave up to 256 workgroups, whose partial
 // sums are then a few percent of the traffic.
-inline int conv_bwd_slices(int B, int T) {
-  const long long runs = (static_cast<long long>(T) + kConvBwdRun - 1) / kConvBwdRun * B;
+inline int conv_bwd_slices(int B, int T, int D) {
+  const int R = conv_bwd_run(B, T, D);
+  const long long runs = (static_cast<long long>(T) + R - 1) / R * B;
   const long long n = (runs + 3) / 4;
   return static_cast<int>(n < 256 ? n : 256);
 }
 
 size_t conv_bwd_workspace_bytes(int B, int T, int D, int W) {
-  return (static_cast<size_t>(conv_bwd_slices(B, T)) * D * (W + 1) * sizeof(float) + 255) &
+  return (static_cast<size_t>(conv_bwd_slices(B, T, D)) * D * (W + 1) * sizeof(float) + 255) &
          ~static_cast<size_t>(255);
 }
 
@@ -343,9 +351,11 @@ template <typename E, int W, int V>
 hipError_t conv_bwd_v(const E* x, const float* w, const float* bias, const E* dy, E* dx, float* dw,
                       float* db, void* ws, const ConvShape& s, hipStream_t st) {
   float* part = static_cast<float*>(ws);
-  const int runs = (s.T + kConvBwdRun - 1) / kConvBwdRun, slices = conv_bwd_slices(s.B, s.T);
+  const int R = conv_bwd_run(s.B, s.T, s.D);
+  const int runs = (s.T + R - 1) / R, slices = conv_bwd_slices(s.B, s.T, s.D);
   const dim3 grid((s.D + 64 * V - 1) / (64 * V), slices);
-  conv_bwd_kernel<E, W, V><<<grid, 256, 0, st>>>(x, w, bias, dy, dx, part, s, runs);
+  if (R == 32) conv_bwd_kernel<E, W, V, 32><<<grid, 256, 0, st>>>(x, w, bias, dy, dx, part, s, runs);
+  else conv_bwd_kernel<E, W, V, 8><<<grid, 256, 0, st>>>(x, w, bias, dy, dx, part, s, runs);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   return launch_sum_partials(part, slices, s.D * (W + 1),

@@ -1300,12 +1300,18 @@ inline int ssm_np(int N) { return N <= 32 ? 32 : (N <= 64 ? 64 : 128); }
 inline int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chunk<float>(); }
 
 // Spans of a head: one workgroup each, so that the heads of a call with few of them
-// still stand on every CU; a span's own state costs one more pass over x and B, and
-// is not made shorter than four chunks.
+// still stand on every CU, four workgroups each where there are as many spans of four chunks:
+// a span's own state costs one more pass over x and B.  (16 heads of 131072 tokens with 512,
+// 768, 1024, 1536 and 2048 workgroups: 309, 291, 278, 295 and 311 us; a training step of
+// 8 x 4096 tokens: 356, 359, 355, 370 and 434 us.)  Spans of two chunks only where those of
+// four would leave CUs without a workgroup: with four and two, 16 heads of 500 tokens 23.2 and
+// 17.4 us, of 2000 25.4 and 21.7, of 4000 31.8 and 30.8; 32 heads of 2000 27.7 and 28.4, 64
+// heads of 2000 34 and 35 us.
 inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
   const int NC = (T + L - 1) / L;
   int n = (1024 + BHP - 1) / BHP;
-  if (n > NC / 4) n = NC / 4;
+  const int least = BHP * (NC / 4) < 256 ? 2 : 4;
+  if (n > NC / least) n = NC / least;
   if (n < 1) n = 1;
   span_chunks = (NC + n - 1) / n;
   spans = (NC + span_chunks - 1) / span_chunks;
