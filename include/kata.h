@@ -531,8 +531,8 @@ KATA_API size_t kata_qk_norm_bwd_workspace_bytes(int B, int T, int Hq, int Hk, i
  *   Computed in chunks of 64 (fp32: 32) tokens on the matrix cores; long sequences of few
  *   heads are split into spans whose states are joined.  bf16: products accumulate in fp32,
  *   the weights of a chunk's pairs and the state that y reads are rounded to bf16 once, the
- *   state itself keeps 2^-18 of every term.  A positive A or a negative step grows the state
- *   as the formula says, until it overflows.
+ *   state itself keeps 2^-17 of every term (all of fp32's bits where S_out is asked for).
+ *   A positive A or a negative step grows the state as the formula says, until it overflows.
  *   strides : element strides over batch, token and head (group); null: contiguous.
  *   workspace : at least kata_ssm_workspace_bytes(..., backward) bytes (0: invalid or
  *   unsupported arguments), 256-byte aligned, contents undefined on exit.

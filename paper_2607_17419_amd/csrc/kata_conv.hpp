@@ -11,6 +11,9 @@
 // once.  A thread owns V neighbouring channels and walks a run of tokens with
 // the last W-1 rows in registers, so that only the run's first rows are read
 // twice; channels go along the lanes, so every row of a wave is one piece.
+// 8 x 4096 tokens of 1152 channels, W = 4, bf16: forward 36 us (165 MB counted, 4.6 TB/s),
+// gradients 55 us (259 MB, 4.7 TB/s) and 5 us for their sums; both together 95 us, with rows
+// that are not aligned 104 us.  One token of 256 sequences: 3.2 us, its launch's latency.
 #pragma once
 
 #include "kata_rows.hpp"
@@ -264,7 +267,9 @@ hipError_t conv_fwd_runs(const E* x, const float* w, const float* bias, const E*
                          hipStream_t st) {
   const int groups = s.D / V;
   // Runs of 16 tokens read 3/16 of the rows twice, runs of 4 3/4 of them (from the L2);
-  // the short ones are for calls whose long runs would leave CUs without a wave.
+  // the short ones are for calls whose long runs would leave SIMDs without a wave.  D 1152
+  // bf16, runs of 16 and of 4: 500 tokens 7.8 and 4.4 us, 2000 8.3 and 6.2, 6000 10.0 and
+  // 10.7; a training step of 32768 tokens 95 and 108.
   const long long threads16 = static_cast<long long>(groups) * ((s.T + 15) / 16) * s.B;
   const bool wide = threads16 >= 256 * 256;
   const int R = wide ? 16 : 4;
@@ -334,7 +339,8 @@ hipError_t conv_step_e(void* state, const void* x, const float* w, const float* 
 }
 
 // Workgroups along the runs: one run per wave up to 256 workgroups, whose partial
-// sums are then a few percent of the traffic.
+// sums are then a few percent of the traffic (training step of 32768 tokens: 95 us; up
+// to 128 97 us, up to 512 95 us).
 inline int conv_bwd_slices(int B, int T, int D) {
   const int R = conv_bwd_run(B, T, D);
   const long long runs = (static_cast<long long>(T) + R - 1) / R * B;

@@ -21,6 +21,13 @@
 // s < t <= r and of the state terms whose path crosses token t.  All products
 // are 16 x 16 tiles on the matrix cores: bf16 tensors on the bf16 ones with fp32
 // accumulation, fp32 tensors on the fp32 ones.
+//
+// Launches.  Forward: logs of all chunks; the states that spans of chunks add, joined over
+// the spans; y, a workgroup per head and span carrying the state in registers.  Backward:
+// logs, span states in both directions and their join; a record of S and R per chunk; the
+// gradients, a workgroup per chunk and group.  The records cost 2 x 2 bytes per state
+// element and chunk each way, but let every chunk stand alone: dB and dC of a group are
+// summed over its heads in registers, with no atomics.
 #pragma once
 
 #include "kata_rows.hpp"
@@ -68,7 +75,7 @@ __device__ __forceinline__ ssm_half<E> to_half(f32x4 v) {
 }
 
 // fp32 values as operands without loss of their leading 16 bits: bf16 as a sum of
-// two (within 2^-18), fp32 as they are.
+// two (within 2^-17), fp32 as they are.
 template <typename E>
 struct SsmSplit {
   ssm_half<E> hi, lo;
@@ -250,7 +257,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // A first kernel forms them once for all others: per token {hi, lo, step, gate} with the
 // running sum l = hi + lo of step A over the chunk in units of log 2 (summed in fp64:
 // differences of l keep 2^-48 of the largest, and exp(l_t - l_s) is right where a strong
-// decay stands before weak ones), and gate the derivative of step by dt.
+// decay stands before weak ones), and gate the derivative of step by dt.  16 heads of 131072
+// tokens: 17 us, a wave waiting for its one load and then for its scan's chain.
 template <typename E, int L>
 __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   const int per = (a.H + 3) / 4;
@@ -331,6 +339,11 @@ __device__ __forceinline__ unsigned ssm_xcd_order() {
 // needed as, and with them and all columns' states (shared through LDS as operands, a
 // chunk behind the accumulators) these tokens' y; then the new state of its columns.
 // The next chunk's rows are on their way meanwhile.  y is turned in LDS into whole lines.
+// The chunk's weights and the state that y reads are rounded to bf16 once (2^-8 of a term
+// each at most, as y itself is rounded), the state that is carried is not.
+// 16 heads of 131072 tokens, N = P = 64, bf16: 185 us, 620 MB counted, 3.4 TB/s; bound by issue,
+// vector instructions taking 62% of a SIMD's cycles and matrix ones 20%.  Rows that are not
+// whole aligned pieces are read element by element: 3 times the time of the whole call.
 constexpr int ssm_most(int a, int b) { return a > b ? a : b; }
 
 template <typename E, int NP>
@@ -372,7 +385,7 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 
 // h <- exp(l_L) h + sum_s B_s (scale_s v_s)^T over the chunk's tokens; keys and v are
 // LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so that
-// the fp32 state keeps 2^-18 of every term: enough for what is rounded to bf16 afterwards (y)
+// the fp32 state keeps 2^-17 of every term: enough for what is rounded to bf16 afterwards (y)
 // and for the sums of the gradients; EXACT, for a state that is returned, with a third part,
 // which keeps all of fp32's bits (the error of a state of 2000 tokens falls from 2e-6 to 1e-7;
 // a forward that returns none would take 1.1 times as long with it).
@@ -615,7 +628,12 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
 // workgroups each.  CHUNKS = false: a span's own contribution and its decay, to rec;
 // true: from the span's state in rec, every chunk's state before its tokens are added (S
 // at the chunk's start, R at its end), to `chunks` (R's behind S's): operand planes (bf16
-// hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.
+// hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.  bf16: two
+// planes keep 2^-17 of an element, for the gradients of A and of the steps, which are sums
+// of products of S and R in which much cancels; one plane would leave 2^-8.
+// Span states of 16 heads of 131072 tokens: 78 us, 333 MB counted, 4.3 TB/s, vector and
+// matrix instructions issuing in 73% of the cycles.  Chunk records of 8 x 4096 tokens of 16 heads:
+// 87 us, 438 MB counted (268 MB of them written), 5.0 TB/s, HBM bound.
 template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1; }
 
 template <typename E, int NP, bool CHUNKS>
@@ -723,7 +741,9 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
 }
 
 // rec: a span's own contribution becomes the state that enters the next span (reverse:
-// the one before), in the same slot.  Grid: V elements a thread, heads, directions.
+// the one before), in the same slot.  Grid: V elements a thread, heads, directions.  A chain
+// of loads eight records deep: 12 us for 63 records of 16 heads, 10 us for 7 of 128 (four
+// elements a thread; with one 2% more of a call of 131072 tokens).
 template <int V>
 __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
   const int NPs = a.N * a.P, gaps = a.spans - 1;
@@ -764,6 +784,9 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
 // there are as many, each operand read serving two products.  Four waves, so that two
 // workgroups share a CU and one works through the other's barriers; eight at N > 64,
 // whose records leave LDS for one workgroup.
+// 8 x 4096 tokens of 16 heads, N = P = 64, bf16: 153 us, 512 MB counted (268 MB of
+// records), 3.3 TB/s; vector instructions take 35% of the cycles, LDS 34%, matrix instructions 10%, the
+// rest are waits at the six barriers of a head, which two workgroups of a CU half cover.
 // part: dA, dD, dbias of the chunk, [B * NC][3][H].
 struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
@@ -863,7 +886,8 @@ __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
 }
 
-// ONE: P <= 64, a head is one block of columns
+// ONE: P <= 64, a head is one block of columns, and M needs no registers between blocks (the
+// training step of 8 x 4096 tokens 347 us, without the distinction 354).
 template <typename E, int NP, bool VEC, bool ONE>
 __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, PT = kSsmP / 16;
@@ -1251,7 +1275,8 @@ __global__ __launch_bounds__(256) void ssm_join_heads(SsmGrads o, size_t all) {
 // ---- one token --------------------------------------------------------------------
 // One workgroup per head: the state is read and written once (HBM bound), a thread
 // holding V columns of every 256 / (columns / V)-th row; y is joined over the rows
-// in LDS.
+// in LDS.  256 sequences of 16 heads, N = P = 64: 22 us, 135 MB at 6.1 TB/s (V = 1, for
+// P that are no multiple of four: 25 us).
 template <typename E, int V>
 __global__ __launch_bounds__(256) void ssm_step_kernel(float* S, SsmArgs a) {
   __shared__ float red[256 * V];

@@ -5,7 +5,7 @@ Tolerances.  An output is rounded once to its type (`ROUND`, relative to the
 value); sums of n fp32 terms and the rounded functions in them are off by at most
 (n + 16) 2^-24 of the terms' magnitudes.  The bf16 scan also rounds a chunk's
 weights and the state that y (dB) reads to bf16, each 2^-8 of the terms'
-magnitudes, and its fp32-typed results keep 2^-18 of every state term."""
+magnitudes, and its fp32-typed results keep 2^-17 of every state term."""
 from __future__ import annotations
 
 import pytest
