@@ -1335,7 +1335,7 @@ inline int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chu
 inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
   const int NC = (T + L - 1) / L;
   int n = (1024 + BHP - 1) / BHP;
-  const int least = BHP * (NC / 4) < 256 ? 2 : 4;
+  const int least = static_cast<long long>(BHP) * (NC / 4) < 256 ? 2 : 4;
   if (n > NC / least) n = NC / least;
   if (n < 1) n = 1;
   span_chunks = (NC + n - 1) / n;
