@@ -25,7 +25,7 @@
 // Launches.  Forward: logs of all chunks; the states that spans of chunks add, joined over
 // the spans; y, a workgroup per head and span carrying the state in registers.  Backward:
 // logs, span states in both directions and their join; a record of S and R per chunk; the
-// gradients, a workgroup per chunk and group.  The records cost 2 x 2 bytes per state
+// gradients, a workgroup per chunk and group.  The records cost 2 x 4 bytes per state
 // element and chunk each way, but let every chunk stand alone: dB and dC of a group are
 // summed over its heads in registers, with no atomics.
 #pragma once
@@ -385,10 +385,10 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 
 // h <- exp(l_L) h + sum_s B_s (scale_s v_s)^T over the chunk's tokens; keys and v are
 // LDS tiles, f the scales of four tokens.  bf16: the scaled values enter as hi + lo, so that
-// the fp32 state keeps 2^-17 of every term: enough for what is rounded to bf16 afterwards (y)
-// and for the sums of the gradients; EXACT, for a state that is returned, with a third part,
-// which keeps all of fp32's bits (the error of a state of 2000 tokens falls from 2e-6 to 1e-7;
-// a forward that returns none would take 1.1 times as long with it).
+// the fp32 state keeps 2^-17 of every term: enough for what is rounded to bf16 afterwards (y);
+// EXACT, for a state that is returned and for the gradients, with a third part, which keeps
+// all of fp32's bits (the error of a state of 2000 tokens falls from 2e-6 to 1e-7; a
+// forward that returns none would take 1.1 times as long with it).
 template <typename E, int NP, int L, bool EXACT, typename F>
 __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::Lane& kt,
                                                  const typename SsmTile<E, kSsmP>::Lane& vt,
@@ -627,27 +627,24 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
 // span's last chunk to its first; a launch does the first `dirs` of the two, half of its
 // workgroups each.  CHUNKS = false: a span's own contribution and its decay, to rec;
 // true: from the span's state in rec, every chunk's state before its tokens are added (S
-// at the chunk's start, R at its end), to `chunks` (R's behind S's): operand planes (bf16
-// hi, lo; fp32 one) of [64 columns][NP], one record per head, block and chunk.  bf16: two
-// planes keep 2^-17 of an element, for the gradients of A and of the steps, which are sums
-// of products of S and R in which much cancels; one plane would leave 2^-8.
+// at the chunk's start, R at its end), to `chunks` (R's behind S's): records of [64
+// columns][NP] fp32, one per head, block and chunk.
 // Span states of 16 heads of 131072 tokens: 78 us, 333 MB counted, 4.3 TB/s, vector and
 // matrix instructions issuing in 73% of the cycles.  Chunk records of 8 x 4096 tokens of 16 heads:
 // 87 us, 438 MB counted (268 MB of them written), 5.0 TB/s, HBM bound.
-template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 2 : 1; }
-
-template <typename E, int NP, bool CHUNKS>
+// An accumulator tile's float4 of a lane is a piece: piece 64 (4 j + w) + lane holds rows
+// 16 j + 4 g .. of column 16 w + c, so that stores are whole lines as they stand.
+template <typename E, int NP>
 struct __attribute__((aligned(16))) SsmStateLds {
   static constexpr int L = ssm_chunk<E>();
   E k[SsmTile<E, NP>::size(L)], v[SsmTile<E, kSsmP>::size(L)];
-  E out[CHUNKS ? SsmTile<E, NP>::size(kSsmP) : 8];  // 16 rows of a record's plane per wave
   SsmChunkLog log;
 };
 
 template <typename E, int NP, bool CHUNKS, bool VEC, bool EXACT>
-__global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, int dirs) {
+__global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, f32x4* chunks, int dirs) {
   constexpr int L = ssm_chunk<E>();
-  __shared__ SsmStateLds<E, NP, CHUNKS> m;
+  __shared__ SsmStateLds<E, NP> m;
   typename SsmTile<E, NP>::Lane kl;
   typename SsmTile<E, kSsmP>::Lane vl;
   // without CHUNKS the forward's last and the reverse's first span go nowhere
@@ -695,31 +692,10 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, E* chunks, in
   for (int i = 0; i < n; ++i) {
     const int t0 = start(i);
     if constexpr (CHUNKS) {
-      E* rec = chunks + ((static_cast<size_t>(bh + (rev ? a.B * a.H : 0)) * blocks + at.pb) * NC + t0 / L) *
-                            (ssm_planes<E>() * kSsmP * NP);
-      // a wave's 16 rows of a plane are one piece of memory: turned in LDS (by this wave for
-      // itself), so that stores are whole lines
-      constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V;
-      typedef SsmTile<E, NP> KT;
-      E* mine = m.out + p0 * KT::stride;
+      f32x4* rec = chunks + ((static_cast<size_t>(bh + (rev ? a.B * a.H : 0)) * blocks + at.pb) * NC + t0 / L) *
+                                (kSsmP * NP / 4);
 #pragma unroll
-      for (int q = 0; q < ssm_planes<E>(); ++q) {
-#pragma unroll
-        for (int j = 0; j < NP / 16; ++j) {
-          const SsmSplit<E> s(st[j]);
-          ssm_half<E> h = s.hi;
-          if constexpr (sizeof(E) == 2) h = q ? s.lo : s.hi;
-          *reinterpret_cast<ssm_half<E>*>(mine + KT::at(c, 16 * j + 4 * g)) = h;
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int j = 0; j < 16 * PER / 64; ++j) {
-          const int at = me.lane + 64 * j;
-          *reinterpret_cast<uint4*>(rec + q * kSsmP * NP + p0 * NP + at * V) =
-              *reinterpret_cast<const uint4*>(mine + KT::at(at / PER, at % PER * V));
-        }
-        __builtin_amdgcn_wave_barrier();
-      }
+      for (int j = 0; j < NP / 16; ++j) rec[(4 * j + wave) * 64 + me.lane] = st[j];
       if (i >= steps) break;
     }
     lds_barrier();
@@ -792,10 +768,16 @@ struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
   float *pB, *pC;  // with several head blocks: their sums, [blocks][B][T][G][N] fp32
   float* part;
-  const void *fwd, *rev;  // chunk records
+  const f32x4 *fwd, *rev;  // chunk records
   int head_block, blocks;
 };
 
+// In LDS a record stands as operand planes, bf16 ones as hi + mid + lo, all of fp32's bits: the
+// gradients of A and of the steps are sums of products of S and R in which much cancels.
+// With hi + lo in state, record and product (2^-17 each) dA or dbias was off by more than 1e-5
+// of itself in 3.6% of a thousand random calls (most of one head) for 1.0%, whose sums cancel
+// in fp32 too; a training step of 8 x 4096 tokens took 352 us for 369.
+template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 3 : 1; }
 constexpr int ssm_grad_threads(int NP) { return NP > 64 ? 512 : 256; }
 
 template <typename E, int NP>
@@ -808,67 +790,56 @@ struct __attribute__((aligned(16))) SsmGradLds {
   SsmChunkLog log[2];                       // of this head and the next
   float row[4][64], col[4][64];             // pair sums by tile of the other index
   float diag[64], trace[64];                // of (C B^T) M exp(l_t - l_s), of M
-  float q[NP / 16][64], k[kSsmP / 16][64];  // state terms by tile of n, of p
+  float q[kWaves / 2][64], k[kWaves / 2][64];  // state terms by the waves' tiles of n, of p
   float dot[kWaves];
 };
 
-// The pieces of a chunk record that a thread moves: the same ones of every plane.
+// The pieces of a chunk record that a thread moves.
 template <typename E, int NP, int THREADS>
 struct SsmRecord {
-  static constexpr int V = 16 / static_cast<int>(sizeof(E)), PER = NP / V, N = kSsmP * PER;
-  static constexpr int K = (N + THREADS - 1) / THREADS, PL = ssm_planes<E>();
-  static_assert(N % THREADS == 0, "every thread moves whole pieces");
-  uint4 r[PL][K];
+  static constexpr int K = kSsmP * NP / 4 / THREADS, PL = ssm_planes<E>();
+  static constexpr int kStep = THREADS / 16;  // rows between pieces
+  static_assert(kSsmP * NP % (4 * THREADS) == 0 && THREADS % 256 == 0, "every thread moves whole pieces");
+  typedef SsmTile<E, NP> KT;
+  f32x4 r[K];
   const SsmSelf& me;
   __device__ __forceinline__ explicit SsmRecord(const SsmSelf& self) : me(self) {}
-  __device__ __forceinline__ void load(const E* rec) {
+  __device__ __forceinline__ void load(const f32x4* rec) {
 #pragma unroll
-    for (int q = 0; q < PL; ++q)
-#pragma unroll
-      for (int j = 0; j < K; ++j)
-        r[q][j] = *reinterpret_cast<const uint4*>(rec + q * kSsmP * NP + (me.thread + j * THREADS) * V);
+    for (int j = 0; j < K; ++j) r[j] = rec[me.thread + j * THREADS];
+  }
+  // The first piece's place in a plane, and the others'.
+  __device__ __forceinline__ int first() const {
+    return KT::at(16 * (me.wave & 3) + me.c, 16 * (me.wave >> 2) + 4 * me.g);
+  }
+  static __device__ __forceinline__ int place(int first, int j) {
+    return KT::kSwizzled ? first ^ j * kStep : first + j * kStep;
   }
   __device__ __forceinline__ void store(E* dst) const {
+    const int o = first();
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      const int i = me.thread + j * THREADS;
-      E* p = dst + SsmTile<E, NP>::at(i / PER, i % PER * V);
+      f32x4 rest = r[j];
 #pragma unroll
-      for (int q = 0; q < PL; ++q)
-        *reinterpret_cast<uint4*>(p + q * SsmTile<E, NP>::size(kSsmP)) = r[q][j];
+      for (int q = 0; q < PL; ++q) {
+        const ssm_half<E> h = to_half<E>(rest);
+        *reinterpret_cast<ssm_half<E>*>(dst + q * KT::size(kSsmP) + place(o, j)) = h;
+        if (q + 1 < PL) rest -= half_f32(h);
+      }
     }
   }
-  // This thread's pieces back.
-  __device__ __forceinline__ void read(const E* src) {
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-      const int i = me.thread + j * THREADS;
-      const E* p = src + SsmTile<E, NP>::at(i / PER, i % PER * V);
-#pragma unroll
-      for (int q = 0; q < PL; ++q)
-        r[q][j] = *reinterpret_cast<const uint4*>(p + q * SsmTile<E, NP>::size(kSsmP));
-    }
-  }
-  // The sum of products of this record's values with another's; bf16 planes: of hi hi,
-  // hi lo and lo hi (lo lo is below 2^-16 of it).
-  __device__ __forceinline__ float dot(const SsmRecord& o) const {
+  // The sum of products of this record's values with those of another that stands in LDS.
+  __device__ __forceinline__ float dot(const E* src) const {
+    const int o = first();
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      if constexpr (PL == 2) {
-        struct Words { bf16x2 w[4]; };
-        const Words a = __builtin_bit_cast(Words, r[0][j]), al = __builtin_bit_cast(Words, r[1][j]);
-        const Words b = __builtin_bit_cast(Words, o.r[0][j]), bl = __builtin_bit_cast(Words, o.r[1][j]);
+      f32x4 v = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sum = __builtin_amdgcn_fdot2_f32_bf16(a.w[i], b.w[i], sum, false);
-          sum = __builtin_amdgcn_fdot2_f32_bf16(a.w[i], bl.w[i], sum, false);
-          sum = __builtin_amdgcn_fdot2_f32_bf16(al.w[i], b.w[i], sum, false);
-        }
-      } else {
-        const float4 a = __builtin_bit_cast(float4, r[0][j]), b = __builtin_bit_cast(float4, o.r[0][j]);
-        sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, sum))));
-      }
+      for (int q = PL - 1; q >= 0; --q)  // exact
+        v += half_f32(*reinterpret_cast<const ssm_half<E>*>(src + q * KT::size(kSsmP) + place(o, j)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = fmaf(r[j][i], v[i], sum);
     }
     return sum;
   }
@@ -897,10 +868,11 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
   // dx: WP x WS, PP x TP tiles of p and tokens
   constexpr int NG = LT == 4 && NT == 2 ? 4 : 2, WN = WV / NG, NN = NT / WN, TN = LT / NG;
   constexpr int WS = WV / 2 < LT ? WV / 2 : LT, WP = WV / WS, PP = PT / WP, TP = LT / WS;
+  static_assert(WN <= WV / 2 && WP <= WV / 2, "places of the state terms");
   typedef SsmTile<E, NP> KT;
   typedef SsmTile<E, kSsmP> VT;
   typedef SsmTile<E, L> WT;
-  constexpr int kRecord = ssm_planes<E>() * kSsmP * NP, kPlane = KT::size(kSsmP);
+  constexpr int kRecord = kSsmP * NP / 4, kPlane = KT::size(kSsmP);
   __shared__ SsmGradLds<E, NP> m;
   typename KT::Lane kt;
   typename VT::Lane vt;
@@ -930,7 +902,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
             a.P - pc);
     ry.load(static_cast<const E*>(a.dy) + b * a.yb + h * a.yh + t0 * a.yt + pc, a.yt, rows,
             a.P - pc);
-    rs.load(static_cast<const E*>(o.fwd) + record(turn));
+    rs.load(o.fwd + record(turn));
     if (wave == 0) rl = ssm_log_row<L>(a, bh, NC)[t0];
   };
   {
@@ -938,7 +910,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     rb.load(static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg + t0 * a.bt, a.bt, rows, a.N);
     rc.load(static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg + t0 * a.ct, a.ct, rows, a.N);
     fetch(0);
-    rr.load(static_cast<const E*>(o.rev) + record(0));
+    rr.load(o.rev + record(0));
     rb.store(m.b);
     rc.store(m.c);
   }
@@ -1062,8 +1034,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       }
     }
     lds_barrier();
-    rs.read(m.st);  // again, its registers having served others meanwhile
-    dot += rs.dot(rr);
+    dot += rr.dot(m.st);  // a thread's own pieces: it may overwrite them
     rr.store(m.st);
     ssm_stretch();
     if (turn + 1 < turns) fetch(turn + 1);
@@ -1154,7 +1125,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     ssm_stretch();
     if (pb + 1 < blocks) {
       lds_barrier();
-      rr.load(static_cast<const E*>(o.rev) + record(turn + 1));
+      rr.load(o.rev + record(turn + 1));
       continue;
     }
     me.fresh();
@@ -1173,7 +1144,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     lds_barrier();
     kt.fresh(), wt.fresh(), me.fresh();
     n0 = 16 * NN * (wave % WN), tn = wave / WN;
-    if (turn + 1 < turns) rr.load(static_cast<const E*>(o.rev) + record(turn + 1));
+    if (turn + 1 < turns) rr.load(o.rev + record(turn + 1));
 #pragma unroll
     for (int k = 0; k < L; k += 32) {
       ssm_half<E> kb[NN][2], kc[NN][2];
@@ -1367,7 +1338,7 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
   w.log = take(dirs * gaps * sizeof(double));
   w.blocks = 1, w.head_block = H / G;
   if (backward) {
-    const size_t rec = static_cast<size_t>(kSsmP) * ssm_np(N) * 4;  // bf16: two planes
+    const size_t rec = static_cast<size_t>(kSsmP) * ssm_np(N) * sizeof(float);
     const size_t all = static_cast<size_t>(B) * H * blocks * NC * rec;
     w.fwd = take(2 * all);
     w.rev = w.fwd + all;
@@ -1436,12 +1407,12 @@ hipError_t ssm_fwd_np(const SsmArgs& a, hipStream_t st) {
 }
 
 template <typename E, int NP, bool VEC>
-hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, E* chunks, float* dA, float* dD,
+hipError_t ssm_bwd_np(const SsmArgs& a, const SsmGrads& o, f32x4* chunks, float* dA, float* dD,
                       float* dbias, hipStream_t st) {
   const int blocks = (a.P + kSsmP - 1) / kSsmP, L = ssm_chunk<E>(), NC = (a.T + L - 1) / L;
   KATA_TRY(ssm_logs<E>(a, st));
-  KATA_TRY((ssm_between_spans<E, NP, VEC, false>(a, 2, st)));
-  ssm_state_kernel<E, NP, true, VEC, false>
+  KATA_TRY((ssm_between_spans<E, NP, VEC, sizeof(E) == 2>(a, 2, st)));
+  ssm_state_kernel<E, NP, true, VEC, sizeof(E) == 2>
       <<<static_cast<unsigned>(a.B) * a.H * blocks * a.spans * 2, 256, 0, st>>>(a, chunks, 2);
   KATA_TRY(hipGetLastError());
   const unsigned grid = static_cast<unsigned>(a.B) * NC * a.G * o.blocks;
@@ -1495,17 +1466,17 @@ hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, 
   a.rec_log = reinterpret_cast<double*>(base + w.log);
   const SsmGrads o = {dx, ddt, dBm, dCm, reinterpret_cast<float*>(base + w.pB),
                       reinterpret_cast<float*>(base + w.pC),
-                      reinterpret_cast<float*>(base + w.part), base + w.fwd, base + w.rev,
-                      w.head_block, w.blocks};
+                      reinterpret_cast<float*>(base + w.part),
+                      reinterpret_cast<const f32x4*>(base + w.fwd),
+                      reinterpret_cast<const f32x4*>(base + w.rev), w.head_block, w.blocks};
+  f32x4* chunks = reinterpret_cast<f32x4*>(base + w.fwd);
   if (bf16) {
-    bf16_t* chunks = reinterpret_cast<bf16_t*>(base + w.fwd);
 #define KATA_CALL(K)                                                        \
   (a.vec ? ssm_bwd_np<bf16_t, K, true>(a, o, chunks, dA, dD, dbias, st)     \
          : ssm_bwd_np<bf16_t, K, false>(a, o, chunks, dA, dD, dbias, st))
     KATA_SSM_NP(KATA_CALL)
 #undef KATA_CALL
   }
-  float* chunks = reinterpret_cast<float*>(base + w.fwd);
 #define KATA_CALL(K)                                                       \
   (a.vec ? ssm_bwd_np<float, K, true>(a, o, chunks, dA, dD, dbias, st)     \
          : ssm_bwd_np<float, K, false>(a, o, chunks, dA, dD, dbias, st))
