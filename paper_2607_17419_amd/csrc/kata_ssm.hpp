@@ -631,7 +631,7 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
 // columns][NP] fp32, one per head, block and chunk.
 // Span states of 16 heads of 131072 tokens: 78 us, 333 MB counted, 4.3 TB/s, vector and
 // matrix instructions issuing in 73% of the cycles.  Chunk records of 8 x 4096 tokens of 16 heads:
-// 87 us, 438 MB counted (268 MB of them written), 5.0 TB/s, HBM bound.
+// 85 us, 434 MB counted (268 MB of them written), 5.1 TB/s, HBM bound.
 // An accumulator tile's float4 of a lane is a piece: piece 64 (4 j + w) + lane holds rows
 // 16 j + 4 g .. of column 16 w + c, so that stores are whole lines as they stand.
 template <typename E, int NP>
@@ -760,9 +760,10 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
 // there are as many, each operand read serving two products.  Four waves, so that two
 // workgroups share a CU and one works through the other's barriers; eight at N > 64,
 // whose records leave LDS for one workgroup.
-// 8 x 4096 tokens of 16 heads, N = P = 64, bf16: 153 us, 512 MB counted (268 MB of
-// records), 3.3 TB/s; vector instructions take 35% of the cycles, LDS 34%, matrix instructions 10%, the
-// rest are waits at the six barriers of a head, which two workgroups of a CU half cover.
+// 8 x 4096 tokens of 16 heads, N = P = 64, bf16: 176 us, 512 MB counted (268 MB of
+// records), 2.9 TB/s; vector instructions take 44% of the cycles, LDS 40%, matrix
+// instructions 11%, the rest are waits at the six barriers of a head, which two workgroups
+// of a CU half cover.
 // part: dA, dD, dbias of the chunk, [B * NC][3][H].
 struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
