@@ -232,7 +232,7 @@ struct SsmRows {
 // moved up, where they would hold registers that the accumulators need.
 __device__ __forceinline__ void ssm_stretch() { __builtin_amdgcn_sched_barrier(0); }
 
-// Inclusive sums over a wave's lanes in fp64: within rows of 16 lanes by DPP shifts, then
+// Inclusive sums in fp64 over the lanes of a row of 16 by DPP shifts, and over a wave's: then
 // the last lane of a row to the next row, of the first two rows to the last two.
 struct Halves64 {
   int lo, hi;
@@ -243,13 +243,20 @@ __device__ __forceinline__ double dpp_add(double x) {
   const Halves64 h = __builtin_bit_cast(Halves64, x);
   return x + __builtin_bit_cast(double, Halves64{move(h.lo), move(h.hi)});
 }
-__device__ __forceinline__ double scan_wave(double x) {
+__device__ __forceinline__ double scan_row(double x) {
   x = dpp_add<0x111, 0xF>(x);
   x = dpp_add<0x112, 0xF>(x);
   x = dpp_add<0x114, 0xF>(x);
-  x = dpp_add<0x118, 0xF>(x);
-  x = dpp_add<0x142, 0xA>(x);
+  return dpp_add<0x118, 0xF>(x);
+}
+__device__ __forceinline__ double scan_wave(double x) {
+  x = dpp_add<0x142, 0xA>(scan_row(x));
   return dpp_add<0x143, 0xC>(x);
+}
+__device__ __forceinline__ double read_lane(double x, int lane) {
+  const Halves64 h = __builtin_bit_cast(Halves64, x);
+  return __builtin_bit_cast(double, Halves64{__builtin_amdgcn_readlane(h.lo, lane),
+                                             __builtin_amdgcn_readlane(h.hi, lane)});
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -775,9 +782,8 @@ struct SsmGrads {
 
 // In LDS a record stands as operand planes, bf16 ones as hi + mid + lo, all of fp32's bits: the
 // gradients of A and of the steps are sums of products of S and R in which much cancels.
-// With hi + lo in state, record and product (2^-17 each) dA or dbias was off by more than 1e-5
-// of itself in 3.6% of a thousand random calls (most of one head) for 1.0%, whose sums cancel
-// in fp32 too; a training step of 8 x 4096 tokens took 352 us for 369.
+// With hi + lo in state, record and product (2^-17 each) a training step of 8 x 4096 tokens took
+// 352 us for 369, and more heads' dA and dbias were off by more than 1e-5 of themselves.
 template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 3 : 1; }
 constexpr int ssm_grad_threads(int NP) { return NP > 64 ? 512 : 256; }
 
@@ -789,7 +795,8 @@ struct __attribute__((aligned(16))) SsmGradLds {
   E st[ssm_planes<E>() * SsmTile<E, NP>::size(kSsmP)];
   E w[SsmTile<E, L>::size(L)], mw[SsmTile<E, L>::size(L)];
   SsmChunkLog log[2];                       // of this head and the next
-  float row[4][64], col[4][64];             // pair sums by tile of the other index
+  // pair sums by tile of the other index; a diagonal tile's row: its pairs across each token
+  float row[4][64], col[4][64];
   float diag[64], trace[64];                // of (C B^T) M exp(l_t - l_s), of M
   float q[kWaves / 2][64], k[kWaves / 2][64];  // state terms by the waves' tiles of n, of p
   float dot[kWaves];
@@ -853,6 +860,13 @@ __device__ __forceinline__ float sum_g(float v) {
   return v + __shfl_xor(v, 32);
 }
 __device__ __forceinline__ float sum_wave(float v) { return sum_group<64>(v); }
+// The sum over the lanes at and past each of a row of 16.
+__device__ __forceinline__ float sum_lanes_from(float v) {
+  v += dpp_move<0x101>(v);
+  v += dpp_move<0x102>(v);
+  v += dpp_move<0x104>(v);
+  return v + dpp_move<0x108>(v);
+}
 
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
@@ -985,8 +999,9 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
       if (pb + 1 != blocks) continue;
-      // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s):
-      // over s < t with step_s (row), over t > s (col), s = t
+      // M exp(l_t - l_s) step_s as an operand, and the sums of (C B^T) M exp(l_t - l_s): over
+      // s with step_s (row), over t > s (col), s = t.  In a diagonal tile row holds, for
+      // each token c of it, the pairs s < c <= t: sums over the lanes t >= c, then over s.
       const f32x4 f = acc * dec;
       f32x4 pair = f * cb[j];
       *reinterpret_cast<ssm_half<E>*>(m.mw + WT::at(t, s)) = to_half<E>(f * step);
@@ -995,7 +1010,15 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         for (int i = 0; i < 4; ++i)
           if (4 * g + i == c) m.diag[t] = pair[i], m.trace[t] = acc[i], pair[i] = 0.f;
       }
-      const float row = sum_g(dot4(pair, step));
+      f32x4 rows = pair * step;
+      if (tt == ss) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          rows[i] = sum_lanes_from(rows[i]);
+          rows[i] = 4 * g + i < c ? rows[i] : 0.f;
+        }
+      }
+      const float row = sum_g((rows[0] + rows[1]) + (rows[2] + rows[3]));
       if (g == 0) m.row[ss][t] = row;
       f32x4 col;
 #pragma unroll
@@ -1171,38 +1194,58 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     }
     // the waves take turns at what one wave does
     if (wave == turn % WV) {
-      // e_t = sum_{u >= t} (q_u + row_u - step_u col_u) + sum_{s < t} step_s k_s + the
-      // state that passes through; in fp64, since the sums over u cancel
-      const int t = min(lane, L - 1);
-      const float step = lg.step[t];
-      float row = 0.f, col = 0.f, q = 0.f, k = 0.f;
-#pragma unroll
-      for (int j = 0; j < LT; ++j) {
-        if (16 * j <= t) row += m.row[j][t];
-        if (j >= t / 16) col += m.col[j][t];
-      }
-#pragma unroll
-      for (int j = 0; j < WN; ++j) q += m.q[j][t];
-#pragma unroll
-      for (int j = 0; j < WP; ++j) k += m.k[j][t];
+      // e_t = sum_{u >= t} q_u + sum_{s < t} step_s k_s + the state that passes through + the
+      // pairs s < t <= u.  These, t being in tile tau: the ones of tiles ss < tau, as
+      // sum_{u >= t} over all tiles (in after) less the tiles ss >= tau (later), which are the same
+      // fp32 numbers and cancel in fp64; of tiles ss = tau < tt, sum_{s < t} step_s col; of the
+      // diagonal tile, row.  So only rounding errors of pairs across t reach e_t: in fp32, all pairs
+      // u >= t less the pairs s >= t would leave those of the whole chunk, which is the larger the
+      // less the tokens cross.
+      const int t = min(lane, L - 1), tau = t >> 4, at = t & 15;
       const bool in = lane < rows;
-      const double after = in ? static_cast<double>(q) + row - static_cast<double>(step) * col : 0.0;
-      const double before = in ? static_cast<double>(step) * k : 0.0;
+      const double step = lg.step[t];
+      // all reads ahead of what selects among them: no branch, and one wait
+      float from[LT - 1], to[LT - 1], of[LT - 1], qk[WN + WP];
+#pragma unroll
+      for (int j = 0; j < WN + WP; ++j) qk[j] = j < WN ? m.q[j][t] : m.k[j - WN][t];
+#pragma unroll
+      for (int j = 0; j + 1 < LT; ++j)
+        from[j] = m.row[j][t], to[j] = m.col[j + 1][t], of[j] = m.row[tau][16 * (j + 1) + at];
+      const float row = m.row[tau][t], own = m.col[tau][t] + m.diag[t];
+      double after = 0.0, tile = 0.0, col = 0.0, k = 0.0;
+#pragma unroll
+      for (int j = 0; j < WN; ++j) after += qk[j];
+#pragma unroll
+      for (int j = WN; j < WN + WP; ++j) k += qk[j];
+#pragma unroll
+      for (int j = 0; j + 1 < LT; ++j) {
+        after += j < tau ? from[j] : 0.f;
+        col += j + 1 > tau ? to[j] : 0.f;
+        tile += j + 1 > tau && 16 * (j + 1) + at < rows ? of[j] : 0.f;
+      }
+      const double direct = in ? own + col + k : 0.0;
+      const double across = in ? step * col : 0.0, before = in ? step * k : 0.0;
+      if (!in) after = tile = 0.0;
       // sum_{u >= t} after + sum_{s < t} before, from one running sum of their difference
-      const double diff = scan_wave(before - after), all = scan_wave(after);
-      const Halves64 last = __builtin_bit_cast(Halves64, all);
-      const double total = __builtin_bit_cast(
-          double, Halves64{__builtin_amdgcn_readlane(last.lo, 63), __builtin_amdgcn_readlane(last.hi, 63)});
+      const double diff = scan_wave(before - after), total = read_lane(scan_wave(after), 63);
+      const double tiles = scan_row(tile), sums = scan_row(across) - across;
+      double later = 0.0;  // of the tiles ss >= tau
+#pragma unroll
+      for (int j = 0; j + 1 < LT; ++j) {
+        const double all = read_lane(tiles, 16 * j + 15);
+        later += j >= tau ? all : 0.0;
+      }
       float through = 0.f;
 #pragma unroll
       for (int j = 0; j < WV; ++j) through += m.dot[j];
-      const float e = static_cast<float>(total + (diff - (before - after)) +
-                                         static_cast<double>(lg.all) * through);
-      const float ddt = (m.diag[t] + col + k + e * a.A[h]) * lg.gate[t];
+      const double e = (total - later + (diff - (before - after))) + sums + row +
+                       static_cast<double>(lg.all) * through;
+      const double ddt = (direct + e * a.A[h]) * lg.gate[t];
       if (in)
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
-                  ddt);
-      const float dA = sum_wave(in ? e * step : 0.f), db = sum_wave(in ? ddt : 0.f);
+                  static_cast<float>(ddt));
+      const float dA = static_cast<float>(read_lane(scan_wave(in ? e * step : 0.0), 63));
+      const float db = static_cast<float>(read_lane(scan_wave(in ? ddt : 0.0), 63));
       const float dD = sum_wave(in ? m.trace[t] : 0.f);
       if (lane == 0) {
         float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
