@@ -533,6 +533,8 @@ KATA_API size_t kata_qk_norm_bwd_workspace_bytes(int B, int T, int Hq, int Hk, i
  *   the weights of a chunk's pairs and the state that y reads are rounded to bf16 once, the
  *   state itself keeps 2^-17 of every term (all of fp32's bits where S_out is asked for).
  *   A positive A or a negative step grows the state as the formula says, until it overflows.
+ *   With softplus a dt of -inf, or of the type's lowest value, is a step of 0: its token leaves
+ *   the state as it is.
  *   strides : element strides over batch, token and head (group); null: contiguous.
  *   workspace : at least kata_ssm_workspace_bytes(..., backward) bytes (0: invalid or
  *   unsupported arguments), 256-byte aligned, contents undefined on exit.

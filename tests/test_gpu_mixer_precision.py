@@ -13,7 +13,8 @@ import torch
 
 import mixer_reference as ref
 from gpu_helpers import log
-from test_gpu_mixer import BF16, DEV, F32, ROUND, kata, near, normal, ssm_inputs, up  # noqa: F401
+from test_gpu_mixer import (BF16, DEV, F32, ROUND, kata, near, normal, ssm_inputs, ssm_tol,  # noqa: F401
+                            state_tol, up)
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +77,48 @@ def test_ssm_parameter_gradients_as_near_as_fp32(kata, dtype):  # noqa: F811
         ours, plain = torch.cat(parts, 1).square().mean(1).sqrt().tolist()
         log(f"  {name}: {ours:.2e}, in fp32 {plain:.2e}")
         assert ours <= 2 * plain, (name, ours, plain)
+
+
+# ---- steps of masked tokens --------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_ssm_steps_of_masked_tokens_are_zero(kata, dtype):  # noqa: F811
+    """dt of -inf, of the type's lowest value and of large negative ones: a step of 0, which
+    leaves the state as it is, in a sequence, its gradients and token by token."""
+    B, T, H, G, N, P = 1, 90, 2, 1, 16, 16
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, T, H, G, N, P, dtype, 17)
+    dy = normal(gen, B, T, H, P, dtype=dtype)
+    low = torch.finfo(dtype).min
+    for at, value in ((0, low), (5, -math.inf), (17, -2.3e38), (31, -2.5e38), (40, -1e30), (63, low), (64, -math.inf),
+                      (70, -200.0), (71, -104.5), (72, -100.0), (73, -88.0), (89, low)):
+        dt[:, at, 0] = value
+    dt = dt.to(dtype).double()
+    log(f"case ssm masked tokens {dtype}")
+    ins = [up(t, dtype) for t in (x, dt, Bm, Cm)]
+    rest = (up(D), up(bias))
+    y, S = kata.ssm_fwd(ins[0], ins[1], up(A), ins[2], ins[3], *rest, final_state=True)
+    want, last = ref.scan(x, dt, A, Bm, Cm, D, bias)
+    mag, smag = ref.scan_mag(x, dt, A, Bm, Cm, D, bias, True, None, None)
+    near(y, want, ssm_tol(want, mag, dtype, N, T), "y")
+    near(S, last, state_tol(smag, N, T, dtype), "state")
+    S = torch.zeros_like(S)
+    for t in range(T):
+        out = kata.ssm_step(S, ins[0][:, t], ins[1][:, t], up(A), ins[2][:, t], ins[3][:, t], *rest)
+        near(out, want[:, t], ssm_tol(want, mag, dtype, N, T)[:, t], f"step {t}")
+    near(S, last, state_tol(smag, N, T, dtype), "state of the steps")
+    got = kata.ssm_bwd(ins[0], ins[1], up(A), ins[2], ins[3], *rest, up(dy, dtype))
+    grads = ref.scan_grads(x, dt, A, Bm, Cm, D, bias, dy)
+    mags = ref.scan_grads_mag(x, dt, A, Bm, Cm, D, bias, dy)
+    # a gate below fp32's smallest normal value, as of the tokens of -88 to -104, may be lost: off by
+    # 2^-126 of what it multiplies, the magnitudes of the same call with the steps themselves as dt
+    steps = ref.softplus(dt + bias)
+    lost = 2.0 ** -126 * ref.scan_grads_mag(x, steps, A, Bm, Cm, D, None, dy, False)[1]
+    for g, r, m, name in zip(got, grads, mags, ("dx", "ddt", "dA", "dB", "dC", "dD", "dbias")):
+        if name in ("dx", "dB", "dC"):
+            tol = ssm_tol(r, m, dtype, N + H, T)
+        elif name == "ddt":
+            tol = (2 * (N + P + 128) + T) * ref.EPS32 * m + ROUND(dtype) * r.abs() + lost
+        else:
+            tol = (2 * (N + P + 128) + T) * ref.EPS32 * m + ref.EPS32 * r.abs()
+        near(g, r, tol, name)
+    assert (got[1][0, [0, 5, 17, 31, 40, 63, 64, 70, 89], 0] == 0).all()
