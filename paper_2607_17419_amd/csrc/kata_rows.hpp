@@ -86,20 +86,6 @@ __device__ __forceinline__ float sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896341f * x));
 }
 
-// log(1 + e^x) to a few ulp: e^x as exp2 of x log2 e in two parts; log(1 + u) by the
-// quotient u log(w) / (w - 1) with w = 1 + u rounded, whose two errors of rounding w cancel
-// (W. Kahan's form), so that small u keep their relative accuracy.  Below -104, where e^x is
-// nothing in fp32, exactly 0: there x log2 e may be infinite, and its two parts' sum NaN.
-__device__ __forceinline__ float softplus(float x) {
-  const float t = 1.44269504088896341f * x;
-  const float rest = fmaf(1.44269504088896341f, x, -t) + 1.92596299e-8f * x;
-  const float e = __builtin_amdgcn_exp2f(t);
-  const float u = fmaf(e, 0.693147180559945309f * rest, e), w = 1.f + u;
-  const float l = 0.693147180559945309f * __builtin_amdgcn_logf(w);
-  const float y = w == 1.f ? u : u * l * __builtin_amdgcn_rcpf(w - 1.f);
-  return x > 20.f ? x : (x < -104.f ? 0.f : y);
-}
-
 // V elements as they stand in memory, loaded some time before they are used.
 template <typename E, int V>
 struct RawVec {

@@ -261,6 +261,38 @@ __device__ __forceinline__ double read_lane(double x, int lane) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A token's step and its derivative by dt.
+struct SsmStep {
+  double step, gate;
+};
+// z = dt + bias, softplus(z) and its derivative, in fp64 to 1e-10 of themselves: z in fp32 would be
+// off by 2^-24 |z|, and a step or gate of e^z, z = -5, by five times its own rounding (dt_dbias
+// of random bf16 calls 1.8e-7 off for 1.2e-7).  With u = e^-|z| from Taylor's series of e^f,
+// |f| <= log(2) / 2, to f^9:
+//   softplus(z) = max(z, 0) + log(1 + u),  log(1 + u) = 2 artanh(s), s = u / (2 + u) <= 1 / 3,
+//   by its series to s^19;  the derivative is 1 / (1 + u), for z < 0 u / (1 + u).
+// u = 0 where e^z is nothing in fp32: -inf and the lowest numbers, as masks use them, give 0.
+__device__ __forceinline__ SsmStep ssm_step_of(double z, bool softplus) {
+  if (!softplus) return {z, 1.0};
+  const double a = -fabs(z), n = rint(a * 1.4426950408889634074), f = a - n * 0.69314718055994530942;
+  double u = 1.0 / 362880.0;
+  constexpr double kSeries[] = {1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (double k : kSeries) u = fma(u, f, k);
+  u = a < -104.0 ? 0.0 : __builtin_amdgcn_ldexp(u, static_cast<int>(n));
+  const double p = 1.0 + u, q = 2.0 + u, d = p * q;
+  double r = __builtin_amdgcn_rcp(d);  // 1 / d, by Newton's iteration
+  r = fma(fma(-d, r, 1.0), r, r);
+  const double s = u * p * r, s2 = s * s;
+  double l = 2.0 / 19;
+#pragma unroll
+  for (int k = 17; k > 0; k -= 2) l = fma(l, s2, 2.0 / k);
+  return {fmax(z, 0.0) + l * s, (z < 0.0 ? u : 1.0) * q * r};
+}
+__device__ __forceinline__ SsmStep ssm_step_of(float dt, const float* bias, int h, bool softplus) {
+  return ssm_step_of(static_cast<double>(dt) + (bias ? static_cast<double>(bias[h]) : 0.0), softplus);
+}
+
 // A first kernel forms them once for all others: per token {hi, lo, step, gate} with the
 // running sum l = hi + lo of step A over the chunk in units of log 2 (summed in fp64:
 // differences of l keep 2^-48 of the largest, and exp(l_t - l_s) is right where a strong
@@ -275,14 +307,11 @@ __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   const int t = chunk * L + lane;
   const bool live = lane < L && t < len;
-  float step = 0.f, gate = 0.f;
-  if (live) {
-    const float z = to_f32(static_cast<const E*>(a.dt)[b * a.db + h * a.dh + t * a.dt_t]) +
-                    (a.bias ? a.bias[h] : 0.f);
-    step = a.softplus ? softplus(z) : z;
-    gate = a.softplus ? sigmoid(z) : 1.f;
-  }
-  double l = static_cast<double>(step) * (static_cast<double>(a.A[h]) * 1.4426950408889634074);
+  SsmStep v = {0.0, 0.0};
+  if (live)
+    v = ssm_step_of(to_f32(static_cast<const E*>(a.dt)[b * a.db + h * a.dh + t * a.dt_t]), a.bias, h,
+                    a.softplus);
+  double l = v.step * (static_cast<double>(a.A[h]) * 1.4426950408889634074);
   // 2^-2000 and 2^2000 are 0 and inf in fp32: bounded, sums and their differences stay finite
   l = l < -2000.0 ? -2000.0 : (l > 2000.0 ? 2000.0 : l);  // (NaN stays)
   if (!live) l = 0.0;
@@ -290,7 +319,8 @@ __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   if (lane >= L) return;
   const float hi = static_cast<float>(l);
   a.logs[(static_cast<size_t>(b * a.H + h) * NC + chunk) * L + lane] =
-      make_float4(hi, isfinite(hi) ? static_cast<float>(l - hi) : 0.f, step, gate);
+      make_float4(hi, isfinite(hi) ? static_cast<float>(l - hi) : 0.f, static_cast<float>(v.step),
+                  static_cast<float>(v.gate));
 }
 
 // A chunk's logs in LDS, with exp(l_t) (since) and exp(l_L - l_t) (left); all = exp(l_L).
@@ -1299,9 +1329,8 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(float* S, SsmArgs a) {
   const E* x = static_cast<const E*>(a.x) + b * a.xb + h * a.xh;
   const E* Bm = static_cast<const E*>(a.Bm) + b * a.bb + grp * a.bg;
   const E* Cm = static_cast<const E*>(a.Cm) + b * a.cb + grp * a.cg;
-  const float z = to_f32(*(static_cast<const E*>(a.dt) + b * a.db + h * a.dh)) +
-                  (a.bias ? a.bias[h] : 0.f);
-  const float step = a.softplus ? softplus(z) : z;
+  const float step = static_cast<float>(
+      ssm_step_of(to_f32(*(static_cast<const E*>(a.dt) + b * a.db + h * a.dh)), a.bias, h, a.softplus).step);
   const float decay = expf(step * a.A[h]);
   const int cols = a.P / V, lanes = 256 / cols;  // rows at once; P / V <= 256
   const int r0 = threadIdx.x / cols, pc = (threadIdx.x % cols) * V;

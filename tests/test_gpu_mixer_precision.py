@@ -122,3 +122,26 @@ def test_ssm_steps_of_masked_tokens_are_zero(kata, dtype):  # noqa: F811
             tol = (2 * (N + P + 128) + T) * ref.EPS32 * m + ref.EPS32 * r.abs()
         near(g, r, tol, name)
     assert (got[1][0, [0, 5, 17, 31, 40, 63, 64, 70, 89], 0] == 0).all()
+
+
+def test_ssm_steps_and_gates_to_fp32(kata):  # noqa: F811
+    """Of one token with one feature all is a product: y = C B step x and ddt = dy C B x gate, each
+    from a step or gate of fp32 precision wherever z = dt + bias lies, and seven roundings."""
+    B, H = 300, 4
+    gen = torch.Generator().manual_seed(3)
+    dt = torch.linspace(-84, 24, B * H, dtype=torch.float64).view(B, 1, H).float().double()
+    x, dy, Bm, Cm = (normal(gen, B, 1, H, 1, dtype=F32) for _ in range(4))
+    A, bias = torch.full((H,), -1.0, dtype=torch.float64), normal(gen, H, dtype=F32)
+    log("case ssm steps and gates")
+    args = (up(x), up(dt), up(A), up(Bm), up(Cm), None, up(bias))
+    y, S = kata.ssm_fwd(*args, final_state=True)
+    step = ref.softplus(dt + bias)[..., None]
+    near(S, (step * Bm * x)[:, 0, :, :, None], 8 * ref.EPS32 * (step * Bm * x).abs()[:, 0, :, :, None], "state")
+    near(y, step * Bm * Cm * x, 8 * ref.EPS32 * (step * Bm * Cm * x).abs(), "y")
+    one = [t[:, 0] for t in (args[0], args[1], args[3], args[4])]
+    y = kata.ssm_step(torch.zeros_like(S), one[0], one[1], args[2], one[2], one[3], None, args[6])
+    near(y, (step * Bm * Cm * x)[:, 0], 8 * ref.EPS32 * (step * Bm * Cm * x).abs()[:, 0], "y of a step")
+    ddt = kata.ssm_bwd(*args, up(dy))[1]
+    want = (dy * x * Bm * Cm)[..., 0] * torch.sigmoid(dt + bias)
+    # (a few lie below 2^-126, where fp32's steps are 2^-149 and a rounding is off by half of one)
+    near(ddt, want, 8 * ref.EPS32 * want.abs() + 2.0 ** -150, "ddt")
