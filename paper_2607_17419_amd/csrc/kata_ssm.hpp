@@ -425,15 +425,22 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 // the fp32 state keeps 2^-17 of every term: enough for what is rounded to bf16 afterwards (y);
 // EXACT, for a state that is returned and for the gradients, with a third part, which keeps
 // all of fp32's bits (the error of a state of 2000 tokens falls from 2e-6 to 1e-7; a
-// forward that returns none would take 1.1 times as long with it).
-template <typename E, int NP, int L, bool EXACT, typename F>
+// forward that returns none would take 1.1 times as long with it).  OWN: the chunk's own
+// sum first, so that the state is rounded once per chunk and not by each of the products
+// added to it, whose errors the states of long memories gather (dA of 16 heads of 1024 tokens
+// 4.4e-7 off for 2.1e-7); for the gradients and fp32.  (ssm_out_kernel's registers do not hold it:
+// a prompt's call 40 us for 38.)
+template <typename E, int NP, int L, bool EXACT, bool OWN, typename F>
 __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::Lane& kt,
                                                  const typename SsmTile<E, kSsmP>::Lane& vt,
                                                  const E* keys, const E* v, int p0, float decay,
                                                  F f, f32x4 (&h)[NP / 16]) {
   const int g = (threadIdx.x >> 4) & 3;
+  f32x4 own[OWN ? NP / 16 : 1] = {};
+  if constexpr (!OWN) {
 #pragma unroll
-  for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
+    for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
+  }
 #pragma unroll
   for (int s0 = 0; s0 < L; s0 += 32) {
     const f32x4 v0 = half_f32(vt.col(v, p0, s0)) * f(s0 + 4 * g);
@@ -446,13 +453,20 @@ __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::
     }
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) {
+      f32x4& sum = OWN ? own[OWN ? j : 0] : h[j];
       const auto k0 = kt.col(keys, 16 * j, s0);
       const auto k1 = kt.col(keys, 16 * j, s0 + 16);
-      h[j] = mac2(k0, k1, a.hi, b.hi, h[j]);
-      if constexpr (sizeof(E) == 2) h[j] = mac2(k0, k1, a.lo, b.lo, h[j]);
-      if constexpr (EXACT) h[j] = mac2(k0, k1, a2, b2, h[j]);
+      sum = mac2(k0, k1, a.hi, b.hi, sum);
+      if constexpr (sizeof(E) == 2) sum = mac2(k0, k1, a.lo, b.lo, sum);
+      if constexpr (EXACT) sum = mac2(k0, k1, a2, b2, sum);
     }
     ssm_stretch();
+  }
+  if constexpr (OWN) {
+#pragma unroll
+    for (int j = 0; j < NP / 16; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[j][i] = fmaf(decay, h[j][i], own[j][i]);
   }
 }
 
@@ -635,7 +649,7 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
     if (__builtin_amdgcn_readfirstlane(m.bad) != t0) columns(std::true_type{});
     else columns(std::false_type{});
     ssm_stretch();
-    ssm_state_update<E, NP, L, EXACT>(
+    ssm_state_update<E, NP, L, EXACT, sizeof(E) == 4>(
         kt, vt, m.b, m.x, 16 * wave, m.log.all, [&](int s) { return m.log.four(m.log.push, s); }, st);
     lds_barrier();
     // a wave's 16 rows of y, turned in its own part of st
@@ -743,7 +757,7 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, f32x4* chunks
     if (i + 1 < steps) fetch(start(i + 1));
     kl.fresh(), vl.fresh(), me.fresh();
     if (!CHUNKS) log_sum += m.log.log;
-    ssm_state_update<E, NP, L, EXACT>(
+    ssm_state_update<E, NP, L, EXACT, EXACT || sizeof(E) == 4>(
         kl, vl, m.k, m.v, p0, m.log.all,
         [&](int s) { return m.log.four(rev ? m.log.since : m.log.push, s); }, st);
   }

@@ -145,3 +145,24 @@ def test_ssm_steps_and_gates_to_fp32(kata):  # noqa: F811
     want = (dy * x * Bm * Cm)[..., 0] * torch.sigmoid(dt + bias)
     # (a few lie below 2^-126, where fp32's steps are 2^-149 and a rounding is off by half of one)
     near(ddt, want, 8 * ref.EPS32 * want.abs() + 2.0 ** -150, "ddt")
+
+
+# ---- states over many chunks --------------------------------------------------------------
+
+def test_ssm_state_rounded_once_a_chunk(kata):  # noqa: F811
+    """The state of 2048 fp32 tokens, decays of 1 and all terms positive, in 64 chunks: the state
+    before it and a chunk's own sum are added with one rounding, off by 2^-24 of the state then at
+    most, so by 2^-24 / sqrt(3) rms; the states grow evenly, so all of them together are off by
+    sqrt(64 / 3 + 1) times that, the 1 for what is rounded within a chunk, on 1/64 of the state."""
+    B, T, H, G, N, P = 64, 2048, 16, 1, 16, 16  # a workgroup for each head: no spans
+    gen = torch.Generator().manual_seed(5)
+    x, Bm = normal(gen, B, T, H, P, dtype=F32).abs(), normal(gen, B, T, G, N, dtype=F32).abs()
+    dt = normal(gen, B, T, H, dtype=F32).abs()
+    log("case ssm state of many chunks")
+    _, S = kata.ssm_fwd(up(x), up(dt), torch.zeros(H, device=DEV), up(Bm), up(Bm), softplus=False, final_state=True)
+    terms = (x * dt[..., None]).to(DEV)
+    want = torch.matmul(Bm.to(DEV)[:, :, 0].transpose(1, 2).contiguous(), terms.flatten(2))
+    want = want.view(B, N, H, P).transpose(1, 2)
+    off = ((S.double() - want) / want).square().mean().sqrt().item()
+    log(f"  state: {off:.2e}")
+    assert off <= ref.EPS32 * math.sqrt((64 / 3 + 1) / 3), off
