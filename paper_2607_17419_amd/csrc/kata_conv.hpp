@@ -16,6 +16,7 @@
 // that are not aligned 104 us.  One token of 256 sequences: 3.2 us, its launch's latency.
 #pragma once
 
+#include "kata_index.hpp"
 #include "kata_rows.hpp"
 
 namespace kata {
@@ -55,8 +56,8 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(const E* __restrict__ x,
   const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
   const long long per = static_cast<long long>(groups) * runs;
   if (id >= per * s.B) return;
-  const int b = static_cast<int>(id / per), rest = static_cast<int>(id - b * per);
-  const int run = rest / groups, c = (rest - run * groups) * V;
+  const ConvPlace at = conv_place(id, groups, runs);
+  const int b = at.b, run = at.run, c = at.group * V;
   const int len = lengths ? min(max(lengths[b], 0), s.T) : s.T;
   const int t0 = run * R, t1 = min(t0 + R, len);
   if (state_out && run == 0) {
