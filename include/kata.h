@@ -530,8 +530,9 @@ KATA_API size_t kata_qk_norm_bwd_workspace_bytes(int B, int T, int Hq, int Hk, i
  *   N <= 128, P <= 256, B*H <= 65535, else KATA_ERR_UNSUPPORTED.
  *   Computed in chunks of 64 (fp32: 32) tokens on the matrix cores; long sequences of few
  *   heads are split into spans whose states are joined.  bf16: products accumulate in fp32,
- *   the weights of a chunk's pairs and the state that y reads are rounded to bf16 once, the
- *   state itself keeps 2^-17 of every term (all of fp32's bits where S_out is asked for).
+ *   the weights of a chunk's pairs and the state that y reads are rounded to bf16 once, D x is
+ *   added in fp32, the state itself keeps 2^-17 of every term (all of fp32's bits where S_out is
+ *   asked for: y of the two calls may differ in a last rounding).
  *   A positive A or a negative step grows the state as the formula says, until it overflows.
  *   With softplus a dt of -inf, or of the type's lowest value, is a step of 0: its token leaves
  *   the state as it is.

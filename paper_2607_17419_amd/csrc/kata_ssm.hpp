@@ -377,7 +377,9 @@ __device__ __forceinline__ unsigned ssm_xcd_order() {
 // chunk behind the accumulators) these tokens' y; then the new state of its columns.
 // The next chunk's rows are on their way meanwhile.  y is turned in LDS into whole lines.
 // The chunk's weights and the state that y reads are rounded to bf16 once (2^-8 of a term
-// each at most, as y itself is rounded), the state that is carried is not.
+// each at most, as y itself is rounded), the state that is carried is not, and D x is added in fp32:
+// on W's diagonal D would be rounded with it, the same factor for all tokens of a head (y 2.3e-3
+// off for 1.8e-3 (rms); 131072 tokens 272 us for 279).
 // 16 heads of 131072 tokens, N = P = 64, bf16: 185 us, 620 MB counted, 3.4 TB/s; bound by issue,
 // vector instructions taking 62% of a SIMD's cycles and matrix ones 20%.  Rows that are not
 // whole aligned pieces are read element by element: 3 times the time of the whole call.
@@ -587,16 +589,15 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
     const int t = 16 * tt + c;
     ssm_half<E> cr[NT], w[LT];
     bool above[4];  // the diagonal
-    float skip[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c, skip[i] = 4 * g + i == c ? D : 0.f;
+    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c;
 #pragma unroll
     for (int k = 0; k < NT; ++k) cr[k] = kt.row(m.c, 16 * tt, 16 * k);
 #pragma unroll
     for (int ss = 0; ss < LT; ++ss) {
       w[ss] = ssm_half<E>{};
       if (ss > tt) continue;
-      // C B^T, rows s, columns t: as a half, row t of W; D on the diagonal
+      // C B^T, rows s, columns t: as a half, row t of W
       f32x4 acc = {};
 #pragma unroll
       for (int k = 0; k < NT; k += 2)
@@ -605,7 +606,7 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
       acc *= m.log.decay(t, s) * m.log.four(m.log.step, s);
       if (tt == ss) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = above[i] ? 0.f : acc[i] + skip[i];
+        for (int i = 0; i < 4; ++i) acc[i] = above[i] ? 0.f : acc[i];
       }
       w[ss] = to_half<E>(acc);
     }
@@ -630,6 +631,9 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
           if (!finite) x0 = ssm_finite<E>(x0), x1 = ssm_finite<E>(x1);
           acc = mac2(x0, x1, w[ss], w[ss + 1], acc);
         }
+        const f32x4 own = half_f32(vt.row(m.x, 16 * tt, p0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(D, own[i], acc[i]);
         if (!finite) {
           bool seen[4] = {};
 #pragma nounroll
@@ -1012,9 +1016,8 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     lds_barrier();
     kt.fresh(), vt.fresh(), wt.fresh(), me.fresh();
     bool above[4];  // the diagonal
-    float skip[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c, skip[i] = 4 * g + i == c ? D : 0.f;
+    for (int i = 0; i < 4; ++i) above[i] = 4 * g + i > c;
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
       if (wave + WV * j >= TRI) break;
@@ -1034,11 +1037,11 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
         for (int i = 0; i < 4; ++i) dec[i] = above[i] ? 0.f : dec[i];
       }
-      if (pb == 0) {  // W, with D on its diagonal
+      if (pb == 0) {  // W
         f32x4 w = cb[j] * dec * step;
         if (tt == ss) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = above[i] ? 0.f : w[i] + skip[i];
+          for (int i = 0; i < 4; ++i) w[i] = above[i] ? 0.f : w[i];
         }
         *reinterpret_cast<ssm_half<E>*>(m.w + WT::at(t, s)) = to_half<E>(w);
       }
@@ -1186,6 +1189,9 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
           const int p = pc + p0 + 16 * i + 4 * g;
+          const f32x4 own = half_f32(vt.row(m.dy, 16 * (tp + WS * j), p0 + 16 * i));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[i][j][k] = fmaf(D, own[k], acc[i][j][k]);
           if (s < rows) ssm_store4<VEC>(row + p, acc[i][j], p, a.P);
         }
       }

@@ -166,3 +166,30 @@ def test_ssm_state_rounded_once_a_chunk(kata):  # noqa: F811
     off = ((S.double() - want) / want).square().mean().sqrt().item()
     log(f"  state: {off:.2e}")
     assert off <= ref.EPS32 * math.sqrt((64 / 3 + 1) / 3), off
+
+
+# ---- the skip parameter ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("B,T,H,G,N,P", ((2, 70, 3, 1, 32, 64), (1, 100, 2, 1, 64, 130), (1, 130, 4, 2, 100, 40)))
+def test_ssm_skip_parameter_keeps_its_bits(kata, B, T, H, G, N, P, dtype):  # noqa: F811
+    """D x and D dy far above the state's terms: D is fp32, so they are off by the output's
+    rounding and 2^-17 (D as two bf16 parts) at most; 2^-8 is for the state's terms alone."""
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, T, H, G, N, P, dtype, T)
+    dy = normal(gen, B, T, H, P, dtype=dtype)
+    D, dt = (D * 1000).float().double(), dt - 3
+    dt = dt.to(dtype).double()
+    log(f"case ssm skip T{T} N{N} P{P} {dtype}")
+    args = (x, dt, A, Bm, Cm)
+    ins = (up(x, dtype), up(dt, dtype), up(A), up(Bm, dtype), up(Cm, dtype), up(D), up(bias))
+    want = ref.scan(*args, D, bias)[0]
+    terms = ref.scan_mag(*args, None, bias, True, None, None)[0]
+    skip = D.abs()[:, None] * x.abs()
+    tol = ssm_tol(want, terms, dtype, N, T) + (2.0 ** -17 + 64 * ref.EPS32) * skip
+    near(kata.ssm_fwd(*ins), want, tol, "y")
+    near(kata.ssm_fwd(*ins, final_state=True)[0], want, tol, "y with a state")
+    dx = kata.ssm_bwd(*ins, up(dy, dtype))[0]
+    want = ref.scan_grads(*args, D, bias, dy)[0]
+    terms = ref.scan_grads_mag(*args, None, bias, dy)[0]
+    near(dx, want, ssm_tol(want, terms, dtype, max(N, P) + H // G, T)
+         + (2.0 ** -17 + 64 * ref.EPS32) * D.abs()[:, None] * dy.abs(), "dx")
