@@ -26,10 +26,7 @@
 #include <cmath>
 
 #include "kata_internal.hpp"
-#include "kata_conv.hpp"
-#include "kata_qknorm.hpp"
 #include "kata_scan.hpp"
-#include "kata_ssm.hpp"
 
 namespace kata {
 

@@ -53,3 +53,18 @@ def test_conv_places_of_sequences_past_2_31_threads(tmp_path):
             continue
         out = subprocess.run([exe, str(T), str(D), str(B)], check=True, capture_output=True, text=True)
         assert out.stdout.strip() == "0" and not out.stderr, (T, D, B, out.stdout, out.stderr)
+
+
+# ---- sources --------------------------------------------------------------------------
+
+def test_mixer_operators_stand_in_a_source_of_their_own():
+    """bench.py reports counted traffic for sources whose hash its record holds: a header of
+    other operators in one of them would drop the record though its kernels are the same."""
+    import bench
+    from paper_2607_17419_amd import build
+    assert "kata_mixer.hip" in build.SOURCES
+    for name in {*bench.M1_SOURCES, *bench.LIN_SOURCES, "kata_fp32.hip"}:
+        with open(os.path.join(os.path.dirname(kata.__file__), "csrc", name)) as f:
+            text = f.read()
+        for header in ("kata_conv.hpp", "kata_qknorm.hpp", "kata_ssm.hpp", "kata_rows.hpp", "kata_mixer"):
+            assert header not in text, (name, header)
