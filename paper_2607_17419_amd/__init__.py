@@ -679,21 +679,26 @@ def _on_stream(call):
     """A call with stream=s runs as on s: the kernels there, and what torch
     allocates for them from s's memory.  The device of the first tensor is made the
     current one meanwhile, if it is not."""
+    name = call.__code__.co_varnames[0]  # the first parameter's
+
     @functools.wraps(call)
-    def run(first, *args, stream=None, **kw):
+    def run(*args, stream=None, **kw):
         import torch
+        first = args[0] if args else kw.get(name)
+        if first is None:
+            raise TypeError(f"{call.__name__}() needs {name}")
         device = first.get_device()
         if device < 0:
             raise ValueError("expected device tensors")
         if stream is None:
             if device == torch._C._cuda_getDevice():
-                return call(first, *args, **kw)
+                return call(*args, **kw)
             with torch.cuda.device(first.device):
-                return call(first, *args, **kw)
+                return call(*args, **kw)
         if stream.device != first.device:
             raise ValueError(f"stream of {stream.device}, tensors of {first.device}")
         with torch.cuda.stream(stream):
-            return call(first, *args, **kw)
+            return call(*args, **kw)
     return run
 
 

@@ -5,6 +5,9 @@ from __future__ import annotations
 import os
 import subprocess
 
+import pytest
+import torch
+
 import paper_2607_17419_amd as kata
 from test_mixer_cpu import _conv_fwd
 
@@ -68,3 +71,19 @@ def test_mixer_operators_stand_in_a_source_of_their_own():
             text = f.read()
         for header in ("kata_conv.hpp", "kata_qknorm.hpp", "kata_ssm.hpp", "kata_rows.hpp", "kata_mixer"):
             assert header not in text, (name, header)
+
+
+# ---- the binding ------------------------------------------------------------------------
+
+def test_first_argument_by_name_or_missing():
+    """A host tensor is refused as one, given by position or by name; none at all is a TypeError."""
+    x, w = torch.zeros(2, 8, 16), torch.zeros(16, 4)
+    for args, named in (((x,), dict(w=w)), ((), dict(x=x, w=w)), ((), dict(w=w, x=x))):
+        with pytest.raises(ValueError, match="device tensors"):
+            kata.conv_fwd(*args, **named)
+    for call, name in ((kata.conv_step, "state"), (kata.conv_bwd, "x"), (kata.qk_norm_fwd, "q"),
+                       (kata.qk_norm_bwd, "q"), (kata.ssm_fwd, "x"), (kata.ssm_step, "S"), (kata.ssm_bwd, "x")):
+        with pytest.raises(ValueError, match="device tensors"):
+            call(**{name: x})
+        with pytest.raises(TypeError, match=name):
+            call()
