@@ -859,6 +859,8 @@ def qk_norm_bwd(q, k=None, wq=None, wk=None, freq=None, dq=None, dk=None, pos=No
     or q's type), via kata_qk_norm_bwd_ws; None where the input is."""
     import torch
     B, T, Hq, Hk, d, r = _norm_sides(q, k, freq)
+    if dq is None or (k is None) != (dk is None):
+        raise ValueError("expected dq, and dk where there is k")
     code, f32, dev = _dtype_code(q), torch.float32, q.get_device()
     if dxq is None:
         dxq = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
