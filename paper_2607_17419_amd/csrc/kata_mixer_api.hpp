@@ -374,9 +374,10 @@ kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, const float
   const kata_status_t c = ssm_check(B, 1, H, G, N, P, softplus, raw(dtype), false);
   if (c != KATA_OK) return c;
   kata::SsmArgs a;
+  kata_ssm_strides_t s = strides ? *strides : ssm_contiguous(1, H, G, N, P);
+  s.x_token = s.dt_token = s.b_token = s.c_token = s.y_token = 0;  // not the caller's: may be anything
   if (!S || !aligned16(S) || !y ||
-      !ssm_tensors(a, x, dt, A, Bm, Cm, D, dt_bias, nullptr, y, B, 1, H, G, N, P, strides, softplus,
-                   dtype))
+      !ssm_tensors(a, x, dt, A, Bm, Cm, D, dt_bias, nullptr, y, B, 1, H, G, N, P, &s, softplus, dtype))
     return KATA_ERR_INVALID_ARG;
   if (!apart({y, S}, {x, dt, A, Bm, Cm, D, dt_bias})) return KATA_ERR_INVALID_ARG;
   return from_hip(kata::launch_ssm_step(S, a, dtype == KATA_BF16, stream));

@@ -33,3 +33,22 @@ def test_norm_gradients_need_the_outputs(kata):  # noqa: F811
     for k, grads in ((None, dict()), (q, dict(dq=dq)), (None, dict(dq=dq, dk=dq)), (q, dict(dk=dq))):
         with pytest.raises(ValueError, match="expected dq"):
             kata.qk_norm_bwd(q, k, **grads)
+
+
+def test_ssm_step_reads_no_token_strides(kata):  # noqa: F811
+    """kata_ssm_step with token strides of anything, as in a struct that is not cleared."""
+    B, H, G, N, P = 3, 2, 1, 16, 16
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, 1, H, G, N, P, F32, 6)
+    x, dt, Bm, Cm = (up(t)[:, 0].contiguous() for t in (x, dt, Bm, Cm))
+    A, D, bias = up(A), up(D), up(bias)
+    S0 = up(normal(gen, B, H, N, P, dtype=F32))
+    S = S0.clone()
+    want = kata.ssm_step(S, x, dt, A, Bm, Cm, D, bias)
+    for junk in (-1, -(1 << 62), (1 << 63) - 1, 7):
+        strides = [H * P, junk, P, H, junk, 1, G * N, junk, N, G * N, junk, N, H * P, junk, P]
+        again, y = S0.clone(), torch.zeros_like(x)
+        rc = kata.lib().kata_ssm_step(*(t.data_ptr() for t in (again, x, dt, A, Bm, Cm, D, bias, y)), B, H, G, N, P,
+                                      kata._SsmStrides(*strides), 1, kata.KATA_F32,
+                                      torch.cuda.current_stream().cuda_stream)
+        assert rc == kata.KATA_OK, junk
+        assert torch.equal(y, want) and torch.equal(again, S)
