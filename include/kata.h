@@ -484,7 +484,8 @@ KATA_API size_t kata_conv_bwd_workspace_bytes(int B, int T, int D, int W, kata_d
 /*
  * Norms of query and key heads with the position rotation in the same pass, from a
  * projection's rows to the head-major tensors of the attention calls above (at T = 1:
- * of the decode step).  For every head row x of width d:
+ * of the decode step), which take as many key heads as query heads.  For every head row x of
+ * width d:
  *     hat = x / sqrt(mean(x^2) + eps)  (KATA_NORM_RMS; KATA_NORM_L2: the sum for the mean;
  *           KATA_NORM_NONE: x),        y = R (w hat),
  * R turning pair i < r/2 of the first r coordinates by the angle pos * freq[i]:
@@ -492,7 +493,7 @@ KATA_API size_t kata_conv_bwd_workspace_bytes(int B, int T, int D, int W, kata_d
  *   q : [B][T][Hq][d], k : [B][T][Hk][d] with strides (batch, token, head); k, wk and the
  *   key outputs are null where Hk = 0.  wq, wk : [d], nullable (ones).
  *   pos : int32 [B][T], nullable (0..T-1);  freq : fp64 [r/2], null where r = 0 (angles are
- *   formed in fp64: positions up to 2^31 lose nothing).
+ *   formed in fp64, off by 2^-52 of themselves: 5e-10 rad at a position of 2^21, 5e-7 at 2^31).
  *   yq : [B][Hq][T][d], yk : [B][Hk][T][d], contiguous, in dtype.
  *   d <= 256 (else KATA_ERR_UNSUPPORTED), r even, 0 <= r <= d, eps >= 0 and finite (a row of
  *   zeros needs eps > 0); Hq + Hk <= 65535.  Squares are summed in fp32.

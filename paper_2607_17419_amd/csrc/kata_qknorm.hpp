@@ -14,8 +14,8 @@
 // (a rotated pair, or two coordinates past the rotation) for every head in turn, so an
 // angle's sine and cosine are formed once per token and not per head, and the sum of squares
 // crosses only the group's lanes.  Angles: the turns pos freq / 2 pi are taken in fp64 and
-// their fraction rounded to fp32 once, so that a position of 2^31 is as exact as
-// one near 0 (fp32 angles are off by 0.06 rad at a position of 10^6).
+// their fraction rounded to fp32 once: off by 2^-52 of the angle, which is more than fp32's
+// rounding of a turn from positions of 2^28 on (fp32 angles are off by 0.06 rad at 10^6).
 #pragma once
 
 #include <type_traits>
