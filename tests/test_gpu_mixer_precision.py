@@ -193,3 +193,21 @@ def test_ssm_skip_parameter_keeps_its_bits(kata, B, T, H, G, N, P, dtype):  # no
     terms = ref.scan_grads_mag(*args, None, bias, dy)[0]
     near(dx, want, ssm_tol(want, terms, dtype, max(N, P) + H // G, T)
          + (2.0 ** -17 + 64 * ref.EPS32) * D.abs()[:, None] * dy.abs(), "dx")
+
+
+def test_ssm_returned_state_keeps_fp32(kata):  # noqa: F811
+    """States of a few tokens' memory from bf16 calls: step, decay, their product, its product with
+    x and the seven sums of a chunk are rounded to fp32, 11 roundings of 2^-24 at most, 2^-24 / sqrt(3)
+    rms each.  (Terms in two bf16 parts would be off by 2^-18.)"""
+    B, T, H, G, N, P = 4, 190, 16, 1, 32, 64
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, T, H, G, N, P, BF16, 23)
+    dt = dt.abs().to(BF16).double() + 0.5
+    dt, A = dt.to(BF16).double(), torch.full((H,), -2.0, dtype=torch.float64)
+    log("case ssm returned state")
+    _, S = kata.ssm_fwd(up(x, BF16), up(dt, BF16), up(A), up(Bm, BF16), up(Cm, BF16), softplus=False,
+                        final_state=True)
+    want = ref.scan(x, dt, A, Bm, Cm, soft=False)[1]
+    mag = ref.scan_mag(x, dt, A, Bm, Cm, None, None, False, None, None)[1]
+    off = ((S.cpu().double() - want) / mag).square().mean().sqrt().item()
+    log(f"  state: {off:.2e}")
+    assert off <= ref.EPS32 * math.sqrt(11 / 3), off
