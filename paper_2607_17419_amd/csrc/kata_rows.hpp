@@ -131,8 +131,8 @@ __device__ __forceinline__ float sum_group(float x) {
   return x;
 }
 
-// Sums of per-workgroup partial sums: part[n][cols] fp32 is summed over n in
-// fp64 in a fixed order, so that results do not depend on the order in which
+// Sums of per-workgroup partial sums: part[n][cols], fp32 or fp64, is summed over n
+// in fp64 in a fixed order, so that results do not depend on the order in which
 // workgroups ran; column c goes to out[0], out[1] or out[2] with their widths
 // one after the other (a null one is dropped).
 struct SumOutputs {
@@ -141,7 +141,8 @@ struct SumOutputs {
 };
 constexpr int kSumCols = 16, kSumRows = 16;  // a workgroup: 16 columns, 16 shares of n each
 
-__global__ __launch_bounds__(kSumCols* kSumRows) void sum_partials(const float* part, int n,
+template <typename Part>
+__global__ __launch_bounds__(kSumCols* kSumRows) void sum_partials(const Part* part, int n,
                                                                    int cols, SumOutputs o) {
   __shared__ double s[kSumRows][kSumCols];
   const int x = threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
@@ -166,8 +167,9 @@ __global__ __launch_bounds__(kSumCols* kSumRows) void sum_partials(const float* 
   }
 }
 
-inline hipError_t launch_sum_partials(const float* part, int n, int cols, const SumOutputs& o,
-                                      hipStream_t st) {
+template <typename Part>
+hipError_t launch_sum_partials(const Part* part, int n, int cols, const SumOutputs& o,
+                               hipStream_t st) {
   sum_partials<<<(cols + kSumCols - 1) / kSumCols, kSumCols * kSumRows, 0, st>>>(part, n, cols, o);
   return hipGetLastError();
 }

@@ -819,11 +819,11 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
 // records), 2.9 TB/s; vector instructions take 44% of the cycles, LDS 40%, matrix
 // instructions 11%, the rest are waits at the six barriers of a head, which two workgroups
 // of a CU half cover.
-// part: dA, dD, dbias of the chunk, [B * NC][3][H].
+// part: dA, dD, dbias of the chunk, [B * NC][3][H], in fp64: a head's chunks may cancel.
 struct SsmGrads {
   void *dx, *ddt, *dBm, *dCm;
   float *pB, *pC;  // with several head blocks: their sums, [blocks][B][T][G][N] fp32
-  float* part;
+  double* part;
   const f32x4 *fwd, *rev;  // chunk records
   int head_block, blocks;
 };
@@ -1294,11 +1294,10 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
       if (in)
         store_f32(static_cast<E*>(o.ddt) + (static_cast<size_t>(b) * a.T + t0 + lane) * a.H + h,
                   static_cast<float>(ddt));
-      const float dA = static_cast<float>(read_lane(scan_wave(in ? e * step : 0.0), 63));
-      const float db = static_cast<float>(read_lane(scan_wave(in ? ddt : 0.0), 63));
-      const float dD = sum_wave(in ? m.trace[t] : 0.f);
-      if (lane == 0) {
-        float* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
+      const double dA = scan_wave(in ? e * step : 0.0), db = scan_wave(in ? ddt : 0.0);
+      const double dD = scan_wave(in ? m.trace[t] : 0.0);
+      if (lane == 63) {
+        double* part = o.part + (static_cast<size_t>(b) * NC + chunk) * 3 * a.H + h;
         part[0] = dA;
         part[a.H] = dD;
         part[2 * a.H] = db;
@@ -1435,7 +1434,7 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     const size_t all = static_cast<size_t>(B) * H * blocks * NC * rec;
     w.fwd = take(2 * all);
     w.rev = w.fwd + all;
-    w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(float));
+    w.part = take(static_cast<size_t>(B) * NC * 3 * H * sizeof(double));
     // Heads of a group are split while there are fewer workgroups than the 256 CUs hold in
     // LDS, two each (N > 64: one); each split adds fp32 sums of dB and dC to write and read.
     // Training steps of B 2, T 2048, H 32, P 64, bf16, with room for 512 and for 256: N 64
@@ -1559,7 +1558,7 @@ hipError_t launch_ssm_bwd(SsmArgs a, void* dx, void* ddt, float* dA, void* dBm, 
   a.rec_log = reinterpret_cast<double*>(base + w.log);
   const SsmGrads o = {dx, ddt, dBm, dCm, reinterpret_cast<float*>(base + w.pB),
                       reinterpret_cast<float*>(base + w.pC),
-                      reinterpret_cast<float*>(base + w.part),
+                      reinterpret_cast<double*>(base + w.part),
                       reinterpret_cast<const f32x4*>(base + w.fwd),
                       reinterpret_cast<const f32x4*>(base + w.rev), w.head_block, w.blocks};
   f32x4* chunks = reinterpret_cast<f32x4*>(base + w.fwd);

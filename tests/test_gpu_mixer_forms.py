@@ -153,7 +153,7 @@ def ssm_parts(B, T, H, G, N, P, dtype):
     logs, gaps = up256(B * H * NC * L * 16), B * H * (spans - 1)
     fwd = logs + up256(gaps * N * P * 4) + up256(gaps * 8)
     bwd = (logs + up256(2 * gaps * N * P * 4) + up256(2 * gaps * 8) + up256(2 * BHP * NC * 64 * NP * 4)
-           + up256(B * NC * 3 * H * 4) + (2 * up256(parts * B * T * G * N * 4) if parts > 1 else 0))
+           + up256(B * NC * 3 * H * 8) + (2 * up256(parts * B * T * G * N * 4) if parts > 1 else 0))
     return spans, heads, fwd, bwd
 
 

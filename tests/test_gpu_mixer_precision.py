@@ -211,3 +211,19 @@ def test_ssm_returned_state_keeps_fp32(kata):  # noqa: F811
     off = ((S.cpu().double() - want) / mag).square().mean().sqrt().item()
     log(f"  state: {off:.2e}")
     assert off <= ref.EPS32 * math.sqrt(11 / 3), off
+
+
+def test_ssm_skip_gradient_of_terms_that_cancel(kata):  # noqa: F811
+    """dD of one column of bf16 values: every x dy is exact in fp32, and so are their sums in fp64.
+    The second half of the tokens is the first's with dy turned around, but for one token."""
+    B, T, H, G, N, P = 1, 1000, 4, 1, 16, 1
+    gen, x, dt, A, Bm, Cm, D, bias = ssm_inputs(B, T, H, G, N, P, BF16, 31)
+    dy = normal(gen, B, T, H, P, dtype=BF16)
+    x[:, T // 2:], dy[:, T // 2:] = x[:, :T // 2], -dy[:, :T // 2]
+    dy[:, 700] += 2.0 ** -7 * dy[:, 700]
+    dy = dy.to(BF16).double()
+    log("case ssm dD cancels")
+    got = kata.ssm_bwd(up(x, BF16), up(dt, BF16), up(A), up(Bm, BF16), up(Cm, BF16), up(D), up(bias), up(dy, BF16))
+    want = (x * dy).sum((0, 1, 3))
+    assert (want != 0).all()
+    near(got[5], want, ref.EPS32 * want.abs(), "dD")
