@@ -495,8 +495,9 @@ KATA_API size_t kata_conv_bwd_workspace_bytes(int B, int T, int D, int W, kata_d
  *   pos : int32 [B][T], nullable (0..T-1);  freq : fp64 [r/2], null where r = 0 (angles are
  *   formed in fp64, off by 2^-52 of themselves: 5e-10 rad at a position of 2^21, 5e-7 at 2^31).
  *   yq : [B][Hq][T][d], yk : [B][Hk][T][d], contiguous, in dtype.
- *   d <= 256 (else KATA_ERR_UNSUPPORTED), r even, 0 <= r <= d, eps >= 0 and finite (a row of
- *   zeros needs eps > 0); Hq + Hk <= 65535.  Squares are summed in fp32.
+ *   d <= 256 (else KATA_ERR_UNSUPPORTED), r even, 0 <= r <= d, eps >= 0 and finite;
+ *   Hq + Hk <= 65535.  Squares are summed in fp32: a row's sum and its mean + eps (L2: sum + eps)
+ *   have to lie between 2^-126 and 2^128, so a row of zeros needs an eps of 2^-126 or more.
  */
 typedef enum { KATA_NORM_NONE = 0, KATA_NORM_RMS = 1, KATA_NORM_L2 = 2 } kata_norm_t;
 KATA_API kata_status_t kata_qk_norm_fwd(const void* q, const void* k, const float* wq,
@@ -558,7 +559,9 @@ KATA_API kata_status_t kata_ssm_fwd_ws(const void* x, const void* dt, const floa
                                        size_t workspace_bytes, hipStream_t stream);
 /* Gradients of kata_ssm_fwd_ws from a zero state, without lengths: dx, ddt, dBm, dCm in
  * dtype, contiguous and shaped as x, dt, Bm, Cm (those of a group summed over its heads);
- * dA, dD, dt_dbias [H], each nullable. */
+ * dA, dD, dt_dbias [H], each nullable.  bf16: the pair weights that dx, dBm and dCm are formed from,
+ * and the state's gradient that dBm reads, are rounded to bf16 once; ddt and the parameters'
+ * gradients keep fp32's bits throughout, their sums over tokens are fp64. */
 KATA_API kata_status_t kata_ssm_bwd_ws(const void* x, const void* dt, const float* A,
                                        const void* Bm, const void* Cm, const float* D,
                                        const float* dt_bias, const void* dy, void* dx, void* ddt,

@@ -711,7 +711,7 @@ __global__ __launch_bounds__(256) void ssm_state_kernel(SsmArgs a, f32x4* chunks
   if (!CHUNKS && rev) ++at.span;
   const int b = at.b, h = at.h, bh = b * a.H + h, grp = h / (a.H / a.G);
   SsmSelf me;
-  const int &wave = me.wave, &c = me.c, &g = me.g;
+  const int &wave = me.wave, &c = me.c;
   const int pc = at.pb * kSsmP, p0 = 16 * wave, p = pc + p0 + c;
   const int NC = (a.T + L - 1) / L, blocks = (a.P + kSsmP - 1) / kSsmP;
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
