@@ -430,7 +430,8 @@ __device__ __forceinline__ void ssm_store_state(float* S, int N, int P, int p,
 // forward that returns none would take 1.1 times as long with it).  OWN: the chunk's own
 // sum first, so that the state is rounded once per chunk and not by each of the products
 // added to it, whose errors the states of long memories gather (dA of 16 heads of 1024 tokens
-// 4.4e-7 off for 2.1e-7); for the gradients and fp32.  (ssm_out_kernel's registers do not hold it:
+// 4.4e-7 off for 2.1e-7), and with EXACT the smaller parts' sum apart (see ssm_add_rest); for the
+// gradients and fp32.  (ssm_out_kernel's registers do not hold it:
 // a prompt's call 40 us for 38.)
 template <typename E, int NP, int L, bool EXACT, bool OWN, typename F>
 __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::Lane& kt,
@@ -438,7 +439,7 @@ __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::
                                                  const E* keys, const E* v, int p0, float decay,
                                                  F f, f32x4 (&h)[NP / 16]) {
   const int g = (threadIdx.x >> 4) & 3;
-  f32x4 own[OWN ? NP / 16 : 1] = {};
+  f32x4 own[OWN ? NP / 16 : 1] = {}, rest[OWN && EXACT ? NP / 16 : 1] = {};
   if constexpr (!OWN) {
 #pragma unroll
     for (int j = 0; j < NP / 16; ++j) h[j] *= decay;
@@ -459,16 +460,19 @@ __device__ __forceinline__ void ssm_state_update(const typename SsmTile<E, NP>::
       const auto k0 = kt.col(keys, 16 * j, s0);
       const auto k1 = kt.col(keys, 16 * j, s0 + 16);
       sum = mac2(k0, k1, a.hi, b.hi, sum);
-      if constexpr (sizeof(E) == 2) sum = mac2(k0, k1, a.lo, b.lo, sum);
-      if constexpr (EXACT) sum = mac2(k0, k1, a2, b2, sum);
+      f32x4& low = OWN && EXACT ? rest[OWN && EXACT ? j : 0] : sum;
+      if constexpr (sizeof(E) == 2) low = mac2(k0, k1, a.lo, b.lo, low);
+      if constexpr (EXACT) low = mac2(k0, k1, a2, b2, low);
     }
     ssm_stretch();
   }
   if constexpr (OWN) {
 #pragma unroll
-    for (int j = 0; j < NP / 16; ++j)
+    for (int j = 0; j < NP / 16; ++j) {
+      if constexpr (EXACT) own[j] += rest[j];
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[j][i] = fmaf(decay, h[j][i], own[j][i]);
+    }
   }
 }
 
@@ -920,6 +924,21 @@ __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) {
   return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3])));
 }
 
+// Adds the sums over the planes past the first to the first's, which they are kept apart from:
+// the bf16 matrix instructions cut off what lies below the largest term's last bits, downwards,
+// and small products added to a large sum lower it by 1.8e-9 of its size on average, products of one
+// size by 1.2e-10 (64 terms).  Sums of 8 x 4096 tokens with B, C and x of mostly one sign gathered
+// that: dA of a training step 0.4-1.2e-6 off for 0.7-2e-7 (371 us for 374).
+template <int PLANES, int M, int N, int K>
+__device__ __forceinline__ void ssm_add_rest(f32x4 (&acc)[M][N], const f32x4 (&rest)[K][N]) {
+  if constexpr (PLANES > 1) {
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) acc[i][j] += rest[i][j];
+  }
+}
+
 // ONE: P <= 64, a head is one block of columns, and M needs no registers between blocks (the
 // training step of 8 x 4096 tokens 347 us, without the distinction 354).
 template <typename E, int NP, bool VEC, bool ONE>
@@ -935,7 +954,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
   typedef SsmTile<E, NP> KT;
   typedef SsmTile<E, kSsmP> VT;
   typedef SsmTile<E, L> WT;
-  constexpr int kRecord = kSsmP * NP / 4, kPlane = KT::size(kSsmP);
+  constexpr int kRecord = kSsmP * NP / 4, kPlane = KT::size(kSsmP), kPlanes = ssm_planes<E>();
   __shared__ SsmGradLds<E, NP> m;
   typename KT::Lane kt;
   typename VT::Lane vt;
@@ -1076,7 +1095,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     // exp(l_t) S dy_t, and its product with C_t
     int n0 = 16 * NN * (wave % WN), tn = wave / WN;  // tiles of tokens tn, tn + NG
     {
-      f32x4 acc[NN][TN] = {};
+      f32x4 acc[NN][TN] = {}, rest[kPlanes > 1 ? NN : 1][TN] = {};
 #pragma unroll
       for (int k = 0; k < kSsmP; k += 32) {
         ssm_half<E> y[TN][2];
@@ -1086,13 +1105,17 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
         for (int i = 0; i < NN; ++i)
 #pragma unroll
-          for (int q = 0; q < ssm_planes<E>(); ++q) {
+          for (int q = 0; q < kPlanes; ++q) {
             const auto s0 = kt.col(m.st + q * kPlane, n0 + 16 * i, k);
             const auto s1 = kt.col(m.st + q * kPlane, n0 + 16 * i, k + 16);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mac2(s0, s1, y[j][0], y[j][1], acc[i][j]);
+            for (int j = 0; j < TN; ++j) {
+              f32x4& sum = q ? rest[kPlanes > 1 ? i : 0][j] : acc[i][j];
+              sum = mac2(s0, s1, y[j][0], y[j][1], sum);
+            }
           }
       }
+      ssm_add_rest<kPlanes>(acc, rest);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const int tt = tn + NG * j;
@@ -1138,7 +1161,7 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
     ssm_stretch();
     const int p0 = 16 * PP * (wave % WP), tp = wave / WP;  // tp, tp + WS
     {
-      f32x4 acc[PP][TP] = {};
+      f32x4 acc[PP][TP] = {}, rest[kPlanes > 1 ? PP : 1][TP] = {};
 #pragma unroll
       for (int k = 0; k < NP; k += 32) {
         ssm_half<E> v[TP][2];
@@ -1148,13 +1171,17 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
 #pragma unroll
         for (int i = 0; i < PP; ++i)
 #pragma unroll
-          for (int q = 0; q < ssm_planes<E>(); ++q) {
+          for (int q = 0; q < kPlanes; ++q) {
             const auto r0 = kt.row(m.st + q * kPlane, p0 + 16 * i, k);
             const auto r1 = kt.row(m.st + q * kPlane, p0 + 16 * i, k + 16);
 #pragma unroll
-            for (int j = 0; j < TP; ++j) acc[i][j] = mac2(r0, r1, v[j][0], v[j][1], acc[i][j]);
+            for (int j = 0; j < TP; ++j) {
+              f32x4& sum = q ? rest[kPlanes > 1 ? i : 0][j] : acc[i][j];
+              sum = mac2(r0, r1, v[j][0], v[j][1], sum);
+            }
           }
       }
+      ssm_add_rest<kPlanes>(acc, rest);
       ssm_stretch();
 #pragma unroll
       for (int j = 0; j < TP; ++j) {

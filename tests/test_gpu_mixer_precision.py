@@ -227,3 +227,25 @@ def test_ssm_skip_gradient_of_terms_that_cancel(kata):  # noqa: F811
     want = (x * dy).sum((0, 1, 3))
     assert (want != 0).all()
     near(got[5], want, ref.EPS32 * want.abs(), "dD")
+
+
+def test_ssm_parameter_gradients_turn_with_dy(kata):  # noqa: F811
+    """The gradients of -dy are the negatives but for what the bf16 matrix cores do not round
+    evenly: they cut off what stands below the last bit of the largest term, by 1.2e-10 of a sum's size
+    on average where the terms are of one size, 1.8e-9 where small ones are added to it.  Of 64 x B T sums
+    with one sign that is 1.2e-10 sqrt(64 B T) = 1.7e-7 of a dA whose terms have both signs; three times
+    that is allowed of the mean over 16 heads."""
+    B, T, H, G, N, P = 8, 4096, 16, 1, 64, 64
+    gen = torch.Generator(device=DEV).manual_seed(8)
+
+    def act(*shape):
+        return torch.nn.functional.silu(torch.randn(shape, generator=gen, device=DEV)).to(BF16)
+    x, Bm, Cm = act(B, T, H, P), act(B, T, G, N), act(B, T, G, N)
+    dt = (torch.randn((B, T, H), generator=gen, device=DEV) * 0.5).to(BF16)
+    dy = (torch.randn((B, T, H, P), generator=gen, device=DEV) * 0.1).to(BF16)
+    A, bias = torch.full((H,), -1.0, device=DEV), torch.full((H,), -4.0, device=DEV)
+    log("case ssm turned dy")
+    dA, ddA = (kata.ssm_bwd(x, dt, A, Bm, Cm, None, bias, g)[2].double() for g in (dy, -dy))
+    off = ((dA + ddA) / 2).mean().abs() / dA.square().mean().sqrt()
+    log(f"  dA: {off.item():.2e}")
+    assert off <= 3 * 1.2e-10 * math.sqrt(64 * B * T), off.item()
