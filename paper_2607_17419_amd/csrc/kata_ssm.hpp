@@ -279,7 +279,8 @@ __device__ __forceinline__ SsmStep ssm_step_of(double z, bool softplus) {
   constexpr double kSeries[] = {1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0, 1.0};
 #pragma unroll
   for (double k : kSeries) u = fma(u, f, k);
-  u = a < -104.0 ? 0.0 : __builtin_amdgcn_ldexp(u, static_cast<int>(n));
+  // (n bounded: it may be infinite or NaN, which is no int; a NaN stays in u)
+  u = a < -104.0 ? 0.0 : __builtin_amdgcn_ldexp(u, static_cast<int>(fmax(n, -2000.0)));
   const double p = 1.0 + u, q = 2.0 + u, d = p * q;
   double r = __builtin_amdgcn_rcp(d);  // 1 / d, by Newton's iteration
   r = fma(fma(-d, r, 1.0), r, r);
@@ -297,7 +298,7 @@ __device__ __forceinline__ SsmStep ssm_step_of(float dt, const float* bias, int 
 // running sum l = hi + lo of step A over the chunk in units of log 2 (summed in fp64:
 // differences of l keep 2^-48 of the largest, and exp(l_t - l_s) is right where a strong
 // decay stands before weak ones), and gate the derivative of step by dt.  16 heads of 131072
-// tokens: 17 us, a wave waiting for its one load and then for its scan's chain.
+// tokens: 17 us, a wave waiting for its one load and then for the chain of its step and its scan.
 template <typename E, int L>
 __global__ __launch_bounds__(256) void ssm_logs_kernel(SsmArgs a, int NC) {
   const int per = (a.H + 3) / 4;
@@ -380,8 +381,8 @@ __device__ __forceinline__ unsigned ssm_xcd_order() {
 // each at most, as y itself is rounded), the state that is carried is not, and D x is added in fp32:
 // on W's diagonal D would be rounded with it, the same factor for all tokens of a head (y 2.3e-3
 // off for 1.8e-3 (rms); 131072 tokens 272 us for 279).
-// 16 heads of 131072 tokens, N = P = 64, bf16: 185 us, 620 MB counted, 3.4 TB/s; bound by issue,
-// vector instructions taking 62% of a SIMD's cycles and matrix ones 20%.  Rows that are not
+// 16 heads of 131072 tokens, N = P = 64, bf16: 222 us, 626 MB counted, 2.8 TB/s; bound by issue,
+// vector instructions taking 62% of a SIMD's cycles and matrix ones 19%.  Rows that are not
 // whole aligned pieces are read element by element: 3 times the time of the whole call.
 constexpr int ssm_most(int a, int b) { return a > b ? a : b; }
 
@@ -688,9 +689,9 @@ __global__ __launch_bounds__(256, NP > 64 ? 2 : (sizeof(E) == 2 ? 4 : 3)) void s
 // true: from the span's state in rec, every chunk's state before its tokens are added (S
 // at the chunk's start, R at its end), to `chunks` (R's behind S's): records of [64
 // columns][NP] fp32, one per head, block and chunk.
-// Span states of 16 heads of 131072 tokens: 78 us, 333 MB counted, 4.3 TB/s, vector and
-// matrix instructions issuing in 73% of the cycles.  Chunk records of 8 x 4096 tokens of 16 heads:
-// 85 us, 434 MB counted (268 MB of them written), 5.1 TB/s, HBM bound.
+// Span states of 16 heads of 131072 tokens: 82 us, 333 MB counted, 4.1 TB/s, vector and
+// matrix instructions issuing in 74% of the cycles.  Chunk records of 8 x 4096 tokens of 16 heads:
+// 81 us, 438 MB counted (268 MB of them written), 5.4 TB/s, HBM bound.
 // An accumulator tile's float4 of a lane is a piece: piece 64 (4 j + w) + lane holds rows
 // 16 j + 4 g .. of column 16 w + c, so that stores are whole lines as they stand.
 template <typename E, int NP>
@@ -819,8 +820,8 @@ __global__ __launch_bounds__(256) void ssm_span_scan(SsmArgs a) {
 // there are as many, each operand read serving two products.  Four waves, so that two
 // workgroups share a CU and one works through the other's barriers; eight at N > 64,
 // whose records leave LDS for one workgroup.
-// 8 x 4096 tokens of 16 heads, N = P = 64, bf16: 176 us, 512 MB counted (268 MB of
-// records), 2.9 TB/s; vector instructions take 44% of the cycles, LDS 40%, matrix
+// 8 x 4096 tokens of 16 heads, N = P = 64, bf16: 190 us, 512 MB counted (268 MB of
+// records), 2.7 TB/s; vector instructions take 45% of the cycles, LDS 37%, matrix
 // instructions 11%, the rest are waits at the six barriers of a head, which two workgroups
 // of a CU half cover.
 // part: dA, dD, dbias of the chunk, [B * NC][3][H], in fp64: a head's chunks may cancel.
@@ -834,8 +835,9 @@ struct SsmGrads {
 
 // In LDS a record stands as operand planes, bf16 ones as hi + mid + lo, all of fp32's bits: the
 // gradients of A and of the steps are sums of products of S and R in which much cancels.
-// With hi + lo in state, record and product (2^-17 each) a training step of 8 x 4096 tokens took
-// 352 us for 369, and more heads' dA and dbias were off by more than 1e-5 of themselves.
+// With hi + lo in state, record and product (2^-17 each) 4.4% of the heads of random calls had a dA
+// and 6% a dbias off by more than 1e-5 of themselves for 0.6% (a plain fp32 form: 0.5 and 1.3%); a
+// training step of 8 x 4096 tokens took 368 us for 379.
 template <typename E> constexpr int ssm_planes() { return sizeof(E) == 2 ? 3 : 1; }
 constexpr int ssm_grad_threads(int NP) { return NP > 64 ? 512 : 256; }
 
@@ -940,7 +942,7 @@ __device__ __forceinline__ void ssm_add_rest(f32x4 (&acc)[M][N], const f32x4 (&r
 }
 
 // ONE: P <= 64, a head is one block of columns, and M needs no registers between blocks (the
-// training step of 8 x 4096 tokens 347 us, without the distinction 354).
+// training step of 8 x 4096 tokens 379 us, without the distinction 411).
 template <typename E, int NP, bool VEC, bool ONE>
 __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmArgs a, SsmGrads o) {
   constexpr int L = ssm_chunk<E>(), LT = L / 16, NT = NP / 16, PT = kSsmP / 16;
@@ -1076,15 +1078,15 @@ __global__ __launch_bounds__(ssm_grad_threads(NP), 2) void ssm_grad_kernel(SsmAr
         for (int i = 0; i < 4; ++i)
           if (4 * g + i == c) m.diag[t] = pair[i], m.trace[t] = acc[i], pair[i] = 0.f;
       }
-      f32x4 rows = pair * step;
+      f32x4 part = pair * step;
       if (tt == ss) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          rows[i] = sum_lanes_from(rows[i]);
-          rows[i] = 4 * g + i < c ? rows[i] : 0.f;
+          part[i] = sum_lanes_from(part[i]);
+          part[i] = 4 * g + i < c ? part[i] : 0.f;
         }
       }
-      const float row = sum_g((rows[0] + rows[1]) + (rows[2] + rows[3]));
+      const float row = sum_g((part[0] + part[1]) + (part[2] + part[3]));
       if (g == 0) m.row[ss][t] = row;
       f32x4 col;
 #pragma unroll
@@ -1417,11 +1419,11 @@ inline int ssm_chunk_of(bool bf16) { return bf16 ? ssm_chunk<bf16_t>() : ssm_chu
 // Spans of a head: one workgroup each, so that the heads of a call with few of them
 // still stand on every CU, four workgroups each where there are as many spans of four chunks:
 // a span's own state costs one more pass over x and B.  (16 heads of 131072 tokens with 512,
-// 768, 1024, 1536 and 2048 workgroups: 309, 291, 278, 295 and 311 us; a training step of
-// 8 x 4096 tokens: 356, 359, 355, 370 and 434 us.)  Spans of two chunks only where those of
-// four would leave CUs without a workgroup: with four and two, 16 heads of 500 tokens 23.2 and
-// 17.4 us, of 2000 25.4 and 21.7, of 4000 31.8 and 30.8; 32 heads of 2000 27.7 and 28.4, 64
-// heads of 2000 34 and 35 us.
+// 768, 1024, 1536 and 2048 workgroups: 325, 310, 299, 311 and 303 us; a training step of
+// 8 x 4096 tokens: 379, 379, 384, 390 and 402 us.)  Spans of two chunks only where those of
+// four would leave CUs without a workgroup: with four and two, 16 heads of 500 tokens 25.1 and
+// 18.9 us, of 2000 27.2 and 23.9, of 4000 34.1 and 33.2; 32 heads of 2000 30.9 and 31.0, 64
+// heads of 2000 38 and 39 us.
 inline void ssm_spans(int BHP, int T, int L, int& spans, int& span_chunks) {
   const int NC = (T + L - 1) / L;
   int n = (1024 + BHP - 1) / BHP;
@@ -1465,7 +1467,7 @@ inline SsmWorkspace ssm_workspace(int B, int T, int H, int G, int N, int P, bool
     // Heads of a group are split while there are fewer workgroups than the 256 CUs hold in
     // LDS, two each (N > 64: one); each split adds fp32 sums of dB and dC to write and read.
     // Training steps of B 2, T 2048, H 32, P 64, bf16, with room for 512 and for 256: N 64
-    // 125 and 142 us, N 128 196 and 185 us; 1024: N 128 219 us.
+    // 135 and 151 us, N 128 207 and 195 us; 1024: N 64 141, N 128 227 us.
     const long long wgs = static_cast<long long>(B) * G * NC, room = N > 64 ? 256 : 512;
     long long split = (room + wgs - 1) / wgs;
     if (split > H / G) split = H / G;
