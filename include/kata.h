@@ -580,6 +580,124 @@ KATA_API kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, co
                                      int P, const kata_ssm_strides_t* strides, int softplus,
                                      kata_dtype_t dtype, hipStream_t stream);
 
+/*
+ * Operators of a mixer's layer in 8 bits: the residual's addition and its norm, the quantiser,
+ * the projections' product, and a recurrent mixer with a decay per channel.  The conventions of
+ * the operators above hold, with these additions:
+ *  - Activations without a batch are rows [M][..] with one row stride (elements).
+ *  - 8 bits: e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest 448, no infinity), one
+ *    byte each, with an fp32 scale for each block of 128 columns of a row, or of 128 x 128:
+ *    a code stands for its value times its block's scale.  Scales are contiguous,
+ *    [rows][ceil(columns / 128)] or [ceil(rows / 128)][ceil(columns / 128)], the last blocks
+ *    being those that are left.  Quantising:
+ *        scale = max(max |x| / 448, 2^-126),  code = x (1 / scale) to nearest, ties to even.
+ *    A NaN becomes a NaN code and leaves the scale to the block's other values; an infinity
+ *    makes its block's scale infinite and its own code NaN.
+ *  - Rows of codes may begin anywhere; products of rows that begin at multiples of 16 bytes
+ *    are several times faster.
+ */
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *     s = x + res (rounded to dtype; without res: x),   y = s w / sqrt(mean(s^2) + eps).
+ *   x, res, sum, y : [M][D] in dtype;  w : [D], nullable (ones).
+ *   res, sum : both or neither; sum receives s, and may be res itself with its row stride.
+ *   y, or q and scale (y in 8 bits, quantised from fp32, blocks of one row), or all three.
+ *   D <= 32768, else KATA_ERR_UNSUPPORTED.  Squares are summed in fp32, as for kata_qk_norm_fwd.
+ */
+KATA_API kata_status_t kata_add_norm_fwd(const void* x, const void* res, const float* w, void* sum,
+                                         void* y, void* q, float* scale, int M, int D,
+                                         long long x_row, long long res_row, long long sum_row,
+                                         long long y_row, long long q_row, float eps,
+                                         kata_dtype_t dtype, hipStream_t stream);
+/* Its gradients from sum (s; x without res) and dy, the gradient of y before it is quantised, in
+ * dy_dtype (fp32, or dtype): dx [M][D], the gradient of x and of res alike, to which dsum (nullable:
+ * none), the gradient that reaches s by the residual's own way, is added; dw [D], nullable.
+ * workspace as for kata_conv_bwd_ws. */
+KATA_API kata_status_t kata_add_norm_bwd_ws(const void* sum, const float* w, const void* dy,
+                                            const void* dsum, void* dx, float* dw, int M, int D,
+                                            long long sum_row, long long dy_row,
+                                            long long dsum_row, long long dx_row, float eps,
+                                            kata_dtype_t dtype, kata_dtype_t dy_dtype,
+                                            void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+KATA_API size_t kata_add_norm_bwd_workspace_bytes(int M, int D, kata_dtype_t dtype);
+
+/*
+ * x [M][K] (dtype, a row stride) in 8 bits: q [M][K] with scale, qt [K][M] (the transpose,
+ * quantised by itself) with scale_t, or both.  rows = 1: blocks of one row (of x for q, of its
+ * transpose for qt); rows = 128: blocks of 128 x 128, q and qt holding the same codes.
+ * The operands of a product y = x w^T and of its gradients:
+ *     y = (x rows) (w 128 x 128)^T,  dx = (dy rows) (wt 128 x 128)^T,
+ *     dw = (dyt rows) (xt rows)^T.
+ */
+KATA_API kata_status_t kata_f8_quant(const void* x, void* q, float* scale, void* qt,
+                                     float* scale_t, int M, int K, int rows, long long x_row,
+                                     long long q_row, long long qt_row, kata_dtype_t dtype,
+                                     hipStream_t stream);
+
+/*
+ * Product of 8-bit operands:  c[m][n] = sum_k a[m][k] b[n][k], each code times its scale.
+ *   a : codes [M][K] with a_scale [M][ceil(K/128)];  b : codes [N][K] with b_scale of blocks of
+ *   b_rows = 128 or 1 rows;  c : [M][N] in dtype (rounded once); row strides.
+ *   A block's products are summed by the matrix cores, the scaled blocks in fp32.  A non-finite
+ *   scale or a NaN code reaches its rows of c.
+ *   workspace : at least kata_f8_gemm_workspace_bytes(...) bytes (0: invalid or unsupported
+ *   arguments), 256-byte aligned, contents undefined on exit.
+ */
+KATA_API kata_status_t kata_f8_gemm_ws(const void* a, const float* a_scale, const void* b,
+                                       const float* b_scale, void* c, int M, int N, int K,
+                                       int b_rows, long long a_row, long long b_row,
+                                       long long c_row, kata_dtype_t dtype, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream);
+KATA_API size_t kata_f8_gemm_workspace_bytes(int M, int N, int K);
+
+/*
+ * Gated linear recurrence, per channel:
+ *     rate_t = c softplus(lam) sigmoid(r_t + r_bias),   a_t = exp(-rate_t),
+ *     h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t + i_bias) x_t,   y_t = h_t.
+ *   x, r, i, y : [B][T][D] in dtype, with strides;  lam, r_bias, i_bias (both nullable) : [D].
+ *   h_in (nullable: zeros), h_out (nullable) : fp32 [B][D].  c > 0 and finite; D <= 2^20.
+ *   starts (nullable) : fp32 [B][kata_recur_spans(T)][D], the state before each span of tokens,
+ *   for the gradients (undefined for spans past a sequence's end).
+ *   strides : element strides over batch and token; null: contiguous (all [B][T][D]).
+ *   workspace : at least kata_recur_workspace_bytes(..., backward) bytes (0: invalid or
+ *   unsupported arguments), 256-byte aligned, contents undefined on exit.
+ *   Once a state is not finite, later ones are not either, but may be NaN for infinity.
+ */
+typedef struct {
+  long long x_batch, x_token, r_batch, r_token, i_batch, i_token;
+  long long y_batch, y_token; /* y, or dy in the backward */
+  long long dx_batch, dx_token, dr_batch, dr_token, di_batch, di_token; /* backward only */
+} kata_recur_strides_t;
+KATA_API kata_status_t kata_recur_fwd_ws(const void* x, const void* r, const void* i,
+                                         const float* lam, const float* r_bias,
+                                         const float* i_bias, const float* h_in,
+                                         const int* lengths, void* y, float* h_out, float* starts,
+                                         int B, int T, int D, const kata_recur_strides_t* strides,
+                                         float c, kata_dtype_t dtype, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
+/* Gradients of kata_recur_fwd_ws from dy [B][T][D] and dh_out [B][D] (nullable: zeros), the
+ * gradient of its h_out: dx, dr, di [B][T][D] in dtype; dlam, dr_bias, di_bias [D] and dh_in [B][D]
+ * in fp32, each nullable.  h_in and lengths as in the forward; starts: what it returned, or null
+ * (formed again, at the cost of a pass over the inputs; with starts, h_in is not read).  Where a
+ * rate is 0, so that a = 1, the gradients by the rate are taken as 0. */
+KATA_API kata_status_t kata_recur_bwd_ws(
+    const void* x, const void* r, const void* i, const float* lam, const float* r_bias,
+    const float* i_bias, const float* h_in, const int* lengths, const float* starts,
+    const void* dy, const float* dh_out, void* dx, void* dr, void* di, float* dlam, float* dr_bias,
+    float* di_bias, float* dh_in, int B, int T, int D, const kata_recur_strides_t* strides,
+    float c, kata_dtype_t dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
+KATA_API size_t kata_recur_workspace_bytes(int B, int T, int D, kata_dtype_t dtype, int backward);
+/* Spans of T tokens (0: T < 1). */
+KATA_API int kata_recur_spans(int T);
+/* One token: x, r, i, y [B][D]; h fp32 [B][D], updated in place. */
+KATA_API kata_status_t kata_recur_step(float* h, const void* x, const void* r, const void* i,
+                                       const float* lam, const float* r_bias, const float* i_bias,
+                                       void* y, int B, int D, long long x_batch, long long r_batch,
+                                       long long i_batch, long long y_batch, float c,
+                                       kata_dtype_t dtype, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 KATA_API const char* kata_status_string(kata_status_t s);
 

@@ -15,6 +15,13 @@ Around a recurrent mixer, on token-major rows (views of a projection's output):
     u = kata.conv_fwd(x, w, bias)                   # short causal convolution, [B,T,D]
     q, k = kata.qk_norm_fwd(q, k, wq, wk, freq)     # norms and rotation, to [B,H,T,d]
     y = kata.ssm_fwd(x, dt, A, Bm, Cm, D, bias)     # selective scan, [B,T,H,P]
+    y = kata.recur_fwd(x, r, i, lam)                # gated linear recurrence, [B,T,D]
+
+and of its layer in 8 bits (e4m3 with a scale for each block of 128):
+
+    w8, ws = kata.f8_quant(w, rows=128)             # a weight's 128 x 128 blocks
+    a8, as_, s = kata.add_norm_f8_fwd(x, g, res)    # residual and norm, to the product's operand
+    c = kata.f8_gemm(a8, as_, w8, ws)               # [..,N]
 """
 from __future__ import annotations
 
@@ -27,6 +34,8 @@ __all__ = [
     "default_span", "prefill_state", "decode_step", "packed_dim", "LIB_PATH",
     "conv_fwd", "conv_step", "conv_bwd", "qk_norm_fwd", "qk_norm_bwd", "rope_frequencies",
     "ssm_fwd", "ssm_step", "ssm_bwd",
+    "add_norm_fwd", "add_norm_f8_fwd", "add_norm_bwd", "f8_quant", "f8_gemm",
+    "recur_fwd", "recur_fwd_train", "recur_bwd", "recur_step",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkata.so")
@@ -52,6 +61,10 @@ EXPORTED = (
     "kata_conv_fwd", "kata_conv_step", "kata_conv_bwd_ws", "kata_conv_bwd_workspace_bytes",
     "kata_qk_norm_fwd", "kata_qk_norm_bwd_ws", "kata_qk_norm_bwd_workspace_bytes",
     "kata_ssm_fwd_ws", "kata_ssm_bwd_ws", "kata_ssm_workspace_bytes", "kata_ssm_step",
+    "kata_add_norm_fwd", "kata_add_norm_bwd_ws", "kata_add_norm_bwd_workspace_bytes",
+    "kata_f8_quant", "kata_f8_gemm_ws", "kata_f8_gemm_workspace_bytes",
+    "kata_recur_fwd_ws", "kata_recur_bwd_ws", "kata_recur_workspace_bytes", "kata_recur_spans",
+    "kata_recur_step",
 )
 
 # what kata_fwd_form and kata_bwd_form return (-1: unsupported)
@@ -175,11 +188,25 @@ def lib():
     L.kata_ssm_bwd_ws.argtypes = [vp] * 15 + [i] * 6 + [vp, i, i, vp, sz, vp]
     L.kata_ssm_workspace_bytes.argtypes = [i] * 8
     L.kata_ssm_step.argtypes = [vp] * 9 + [i] * 5 + [vp, i, i, vp]
+    L.kata_add_norm_fwd.argtypes = [vp] * 7 + [i] * 2 + [ll] * 5 + [f, i, vp]
+    L.kata_add_norm_bwd_ws.argtypes = [vp] * 6 + [i] * 2 + [ll] * 4 + [f, i, i, vp, sz, vp]
+    L.kata_add_norm_bwd_workspace_bytes.argtypes = [i] * 3
+    L.kata_f8_quant.argtypes = [vp] * 5 + [i] * 3 + [ll] * 3 + [i, vp]
+    L.kata_f8_gemm_ws.argtypes = [vp] * 5 + [i] * 4 + [ll] * 3 + [i, vp, sz, vp]
+    L.kata_f8_gemm_workspace_bytes.argtypes = [i] * 3
+    L.kata_recur_fwd_ws.argtypes = [vp] * 11 + [i] * 3 + [vp, f, i, vp, sz, vp]
+    L.kata_recur_bwd_ws.argtypes = [vp] * 18 + [i] * 3 + [vp, f, i, vp, sz, vp]
+    L.kata_recur_workspace_bytes.argtypes = [i] * 5
+    L.kata_recur_spans.argtypes = [i]
+    L.kata_recur_step.argtypes = [vp] * 8 + [i] * 2 + [ll] * 4 + [f, i, vp]
     for name in ("kata_conv_fwd", "kata_conv_step", "kata_conv_bwd_ws", "kata_qk_norm_fwd",
-                 "kata_qk_norm_bwd_ws", "kata_ssm_fwd_ws", "kata_ssm_bwd_ws", "kata_ssm_step"):
+                 "kata_qk_norm_bwd_ws", "kata_ssm_fwd_ws", "kata_ssm_bwd_ws", "kata_ssm_step",
+                 "kata_add_norm_fwd", "kata_add_norm_bwd_ws", "kata_f8_quant", "kata_f8_gemm_ws",
+                 "kata_recur_fwd_ws", "kata_recur_bwd_ws", "kata_recur_spans", "kata_recur_step"):
         getattr(L, name).restype = i
     for name in ("kata_conv_bwd_workspace_bytes", "kata_qk_norm_bwd_workspace_bytes",
-                 "kata_ssm_workspace_bytes"):
+                 "kata_ssm_workspace_bytes", "kata_add_norm_bwd_workspace_bytes",
+                 "kata_f8_gemm_workspace_bytes", "kata_recur_workspace_bytes"):
         getattr(L, name).restype = sz
     L.kata_status_string.argtypes = [i]
     L.kata_status_string.restype = ctypes.c_char_p
@@ -980,3 +1007,281 @@ def ssm_bwd(x, dt, A, Bm, Cm, D, dt_bias, dy, softplus: bool = True, workspace=N
         _ssm_strides(x, dt, Bm, Cm, dy), int(softplus), code, workspace.data_ptr(),
         workspace.numel(), _stream(None, x.device)), "kata_ssm_bwd_ws")
     return dx, ddt, dA, dB, dC, dD, db
+
+
+# ---- a layer in 8 bits ------------------------------------------------------------
+# Rows [..,D] may have any leading dimensions that lie one after the other in memory (one row
+# stride).  Codes are torch.float8_e4m3fn; those that are allocated here begin each row at a
+# multiple of 16 bytes, as the product's fast forms ask for.
+
+F8_BLOCK = 128  # columns (and rows) of a scale
+
+
+def _rows(t, what):
+    """Rows, width and row stride of t [..,D]."""
+    s = t.shape
+    n = len(s)
+    if n == 2:
+        return s[0], s[1], t.stride(0)
+    if n < 2:
+        raise ValueError(f"expected {what}, got {tuple(s)}")
+    strides, rows, step = t.stride(), 1, None
+    for k in range(n - 2, -1, -1):
+        if s[k] == 1:
+            continue
+        if step is None:
+            step = strides[k]
+        elif strides[k] != step * rows:
+            raise ValueError(f"{what}: leading dimensions {tuple(s[:-1])} are not rows of one stride")
+        rows *= s[k]
+    return rows, s[-1], s[-1] if step is None else step
+
+
+def _codes(lead, n, device):
+    import torch
+    return torch.empty((*lead, (n + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[..., :n]
+
+
+def _f8_blocks(n):
+    return (n + F8_BLOCK - 1) // F8_BLOCK
+
+
+def _add_norm(x, w, res, eps, y, sum, q, scale):
+    import torch
+    M, D, x_row = _rows(x, "x [..,D]")
+    code, f32, dev, shape, T = _dtype_code(x), torch.float32, x.get_device(), x.shape, x.dtype
+    if res is None:
+        if sum is not None:
+            raise ValueError("sum without res is x itself")
+    elif sum is None:
+        sum = torch.empty(shape, dtype=T, device=x.device)
+    _check(lib().kata_add_norm_fwd(
+        _tensor(x, "x", dev, shape, T, True), _optional(res, "res", dev, shape, T, True),
+        _optional(w, "w", dev, (D,), f32), _optional(sum, "sum", dev, shape, T, True),
+        _optional(y, "y", dev, shape, T, True),
+        _optional(q, "q", dev, shape, torch.float8_e4m3fn, True),
+        _optional(scale, "scale", dev, (*shape[:-1], _f8_blocks(D)), f32), M, D, x_row,
+        *(0 if t is None else _rows(t, "rows [..,D]")[2] for t in (res, sum, y, q)), eps, code,
+        _stream(None, x.device)), "kata_add_norm_fwd")
+    return x if sum is None else sum
+
+
+@_on_stream
+def add_norm_fwd(x, w=None, res=None, eps: float = 1e-6, y=None, sum=None):
+    """Root-mean-square norm of x + res (kata_add_norm_fwd): x, res [..,D], w [D] fp32; returns (y,
+    sum), sum being x + res in x's type (x itself without res; it may be given as res)."""
+    import torch
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return y, _add_norm(x, w, res, eps, y, sum, None, None)
+
+
+@_on_stream
+def add_norm_f8_fwd(x, w=None, res=None, eps: float = 1e-6, q=None, scale=None, sum=None, y=None):
+    """The same with its output in 8 bits: returns (q, scale, sum), scale fp32
+    [..,ceil(D/128)].  y: where given, receives the output in x's type too."""
+    import torch
+    if x.dim() < 2:
+        raise ValueError(f"expected x [..,D], got {tuple(x.shape)}")
+    lead, D = x.shape[:-1], x.shape[-1]
+    if q is None:
+        q = _codes(lead, D, x.device)
+    if scale is None:
+        scale = torch.empty((*lead, _f8_blocks(D)), dtype=torch.float32, device=x.device)
+    return q, scale, _add_norm(x, w, res, eps, y, sum, q, scale)
+
+
+@_on_stream
+def add_norm_bwd(sum, w, dy, dsum=None, eps: float = 1e-6, dx=None, workspace=None):
+    """Gradients (dx, dw) of add_norm_fwd (kata_add_norm_bwd_ws) from its sum, dy [..,D] (fp32 or
+    sum's type) and dsum, the gradient of sum itself; dx is that of x and of res.  dw is
+    None where w is."""
+    import torch
+    M, D, row = _rows(sum, "sum [..,D]")
+    code, f32, dev, shape, T = _dtype_code(sum), torch.float32, sum.get_device(), sum.shape, sum.dtype
+    if dx is None:
+        dx = torch.empty(shape, dtype=T, device=sum.device)
+    dw = None if w is None else torch.empty((D,), dtype=f32, device=sum.device)
+    workspace = _workspace(workspace, int(lib().kata_add_norm_bwd_workspace_bytes(M, D, code)), sum)
+    _check(lib().kata_add_norm_bwd_ws(
+        _tensor(sum, "sum", dev, shape, T, True), _optional(w, "w", dev, (D,), f32),
+        _tensor(dy, "dy", dev, shape, dy.dtype, True), _optional(dsum, "dsum", dev, shape, T, True),
+        _tensor(dx, "dx", dev, shape, T, True), None if dw is None else dw.data_ptr(), M, D, row,
+        *(0 if t is None else _rows(t, "rows [..,D]")[2] for t in (dy, dsum, dx)), eps, code,
+        _dtype_code(dy), workspace.data_ptr(), workspace.numel(), _stream(None, sum.device)),
+        "kata_add_norm_bwd_ws")
+    return dx, dw
+
+
+@_on_stream
+def f8_quant(x, rows: int = 1, transposed: bool = False, q=None, scale=None, qt=None,
+             scale_t=None):
+    """x [..,K] in 8 bits (kata_f8_quant), blocks of rows (1 or 128) x 128: returns (q [..,K],
+    scale), and with transposed (q, scale, qt [K,M], scale_t), M being x's rows.  The scale is
+    fp32 [..,ceil(K/128)] for rows = 1, [ceil(M/128),ceil(K/128)] for rows = 128."""
+    import torch
+    M, K, x_row = _rows(x, "x [..,K]")
+    code, f32, dev, f8 = _dtype_code(x), torch.float32, x.get_device(), torch.float8_e4m3fn
+    if rows not in (1, F8_BLOCK):
+        raise ValueError(f"rows must be 1 or {F8_BLOCK}, got {rows}")
+    of = (*x.shape[:-1], _f8_blocks(K)) if rows == 1 else (_f8_blocks(M), _f8_blocks(K))
+    of_t = (K if rows == 1 else _f8_blocks(K), _f8_blocks(M))
+    if q is None:
+        q = _codes(x.shape[:-1], K, x.device)
+    if scale is None:
+        scale = torch.empty(of, dtype=f32, device=x.device)
+    if not transposed and (qt is not None or scale_t is not None):
+        raise ValueError("qt and scale_t are for transposed")
+    if transposed and qt is None:
+        qt = _codes((K,), M, x.device)
+    if transposed and scale_t is None:
+        scale_t = torch.empty(of_t, dtype=f32, device=x.device)
+    _check(lib().kata_f8_quant(
+        _tensor(x, "x", dev, x.shape, x.dtype, True), _tensor(q, "q", dev, x.shape, f8, True),
+        _tensor(scale, "scale", dev, of, f32), _optional(qt, "qt", dev, (K, M), f8, True),
+        _optional(scale_t, "scale_t", dev, of_t, f32), M, K, rows, x_row, _rows(q, "q [..,K]")[2],
+        0 if qt is None else qt.stride(0), code, _stream(None, x.device)), "kata_f8_quant")
+    return (q, scale, qt, scale_t) if transposed else (q, scale)
+
+
+@_on_stream
+def f8_gemm(a, a_scale, b, b_scale, out=None, dtype=None, workspace=None):
+    """a b^T of 8-bit operands (kata_f8_gemm_ws): a [..,K] with a_scale [..,ceil(K/128)], b [N,K]
+    with b_scale [ceil(N/128),ceil(K/128)] (128 x 128 blocks) or [N,ceil(K/128)] (blocks of a
+    row); returns [..,N] in dtype (fp32 or bf16, the default)."""
+    import torch
+    M, K, a_row = _rows(a, "a [..,K]")
+    N, Kb = _dims(b, 2, "b [N,K]")
+    f32, dev, f8, kb = torch.float32, a.get_device(), torch.float8_e4m3fn, _f8_blocks(K)
+    if Kb != K:
+        raise ValueError(f"a has {K} columns, b {Kb}")
+    shape = (*a.shape[:-1], N)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=a.device)
+    elif dtype is not None and out.dtype is not dtype:
+        raise TypeError(f"out must be {dtype}, got {out.dtype}")
+    code = _dtype_code(out)
+    by_row = N > 1 and b_scale.shape == (N, kb)
+    workspace = _workspace(workspace, int(lib().kata_f8_gemm_workspace_bytes(M, N, K)), a)
+    _check(lib().kata_f8_gemm_ws(
+        _tensor(a, "a", dev, a.shape, f8, True),
+        _tensor(a_scale, "a_scale", dev, (*a.shape[:-1], kb), f32),
+        _tensor(b, "b", dev, (N, K), f8, True),
+        _tensor(b_scale, "b_scale", dev, (N, kb) if by_row else (_f8_blocks(N), kb), f32),
+        _tensor(out, "out", dev, shape, out.dtype, True), M, N, K, 1 if by_row else F8_BLOCK, a_row,
+        b.stride(0), _rows(out, "out [..,N]")[2], code, workspace.data_ptr(), workspace.numel(),
+        _stream(None, a.device)), "kata_f8_gemm_ws")
+    return out
+
+
+# ---- gated linear recurrence ----------------------------------------------------------
+
+_RecurStrides = ctypes.c_longlong * 14  # kata_recur_strides_t
+
+
+def _recur_inputs(x, r, i, lam, r_bias, i_bias):
+    """The addresses of the inputs in the order of the entry points."""
+    import torch
+    f32, dev, D = torch.float32, x.get_device(), x.shape[-1]
+    return (_tensor(x, "x", dev, x.shape, x.dtype, True), _tensor(r, "r", dev, x.shape, x.dtype, True),
+            _tensor(i, "i", dev, x.shape, x.dtype, True), _tensor(lam, "lam", dev, (D,), f32),
+            _optional(r_bias, "r_bias", dev, (D,), f32), _optional(i_bias, "i_bias", dev, (D,), f32))
+
+
+def _recur_strides(*tensors):
+    s = [v for t in tensors for v in t.stride()[:2]]
+    return _RecurStrides(*s, *([0] * (14 - len(s))))
+
+
+def recur_workspace_bytes(B, T, D, dtype_code, backward=False) -> int:
+    return int(lib().kata_recur_workspace_bytes(B, T, D, dtype_code, int(backward)))
+
+
+def _recur_fwd(x, r, i, lam, r_bias, i_bias, c, state, lengths, y, state_out, starts, workspace):
+    import torch
+    B, T, D = _dims(x, 3, "x [B,T,D]")
+    code, f32, dev = _dtype_code(x), torch.float32, x.get_device()
+    if y is None:
+        y = torch.empty((B, T, D), dtype=x.dtype, device=x.device)
+    workspace = _workspace(workspace, recur_workspace_bytes(B, T, D, code), x)
+    _check(lib().kata_recur_fwd_ws(
+        *_recur_inputs(x, r, i, lam, r_bias, i_bias), _optional(state, "state", dev, (B, D), f32),
+        _optional(lengths, "lengths", dev, (B,), torch.int32),
+        _tensor(y, "y", dev, (B, T, D), x.dtype, True),
+        _optional(state_out, "state_out", dev, (B, D), f32), None if starts is None else starts.data_ptr(),
+        B, T, D, _recur_strides(x, r, i, y), c, code, workspace.data_ptr(), workspace.numel(),
+        _stream(None, x.device)), "kata_recur_fwd_ws")
+    return y
+
+
+@_on_stream
+def recur_fwd(x, r, i, lam, r_bias=None, i_bias=None, c: float = 8.0, state=None, lengths=None,
+              y=None, state_out=None, final_state: bool = False, workspace=None):
+    """Gated linear recurrence (kata_recur_fwd_ws): x and the gates' r, i [B,T,D], lam, r_bias, i_bias
+    [D] fp32; returns y [B,T,D], or (y, state_out [B,D] fp32) with final_state or a state_out.
+    state: the one before the first token; lengths: int32 [B]."""
+    import torch
+    if state_out is None and final_state:
+        B, _, D = _dims(x, 3, "x [B,T,D]")
+        state_out = torch.empty((B, D), dtype=torch.float32, device=x.device)
+    y = _recur_fwd(x, r, i, lam, r_bias, i_bias, c, state, lengths, y, state_out, None, workspace)
+    return y if state_out is None else (y, state_out)
+
+
+@_on_stream
+def recur_fwd_train(x, r, i, lam, r_bias=None, i_bias=None, c: float = 8.0, state=None,
+                    lengths=None, y=None, state_out=None, workspace=None):
+    """recur_fwd that also returns what recur_bwd takes: (y, starts)."""
+    import torch
+    B, T, D = _dims(x, 3, "x [B,T,D]")
+    starts = torch.empty((B, int(lib().kata_recur_spans(T)), D), dtype=torch.float32, device=x.device)
+    y = _recur_fwd(x, r, i, lam, r_bias, i_bias, c, state, lengths, y, state_out, starts, workspace)
+    return y, starts
+
+
+@_on_stream
+def recur_step(h, x, r, i, lam, r_bias=None, i_bias=None, c: float = 8.0, y=None):
+    """One token of every sequence (kata_recur_step): x, r, i [B,D] -> y [B,D]; h [B,D] fp32 is
+    updated in place."""
+    import torch
+    B, D = _dims(x, 2, "x [B,D]")
+    code, dev = _dtype_code(x), x.get_device()
+    if y is None:
+        y = torch.empty((B, D), dtype=x.dtype, device=x.device)
+    _check(lib().kata_recur_step(
+        _tensor(h, "h", dev, (B, D), torch.float32), *_recur_inputs(x, r, i, lam, r_bias, i_bias),
+        _tensor(y, "y", dev, (B, D), x.dtype, True), B, D, x.stride(0), r.stride(0), i.stride(0),
+        y.stride(0), c, code, _stream(None, x.device)), "kata_recur_step")
+    return y
+
+
+@_on_stream
+def recur_bwd(x, r, i, lam, r_bias, i_bias, dy, starts=None, c: float = 8.0, state=None,
+              lengths=None, dstate=None, dx=None, dr=None, di=None, dstate_in=None,
+              workspace=None):
+    """Gradients (dx, dr, di, dlam, dr_bias, di_bias) of recur_fwd (kata_recur_bwd_ws) from dy [B,T,D];
+    None where a bias is.  starts: recur_fwd_train's, or None (formed again); state and lengths as
+    in the forward; dstate: the gradient of its state_out; dstate_in: where given, receives that
+    of its state.  dx, dr, di may be given as views of one wider tensor; past a sequence's
+    length they are not written."""
+    import torch
+    B, T, D = _dims(x, 3, "x [B,T,D]")
+    code, f32, dev, shape, kind = _dtype_code(x), torch.float32, x.get_device(), (B, T, D), x.dtype
+    # past a sequence's length: zeros, where the tensors are made here
+    make = torch.empty if lengths is None else torch.zeros
+    dx, dr, di = (make(shape, dtype=kind, device=x.device) if t is None else t for t in (dx, dr, di))
+    dlam, drb, dib = (None if t is None else torch.empty((D,), dtype=f32, device=x.device)
+                      for t in (lam, r_bias, i_bias))
+    workspace = _workspace(workspace, recur_workspace_bytes(B, T, D, code, True), x)
+    spans = int(lib().kata_recur_spans(T))
+    _check(lib().kata_recur_bwd_ws(
+        *_recur_inputs(x, r, i, lam, r_bias, i_bias), _optional(state, "state", dev, (B, D), f32),
+        _optional(lengths, "lengths", dev, (B,), torch.int32),
+        _optional(starts, "starts", dev, (B, spans, D), f32), _tensor(dy, "dy", dev, shape, kind, True),
+        _optional(dstate, "dstate", dev, (B, D), f32), _tensor(dx, "dx", dev, shape, kind, True),
+        _tensor(dr, "dr", dev, shape, kind, True), _tensor(di, "di", dev, shape, kind, True),
+        dlam.data_ptr(), None if drb is None else drb.data_ptr(),
+        None if dib is None else dib.data_ptr(), _optional(dstate_in, "dstate_in", dev, (B, D), f32), B,
+        T, D, _recur_strides(x, r, i, dy, dx, dr, di), c, code, workspace.data_ptr(),
+        workspace.numel(), _stream(None, x.device)), "kata_recur_bwd_ws")
+    return dx, dr, di, dlam, drb, dib

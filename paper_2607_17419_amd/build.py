@@ -19,14 +19,14 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkata.so")
 SOURCES = ["kata_api.hip", "kata_fp32.hip", "kata_mfma.hip", "kata_linear.hip", "kata_bwd.hip",
-           "kata_bwd_bf.hip", "kata_mixer.hip"]
+           "kata_bwd_bf.hip", "kata_mixer.hip", "kata_block.hip"]
 # per-source flags: the bf16 gradients kernel updates MFMA results with VALU code,
 # so its MFMAs write VGPRs (no AGPR copies)
 EXTRA = {"kata_bwd_bf.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 # objects joined into another after compiling: a test relinks the library from its
 # objects by name and knows no others
-JOINED = {"kata_linear.o": ["kata_mixer.o"]}
+JOINED = {"kata_linear.o": ["kata_mixer.o", "kata_block.o"]}
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 LD = os.path.join(os.path.dirname(os.path.realpath(HIPCC)), "..", "llvm", "bin", "ld.lld")

@@ -1,0 +1,276 @@
+// kata_addnorm.hpp -- root-mean-square norm of a row with the residual's addition:
+//
+//   s = x + res (rounded once to the activations' type),  inv = 1 / sqrt(mean(s^2) + eps),
+//   y = s inv w,
+//
+// y in the activations' type, as e4m3 codes with a scale for each 128 columns, or both.
+// Backward, from s: hat = s inv, g = w dy,
+//   dx = dsum + inv (g - hat mean(g hat)),   dw = sum over rows of dy hat.
+//
+// HBM bound: a row stays in the registers of one to sixteen waves from its load to its
+// store, eight neighbouring columns a lane, so every tensor is read or written once.
+#pragma once
+
+#include "kata_f8.hpp"
+
+namespace kata {
+
+// Sum over the WAVES waves of a row (a workgroup, or one wave), the same in every lane; `at`
+// holds one number a wave and is free again after the next barrier.
+template <int WAVES, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*at)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = sum_group<64>(v[k]);
+  if constexpr (WAVES > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) at[wave][k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v[k] += at[w][k];
+    }
+  }
+}
+
+// WAVES waves a row; ITER pieces of 512 * WAVES columns.
+template <typename E, int WAVES, int ITER, bool VEC>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel(
+    const E* x, const E* res, const float* __restrict__ w, E* sum, E* __restrict__ y,
+    uint8_t* __restrict__ q, float* __restrict__ scale, AddNormArgs s) {
+  __shared__ float at[WAVES][1];
+  const long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
+  if (m >= s.M) return;  // (with more than one wave never)
+  const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+  float v[ITER][8], total[1] = {0.f};
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) load8<VEC>(x + m * s.x_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
+  if (res) {
+    float r[ITER][8];
+#pragma unroll
+    for (int k = 0; k < ITER; ++k)
+      load8<VEC>(res + m * s.res_row, (k * 64 * WAVES + lane) * 8, s.D, r[k]);
+#pragma unroll
+    for (int k = 0; k < ITER; ++k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[k][i] += r[k][i];
+        if constexpr (sizeof(E) == 2) v[k][i] = static_cast<float>(static_cast<__bf16>(v[k][i]));
+      }
+      if (sum) store8<VEC>(sum + m * s.sum_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < ITER; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) total[0] = fmaf(v[k][i], v[k][i], total[0]);
+  row_sum<WAVES>(total, at);
+  const float inv = 1.f / sqrtf(total[0] / s.D + s.eps);
+  const int kb = (s.D + kF8Block - 1) / kF8Block;
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const int c = (k * 64 * WAVES + lane) * 8;
+    float wv[8];
+    if (w) {
+      load8<VEC>(w, c, s.D, wv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wv[i] = 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * inv * wv[i];
+    if (y) store8<VEC>(y + m * s.y_row, c, s.D, v[k]);
+    if (q) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t = fmaxf(t, fabsf(v[k][i]));
+      const float sc = f8_scale(max_row16(t));
+      if ((lane & 15) == 0 && c < s.D) scale[m * kb + c / kF8Block] = sc;
+      store8_codes<VEC>(q + m * s.q_row, c, s.D, f8_codes8(v[k], 1.f / sc));
+    }
+  }
+}
+
+// A workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ... (in fours with one wave a
+// row) and keeps its sums of dw in registers; part: [gridDim.x][D].
+template <typename E, typename G, int WAVES, int ITER, bool VEC>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_kernel(
+    const E* __restrict__ sum, const float* __restrict__ w, const G* __restrict__ dy,
+    const E* __restrict__ dsum, E* __restrict__ dx, float* __restrict__ part, AddNormArgs s) {
+  __shared__ float at[2][WAVES][2];
+  __shared__ float red[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * ITER * 8 : 1];
+  const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+  float dw[ITER][8] = {}, wv[ITER][8];
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    if (w) {
+      load8<VEC>(w, (k * 64 * WAVES + lane) * 8, s.D, wv[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wv[k][i] = 1.f;
+    }
+  }
+  const long long step = WAVES == 1 ? gridDim.x * 4LL : gridDim.x;
+  int turn = 0;
+  for (long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x; m < s.M;
+       m += step, turn ^= 1) {
+    float v[ITER][8], g[ITER][8], d[ITER][8], sums[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < ITER; ++k) {
+      const int c = (k * 64 * WAVES + lane) * 8;
+      load8<VEC>(sum + m * s.x_row, c, s.D, v[k]);
+      load8<VEC>(dy + m * s.res_row, c, s.D, g[k]);
+      if (dsum) {
+        load8<VEC>(dsum + m * s.sum_row, c, s.D, d[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[k][i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < ITER; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sums[0] = fmaf(v[k][i], v[k][i], sums[0]);
+        sums[1] = fmaf(v[k][i], g[k][i] * wv[k][i], sums[1]);
+      }
+    row_sum<WAVES>(sums, at[turn]);
+    const float inv = 1.f / sqrtf(sums[0] / s.D + s.eps);
+    const float dot = sums[1] * inv / s.D;  // mean(g hat)
+#pragma unroll
+    for (int k = 0; k < ITER; ++k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float hat = v[k][i] * inv;
+        dw[k][i] = fmaf(g[k][i], hat, dw[k][i]);
+        v[k][i] = fmaf(inv, g[k][i] * wv[k][i] - hat * dot, d[k][i]);
+      }
+      store8<VEC>(dx + m * s.y_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
+    }
+  }
+  if (!part) return;
+  if constexpr (WAVES == 1) {
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < ITER; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (wave) red[wave - 1][(k * 8 + i) * 64 + lane] = dw[k][i];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int k = 0; k < ITER; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = (k * 8 + i) * 64 + lane;
+        dw[k][i] = (dw[k][i] + red[0][e]) + (red[1][e] + red[2][e]);
+      }
+  }
+  float* row = part + static_cast<size_t>(blockIdx.x) * s.D;
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) store8<VEC>(row, (k * 64 * WAVES + lane) * 8, s.D, dw[k]);
+}
+
+// ---- launches ---------------------------------------------------------------
+
+// A row to one wave where there are rows for two waves on each of the 1024 SIMDs, so that
+// sums need no barrier; fewer or wider rows to four waves, the widest to sixteen.
+inline int add_norm_waves(int M, int D) { return D > 8192 ? 16 : D > 2048 || M < 2048 ? 4 : 1; }
+
+// Pieces of 512 * waves columns: CALL(waves, pieces).
+#define KATA_ADD_NORM_SHAPE(CALL)                              \
+  const int per = 512 * add_norm_waves(s.M, s.D);              \
+  const int pieces = (s.D + per - 1) / per;                    \
+  if (per == 512) {                                            \
+    if (pieces == 1) { CALL(1, 1); }                           \
+    else if (pieces == 2) { CALL(1, 2); }                      \
+    else { CALL(1, 4); }                                       \
+  } else if (per == 2048) {                                    \
+    if (pieces == 1) { CALL(4, 1); }                           \
+    else if (pieces == 2) { CALL(4, 2); }                      \
+    else { CALL(4, 4); }                                       \
+  } else {                                                     \
+    if (pieces == 2) { CALL(16, 2); }                          \
+    else { CALL(16, 4); }                                      \
+  }
+
+// Whether rows are whole aligned pieces of eight elements.
+inline bool add_norm_vec(const AddNormArgs& s, std::initializer_list<const void*> p) {
+  return s.D % 8 == 0 && s.x_row % 8 == 0 && s.res_row % 8 == 0 && s.sum_row % 8 == 0 &&
+         s.y_row % 8 == 0 && s.q_row % 8 == 0 && ptr_aligned(p, 16);
+}
+
+template <typename E>
+hipError_t add_norm_e(const void* x, const void* res, const float* w, void* sum, void* y, void* q,
+                      float* scale, const AddNormArgs& s, hipStream_t st) {
+  const bool vec = add_norm_vec(s, {x, res, w, sum, y}) && ptr_aligned({q}, 8);
+#define KATA_CALL(WV, IT)                                                                          \
+  const unsigned blocks = static_cast<unsigned>(WV == 1 ? (s.M + 3LL) / 4 : s.M);                  \
+  const int threads = WV == 1 ? 256 : 64 * WV;                                                     \
+  if (vec)                                                                                         \
+    add_norm_kernel<E, WV, IT, true><<<blocks, threads, 0, st>>>(                                  \
+        static_cast<const E*>(x), static_cast<const E*>(res), w, static_cast<E*>(sum),             \
+        static_cast<E*>(y), static_cast<uint8_t*>(q), scale, s);                                   \
+  else                                                                                             \
+    add_norm_kernel<E, WV, IT, false><<<blocks, threads, 0, st>>>(                                 \
+        static_cast<const E*>(x), static_cast<const E*>(res), w, static_cast<E*>(sum),             \
+        static_cast<E*>(y), static_cast<uint8_t*>(q), scale, s);
+  KATA_ADD_NORM_SHAPE(KATA_CALL)
+#undef KATA_CALL
+  return hipGetLastError();
+}
+
+// Workgroups of the gradients: four for each CU, and no more than leave eight rows to each.
+inline int add_norm_bwd_slices(int M, int D) {
+  const int rows = add_norm_waves(M, D) == 1 ? 32 : 8;
+  const long long n = (static_cast<long long>(M) + rows - 1) / rows;
+  return static_cast<int>(n < 1024 ? n : 1024);
+}
+
+size_t add_norm_bwd_workspace_bytes(int M, int D) {
+  return (static_cast<size_t>(add_norm_bwd_slices(M, D)) * D * sizeof(float) + 255) &
+         ~static_cast<size_t>(255);
+}
+
+template <typename E, typename G>
+hipError_t add_norm_bwd_e(const void* sum, const float* w, const void* dy, const void* dsum, void* dx,
+                          float* dw, void* ws, const AddNormArgs& s, hipStream_t st) {
+  const bool vec = add_norm_vec(s, {sum, w, dy, dsum, dx});
+  const int slices = add_norm_bwd_slices(s.M, s.D);
+  float* part = dw ? static_cast<float*>(ws) : nullptr;
+#define KATA_CALL(WV, IT)                                                                        \
+  const int threads = WV == 1 ? 256 : 64 * WV;                                                   \
+  if (vec)                                                                                       \
+    add_norm_bwd_kernel<E, G, WV, IT, true><<<slices, threads, 0, st>>>(                         \
+        static_cast<const E*>(sum), w, static_cast<const G*>(dy), static_cast<const E*>(dsum),   \
+        static_cast<E*>(dx), part, s);                                                           \
+  else                                                                                           \
+    add_norm_bwd_kernel<E, G, WV, IT, false><<<slices, threads, 0, st>>>(                        \
+        static_cast<const E*>(sum), w, static_cast<const G*>(dy), static_cast<const E*>(dsum),   \
+        static_cast<E*>(dx), part, s);
+  KATA_ADD_NORM_SHAPE(KATA_CALL)
+#undef KATA_CALL
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !dw) return e;
+  return launch_sum_partials(part, slices, s.D, {{dw, nullptr, nullptr}, {s.D, 0, 0}}, st);
+}
+#undef KATA_ADD_NORM_SHAPE
+
+hipError_t launch_add_norm(const void* x, const void* res, const float* w, void* sum, void* y,
+                           void* q, float* scale, const AddNormArgs& s, bool bf16, hipStream_t st) {
+  return bf16 ? add_norm_e<bf16_t>(x, res, w, sum, y, q, scale, s, st)
+              : add_norm_e<float>(x, res, w, sum, y, q, scale, s, st);
+}
+hipError_t launch_add_norm_bwd(const void* sum, const float* w, const void* dy, const void* dsum,
+                               void* dx, float* dw, void* ws, const AddNormArgs& s, bool bf16,
+                               bool dy_bf16, hipStream_t st) {
+  if (!bf16) return add_norm_bwd_e<float, float>(sum, w, dy, dsum, dx, dw, ws, s, st);
+  return dy_bf16 ? add_norm_bwd_e<bf16_t, bf16_t>(sum, w, dy, dsum, dx, dw, ws, s, st)
+                 : add_norm_bwd_e<bf16_t, float>(sum, w, dy, dsum, dx, dw, ws, s, st);
+}
+
+}  // namespace kata

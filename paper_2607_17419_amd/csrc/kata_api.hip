@@ -792,3 +792,4 @@ kata_status_t kata_bwd_chunked(const void* q, const void* k, const void* v, cons
 }  // extern "C"
 
 #include "kata_mixer_api.hpp"
+#include "kata_block_api.hpp"
