@@ -42,7 +42,7 @@ struct F8GemmArgs {
 size_t f8_gemm_workspace_bytes(int M, int N, int K);
 hipError_t launch_f8_gemm(const F8GemmArgs& s, int rows, bool bf16, void* ws, hipStream_t st);
 
-constexpr int kRecurSpan = 128;  // tokens of a workgroup, and of a state kept for the gradients
+constexpr int kRecurSpan = 64;   // tokens of a state kept for the gradients
 constexpr int kRecurCols = 128;  // channels of a workgroup
 struct RecurArgs {
   const void *x, *r, *i, *dy;
@@ -50,19 +50,19 @@ struct RecurArgs {
   const int* lengths;
   void *y, *dx, *dr, *di;
   float *h_out, *dh_in;
-  float* starts;  // [B][spans][D]: the state before each span (gradients: read)
-  float* sums;    // [B][spans][2][D]: a span's (L, H); gradients: (L, R)
-  float* behind;  // [B][spans][D]: the values a_t G_t behind each span
-  float* part;    // [B * spans][3 D]: sums for dlam, drb, dib
-  int B, T, D, spans, tiles;
+  float* starts;    // [B][ceil(T / kRecurSpan)][D]: the state before each span (gradients: read)
+  float* part;      // [B * spans][3 D]: sums for dlam, drb, dib
+  unsigned* ticket;  // the chain: see kata_recur.hpp
+  uint64_t* words;
+  int B, T, D, spans, tiles, cols;
   long long xb, xt, rb_, rt, ib_, it, yb, yt;  // y, or dy in the backward
   long long dxb, dxt, drb, drt, dib, dit;
   float c;
 };
 size_t recur_workspace_bytes(int B, int T, int D, bool backward);
-hipError_t launch_recur_fwd(RecurArgs s, void* ws, bool bf16, hipStream_t st);
-hipError_t launch_recur_bwd(RecurArgs s, float* dlam, float* drb, float* dib, void* ws, bool bf16,
+hipError_t launch_recur_fwd(const RecurArgs& s, void* ws, bool bf16, hipStream_t st);
+hipError_t launch_recur_bwd(const RecurArgs& s, float* dlam, float* drb, float* dib, void* ws, bool bf16,
                             hipStream_t st);
-hipError_t launch_recur_step(float* h, RecurArgs s, bool bf16, hipStream_t st);
+hipError_t launch_recur_step(float* h, const RecurArgs& s, bool bf16, hipStream_t st);
 
 }  // namespace kata

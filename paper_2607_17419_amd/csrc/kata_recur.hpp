@@ -9,11 +9,13 @@
 //   dlam = sigmoid(lam) / softplus(lam) sum drate rate,
 //   dx = G beta sigmoid(i),   di = G beta u (1 - sigmoid(i)).
 //
-// A workgroup takes a span of 128 tokens of 128 channels: a lane two channels, a wave 16
-// tokens.  Each wave's tokens act on a state as h -> exp(-L) h + H, L the sum of their rates; the
-// waves' and the spans' (L, H) are joined in order, whatever order workgroups run in.  L and not
-// the product of the a: where a = 1 - m 2^-24, its products round to 1 - (m + n) 2^-24 token
-// by token, always to the same side (state after 20000 tokens at rates of 2e-5: 1.2e-5 off).
+// A workgroup takes a span of tokens of 128 channels: a lane two channels, a wave a run of
+// tokens, whose inputs it reads once and holds in registers.  A run's tokens act on a state as
+// h -> exp(-L) h + H, L the sum of their rates.  The waves' (L, H) are joined in LDS.  A span's
+// is published in the workspace, and the state before it found from those of the spans before,
+// in one fixed order, so that results do not depend on the order in which workgroups run.
+// L and not the product of the a: where a = 1 - m 2^-24, its products round to 1 - (m + n) 2^-24
+// token by token, always to the same side (state after 20000 tokens at rates of 2e-5: 1.2e-5 off).
 #pragma once
 
 #include "kata_block.hpp"
@@ -21,73 +23,93 @@
 
 namespace kata {
 
-// c softplus(lam)
+// c softplus(lam) = c (max(lam, 0) + log(1 + e)), e = exp(-|lam|) <= 1: the logarithm as
+// 2 atanh(z), z = e / (2 + e) <= 1/3, by its series (the first term left out is 2e-8 of it).
 __device__ __forceinline__ float recur_slope(float lam, float c) {
-  return c * (fmaxf(lam, 0.f) + log1pf(expf(-fabsf(lam))));
+  const float e = expf(-fabsf(lam)), z = e / (2.f + e), q = z * z;
+  float s = fmaf(q, 1.f / 13.f, 1.f / 11.f);
+  s = fmaf(q, s, 1.f / 9.f);
+  s = fmaf(q, s, 1.f / 7.f);
+  s = fmaf(q, s, 1.f / 5.f);
+  s = fmaf(q, s, 1.f / 3.f);
+  s = fmaf(q, s, 1.f);
+  return c * (fmaxf(lam, 0.f) + 2.f * z * s);
 }
 
-// sigmoid(x) and 1 - sigmoid(x), both to a few 2^-24 of themselves.
-__device__ __forceinline__ void recur_sigmoid(float x, float& sig, float& rest) {
-  const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * x);
+// sigmoid of a gate and what is left of 1, both to a few 2^-24 of themselves: v log2(e) + b is the
+// exponent of exp(-gate), b the bias's part.
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float recur_sigmoid(float v, float b) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(fmaf(v, -kLog2e, b)));
+}
+__device__ __forceinline__ void recur_sigmoid(float v, float b, float& sig, float& rest) {
+  const float e = __builtin_amdgcn_exp2f(fmaf(v, -kLog2e, b));
   sig = __builtin_amdgcn_rcpf(1.f + e);
   rest = e < 1.f ? e * sig : 1.f - sig;
 }
+
 // Small rates make a near 1, where exp's own error is that of many tokens' product and
-// 1 - a^2 cancels: below 1/4, 1 - a is formed first, by its series (the first term left out
-// is 1e-8 of the sum), and a from it.
+// 1 - a^2 cancels: below 1/8, 1 - a is formed first, by its series (the first term left out
+// is 1e-9 of the sum), and a from it.  near (of the whole wave): all rates are below 1/8.
+constexpr float kRecurNear = 0.125f;
 __device__ __forceinline__ float recur_less(float w) {
-  float s = fmaf(w, -1.f / 5040.f, 1.f / 720.f);
-  s = fmaf(w, -s, 1.f / 120.f);
+  float s = fmaf(w, -1.f / 720.f, 1.f / 120.f);
   s = fmaf(w, -s, 1.f / 24.f);
   s = fmaf(w, -s, 1.f / 6.f);
   s = fmaf(w, -s, 0.5f);
   s = fmaf(w, -s, 1.f);
   return w * s;
 }
-__device__ __forceinline__ void recur_decay(float rate, float& a, float& beta) {
-  const float small = recur_less(rate), e = __builtin_amdgcn_exp2f(-1.44269504088896341f * rate);
-  const bool near = rate < 0.25f;
-  const float less = near ? small : 1.f - e;  // 1 - a
-  a = near ? 1.f - small : e;
+__device__ __forceinline__ void recur_decay(float rate, bool near, float& a, float& beta) {
+  float less = recur_less(rate);
+  a = 1.f - less;
+  if (!near) {
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * rate);
+    const bool small = rate < kRecurNear;
+    less = small ? less : 1.f - e;
+    a = small ? a : e;
+  }
   beta = __builtin_amdgcn_sqrtf(less * (1.f + a));
 }
-
-// How tokens whose rates sum to L act on a state, in one number: exp(-L), or -(1 - exp(-L)) where
-// that is the more exact one.
+// How tokens whose rates sum to L act on a state, in one number that is no NaN: exp(-L), or
+// -(1 - exp(-L)) where that is the more exact one.
 __device__ __forceinline__ float recur_factor(float L) {
-  const float w = L;
-  float a, beta;
-  recur_decay(w, a, beta);
-  return w < 0.25f ? -recur_less(w) : fmaxf(a, 0x1p-126f);
+  return L < kRecurNear ? -recur_less(L) : fmaxf(__builtin_amdgcn_exp2f(-kLog2e * L), 0x1p-126f);
 }
 __device__ __forceinline__ float recur_act(float factor, float h, float H) {
   const float f = fmaf(factor, h, H);
   return factor > 0.f ? f : h + f;
 }
 
-// V channels' constants.
-template <int V>
+// Two channels' constants: slope = c softplus(lam), the biases as recur_sigmoid takes them.
 struct RecurChannel {
-  float slope[V], rb[V], ib[V];
+  float slope[2], rb[2], ib[2];
+  bool near;  // of the whole wave
 };
-template <int V>
-__device__ __forceinline__ RecurChannel<V> recur_channel(const RecurArgs& s, int c) {
-  RecurChannel<V> p;
+__device__ __forceinline__ RecurChannel recur_channel(const RecurArgs& s, int c) {
+  RecurChannel p;
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
+  for (int k = 0; k < 2; ++k) {
     const int at = min(c + k, s.D - 1);
     p.slope[k] = recur_slope(s.lam[at], s.c);
-    p.rb[k] = s.rb ? s.rb[at] : 0.f;
-    p.ib[k] = s.ib ? s.ib[at] : 0.f;
+    p.rb[k] = s.rb ? -kLog2e * s.rb[at] : 0.f;
+    p.ib[k] = s.ib ? -kLog2e * s.ib[at] : 0.f;
   }
+  p.near = __all(p.slope[0] < kRecurNear && p.slope[1] < kRecurNear);
   return p;
 }
 
 // Channels c, c + 1 of a row (VEC: both there and aligned as a pair), raw.
 template <bool VEC, typename E>
 __device__ __forceinline__ RawVec<E, 2> recur_load(const E* row, int c, int D) {
-  if constexpr (VEC) return load_raw<E, 2>(row + min(c, D - 2));
-  else return RawVec<E, 2>{{row[min(c, D - 1)], row[min(c + 1, D - 1)]}};
+  if constexpr (VEC) {
+    if constexpr (sizeof(E) == 2)
+      return __builtin_bit_cast(RawVec<E, 2>, *reinterpret_cast<const uint32_t*>(row + min(c, D - 2)));
+    else
+      return load_raw<E, 2>(row + min(c, D - 2));
+  } else {
+    return RawVec<E, 2>{{row[min(c, D - 1)], row[min(c + 1, D - 1)]}};
+  }
 }
 template <bool VEC, typename E>
 __device__ __forceinline__ void recur_store(E* row, int c, int D, const float (&v)[2]) {
@@ -104,7 +126,7 @@ __device__ __forceinline__ void recur_store(E* row, int c, int D, const float (&
 
 // rate, a and beta u of a token.
 template <typename E>
-__device__ __forceinline__ void recur_token(const RecurChannel<2>& p, const RawVec<E, 2>& x,
+__device__ __forceinline__ void recur_token(const RecurChannel& p, const RawVec<E, 2>& x,
                                             const RawVec<E, 2>& r, const RawVec<E, 2>& i,
                                             float (&rate)[2], float (&a)[2], float (&b)[2]) {
   float xv[2], rv[2], iv[2];
@@ -114,285 +136,379 @@ __device__ __forceinline__ void recur_token(const RecurChannel<2>& p, const RawV
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     float beta;
-    rate[k] = p.slope[k] * sigmoid(rv[k] + p.rb[k]);
-    recur_decay(rate[k], a[k], beta);
-    b[k] = beta * (sigmoid(iv[k] + p.ib[k]) * xv[k]);
+    rate[k] = p.slope[k] * recur_sigmoid(rv[k], p.rb[k]);
+    recur_decay(rate[k], p.near, a[k], beta);
+    b[k] = beta * (recur_sigmoid(iv[k], p.ib[k]) * xv[k]);
   }
+}
+
+// In the place of tokens past a sequence's end: a gate shut (a rate of 0), an input of 0, so
+// that they leave the state as it is.
+template <typename E>
+__device__ __forceinline__ RawVec<E, 2> recur_pair(float v) {
+  RawVec<E, 2> p;
+  store_f32(&p.e[0], v);
+  store_f32(&p.e[1], v);
+  return p;
 }
 
 __device__ __forceinline__ int recur_length(const RecurArgs& s, int b) {
   return s.lengths ? min(max(s.lengths[b], 0), s.T) : s.T;
 }
 
-constexpr int kRecurRun = 16;    // tokens of a wave
-constexpr int kRecurWaves = kRecurSpan / kRecurRun;
+// ---- the chain of spans -----------------------------------------------------------
+// A column is 128 channels of a sequence; its spans follow each other (backward: from the last
+// on) in an order.  A word of 64 bits for each span and channel holds (factor, H), and one for
+// each sixteenth span (state behind it, 0); all ones: not there yet, which no such word is.  It
+// is written and read as one relaxed atomic, so it needs no fence.  Workgroups take their spans
+// from a counter, order by order: one that waits does so for workgroups that took theirs
+// before it and are running, so every wait ends.  Should one not, it gives up after
+// seconds, and its states are NaN.
 
-struct RecurPlace {
-  int b, span, c, lane, wave, t0, len;
-};
-__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& s) {
-  RecurPlace p;
-  const int tile = blockIdx.x % s.tiles, rest = blockIdx.x / s.tiles;
-  p.b = rest % s.B, p.span = rest / s.B;
-  p.lane = threadIdx.x & 63, p.wave = threadIdx.x >> 6;
-  p.c = tile * kRecurCols + p.lane * 2;
-  p.t0 = p.span * kRecurSpan + p.wave * kRecurRun;
-  p.len = recur_length(s, p.b);
-  return p;
+constexpr int kRecurGroup = 16;
+constexpr uint64_t kRecurNone = ~0ull;
+
+__device__ __forceinline__ uint64_t recur_word(float lo, float hi) {
+  return static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo);
+}
+__device__ __forceinline__ float recur_lo(uint64_t w) { return __uint_as_float(static_cast<uint32_t>(w)); }
+__device__ __forceinline__ float recur_hi(uint64_t w) { return __uint_as_float(static_cast<uint32_t>(w >> 32)); }
+__device__ __forceinline__ uint64_t recur_peek(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void recur_publish(uint64_t* p, uint64_t w) {
+  __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t recur_wait(const uint64_t* p, uint64_t w) {
+  for (int n = 0; w == kRecurNone && n < (1 << 22); ++n) {
+    __builtin_amdgcn_s_sleep(2);
+    w = recur_peek(p);
+  }
+  return w == kRecurNone ? recur_word(__builtin_nanf(""), __builtin_nanf("")) : w;
 }
 
-// FINAL: y and the last state from the states before the spans; else a span's (L, H).
-template <typename E, bool VEC, bool FINAL>
-__global__ __launch_bounds__(64 * kRecurWaves) void recur_fwd_kernel(RecurArgs s) {
-  __shared__ float2 act[kRecurWaves][kRecurCols];
-  const RecurPlace at = recur_place(s);
-  const size_t span = static_cast<size_t>(at.b) * s.spans + at.span;
-  if (FINAL && at.span == 0 && at.len == 0 && s.h_out && at.wave == 0) {
+struct RecurTurn {
+  int order, col;
+};
+__device__ __forceinline__ RecurTurn recur_turn(const RecurArgs& s, unsigned* shared) {
+  if (threadIdx.x == 0) *shared = atomicAdd(s.ticket, 1u);
+  __syncthreads();
+  const unsigned id = __builtin_amdgcn_readfirstlane(*shared);
+  const unsigned order = id / s.cols;
+  return {static_cast<int>(order), static_cast<int>(id - order * s.cols)};
+}
+
+// The state before the span of this order, of channel threadIdx.x of the first 128 threads;
+// publishes the span's own (factor, H).  first: the state before order 0.  All threads of the
+// workgroup fetch words, into `found`.
+__device__ __forceinline__ float recur_before(const RecurArgs& s, const RecurTurn& t, float factor, float H,
+                                              float first, uint64_t (*found)[kRecurCols]) {
+  const int ch = threadIdx.x % kRecurCols, q = threadIdx.x / kRecurCols;
+  uint64_t* mine = s.words + (static_cast<size_t>(t.col) * s.spans + t.order) * kRecurCols + ch;
+  if (q == 0) recur_publish(mine, recur_word(factor, H));
+  const int groups = s.spans / kRecurGroup, g = t.order / kRecurGroup, n = t.order % kRecurGroup;
+  uint64_t* ends = s.words + (static_cast<size_t>(s.cols) * s.spans + static_cast<size_t>(t.col) * groups) * kRecurCols + ch;
+  // slot 0: behind the last whole group; slot k + 1: the group's span k
+  const uint64_t* first_word = ends + static_cast<size_t>(g - 1) * kRecurCols;
+  const uint64_t* back = mine - static_cast<size_t>(n + 1) * kRecurCols;
+  uint64_t w[kRecurGroup / 4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (at.c + k < s.D) {
-        const size_t e = static_cast<size_t>(at.b) * s.D + at.c + k;
-        s.h_out[e] = s.h_in ? s.h_in[e] : 0.f;
-      }
+  for (int k = 0; k < kRecurGroup / 4; ++k) {
+    const int slot = 4 * k + q;
+    if (slot == 0 ? g > 0 : slot <= n) w[k] = recur_peek(slot == 0 ? first_word : back + slot * kRecurCols);
   }
-  if (at.span * kRecurSpan >= at.len) return;
-  const E* x = static_cast<const E*>(s.x) + at.b * s.xb;
-  const E* r = static_cast<const E*>(s.r) + at.b * s.rb_;
-  const E* i = static_cast<const E*>(s.i) + at.b * s.ib_;
+#pragma unroll
+  for (int k = 0; k < kRecurGroup / 4; ++k) {
+    const int slot = 4 * k + q;
+    if (slot == 0 ? g > 0 : slot <= n)
+      found[slot][ch] = recur_wait(slot == 0 ? first_word : back + slot * kRecurCols, w[k]);
+  }
+  __syncthreads();
+  if (q != 0) return 0.f;
+  float h = g > 0 ? recur_lo(found[0][ch]) : first;
+  for (int k = 1; k <= n; ++k) h = recur_act(recur_lo(found[k][ch]), h, recur_hi(found[k][ch]));
+  if (n == kRecurGroup - 1)
+    recur_publish(ends + static_cast<size_t>(g) * kRecurCols, recur_word(recur_act(factor, h, H), 0.f));
+  return h;
+}
+
+// No words yet, no turn taken: 16 bytes a thread, the first 256 bytes zero.
+__global__ __launch_bounds__(256) void recur_clear_kernel(uint4* ws, size_t n) {
+  const size_t id = blockIdx.x * 256ull + threadIdx.x;
+  const uint32_t v = id < 16 ? 0u : ~0u;
+  if (id < n) ws[id] = make_uint4(v, v, v, v);
+}
+
+// ---- forward ------------------------------------------------------------------------
+
+constexpr int kRecurRun = 16;                                // tokens of a wave
+constexpr int kRecurWaves = 8;
+constexpr int kRecurFwdSpan = kRecurRun * kRecurWaves;       // tokens of a workgroup
+constexpr int kRecurBackRun = 8;
+static_assert(kRecurBackRun * kRecurWaves == kRecurSpan && kRecurFwdSpan % kRecurSpan == 0, "");
+
+// CHAIN: the sequences have more than one span.
+template <typename E, bool VEC, bool CHAIN>
+__global__ __launch_bounds__(64 * kRecurWaves, 4) void recur_fwd_kernel(RecurArgs s) {
+  __shared__ float2 act[kRecurWaves][kRecurCols];
+  __shared__ float sums[kRecurWaves][kRecurCols];
+  __shared__ uint64_t found[CHAIN ? kRecurGroup : 1][kRecurCols];
+  __shared__ float from[kRecurCols];
+  __shared__ unsigned turn;
+  RecurTurn at = {0, static_cast<int>(blockIdx.x)};
+  if constexpr (CHAIN) at = recur_turn(s, &turn);
+  const int b = at.col / s.tiles, c0 = (at.col - b * s.tiles) * kRecurCols;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int c = c0 + lane * 2, t0 = at.order * kRecurFwdSpan + wave * kRecurRun;
+  const int len = recur_length(s, b), ch = threadIdx.x, col = c0 + ch;  // (ch: of the first 128 threads)
+  const size_t state = static_cast<size_t>(b) * s.D;
+  if (len == 0 && at.order == 0 && s.h_out && ch < kRecurCols && col < s.D)
+    s.h_out[state + col] = s.h_in ? s.h_in[state + col] : 0.f;
+  if (at.order * kRecurFwdSpan >= len) return;
+  const E* x = static_cast<const E*>(s.x) + b * s.xb;
+  const E* r = static_cast<const E*>(s.r) + b * s.rb_;
+  const E* i = static_cast<const E*>(s.i) + b * s.ib_;
   RawVec<E, 2> xs[kRecurRun], rs[kRecurRun], is[kRecurRun];
 #pragma unroll
   for (int k = 0; k < kRecurRun; ++k) {
-    const long long t = min(at.t0 + k, at.len - 1);
-    xs[k] = recur_load<VEC>(x + t * s.xt, at.c, s.D);
-    rs[k] = recur_load<VEC>(r + t * s.rt, at.c, s.D);
-    is[k] = recur_load<VEC>(i + t * s.it, at.c, s.D);
+    const long long t = min(t0 + k, len - 1);
+    xs[k] = recur_load<VEC>(x + t * s.xt, c, s.D);
+    rs[k] = recur_load<VEC>(r + t * s.rt, c, s.D);
+    is[k] = recur_load<VEC>(i + t * s.it, c, s.D);
   }
-  const RecurChannel<2> p = recur_channel<2>(s, at.c);
-  float a[kRecurRun][2], b[kRecurRun][2], L[2] = {0.f, 0.f}, H[2] = {0.f, 0.f};
+  __builtin_amdgcn_sched_barrier(0);  // the loads first
+  const RecurChannel p = recur_channel(s, c);
+  float a[kRecurRun][2], bu[kRecurRun][2], L[2] = {0.f, 0.f}, H[2] = {0.f, 0.f};
+  if (t0 + kRecurRun > len) {
+#pragma unroll
+    for (int k = 0; k < kRecurRun; ++k)
+      if (t0 + k >= len) {
+        rs[k] = recur_pair<E>(-__builtin_inff());
+        xs[k] = is[k] = recur_pair<E>(0.f);
+      }
+  }
 #pragma unroll
   for (int k = 0; k < kRecurRun; ++k) {
     float rate[2];
-    recur_token<E>(p, xs[k], rs[k], is[k], rate, a[k], b[k]);
+    recur_token<E>(p, xs[k], rs[k], is[k], rate, a[k], bu[k]);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      if (at.t0 + k >= at.len) rate[e] = 0.f, a[k][e] = 1.f, b[k][e] = 0.f;
       L[e] += rate[e];
-      H[e] = fmaf(a[k][e], H[e], b[k][e]);
+      H[e] = fmaf(a[k][e], H[e], bu[k][e]);
     }
-  }
-#pragma unroll
-  for (int e = 0; e < 2; ++e) act[at.wave][at.lane * 2 + e] = make_float2(FINAL ? recur_factor(L[e]) : L[e], H[e]);
-  __syncthreads();
-  if constexpr (!FINAL) {
-    const int c = threadIdx.x, col = at.c - at.lane * 2 + c;
-    if (c >= kRecurCols || col >= s.D) return;
-    float2 all = act[0][c];
-#pragma unroll
-    for (int w = 1; w < kRecurWaves; ++w) {
-      const float2 m = act[w][c];
-      all = make_float2(all.x + m.x, recur_act(recur_factor(m.x), all.y, m.y));
-    }
-    s.sums[span * 2 * s.D + col] = all.x;
-    s.sums[(span * 2 + 1) * s.D + col] = all.y;
-  } else {
-    E* y = static_cast<E*>(s.y) + at.b * s.yb;
-    float h[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      h[e] = s.starts[span * s.D + min(at.c + e, s.D - 1)];
-      for (int w = 0; w < at.wave; ++w) {
-        const float2 m = act[w][at.lane * 2 + e];
-        h[e] = recur_act(m.x, h[e], m.y);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kRecurRun; ++k) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) h[e] = fmaf(a[k][e], h[e], b[k][e]);
-      if (at.t0 + k < at.len) recur_store<VEC>(y + (at.t0 + k) * s.yt, at.c, s.D, h);
-    }
-    if (s.h_out && at.t0 < at.len && at.len <= at.t0 + kRecurRun) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (at.c + e < s.D) s.h_out[static_cast<size_t>(at.b) * s.D + at.c + e] = h[e];
-    }
-  }
-}
-
-// States between spans: forward from h_in into starts; REVERSE the values a_t G_t behind each
-// span from the last on, and dh_in.
-template <bool REVERSE>
-__global__ __launch_bounds__(256) void recur_join_kernel(RecurArgs s) {
-  const long long id = blockIdx.x * 256LL + threadIdx.x;
-  if (id >= static_cast<long long>(s.B) * s.D) return;
-  const int b = static_cast<int>(id / s.D), c = static_cast<int>(id - 1LL * b * s.D);
-  const int len = recur_length(s, b), n = (len + kRecurSpan - 1) / kRecurSpan;
-  const float* first = REVERSE ? s.dh_out : s.h_in;
-  const float* __restrict__ sums = s.sums;
-  float* __restrict__ out = REVERSE ? s.behind : s.starts;
-  float h = first ? first[id] : 0.f;
-  const size_t base = static_cast<size_t>(b) * s.spans;
-#pragma unroll 8
-  for (int k = 0; k < n; ++k) {
-    const size_t span = base + (REVERSE ? n - 1 - k : k);
-    const float L = sums[span * 2 * s.D + c], H = sums[(span * 2 + 1) * s.D + c];
-    out[span * s.D + c] = h;
-    h = recur_act(recur_factor(L), h, H);
-  }
-  if (REVERSE && s.dh_in) s.dh_in[id] = h;
-}
-
-// Gradients.  FINAL from the states before the spans and the values behind them; else a span's
-// (L, R): the value a_t G_t of its first token from one behind it.
-template <typename E, bool VEC, bool FINAL>
-__global__ __launch_bounds__(64 * kRecurWaves) void recur_bwd_kernel(RecurArgs s) {
-  __shared__ float2 act[kRecurWaves][kRecurCols];
-  __shared__ float back[FINAL ? kRecurWaves : 1][kRecurCols];
-  __shared__ float red[FINAL ? kRecurWaves : 1][3][kRecurCols];
-  const RecurPlace at = recur_place(s);
-  const size_t span = static_cast<size_t>(at.b) * s.spans + at.span;
-  const int c = threadIdx.x, col = at.c - at.lane * 2 + c;  // of the sums over waves
-  if (at.span * kRecurSpan >= at.len) {
-    if (FINAL && c < kRecurCols && col < s.D)
-      for (int k = 0; k < 3; ++k) s.part[(span * 3 + k) * s.D + col] = 0.f;
-    return;
-  }
-  const E* x = static_cast<const E*>(s.x) + at.b * s.xb;
-  const E* r = static_cast<const E*>(s.r) + at.b * s.rb_;
-  const E* i = static_cast<const E*>(s.i) + at.b * s.ib_;
-  const E* dy = static_cast<const E*>(s.dy) + at.b * s.yb;
-  RawVec<E, 2> xs[FINAL ? kRecurRun : 1], rs[kRecurRun], is[FINAL ? kRecurRun : 1], gs[kRecurRun];
-#pragma unroll
-  for (int k = 0; k < kRecurRun; ++k) {
-    const long long t = min(at.t0 + k, at.len - 1);
-    rs[k] = recur_load<VEC>(r + t * s.rt, at.c, s.D);
-    gs[k] = recur_load<VEC>(dy + t * s.yt, at.c, s.D);
-    if constexpr (FINAL) {
-      xs[k] = recur_load<VEC>(x + t * s.xt, at.c, s.D);
-      is[k] = recur_load<VEC>(i + t * s.it, at.c, s.D);
-    }
-  }
-  const RecurChannel<2> p = recur_channel<2>(s, at.c);
-  float L[2] = {0.f, 0.f}, H[2] = {0.f, 0.f}, R[2] = {0.f, 0.f};
-  float before[FINAL ? kRecurRun : 1][2];
-  float a[kRecurRun][2];
-#pragma unroll
-  for (int k = 0; k < kRecurRun; ++k) {
-    const bool there = at.t0 + k < at.len;
-    float b[2] = {0.f, 0.f}, rate[2];
-    if constexpr (FINAL) {
-      recur_token<E>(p, xs[k], rs[k], is[k], rate, a[k], b);
-    } else {
-      float rv[2], beta;
-      raw_f32<E, 2>(rs[k], rv);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        rate[e] = p.slope[e] * sigmoid(rv[e] + p.rb[e]);
-        recur_decay(rate[e], a[k][e], beta);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      if (!there) rate[e] = 0.f, a[k][e] = 1.f, b[e] = 0.f;
-      if constexpr (FINAL) before[k][e] = H[e];  // from a zero state at the wave's first token
-      L[e] += rate[e];
-      H[e] = fmaf(a[k][e], H[e], b[e]);
-    }
-  }
-#pragma unroll
-  for (int k = kRecurRun - 1; k >= 0; --k) {
-    float g[2];
-    raw_f32<E, 2>(gs[k], g);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (at.t0 + k < at.len) R[e] = a[k][e] * (g[e] + R[e]);
+    __builtin_amdgcn_sched_barrier(0);  // tokens one by one: more of them at once spill
   }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    act[at.wave][at.lane * 2 + e] = make_float2(FINAL ? recur_factor(L[e]) : L[e], FINAL ? H[e] : R[e]);
-    if constexpr (FINAL) back[at.wave][at.lane * 2 + e] = R[e];
+    act[wave][lane * 2 + e] = make_float2(recur_factor(L[e]), H[e]);
+    sums[wave][lane * 2 + e] = L[e];
   }
   __syncthreads();
-  if constexpr (!FINAL) {
-    if (c >= kRecurCols || col >= s.D) return;
-    float2 all = act[kRecurWaves - 1][c];
+  float first = ch < kRecurCols && s.h_in && col < s.D ? s.h_in[state + col] : 0.f;
+  if constexpr (CHAIN) {
+    float all = 0.f, own = 0.f;
+    if (ch < kRecurCols) {
 #pragma unroll
-    for (int w = kRecurWaves - 2; w >= 0; --w) {
-      const float2 m = act[w][c];
-      all = make_float2(all.x + m.x, recur_act(recur_factor(m.x), all.y, m.y));
+      for (int w = 0; w < kRecurWaves; ++w) {
+        all += sums[w][ch];
+        own = recur_act(act[w][ch].x, own, act[w][ch].y);
+      }
     }
-    s.sums[span * 2 * s.D + col] = all.x;
-    s.sums[(span * 2 + 1) * s.D + col] = all.y;
-  } else {
-    float h[2], g[2], sum[3][2] = {};
+    first = recur_before(s, at, recur_factor(all), own, first, found);
+  }
+  if (ch < kRecurCols) from[ch] = first;
+  __syncthreads();
+  float h[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    h[e] = from[lane * 2 + e];
+    for (int w = 0; w < wave; ++w) h[e] = recur_act(act[w][lane * 2 + e].x, h[e], act[w][lane * 2 + e].y);
+  }
+  if (s.starts && t0 % kRecurSpan == 0 && t0 < len)
+    recur_store<false>(s.starts + (static_cast<size_t>(b) * ((s.T + kRecurSpan - 1) / kRecurSpan) + t0 / kRecurSpan) * s.D,
+                       c, s.D, h);
+  if (!s.y) return;
+  E* y = static_cast<E*>(s.y) + b * s.yb;
+#pragma unroll
+  for (int k = 0; k < kRecurRun; ++k) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) h[e] = fmaf(a[k][e], h[e], bu[k][e]);
+    if (t0 + k < len) recur_store<VEC>(y + static_cast<long long>(t0 + k) * s.yt, c, s.D, h);
+  }
+  if (s.h_out && t0 < len && len <= t0 + kRecurRun) recur_store<false>(s.h_out + state, c, s.D, h);
+}
+
+// ---- gradients ------------------------------------------------------------------------
+
+template <typename E, bool VEC, bool CHAIN>
+__global__ __launch_bounds__(64 * kRecurWaves, 2) void recur_bwd_kernel(RecurArgs s) {
+  __shared__ float2 act[kRecurWaves][kRecurCols];
+  __shared__ float sums[kRecurWaves][kRecurCols], back[kRecurWaves][kRecurCols];
+  // the words found, then the sums over tokens
+  __shared__ __align__(16) char both[sizeof(uint64_t) * kRecurGroup * kRecurCols];
+  uint64_t(*found)[kRecurCols] = reinterpret_cast<uint64_t(*)[kRecurCols]>(both);
+  float(*red)[3][kRecurCols] = reinterpret_cast<float(*)[3][kRecurCols]>(both);
+  static_assert(sizeof(float) * kRecurWaves * 3 * kRecurCols <= sizeof(both), "");
+  __shared__ float from[kRecurCols];
+  __shared__ unsigned turn;
+  RecurTurn at = {0, static_cast<int>(blockIdx.x)};
+  if constexpr (CHAIN) at = recur_turn(s, &turn);
+  const int b = at.col / s.tiles, c0 = (at.col - b * s.tiles) * kRecurCols;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int len = recur_length(s, b), ch = threadIdx.x, col = c0 + ch;  // (ch: of the first 128 threads)
+  const int n = (len + kRecurSpan - 1) / kRecurSpan;
+  const size_t state = static_cast<size_t>(b) * s.D;
+  if (at.order >= n) {  // the spans past the end
+    if (ch < kRecurCols && col < s.D) {
+      for (int k = 0; k < 3; ++k) s.part[((static_cast<size_t>(b) * s.spans + at.order) * 3 + k) * s.D + col] = 0.f;
+      if (n == 0 && at.order == 0 && s.dh_in) s.dh_in[state + col] = s.dh_out ? s.dh_out[state + col] : 0.f;
+    }
+    return;
+  }
+  const int which = n - 1 - at.order, c = c0 + lane * 2, t0 = which * kRecurSpan + wave * kRecurBackRun;
+  const size_t span = static_cast<size_t>(b) * s.spans + which;
+  const E* x = static_cast<const E*>(s.x) + b * s.xb;
+  const E* r = static_cast<const E*>(s.r) + b * s.rb_;
+  const E* i = static_cast<const E*>(s.i) + b * s.ib_;
+  const E* dy = static_cast<const E*>(s.dy) + b * s.yb;
+  RawVec<E, 2> xs[kRecurBackRun], rs[kRecurBackRun], is[kRecurBackRun], gs[kRecurBackRun];
+#pragma unroll
+  for (int k = 0; k < kRecurBackRun; ++k) {
+    const long long t = min(t0 + k, len - 1);
+    xs[k] = recur_load<VEC>(x + t * s.xt, c, s.D);
+    rs[k] = recur_load<VEC>(r + t * s.rt, c, s.D);
+    is[k] = recur_load<VEC>(i + t * s.it, c, s.D);
+    gs[k] = recur_load<VEC>(dy + t * s.yt, c, s.D);
+  }
+  __builtin_amdgcn_sched_barrier(0);  // the loads first
+  const RecurChannel p = recur_channel(s, c);
+  float L[2] = {0.f, 0.f}, H[2] = {0.f, 0.f}, R[2] = {0.f, 0.f};
+  float a[kRecurBackRun][2], rate[kRecurBackRun][2], beta[kRecurBackRun][2], rest[kRecurBackRun][2];
+  float before[kRecurBackRun][2];  // the state before a token, from a zero state at the run's first
+  if (t0 + kRecurBackRun > len) {
+#pragma unroll
+    for (int k = 0; k < kRecurBackRun; ++k)
+      if (t0 + k >= len) {
+        rs[k] = recur_pair<E>(-__builtin_inff());
+        xs[k] = is[k] = gs[k] = recur_pair<E>(0.f);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < kRecurBackRun; ++k) {
+    float xv[2], rv[2], iv[2];
+    raw_f32<E, 2>(xs[k], xv);
+    raw_f32<E, 2>(rs[k], rv);
+    raw_f32<E, 2>(is[k], iv);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int ch = min(at.c + e, s.D - 1), l = at.lane * 2 + e;
-      h[e] = s.starts[span * s.D + ch];
-      for (int w = 0; w < at.wave; ++w) h[e] = recur_act(act[w][l].x, h[e], act[w][l].y);
-      g[e] = s.behind[span * s.D + ch];
-      for (int w = kRecurWaves - 1; w > at.wave; --w) g[e] = recur_act(act[w][l].x, g[e], back[w][l]);
+      float sig;
+      recur_sigmoid(rv[e], p.rb[e], sig, rest[k][e]);
+      rate[k][e] = p.slope[e] * sig;
+      recur_decay(rate[k][e], p.near, a[k][e], beta[k][e]);
+      const float bu = beta[k][e] * (recur_sigmoid(iv[e], p.ib[e]) * xv[e]);
+      before[k][e] = H[e];
+      L[e] += rate[k][e];
+      H[e] = fmaf(a[k][e], H[e], bu);
     }
-    // the states before each token: what the state before the wave's first has become is added
+    __builtin_amdgcn_sched_barrier(0);  // tokens one by one: more of them at once spill
+  }
 #pragma unroll
-    for (int k = 0; k < kRecurRun; ++k)
+  for (int k = kRecurBackRun - 1; k >= 0; --k) {
+    float g[2];
+    raw_f32<E, 2>(gs[k], g);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        before[k][e] += h[e];
-        h[e] *= a[k][e];
+    for (int e = 0; e < 2; ++e) R[e] = a[k][e] * (g[e] + R[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    act[wave][lane * 2 + e] = make_float2(recur_factor(L[e]), H[e]);
+    sums[wave][lane * 2 + e] = L[e];
+    back[wave][lane * 2 + e] = R[e];
+  }
+  __syncthreads();
+  {
+    float first = ch < kRecurCols && s.dh_out && col < s.D ? s.dh_out[state + col] : 0.f;
+    float all = 0.f, own = 0.f;
+    if (ch < kRecurCols) {
+#pragma unroll
+      for (int w = kRecurWaves - 1; w >= 0; --w) {
+        all += sums[w][ch];
+        own = recur_act(act[w][ch].x, own, back[w][ch]);
       }
-    E* dx = static_cast<E*>(s.dx) + at.b * s.dxb;
-    E* dr = static_cast<E*>(s.dr) + at.b * s.drb;
-    E* di = static_cast<E*>(s.di) + at.b * s.dib;
-#pragma unroll
-    for (int k = kRecurRun - 1; k >= 0; --k) {
-      if (at.t0 + k >= at.len) continue;
-      float xv[2], rv[2], iv[2], dyv[2], ox[2], orr[2], oi[2];
-      raw_f32<E, 2>(xs[k], xv);
-      raw_f32<E, 2>(rs[k], rv);
-      raw_f32<E, 2>(is[k], iv);
-      raw_f32<E, 2>(gs[k], dyv);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float sig, rest, take, left, beta, same;
-        recur_sigmoid(rv[e] + p.rb[e], sig, rest);
-        recur_sigmoid(iv[e] + p.ib[e], take, left);
-        const float rate = p.slope[e] * sig, u = take * xv[e];
-        recur_decay(rate, same, beta);
-        const float G = dyv[e] + g[e], ak = a[k][e];
-        // rate / beta -> 0 with the rate
-        const float ratio = beta > 0.f ? rate * __builtin_amdgcn_rcpf(beta) : 0.f;
-        const float by_rate = -G * ak * (rate * before[k][e] - u * ak * ratio);
-        const float du = G * beta;
-        ox[e] = du * take;
-        orr[e] = by_rate * rest;
-        oi[e] = du * u * left;
-        sum[0][e] += by_rate;
-        sum[1][e] += orr[e];
-        sum[2][e] += oi[e];
-        g[e] = ak * G;
-      }
-      const long long t = at.t0 + k;
-      recur_store<VEC>(dx + t * s.dxt, at.c, s.D, ox);
-      recur_store<VEC>(dr + t * s.drt, at.c, s.D, orr);
-      recur_store<VEC>(di + t * s.dit, at.c, s.D, oi);
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) red[at.wave][k][at.lane * 2 + e] = sum[k][e];
-    __syncthreads();
-    if (c >= kRecurCols || col >= s.D) return;
-    // sigmoid(lam) / softplus(lam)
-    const float lam = s.lam[col];
-    const float per = lam < -15.f ? 1.f : 1.f / ((1.f + expf(-lam)) * recur_slope(lam, 1.f));
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < kRecurWaves; ++w) v += red[w][k][c];
-      s.part[(span * 3 + k) * s.D + col] = k == 0 ? v * per : v;
+    const float factor = recur_factor(all);
+    if constexpr (CHAIN) first = recur_before(s, at, factor, own, first, found);
+    if (ch < kRecurCols) {
+      from[ch] = first;
+      if (which == 0 && s.dh_in && col < s.D) s.dh_in[state + col] = recur_act(factor, first, own);
     }
+  }
+  __syncthreads();
+  float h[2], g[2], sum[3][2] = {};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int l = lane * 2 + e;
+    h[e] = s.starts[span * s.D + min(c + e, s.D - 1)];
+    for (int w = 0; w < wave; ++w) h[e] = recur_act(act[w][l].x, h[e], act[w][l].y);
+    g[e] = from[l];
+    for (int w = kRecurWaves - 1; w > wave; --w) g[e] = recur_act(act[w][l].x, g[e], back[w][l]);
+  }
+  // what the state before the run's first token has become is added to the states before each
+#pragma unroll
+  for (int k = 0; k < kRecurBackRun; ++k)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      before[k][e] += h[e];
+      h[e] *= a[k][e];
+    }
+  E* dx = static_cast<E*>(s.dx) + b * s.dxb;
+  E* dr = static_cast<E*>(s.dr) + b * s.drb;
+  E* di = static_cast<E*>(s.di) + b * s.dib;
+#pragma unroll
+  for (int k = kRecurBackRun - 1; k >= 0; --k) {
+    if (t0 + k >= len) continue;
+    float xv[2], iv[2], dyv[2], ox[2], orr[2], oi[2];
+    raw_f32<E, 2>(xs[k], xv);
+    raw_f32<E, 2>(is[k], iv);
+    raw_f32<E, 2>(gs[k], dyv);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float take, left;
+      recur_sigmoid(iv[e], p.ib[e], take, left);
+      const float u = take * xv[e], G = dyv[e] + g[e], ag = a[k][e] * G;
+      // rate / beta -> 0 with the rate
+      const float ratio = beta[k][e] > 0.f ? rate[k][e] * __builtin_amdgcn_rcpf(beta[k][e]) : 0.f;
+      const float by_rate = ag * (u * a[k][e] * ratio - rate[k][e] * before[k][e]);
+      const float du = G * beta[k][e];
+      ox[e] = du * take;
+      orr[e] = by_rate * rest[k][e];
+      oi[e] = du * u * left;
+      sum[0][e] += by_rate;
+      sum[1][e] += orr[e];
+      sum[2][e] += oi[e];
+      g[e] = ag;
+    }
+    const long long t = t0 + k;
+    recur_store<VEC>(dx + t * s.dxt, c, s.D, ox);
+    recur_store<VEC>(dr + t * s.drt, c, s.D, orr);
+    recur_store<VEC>(di + t * s.dit, c, s.D, oi);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) red[wave][k][lane * 2 + e] = sum[k][e];
+  __syncthreads();
+  if (ch >= kRecurCols || col >= s.D) return;
+  // sigmoid(lam) / softplus(lam)
+  const float lam = s.lam[col];
+  const float per = lam < -15.f ? 1.f : 1.f / ((1.f + expf(-lam)) * recur_slope(lam, 1.f));
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRecurWaves; ++w) v += red[w][k][ch];
+    s.part[(span * 3 + k) * s.D + col] = k == 0 ? v * per : v;
   }
 }
 
@@ -407,7 +523,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(float* __restrict__ h, 
   const RawVec<E, 2> i = recur_load<VEC>(static_cast<const E*>(s.i) + b * s.ib_, c, s.D);
   float* state = h + static_cast<long long>(b) * s.D;
   float hv[2] = {state[c], state[min(c + 1, s.D - 1)]}, rate[2], a[2], u[2];
-  recur_token<E>(recur_channel<2>(s, c), x, r, i, rate, a, u);
+  recur_token<E>(recur_channel(s, c), x, r, i, rate, a, u);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     hv[e] = fmaf(a[e], hv[e], u[e]);
@@ -420,11 +536,19 @@ __global__ __launch_bounds__(256) void recur_step_kernel(float* __restrict__ h, 
 
 int recur_spans(int T) { return (T + kRecurSpan - 1) / kRecurSpan; }
 
-// The spans' (L, H) or (L, R), the states before or values behind them; gradients: partial sums,
-// and the states before the spans.
+// Bytes of the chain of `spans` spans of each column: the counter, the words.
+inline size_t recur_chain_bytes(int B, int D, int spans) {
+  const size_t cols = static_cast<size_t>(B) * ((D + kRecurCols - 1) / kRecurCols);
+  if (spans < 2) return 0;
+  return 256 + cols * (spans + spans / kRecurGroup) * kRecurCols * sizeof(uint64_t);
+}
+// A chain; gradients: partial sums, and the states before the spans.
 size_t recur_workspace_bytes(int B, int T, int D, bool backward) {
-  const size_t rows = static_cast<size_t>(B) * recur_spans(T) * D * sizeof(float);
-  return ((backward ? 7 : 3) * rows + 255) & ~static_cast<size_t>(255);
+  const int fwd = (T + kRecurFwdSpan - 1) / kRecurFwdSpan, bwd = recur_spans(T);
+  const size_t chain = recur_chain_bytes(B, D, backward ? bwd : fwd);
+  const size_t rows = backward ? 4 * static_cast<size_t>(B) * bwd * D * sizeof(float) : 0;
+  const size_t all = (chain + rows + 255) & ~static_cast<size_t>(255);
+  return all ? all : 256;
 }
 
 template <typename E>
@@ -435,75 +559,71 @@ bool recur_vec(const RecurArgs& s) {
          ptr_aligned({s.x, s.r, s.i, s.dy, s.y, s.dx, s.dr, s.di}, 2 * sizeof(E));
 }
 
-inline unsigned recur_blocks(const RecurArgs& s) {
-  return static_cast<unsigned>(static_cast<long long>(s.B) * s.spans * s.tiles);
-}
-inline unsigned recur_join_blocks(const RecurArgs& s) {
-  return static_cast<unsigned>((static_cast<long long>(s.B) * s.D + 255) / 256);
-}
-
-// The states before the spans, from s.sums on.
-template <typename E, bool VEC>
-hipError_t recur_states(const RecurArgs& s, hipStream_t st) {
-  recur_fwd_kernel<E, VEC, false><<<recur_blocks(s), 64 * kRecurWaves, 0, st>>>(s);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  recur_join_kernel<false><<<recur_join_blocks(s), 256, 0, st>>>(s);
+// The chain in `ws`, cleared; the grid.
+inline hipError_t recur_chain(RecurArgs& s, int spans, void* ws, unsigned& blocks, hipStream_t st) {
+  s.spans = spans;
+  s.tiles = (s.D + kRecurCols - 1) / kRecurCols;
+  s.cols = s.B * s.tiles;
+  s.ticket = static_cast<unsigned*>(ws);
+  s.words = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + 256);
+  blocks = static_cast<unsigned>(static_cast<long long>(s.cols) * spans);
+  if (spans < 2) return hipSuccess;
+  const size_t n = recur_chain_bytes(s.B, s.D, spans) / 16;
+  recur_clear_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(static_cast<uint4*>(ws), n);
   return hipGetLastError();
 }
 
 template <typename E, bool VEC>
-hipError_t recur_fwd_v(const RecurArgs& s, hipStream_t st) {
-  const hipError_t e = recur_states<E, VEC>(s, st);
+hipError_t recur_fwd_v(RecurArgs s, void* ws, hipStream_t st) {
+  unsigned blocks;
+  const hipError_t e = recur_chain(s, (s.T + kRecurFwdSpan - 1) / kRecurFwdSpan, ws, blocks, st);
   if (e != hipSuccess) return e;
-  recur_fwd_kernel<E, VEC, true><<<recur_blocks(s), 64 * kRecurWaves, 0, st>>>(s);
+  if (s.spans > 1) recur_fwd_kernel<E, VEC, true><<<blocks, 64 * kRecurWaves, 0, st>>>(s);
+  else recur_fwd_kernel<E, VEC, false><<<blocks, 64 * kRecurWaves, 0, st>>>(s);
   return hipGetLastError();
 }
 
 template <typename E, bool VEC>
-hipError_t recur_bwd_v(const RecurArgs& s, bool have_starts, float* const (&sums)[3], hipStream_t st) {
-  hipError_t e = have_starts ? hipSuccess : recur_states<E, VEC>(s, st);
+hipError_t recur_bwd_v(RecurArgs s, float* const (&sums)[3], void* ws, hipStream_t st) {
+  const int spans = recur_spans(s.T);
+  float* rows = reinterpret_cast<float*>(static_cast<char*>(ws) + recur_chain_bytes(s.B, s.D, spans));
+  s.part = rows;
+  hipError_t e;
+  if (!s.starts) {
+    // the forward's chain first, in the same place (it is the shorter one)
+    RecurArgs f = s;
+    f.y = nullptr, f.h_out = nullptr;
+    f.starts = s.starts = rows + 3 * static_cast<size_t>(s.B) * spans * s.D;
+    e = recur_fwd_v<E, VEC>(f, ws, st);
+    if (e != hipSuccess) return e;
+  }
+  unsigned blocks;
+  e = recur_chain(s, spans, ws, blocks, st);
   if (e != hipSuccess) return e;
-  recur_bwd_kernel<E, VEC, false><<<recur_blocks(s), 64 * kRecurWaves, 0, st>>>(s);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  recur_join_kernel<true><<<recur_join_blocks(s), 256, 0, st>>>(s);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  recur_bwd_kernel<E, VEC, true><<<recur_blocks(s), 64 * kRecurWaves, 0, st>>>(s);
+  if (spans > 1) recur_bwd_kernel<E, VEC, true><<<blocks, 64 * kRecurWaves, 0, st>>>(s);
+  else recur_bwd_kernel<E, VEC, false><<<blocks, 64 * kRecurWaves, 0, st>>>(s);
   e = hipGetLastError();
   if (e != hipSuccess || (!sums[0] && !sums[1] && !sums[2])) return e;
-  return launch_sum_partials(s.part, s.B * s.spans, 3 * s.D,
+  return launch_sum_partials(s.part, s.B * spans, 3 * s.D,
                              {{sums[0], sums[1], sums[2]}, {s.D, s.D, s.D}}, st);
 }
 
-hipError_t launch_recur_fwd(RecurArgs s, void* ws, bool bf16, hipStream_t st) {
-  s.spans = recur_spans(s.T), s.tiles = (s.D + kRecurCols - 1) / kRecurCols;
-  const size_t rows = static_cast<size_t>(s.B) * s.spans * s.D;
-  s.sums = static_cast<float*>(ws);
-  if (!s.starts) s.starts = s.sums + 2 * rows;
-  if (bf16) return recur_vec<bf16_t>(s) ? recur_fwd_v<bf16_t, true>(s, st) : recur_fwd_v<bf16_t, false>(s, st);
-  return recur_vec<float>(s) ? recur_fwd_v<float, true>(s, st) : recur_fwd_v<float, false>(s, st);
+hipError_t launch_recur_fwd(const RecurArgs& s, void* ws, bool bf16, hipStream_t st) {
+  if (bf16) return recur_vec<bf16_t>(s) ? recur_fwd_v<bf16_t, true>(s, ws, st) : recur_fwd_v<bf16_t, false>(s, ws, st);
+  return recur_vec<float>(s) ? recur_fwd_v<float, true>(s, ws, st) : recur_fwd_v<float, false>(s, ws, st);
 }
 
-hipError_t launch_recur_bwd(RecurArgs s, float* dlam, float* drb, float* dib, void* ws, bool bf16,
+hipError_t launch_recur_bwd(const RecurArgs& s, float* dlam, float* drb, float* dib, void* ws, bool bf16,
                             hipStream_t st) {
-  s.spans = recur_spans(s.T), s.tiles = (s.D + kRecurCols - 1) / kRecurCols;
-  const size_t rows = static_cast<size_t>(s.B) * s.spans * s.D;
-  s.sums = static_cast<float*>(ws);
-  s.behind = s.sums + 2 * rows;
-  s.part = s.behind + rows;
-  const bool have = s.starts != nullptr;
-  if (!have) s.starts = s.part + 3 * rows;
   float* const sums[3] = {dlam, drb, dib};
   if (bf16)
-    return recur_vec<bf16_t>(s) ? recur_bwd_v<bf16_t, true>(s, have, sums, st)
-                                : recur_bwd_v<bf16_t, false>(s, have, sums, st);
-  return recur_vec<float>(s) ? recur_bwd_v<float, true>(s, have, sums, st)
-                             : recur_bwd_v<float, false>(s, have, sums, st);
+    return recur_vec<bf16_t>(s) ? recur_bwd_v<bf16_t, true>(s, sums, ws, st)
+                                : recur_bwd_v<bf16_t, false>(s, sums, ws, st);
+  return recur_vec<float>(s) ? recur_bwd_v<float, true>(s, sums, ws, st)
+                             : recur_bwd_v<float, false>(s, sums, ws, st);
 }
 
-hipError_t launch_recur_step(float* h, RecurArgs s, bool bf16, hipStream_t st) {
+hipError_t launch_recur_step(float* h, const RecurArgs& s, bool bf16, hipStream_t st) {
   const int pairs = (s.D + 1) / 2;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(pairs) * s.B + 255) / 256);
 #define KATA_STEP(E, VEC) recur_step_kernel<E, VEC><<<blocks, 256, 0, st>>>(h, s, pairs)
