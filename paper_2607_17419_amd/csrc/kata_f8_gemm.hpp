@@ -18,7 +18,6 @@
 #pragma once
 
 #include "kata_f8.hpp"
-#include "kata_quad.hpp"
 
 namespace kata {
 
@@ -27,8 +26,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ f32x4 f8_mfma(const i32x8& a, const i32x8& b) {
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0x7F7F7F7F, 0,
-                                                          0x7F7F7F7F);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);  // unscaled
 }
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -47,11 +45,13 @@ __device__ __forceinline__ f16x8 f8_as_f16(int lo, int hi) {
 template <bool F16>
 struct F8Operand {
   i32x8 v;
+  F8Operand() = default;
   __device__ __forceinline__ explicit F8Operand(const i32x8& codes) : v(codes) {}
 };
 template <>
 struct F8Operand<true> {
   f16x8 v[4];
+  F8Operand() = default;
   __device__ __forceinline__ explicit F8Operand(const i32x8& codes) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = f8_as_f16(codes[2 * k], codes[2 * k + 1]);
@@ -67,15 +67,64 @@ __device__ __forceinline__ f32x4 f8_block(const F8Operand<true>& a, const F8Oper
   return p;
 }
 
-// 16 codes of a row of K from k on, zeros past its end.
+// The products of TN operands with one.
+template <int TN>
+__device__ __forceinline__ void f8_row(const F8Operand<false> (&b)[TN], const F8Operand<false>& a,
+                                       f32x4 (&p)[TN]) {
+#pragma unroll
+  for (int j = 0; j < TN; ++j) p[j] = f8_mfma(b[j].v, a.v);
+}
+template <int TN>
+__device__ __forceinline__ void f8_row(const F8Operand<true> (&b)[TN], const F8Operand<true>& a,
+                                       f32x4 (&p)[TN]) {
+#pragma unroll
+  for (int j = 0; j < TN; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      p[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j].v[k], a.v[k], p[j], 0, 0, 0);
+}
+// The order of instructions that the scheduler is to keep for a row: its LDS reads, then
+// matrix instructions with the vector work of the row before spread between them.
+template <bool F16, int TN, int VALU>
+__device__ __forceinline__ void f8_order(bool both) {
+  __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+  if (both) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+#pragma unroll
+      for (int k = 0; k < (F16 ? 4 : 1); ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, F16 ? (VALU + 4) / 4 : VALU, 0);
+      }
+    }
+  } else {
+    __builtin_amdgcn_sched_group_barrier(0x008, F16 ? 4 * TN : TN, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// 16 codes of a row of K from k on, zeros past its end.  VEC: aligned rows, whose chunk that K
+// ends in is read whole, but of the tensor's last row, where its end may be the memory's.
 template <bool VEC>
-__device__ __forceinline__ uint4 f8_chunk(const uint8_t* row, int k, int K) {
-  if (VEC && k + 16 <= K) return *reinterpret_cast<const uint4*>(row + k);
+__device__ __forceinline__ uint4 f8_chunk(const uint8_t* row, int k, int K, bool last_row) {
   uint32_t w[4] = {0, 0, 0, 0};
-  if (k < K) {
+  const int n = K - k;  // codes that are there
+  if (VEC && (n >= 16 || (n > 0 && !last_row))) {
+    const uint4 v = *reinterpret_cast<const uint4*>(row + k);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    if (n < 16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int there = n - 4 * i;
+        w[i] = there >= 4 ? w[i] : there <= 0 ? 0u : w[i] & ((1u << (8 * there)) - 1u);
+      }
+    }
+  } else if (n > 0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (k + i < K) w[i >> 2] |= static_cast<uint32_t>(row[k + i]) << (8 * (i & 3));
+      if (i < n) w[i >> 2] |= static_cast<uint32_t>(row[k + i]) << (8 * (i & 3));
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -98,107 +147,186 @@ __device__ __forceinline__ void f8_store4(E* row, int n, int N, bool whole, cons
 }
 
 // ---- tiles --------------------------------------------------------------------
-// A staged row is its 128 codes of one block; its 16-byte chunk c lies at chunk
-// c ^ ((row >> 1) & 7), so that the 16 rows of a fragment read meet no bank conflict.
+// A workgroup forms BM x BN of c over blocks of K one after the other: the next block's rows
+// are copied to LDS (global_load_lds) while this one's are multiplied.  A staged row is its 128
+// codes; its 16-byte chunk c lies at chunk c ^ ((row >> 1) & 7), so that the 16 rows of a
+// fragment read meet no bank conflict.  The scales of all rows of four blocks at a time go
+// through registers to LDS a group ahead.
 
 __device__ __forceinline__ int f8_swz(int row) { return (row >> 1) & 7; }
 
-// Rows 8 i .. 8 i + 7 of a tile, one 16-byte chunk a lane, by registers: any alignment, any K.
-template <bool VEC>
-__device__ __forceinline__ void f8_stage_slow(const uint8_t* src, long long ld, int row0, int rows,
-                                              int k0, int K, int i, char* lds) {
-  const int lane = threadIdx.x & 63, r = i * 8 + (lane >> 3), pos = lane & 7;
-  const int at = min(row0 + r, rows - 1);
-  const uint4 v = f8_chunk<VEC>(src + at * ld, k0 + 16 * (pos ^ f8_swz(r)), K);
-  *reinterpret_cast<uint4*>(lds + i * 1024 + lane * 16) = v;
-}
-// The same of a whole block of aligned rows, straight to LDS.
-__device__ __forceinline__ void f8_stage_fast(const uint8_t* src, long long ld, int row0, int rows,
-                                              int k0, int i, char* lds) {
-  const int lane = threadIdx.x & 63, r = i * 8 + (lane >> 3), pos = lane & 7;
-  const int at = min(row0 + r, rows - 1);
-  qd_copy16(src + at * ld + k0 + 16 * (pos ^ f8_swz(r)), lds + i * 1024);
+// One 16-byte chunk a lane from base + offset to LDS at lds + 16 lane, counted by vmcnt.  In
+// inline assembly because the compiler would drive every copy in flight home before each LDS
+// read; the kernel waits with wait_vmcnt, before which it uses no vector load's result.
+__device__ __forceinline__ void f8_copy16(const uint8_t* base, uint32_t offset, void* lds) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(offset), "s"(base), "s"(at)
+               : "memory", "m0");
 }
 
-// Fragment of 16 rows: lane l holds chunks 2 (l / 16) and the next of row l % 16.
+// Fragment of 16 rows: lane l holds chunks l / 16 and l / 16 + 4 of row l % 16 (a and b alike,
+// so which k they are does not matter).  So read, 16 bytes a lane take four cycles a wave;
+// as chunks 2 (l / 16) and the next, eight (measured by themselves).
 __device__ __forceinline__ i32x8 f8_fragment(const char* tile, int row0) {
-  const int lane = threadIdx.x & 63, r = row0 + (lane & 15), g = lane >> 4, z = f8_swz(r);
+  const int lane = threadIdx.x & 63, r = row0 + (lane & 15), at = (lane >> 4) ^ f8_swz(r);
   const char* row = tile + r * 128;
-  return f8_operand(*reinterpret_cast<const uint4*>(row + 16 * ((2 * g) ^ z)),
-                    *reinterpret_cast<const uint4*>(row + 16 * ((2 * g + 1) ^ z)));
+  return f8_operand(*reinterpret_cast<const uint4*>(row + 16 * at),
+                    *reinterpret_cast<const uint4*>(row + 16 * (at ^ 4)));
 }
 
-// BM x BN tiles of c; WM x WN waves.  ROWS: rows of a block of b.  FAST: aligned rows.
+// Tiles in an order in which those that run on one XCD at a time share rows of a and of b:
+// each XCD (launch index mod 8) takes a run of tiles, eight rows of tiles by column.
+__device__ __forceinline__ void f8_place(const F8GemmArgs& s, int& split, int& tm, int& tn) {
+  const int all = s.tm * s.tn * s.splits, xcd = blockIdx.x & 7, q = all >> 3, r = all & 7;
+  int id = xcd * q + min(xcd, r) + (blockIdx.x >> 3);
+  const int tiles = s.tm * s.tn;
+  split = id / tiles;
+  id -= split * tiles;
+  const int band = id / (8 * s.tn), rows = min(8, s.tm - 8 * band);
+  id -= band * 8 * s.tn;
+  tn = id / rows;
+  tm = 8 * band + (id - tn * rows);
+}
+
+template <bool V>
+struct F8Bool {
+  static constexpr bool value = V;
+};
+
+// WM x WN waves.  ROWS: rows of a block of b.  FAST: aligned rows.
 template <typename E, int BM, int BN, int WM, int WN, int ROWS, bool FAST>
-__global__ __launch_bounds__(64 * WM * WN) void f8_tile_kernel(F8GemmArgs s) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) {
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  constexpr int STAGE = (BM + BN) * 128;
+  constexpr int STAGE = (BM + BN) * 128, COPIES = (BM + BN) / 8 / WAVES, ROWS_ALL = BM + BN;
   constexpr bool F16 = sizeof(E) == 4;
+  static_assert(ROWS_ALL <= 64 * WAVES && (BM / 8) % WAVES == 0 && (BN / 8) % WAVES == 0, "");
   __shared__ __align__(16) char lds[2 * STAGE];
+  __shared__ __align__(16) float scales[2][4][ROWS_ALL];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int tiles = s.tm * s.tn, split = blockIdx.x / tiles;
-  int id = blockIdx.x - split * tiles;
-  const int tn = id / s.tm, tm = id - tn * s.tm;
+  int split, tm, tn;
+  f8_place(s, split, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN, wm = wave % WM, wn = wave / WM;
   const int first = split * s.per, last = min(first + s.per, s.kb);
   const int whole = s.K / 128;  // blocks without a tail
 
-  const auto stage = [&](int kb, char* to) {
-    const bool fast = FAST && kb < whole;
+  // copy j of a wave: rows 8 (j WAVES + wave) .. of a's tile, then of b's, one chunk a lane
+  const int crow = wave * 8 + (lane >> 3);
+  const uint32_t cchunk = 16 * ((lane & 7) ^ f8_swz(crow));  // (the same for all j)
+  static_assert(8 * WAVES % 16 == 0, "");
+  const auto copy = [&](int crow, int j, int kb, char* to) {
+    constexpr int A = BM / 8 / WAVES;
+    const bool is_a = j < A;
+    const uint8_t* base = (is_a ? s.a + m0 * s.a_row : s.b + n0 * s.b_row) + kb * 128LL;
+    const int r = min(crow + (is_a ? j : j - A) * 8 * WAVES, (is_a ? s.M - m0 : s.N - n0) - 1);
+    const uint32_t ld = static_cast<uint32_t>(is_a ? s.a_row : s.b_row);  // (24 bits: f8_fast)
+    f8_copy16(base, __umul24(r, ld) + cchunk, to + (j * WAVES + wave) * 1024);
+  };
+  const auto stage_slow = [&](int kb, char* to) {  // by registers: any alignment, any K
 #pragma unroll
-    for (int j = 0; j < (BM + BN) / 8 / WAVES; ++j) {
-      const int i = j * WAVES + wave;
-      const bool is_a = i < BM / 8;
-      const uint8_t* src = is_a ? s.a : s.b;
-      const long long ld = is_a ? s.a_row : s.b_row;
-      const int row0 = is_a ? m0 : n0, rows = is_a ? s.M : s.N;
-      const int at = is_a ? i : i - BM / 8;
-      char* tile = is_a ? to : to + BM * 128;
-      if (fast) f8_stage_fast(src, ld, row0, rows, kb * 128, at, tile);
-      else f8_stage_slow<FAST>(src, ld, row0, rows, kb * 128, s.K, at, tile);
+    for (int j = 0; j < COPIES; ++j) {
+      constexpr int A = BM / 8 / WAVES;
+      const bool is_a = j < A;
+      const int r = crow + (is_a ? j : j - A) * 8 * WAVES, end = is_a ? s.M - m0 : s.N - n0;
+      const int at = min(r, end - 1);
+      const uint8_t* row = is_a ? s.a + (m0 + at) * s.a_row : s.b + (n0 + at) * s.b_row;
+      const uint4 v = f8_chunk<FAST>(row, kb * 128 + static_cast<int>(cchunk), s.K, at == end - 1);
+      *reinterpret_cast<uint4*>(to + (j * WAVES + wave) * 1024 + lane * 16) = v;
+    }
+  };
+  // a thread's row of scales (past the end of c: of its last row or column)
+  const bool row_a = threadIdx.x < BM;
+  const int sr = row_a ? min(m0 + static_cast<int>(threadIdx.x), s.M - 1)
+                       : min(n0 + static_cast<int>(threadIdx.x) - BM, s.N - 1);
+  const float* srow = row_a ? s.sa + static_cast<size_t>(sr) * s.kb
+                            : s.sb + static_cast<size_t>(sr / ROWS) * s.kb;
+  float four[4];
+  const auto fetch = [&](int kb) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) four[k] = srow[min(kb + k, s.kb - 1)];
+  };
+  const auto put = [&](int group) {
+    if (threadIdx.x < ROWS_ALL) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) scales[group & 1][k][threadIdx.x] = four[k];
     }
   };
 
   f32x4 acc[TM][TN] = {};
-  stage(first, lds);
-  for (int kb = first; kb < last; ++kb) {
-    char* now = lds + ((kb - first) & 1) * STAGE;
-    // scales of this block
-    float sa[TM], sb[TN][ROWS == 1 ? 4 : 1];
+  if (FAST && first < whole) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m = min(m0 + (wm * TM + i) * 16 + (lane & 15), s.M - 1);
-      sa[i] = s.sa[static_cast<size_t>(m) * s.kb + kb];
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int n = n0 + (wn * TN + j) * 16;
-      if constexpr (ROWS == 1) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sb[j][e] = s.sb[static_cast<size_t>(min(n + 4 * (lane >> 4) + e, s.N - 1)) * s.kb + kb];
-      } else {
-        sb[j][0] = s.sb[static_cast<size_t>(min(n, s.N - 1) / kF8Block) * s.kb + kb];
-      }
-    }
+    for (int j = 0; j < COPIES; ++j) copy(crow, j, first, lds);
+  } else {
+    stage_slow(first, lds);
+  }
+  fetch(first);
+  put(0);
+  const auto block = [&](int kb, auto with_copies) {
+    constexpr bool COPY = decltype(with_copies)::value;
+    const int step = kb - first;
+    const char* now = lds + (step & 1) * STAGE;
     wait_vmcnt<0>();
-    __syncthreads();
-    if (kb + 1 < last) stage(kb + 1, lds + ((kb + 1 - first) & 1) * STAGE);
-    i32x8 fb[TN];
+    if ((step & 3) == 0 && step) put(step >> 2);
+    lds_barrier();
+    // the next block's copies are issued between the first rows of products; a tail here
+    char* next = lds + ((step + 1) & 1) * STAGE;
+    if (!COPY && kb + 1 < last) stage_slow(kb + 1, next);
+    if ((step & 3) == 0) fetch(kb + 4);
+    int row = crow;
+    if (COPY) asm volatile("" : "+v"(row));  // so that the copies' offsets are formed here, not kept
+    // fragments in the order in which they are needed
+    i32x8 raw = f8_fragment(now, wm * TM * 16);
+    F8Operand<F16> fb[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j] = f8_fragment(now + BM * 128, (wn * TN + j) * 16);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const F8Operand<F16> fa(f8_fragment(now, (wm * TM + i) * 16));
+    for (int j = 0; j < TN; ++j) fb[j] = F8Operand<F16>(f8_fragment(now + BM * 128, (wn * TN + j) * 16));
+    const float* sc = scales[(step >> 2) & 1][step & 3];
+    const float* sca = sc + wm * TM * 16 + (lane & 15);
+    float sa[2], sb[TN][ROWS == 1 ? 4 : 1];
+    sa[0] = sca[0];
+    if constexpr (ROWS == 1) {
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const f32x4 p = f8_block(F8Operand<F16>(fb[j]), fa);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc[i][j][e] = fmaf(p[e], sa[i] * sb[j][ROWS == 1 ? e : 0], acc[i][j][e]);
+        const float4 v = *reinterpret_cast<const float4*>(sc + BM + (wn * TN + j) * 16 + 4 * (lane >> 4));
+        sb[j][0] = v.x, sb[j][1] = v.y, sb[j][2] = v.z, sb[j][3] = v.w;
       }
+    } else {
+      sb[0][0] = sc[BM + wn * TN * 16];
     }
+    // the products of one row of fragments while those of the row before are scaled and added
+    // and the next row's fragment is on its way
+    f32x4 p[2][TN];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i <= TM; ++i) {
+      if (COPY && i < TM / 2) {
+#pragma unroll
+        for (int k = 0; k < 2 * COPIES / TM; ++k) copy(row, i * 2 * COPIES / TM + k, kb + 1, next);
+      }
+      if (i < TM) {
+        const F8Operand<F16> fa(raw);
+        if (i + 1 < TM) raw = f8_fragment(now, (wm * TM + i + 1) * 16);
+        f8_row<TN>(fb, fa, p[i & 1]);
+      }
+      if (i > 0) {
+        const float si = ROWS == 1 ? sa[(i - 1) & 1] : sa[(i - 1) & 1] * sb[0][0];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i - 1][j][e] = fmaf(p[(i - 1) & 1][j][e],
+                                    ROWS == 1 ? si * sb[j][ROWS == 1 ? e : 0] : si, acc[i - 1][j][e]);
+      }
+      if (i + 1 < TM) sa[(i + 1) & 1] = sca[(i + 1) * 16];
+      f8_order<F16, TN, (ROWS == 1 ? 8 : 4)>(i > 0 && i < TM);
+    }
+  };
+  int kb = first;
+  if constexpr (FAST) {
+    for (; kb + 1 < min(last, whole); ++kb) block(kb, F8Bool<true>());
   }
+  for (; kb < last; ++kb) block(kb, F8Bool<false>());
   const bool pieces = s.part ? s.N % 4 == 0
                              : s.c_row % 4 == 0 &&
                                    (reinterpret_cast<uintptr_t>(s.c) & (4 * sizeof(E) - 1)) == 0;
@@ -218,15 +346,22 @@ __global__ __launch_bounds__(64 * WM * WN) void f8_tile_kernel(F8GemmArgs s) {
   }
 }
 
-// The sum of the splits' parts, in order.
-template <typename E>
+// The sum of the splits' parts, in order, V neighbouring values a thread.
+template <typename E, int V>
 __global__ __launch_bounds__(256) void f8_join_kernel(F8GemmArgs s) {
-  const long long id = (blockIdx.x * 256LL + threadIdx.x), all = static_cast<long long>(s.M) * s.N;
+  const long long id = (blockIdx.x * 256LL + threadIdx.x) * V, all = static_cast<long long>(s.M) * s.N;
   if (id >= all) return;
-  float v = s.part[id];
-  for (int k = 1; k < s.splits; ++k) v += s.part[k * all + id];
+  const float* part = s.part + id;
+  float v[V] = {};
+#pragma unroll 8
+  for (int k = 0; k < s.splits; ++k) {
+    float t[V];
+    load_vec<V>(part + k * all, t);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] += t[e];
+  }
   const long long m = id / s.N;
-  store_f32(static_cast<E*>(s.c) + m * s.c_row + (id - m * s.N), v);
+  store_vec<V>(static_cast<E*>(s.c) + m * s.c_row + (id - m * s.N), v);
 }
 
 // ---- few rows of a --------------------------------------------------------------
@@ -249,12 +384,12 @@ __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
       const int kb = kb0 + 8 * u, k = kb * 128 + g * 32;  // (past the end: zeros)
       const int kc = min(kb, s.kb - 1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) fb[u][h] = f8_chunk<true>(brow, k + 16 * h, s.K);
+      for (int h = 0; h < 2; ++h) fb[u][h] = f8_chunk<true>(brow, k + 16 * h, s.K, n0 + r >= s.N - 1);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int m = min(i * 16 + r, s.M - 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) fa[u][i][h] = f8_chunk<true>(s.a + m * s.a_row, k + 16 * h, s.K);
+        for (int h = 0; h < 2; ++h) fa[u][i][h] = f8_chunk<true>(s.a + m * s.a_row, k + 16 * h, s.K, m == s.M - 1);
         sa[u][i] = s.sa[static_cast<size_t>(m) * s.kb + kc];
       }
       if constexpr (ROWS == 1) {
@@ -305,8 +440,14 @@ struct F8Plan {
   int splits, per;
 };
 
-// Splits of K where the tiles leave CUs idle.
-inline F8Plan f8_plan(int M, int N, int K, bool fast) {
+// Tiles of 256 x 256 where there is one for each of the 256 CUs (4096 x 4096 x 4096 in bf16: 74 us
+// for 88 in tiles of 128 x 128; 2048 x 2048 x 2048: 34 for 17; in fp32 their operands in f16 do
+// not fit the registers).  Else tiles of 128 x 128, and K in as many splits as the model of
+// the time says: a block of K takes a workgroup 0.8 us (fp32: 1.3) while it has a CU for itself
+// and 0.7 (1.05) of that for each that share one; the parts' sum costs a launch, 3 us, and its
+// bytes at 4 TB/s.  256 x 4096 x 4096: 1, 2, 4, 14 splits 25, 22, 22, 29 us; 1152 x 1024 x 32768 in
+// fp32: 1, 2, 7, 14 splits 314, 170, 113, 133 us.
+inline F8Plan f8_plan(int M, int N, int K, bool fast, bool f16) {
   const int kb = (K + 127) / 128;
   F8Plan p = {0, 0, 1, kb};
   if (fast && M <= 64) {
@@ -314,28 +455,34 @@ inline F8Plan f8_plan(int M, int N, int K, bool fast) {
     return p;
   }
   const long long big = ((M + 255LL) / 256) * ((N + 255LL) / 256);
-  p.big = big >= 256;
-  const long long tiles = p.big ? big : ((M + 127LL) / 128) * ((N + 127LL) / 128);
-  if (tiles < 256) {
-    long long n = 512 / tiles;
-    if (n > kb / 2) n = kb / 2;  // two blocks at least
-    if (n > 32) n = 32;
-    if (n > 1) {
-      p.per = static_cast<int>((kb + n - 1) / n);
-      p.splits = (kb + p.per - 1) / p.per;
-    }
+  p.big = !f16 && big >= 256;
+  const long long tiles = ((M + 127LL) / 128) * ((N + 127LL) / 128);
+  if (p.big || tiles >= 256) return p;
+  double best = 0.0;
+  for (int n = 1; n <= 32 && n <= kb; ++n) {
+    const int per = (kb + n - 1) / n, splits = (kb + per - 1) / per;
+    if (splits != n) continue;
+    const double share = (f16 ? 1.05 : 0.7) * static_cast<double>((tiles * n + 255) / 256);
+    double us = per * (f16 ? 1.3 : 0.8) * (share > 1.0 ? share : 1.0);
+    if (n > 1) us += 3.0 + 8e-6 / 4 * static_cast<double>(M) * N * n;
+    if (n == 1 || us < best) best = us, p.splits = n, p.per = per;
   }
   return p;
 }
 
+// Rows of whole aligned chunks, 256 of them within 32 bits of an offset.
 inline bool f8_fast(const void* a, const void* b, long long a_row, long long b_row) {
-  return a_row % 16 == 0 && b_row % 16 == 0 && ptr_aligned({a, b}, 16);
+  return a_row % 16 == 0 && b_row % 16 == 0 && a_row < (1 << 23) && b_row < (1 << 23) &&
+         ptr_aligned({a, b}, 16);
 }
 
 // For any alignment: the splits do not depend on it.
 size_t f8_gemm_workspace_bytes(int M, int N, int K) {
-  const F8Plan p = f8_plan(M, N, K, false), f = f8_plan(M, N, K, true);
-  const long long splits = p.splits > f.splits ? p.splits : f.splits;
+  long long splits = 1;
+  for (int k = 0; k < 4; ++k) {
+    const F8Plan p = f8_plan(M, N, K, k & 1, k & 2);
+    if (p.splits > splits) splits = p.splits;
+  }
   return splits == 1 ? 256
                      : (static_cast<size_t>(splits) * M * N * sizeof(float) + 255) &
                            ~static_cast<size_t>(255);
@@ -344,7 +491,7 @@ size_t f8_gemm_workspace_bytes(int M, int N, int K) {
 template <typename E, int ROWS>
 hipError_t f8_gemm_e(F8GemmArgs s, void* ws, hipStream_t st) {
   const bool fast = f8_fast(s.a, s.b, s.a_row, s.b_row);
-  const F8Plan p = f8_plan(s.M, s.N, s.K, fast);
+  const F8Plan p = f8_plan(s.M, s.N, s.K, fast, sizeof(E) == 4);
   s.kb = (s.K + 127) / 128;
   s.splits = p.splits, s.per = p.per;
   s.part = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
@@ -358,14 +505,20 @@ hipError_t f8_gemm_e(F8GemmArgs s, void* ws, hipStream_t st) {
   const int B = p.big ? 256 : 128;
   s.tm = (s.M + B - 1) / B, s.tn = (s.N + B - 1) / B;
   const unsigned grid = static_cast<unsigned>(static_cast<long long>(s.tm) * s.tn * s.splits);
-  if (p.big && fast) f8_tile_kernel<E, 256, 256, 2, 4, ROWS, true><<<grid, 512, 0, st>>>(s);
-  else if (p.big) f8_tile_kernel<E, 256, 256, 2, 4, ROWS, false><<<grid, 512, 0, st>>>(s);
-  else if (fast) f8_tile_kernel<E, 128, 128, 2, 2, ROWS, true><<<grid, 256, 0, st>>>(s);
+  if (p.big) {
+    if constexpr (sizeof(E) == 2) {
+      if (fast) f8_tile_kernel<E, 256, 256, 2, 4, ROWS, true><<<grid, 512, 0, st>>>(s);
+      else f8_tile_kernel<E, 256, 256, 2, 4, ROWS, false><<<grid, 512, 0, st>>>(s);
+    }
+  } else if (fast) f8_tile_kernel<E, 128, 128, 2, 2, ROWS, true><<<grid, 256, 0, st>>>(s);
   else f8_tile_kernel<E, 128, 128, 2, 2, ROWS, false><<<grid, 256, 0, st>>>(s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !s.part) return e;
   const long long all = static_cast<long long>(s.M) * s.N;
-  f8_join_kernel<E><<<static_cast<unsigned>((all + 255) / 256), 256, 0, st>>>(s);
+  const bool four = s.N % 4 == 0 && s.c_row % 4 == 0 && ptr_aligned({s.c}, 4 * sizeof(E));
+  const unsigned blocks = static_cast<unsigned>((all / (four ? 4 : 1) + 255) / 256);
+  if (four) f8_join_kernel<E, 4><<<blocks, 256, 0, st>>>(s);
+  else f8_join_kernel<E, 1><<<blocks, 256, 0, st>>>(s);
   return hipGetLastError();
 }
 
