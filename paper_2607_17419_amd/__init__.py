@@ -1037,8 +1037,27 @@ def _rows(t, what):
     return rows, s[-1], s[-1] if step is None else step
 
 
+def _row_of(t, name, device, shape, dtype):
+    """The address and the row stride of a tensor of rows (None: none)."""
+    if t is None:
+        return None, 0
+    if t.is_contiguous() and t.shape == shape and t.dtype is dtype and t.get_device() == device:
+        return t.data_ptr(), shape[-1]
+    return _tensor(t, name, device, shape, dtype, True), _rows(t, name)[2]
+
+
+def _like(t):
+    """An uninitialised contiguous tensor like t."""
+    import torch
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _codes(lead, n, device):
     import torch
+    if n % 16 == 0:
+        return torch.empty((*lead, n), dtype=torch.float8_e4m3fn, device=device)
     return torch.empty((*lead, (n + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[..., :n]
 
 
@@ -1054,15 +1073,15 @@ def _add_norm(x, w, res, eps, y, sum, q, scale):
         if sum is not None:
             raise ValueError("sum without res is x itself")
     elif sum is None:
-        sum = torch.empty(shape, dtype=T, device=x.device)
+        sum = _like(x)
+    res_at, res_row = _row_of(res, "res", dev, shape, T)
+    sum_at, sum_row = _row_of(sum, "sum", dev, shape, T)
+    y_at, y_row = _row_of(y, "y", dev, shape, T)
+    q_at, q_row = _row_of(q, "q", dev, shape, torch.float8_e4m3fn)
     _check(lib().kata_add_norm_fwd(
-        _tensor(x, "x", dev, shape, T, True), _optional(res, "res", dev, shape, T, True),
-        _optional(w, "w", dev, (D,), f32), _optional(sum, "sum", dev, shape, T, True),
-        _optional(y, "y", dev, shape, T, True),
-        _optional(q, "q", dev, shape, torch.float8_e4m3fn, True),
-        _optional(scale, "scale", dev, (*shape[:-1], _f8_blocks(D)), f32), M, D, x_row,
-        *(0 if t is None else _rows(t, "rows [..,D]")[2] for t in (res, sum, y, q)), eps, code,
-        _stream(None, x.device)), "kata_add_norm_fwd")
+        _tensor(x, "x", dev, shape, T, True), res_at, _optional(w, "w", dev, (D,), f32), sum_at, y_at,
+        q_at, _optional(scale, "scale", dev, (*shape[:-1], _f8_blocks(D)), f32), M, D, x_row, res_row,
+        sum_row, y_row, q_row, eps, code, _stream(None, x.device)), "kata_add_norm_fwd")
     return x if sum is None else sum
 
 
@@ -1070,9 +1089,8 @@ def _add_norm(x, w, res, eps, y, sum, q, scale):
 def add_norm_fwd(x, w=None, res=None, eps: float = 1e-6, y=None, sum=None):
     """Root-mean-square norm of x + res (kata_add_norm_fwd): x, res [..,D], w [D] fp32; returns (y,
     sum), sum being x + res in x's type (x itself without res; it may be given as res)."""
-    import torch
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = _like(x)
     return y, _add_norm(x, w, res, eps, y, sum, None, None)
 
 
@@ -1100,14 +1118,15 @@ def add_norm_bwd(sum, w, dy, dsum=None, eps: float = 1e-6, dx=None, workspace=No
     M, D, row = _rows(sum, "sum [..,D]")
     code, f32, dev, shape, T = _dtype_code(sum), torch.float32, sum.get_device(), sum.shape, sum.dtype
     if dx is None:
-        dx = torch.empty(shape, dtype=T, device=sum.device)
+        dx = _like(sum)
     dw = None if w is None else torch.empty((D,), dtype=f32, device=sum.device)
     workspace = _workspace(workspace, int(lib().kata_add_norm_bwd_workspace_bytes(M, D, code)), sum)
+    dy_at, dy_row = _row_of(dy, "dy", dev, shape, dy.dtype)
+    dsum_at, dsum_row = _row_of(dsum, "dsum", dev, shape, T)
+    dx_at, dx_row = _row_of(dx, "dx", dev, shape, T)
     _check(lib().kata_add_norm_bwd_ws(
-        _tensor(sum, "sum", dev, shape, T, True), _optional(w, "w", dev, (D,), f32),
-        _tensor(dy, "dy", dev, shape, dy.dtype, True), _optional(dsum, "dsum", dev, shape, T, True),
-        _tensor(dx, "dx", dev, shape, T, True), None if dw is None else dw.data_ptr(), M, D, row,
-        *(0 if t is None else _rows(t, "rows [..,D]")[2] for t in (dy, dsum, dx)), eps, code,
+        _tensor(sum, "sum", dev, shape, T, True), _optional(w, "w", dev, (D,), f32), dy_at, dsum_at,
+        dx_at, None if dw is None else dw.data_ptr(), M, D, row, dy_row, dsum_row, dx_row, eps, code,
         _dtype_code(dy), workspace.data_ptr(), workspace.numel(), _stream(None, sum.device)),
         "kata_add_norm_bwd_ws")
     return dx, dw
@@ -1136,10 +1155,10 @@ def f8_quant(x, rows: int = 1, transposed: bool = False, q=None, scale=None, qt=
         qt = _codes((K,), M, x.device)
     if transposed and scale_t is None:
         scale_t = torch.empty(of_t, dtype=f32, device=x.device)
+    q_at, q_row = _row_of(q, "q", dev, x.shape, f8)
     _check(lib().kata_f8_quant(
-        _tensor(x, "x", dev, x.shape, x.dtype, True), _tensor(q, "q", dev, x.shape, f8, True),
-        _tensor(scale, "scale", dev, of, f32), _optional(qt, "qt", dev, (K, M), f8, True),
-        _optional(scale_t, "scale_t", dev, of_t, f32), M, K, rows, x_row, _rows(q, "q [..,K]")[2],
+        _tensor(x, "x", dev, x.shape, x.dtype, True), q_at, _tensor(scale, "scale", dev, of, f32), _optional(qt, "qt", dev, (K, M), f8, True),
+        _optional(scale_t, "scale_t", dev, of_t, f32), M, K, rows, x_row, q_row,
         0 if qt is None else qt.stride(0), code, _stream(None, x.device)), "kata_f8_quant")
     return (q, scale, qt, scale_t) if transposed else (q, scale)
 
@@ -1161,6 +1180,7 @@ def f8_gemm(a, a_scale, b, b_scale, out=None, dtype=None, workspace=None):
     elif dtype is not None and out.dtype is not dtype:
         raise TypeError(f"out must be {dtype}, got {out.dtype}")
     code = _dtype_code(out)
+    out_at, out_row = _row_of(out, "out", dev, shape, out.dtype)
     by_row = N > 1 and b_scale.shape == (N, kb)
     workspace = _workspace(workspace, int(lib().kata_f8_gemm_workspace_bytes(M, N, K)), a)
     _check(lib().kata_f8_gemm_ws(
@@ -1168,8 +1188,7 @@ def f8_gemm(a, a_scale, b, b_scale, out=None, dtype=None, workspace=None):
         _tensor(a_scale, "a_scale", dev, (*a.shape[:-1], kb), f32),
         _tensor(b, "b", dev, (N, K), f8, True),
         _tensor(b_scale, "b_scale", dev, (N, kb) if by_row else (_f8_blocks(N), kb), f32),
-        _tensor(out, "out", dev, shape, out.dtype, True), M, N, K, 1 if by_row else F8_BLOCK, a_row,
-        b.stride(0), _rows(out, "out [..,N]")[2], code, workspace.data_ptr(), workspace.numel(),
+        out_at, M, N, K, 1 if by_row else F8_BLOCK, a_row, b.stride(0), out_row, code, workspace.data_ptr(), workspace.numel(),
         _stream(None, a.device)), "kata_f8_gemm_ws")
     return out
 

@@ -191,9 +191,9 @@ __device__ __forceinline__ void f8_place(const F8GemmArgs& s, int& split, int& t
   tm = 8 * band + (id - tn * rows);
 }
 
-template <bool V>
-struct F8Bool {
-  static constexpr bool value = V;
+template <int V>
+struct F8Int {
+  static constexpr int value = V;
 };
 
 // WM x WN waves.  ROWS: rows of a block of b.  FAST: aligned rows.
@@ -324,9 +324,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) 
   };
   int kb = first;
   if constexpr (FAST) {
-    for (; kb + 1 < min(last, whole); ++kb) block(kb, F8Bool<true>());
+    for (; kb + 1 < min(last, whole); ++kb) block(kb, F8Int<1>());
   }
-  for (; kb < last; ++kb) block(kb, F8Bool<false>());
+  for (; kb < last; ++kb) block(kb, F8Int<0>());
   const bool pieces = s.part ? s.N % 4 == 0
                              : s.c_row % 4 == 0 &&
                                    (reinterpret_cast<uintptr_t>(s.c) & (4 * sizeof(E) - 1)) == 0;
@@ -372,37 +372,46 @@ __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
   constexpr bool F16 = sizeof(E) == 4;
   constexpr int U = MT <= 2 ? 4 : 2;  // blocks on their way at once
   __shared__ float red[8][MT][64][4];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * 16;
-  const uint8_t* brow = s.b + min(n0 + r, s.N - 1) * s.b_row;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16, whole = s.K / 128;
+  const int nr = min(n0 + r, s.N - 1);
+  const uint8_t* brow = s.b + nr * s.b_row;
   f32x4 acc[MT] = {};
-  for (int kb0 = wave; kb0 < s.kb; kb0 += 8 * U) {
-    uint4 fb[U][2], fa[U][MT][2];
-    float sa[U][MT], sb[U][ROWS == 1 ? 4 : 1];
+  // N blocks from kb on, every eighth; TAIL: the one that K ends in
+  const auto blocks = [&](int kb, auto count, auto tail) {
+    constexpr int N = decltype(count)::value;
+    constexpr bool TAIL = decltype(tail)::value;
+    uint4 fb[N][2], fa[N][MT][2];
+    float sa[N][MT], sb[N][ROWS == 1 ? 4 : 1];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int kb = kb0 + 8 * u, k = kb * 128 + g * 32;  // (past the end: zeros)
-      const int kc = min(kb, s.kb - 1);
+    for (int u = 0; u < N; ++u) {
+      const int at = kb + 8 * u, k = at * 128 + g * 32;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) fb[u][h] = f8_chunk<true>(brow, k + 16 * h, s.K, n0 + r >= s.N - 1);
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (TAIL) fb[u][h] = f8_chunk<true>(brow, k + 16 * h, s.K, nr == s.N - 1);
+        else fb[u][h] = *reinterpret_cast<const uint4*>(brow + k + 16 * h);
+      }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int m = min(i * 16 + r, s.M - 1);
+        const uint8_t* arow = s.a + m * s.a_row;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) fa[u][i][h] = f8_chunk<true>(s.a + m * s.a_row, k + 16 * h, s.K, m == s.M - 1);
-        sa[u][i] = s.sa[static_cast<size_t>(m) * s.kb + kc];
+        for (int h = 0; h < 2; ++h) {
+          if constexpr (TAIL) fa[u][i][h] = f8_chunk<true>(arow, k + 16 * h, s.K, m == s.M - 1);
+          else fa[u][i][h] = *reinterpret_cast<const uint4*>(arow + k + 16 * h);
+        }
+        sa[u][i] = s.sa[static_cast<size_t>(m) * s.kb + at];
       }
       if constexpr (ROWS == 1) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          sb[u][e] = s.sb[static_cast<size_t>(min(n0 + 4 * g + e, s.N - 1)) * s.kb + kc];
+          sb[u][e] = s.sb[static_cast<size_t>(min(n0 + 4 * g + e, s.N - 1)) * s.kb + at];
       } else {
-        sb[u][0] = s.sb[static_cast<size_t>(n0 / kF8Block) * s.kb + kc];
+        sb[u][0] = s.sb[static_cast<size_t>(n0 / kF8Block) * s.kb + at];
       }
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (kb0 + 8 * u >= s.kb) break;
+    for (int u = 0; u < N; ++u)
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const f32x4 p = f8_block(F8Operand<F16>(f8_operand(fb[u][0], fb[u][1])),
@@ -411,8 +420,11 @@ __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
         for (int e = 0; e < 4; ++e)
           acc[i][e] = fmaf(p[e], sa[u][i] * sb[u][ROWS == 1 ? e : 0], acc[i][e]);
       }
-    }
-  }
+  };
+  int kb = wave;
+  for (; kb + 8 * (U - 1) < whole; kb += 8 * U) blocks(kb, F8Int<U>(), F8Int<0>());
+  for (; kb < whole; kb += 8) blocks(kb, F8Int<1>(), F8Int<0>());
+  if (kb < s.kb) blocks(kb, F8Int<1>(), F8Int<1>());
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll

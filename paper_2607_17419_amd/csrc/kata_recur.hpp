@@ -111,6 +111,15 @@ __device__ __forceinline__ RawVec<E, 2> recur_load(const E* row, int c, int D) {
     return RawVec<E, 2>{{row[min(c, D - 1)], row[min(c + 1, D - 1)]}};
   }
 }
+// The same value, as far as the compiler can tell another: what was formed from it is formed again.
+template <typename E>
+__device__ __forceinline__ void recur_forget(RawVec<E, 2>& v) {
+  struct Words { uint32_t w[sizeof(E) / 2]; };
+  Words u = __builtin_bit_cast(Words, v);
+#pragma unroll
+  for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) asm volatile("" : "+v"(u.w[k]));
+  v = __builtin_bit_cast(RawVec<E, 2>, u);
+}
 template <bool VEC, typename E>
 __device__ __forceinline__ void recur_store(E* row, int c, int D, const float (&v)[2]) {
   if constexpr (VEC) {
@@ -341,7 +350,7 @@ __global__ __launch_bounds__(64 * kRecurWaves, 4) void recur_fwd_kernel(RecurArg
 // ---- gradients ------------------------------------------------------------------------
 
 template <typename E, bool VEC, bool CHAIN>
-__global__ __launch_bounds__(64 * kRecurWaves, 2) void recur_bwd_kernel(RecurArgs s) {
+__global__ __launch_bounds__(64 * kRecurWaves, sizeof(E) == 2 ? 4 : 2) void recur_bwd_kernel(RecurArgs s) {
   __shared__ float2 act[kRecurWaves][kRecurCols];
   __shared__ float sums[kRecurWaves][kRecurCols], back[kRecurWaves][kRecurCols];
   // the words found, then the sums over tokens
@@ -383,7 +392,7 @@ __global__ __launch_bounds__(64 * kRecurWaves, 2) void recur_bwd_kernel(RecurArg
   __builtin_amdgcn_sched_barrier(0);  // the loads first
   const RecurChannel p = recur_channel(s, c);
   float L[2] = {0.f, 0.f}, H[2] = {0.f, 0.f}, R[2] = {0.f, 0.f};
-  float a[kRecurBackRun][2], rate[kRecurBackRun][2], beta[kRecurBackRun][2], rest[kRecurBackRun][2];
+  float a[kRecurBackRun][2], rate[kRecurBackRun][2];
   float before[kRecurBackRun][2];  // the state before a token, from a zero state at the run's first
   if (t0 + kRecurBackRun > len) {
 #pragma unroll
@@ -401,11 +410,10 @@ __global__ __launch_bounds__(64 * kRecurWaves, 2) void recur_bwd_kernel(RecurArg
     raw_f32<E, 2>(is[k], iv);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float sig;
-      recur_sigmoid(rv[e], p.rb[e], sig, rest[k][e]);
-      rate[k][e] = p.slope[e] * sig;
-      recur_decay(rate[k][e], p.near, a[k][e], beta[k][e]);
-      const float bu = beta[k][e] * (recur_sigmoid(iv[e], p.ib[e]) * xv[e]);
+      float beta;
+      rate[k][e] = p.slope[e] * recur_sigmoid(rv[e], p.rb[e]);
+      recur_decay(rate[k][e], p.near, a[k][e], beta);
+      const float bu = beta * (recur_sigmoid(iv[e], p.ib[e]) * xv[e]);
       before[k][e] = H[e];
       L[e] += rate[k][e];
       H[e] = fmaf(a[k][e], H[e], bu);
@@ -467,21 +475,27 @@ __global__ __launch_bounds__(64 * kRecurWaves, 2) void recur_bwd_kernel(RecurArg
 #pragma unroll
   for (int k = kRecurBackRun - 1; k >= 0; --k) {
     if (t0 + k >= len) continue;
-    float xv[2], iv[2], dyv[2], ox[2], orr[2], oi[2];
+    // the gates once more: kept, they would halve the waves of a CU (training step 276 us)
+    float xv[2], rv[2], iv[2], dyv[2], ox[2], orr[2], oi[2];
+    for (auto* v : {&xs[k], &rs[k], &is[k], &gs[k]}) recur_forget<E>(*v);
+    asm volatile("" : "+v"(rate[k][0]), "+v"(rate[k][1]));
     raw_f32<E, 2>(xs[k], xv);
+    raw_f32<E, 2>(rs[k], rv);
     raw_f32<E, 2>(is[k], iv);
     raw_f32<E, 2>(gs[k], dyv);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float take, left;
+      float take, left, sig, rest, same, beta;
       recur_sigmoid(iv[e], p.ib[e], take, left);
+      recur_sigmoid(rv[e], p.rb[e], sig, rest);
+      recur_decay(rate[k][e], p.near, same, beta);
       const float u = take * xv[e], G = dyv[e] + g[e], ag = a[k][e] * G;
       // rate / beta -> 0 with the rate
-      const float ratio = beta[k][e] > 0.f ? rate[k][e] * __builtin_amdgcn_rcpf(beta[k][e]) : 0.f;
+      const float ratio = beta > 0.f ? rate[k][e] * __builtin_amdgcn_rcpf(beta) : 0.f;
       const float by_rate = ag * (u * a[k][e] * ratio - rate[k][e] * before[k][e]);
-      const float du = G * beta[k][e];
+      const float du = G * beta;
       ox[e] = du * take;
-      orr[e] = by_rate * rest[k][e];
+      orr[e] = by_rate * rest;
       oi[e] = du * u * left;
       sum[0][e] += by_rate;
       sum[1][e] += orr[e];

@@ -191,7 +191,7 @@ def test_sizes():
     assert L.kata_recur_workspace_bytes(1, 1, 1, 2, 0) == 0 and L.kata_recur_workspace_bytes(1, 1, 1, 1, 1) > 0
     assert L.kata_recur_spans(0) == 0 == L.kata_recur_spans(-5)
     assert L.kata_recur_spans(1) == 1 and L.kata_recur_spans(1 << 30) >= 1
-    big = L.kata_recur_workspace_bytes(1, 1 << 29, 128, 0, 1)
+    big = L.kata_recur_workspace_bytes(1, 1 << 28, 128, 0, 1)
     assert big > 1 << 32  # sizes past 32 bits
 
 
