@@ -482,10 +482,11 @@ inline F8Plan f8_plan(int M, int N, int K, bool fast, bool f16) {
   return p;
 }
 
-// Rows of whole aligned chunks, 256 of them within 32 bits of an offset.
+// Rows of whole aligned chunks, 256 of them within 32 bits of an offset, the next one not before
+// the end of a row's last chunk (which is read whole but of the last row).
 inline bool f8_fast(const void* a, const void* b, long long a_row, long long b_row) {
-  return a_row % 16 == 0 && b_row % 16 == 0 && a_row < (1 << 23) && b_row < (1 << 23) &&
-         ptr_aligned({a, b}, 16);
+  const auto fits = [](long long row) { return row % 16 == 0 && row >= 16 && row < (1 << 23); };
+  return fits(a_row) && fits(b_row) && ptr_aligned({a, b}, 16);
 }
 
 // For any alignment: the splits do not depend on it.
@@ -502,6 +503,8 @@ size_t f8_gemm_workspace_bytes(int M, int N, int K) {
 
 template <typename E, int ROWS>
 hipError_t f8_gemm_e(F8GemmArgs s, void* ws, hipStream_t st) {
+  if (s.M == 1) s.a_row = 16;  // one row: its stride is not used
+  if (s.N == 1) s.b_row = 16;
   const bool fast = f8_fast(s.a, s.b, s.a_row, s.b_row);
   const F8Plan p = f8_plan(s.M, s.N, s.K, fast, sizeof(E) == 4);
   s.kb = (s.K + 127) / 128;

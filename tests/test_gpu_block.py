@@ -271,6 +271,25 @@ def test_f8_gemm_non_finite_scales_shapes(kata):
         kata.f8_gemm(a, up(sa), b, up(sb), dtype=torch.float16)
 
 
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_f8_gemm_single_rows_and_repeated_rows(kata, dtype):
+    """One row of either operand with any stride, and a row that stands for many."""
+    gen = torch.Generator().manual_seed(6)
+    (a, sa), (b, sb) = operand(gen, 90, 200, 1), operand(gen, 150, 200, 128)
+    da, db, ua, ub = laid(a, "even"), laid(b, "even"), up(sa), up(sb)
+    whole = kata.f8_gemm(da, ua, db, ub, dtype=dtype)
+    row = da[:1].as_strided((1, 200), (7, 1))
+    near(kata.f8_gemm(row, ua[:1], db, ub, dtype=dtype), whole[:1].cpu().double(),
+         2 * ref.ROUND[dtype] * whole[:1].cpu().double().abs() + 2.0 ** -20, "one row of a")
+    col = kata.f8_gemm(da, ua, db[:1].as_strided((1, 200), (3, 1)), ub[:1], dtype=dtype)
+    near(col, whole[:, :1].cpu().double(), 2 * ref.ROUND[dtype] * whole[:, :1].cpu().double().abs() + 2.0 ** -20, "one of b")
+    for rows in (5, 90):
+        same_rows = da[3:4].expand(rows, 200)
+        got = kata.f8_gemm(same_rows, ua[3:4].expand(rows, 2).contiguous(), db, ub, dtype=dtype)
+        near(got, whole[3:4].expand(rows, 150).cpu().double(),
+             2 * ref.ROUND[dtype] * whole[3:4].cpu().double().abs().expand(rows, 150) + 2.0 ** -20, "repeated rows")
+
+
 def test_offsets_past_32_bits(kata):
     """Rows of one tensor further apart than 2^32 elements."""
     gen = torch.Generator().manual_seed(4)
