@@ -590,7 +590,8 @@ KATA_API kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, co
  *    a code stands for its value times its block's scale.  Scales are contiguous,
  *    [rows][ceil(columns / 128)] or [ceil(rows / 128)][ceil(columns / 128)], the last blocks
  *    being those that are left.  Quantising:
- *        scale = max(max |x| / 448, 2^-126),  code = x (1 / scale) to nearest, ties to even.
+ *        scale = max(max |x| / 448, 2^-126),  code = x / scale to nearest, ties to even
+ *    (of bf16 inputs to kata_f8_quant: x (1 / scale) in fp32, to nearest).
  *    A NaN becomes a NaN code and leaves the scale to the block's other values; an infinity
  *    makes its block's scale infinite and its own code NaN.
  *  - Rows of codes may begin anywhere; products of rows that begin at multiples of 16 bytes
@@ -603,7 +604,8 @@ KATA_API kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, co
  *   x, res, sum, y : [M][D] in dtype;  w : [D], nullable (ones).
  *   res, sum : both or neither; sum receives s, and may be res itself with its row stride.
  *   y, or q and scale (y in 8 bits, quantised from fp32, blocks of one row), or all three.
- *   D <= 32768, else KATA_ERR_UNSUPPORTED.  Squares are summed in fp32, as for kata_qk_norm_fwd.
+ *   D <= 32768, else KATA_ERR_UNSUPPORTED.  Squares are summed in fp64;
+ *   mean + eps has to lie between 2^-250 and 2^250.
  */
 KATA_API kata_status_t kata_add_norm_fwd(const void* x, const void* res, const float* w, void* sum,
                                          void* y, void* q, float* scale, int M, int D,
@@ -613,7 +615,7 @@ KATA_API kata_status_t kata_add_norm_fwd(const void* x, const void* res, const f
 /* Its gradients from sum (s; x without res) and dy, the gradient of y before it is quantised, in
  * dy_dtype (fp32, or dtype): dx [M][D], the gradient of x and of res alike, to which dsum (nullable:
  * none), the gradient that reaches s by the residual's own way, is added; dw [D], nullable.
- * workspace as for kata_conv_bwd_ws. */
+ * Squares are summed in fp32 here, as for kata_qk_norm_fwd.  workspace as for kata_conv_bwd_ws. */
 KATA_API kata_status_t kata_add_norm_bwd_ws(const void* sum, const float* w, const void* dy,
                                             const void* dsum, void* dx, float* dw, int M, int D,
                                             long long sum_row, long long dy_row,

@@ -37,16 +37,47 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*at)[N]) {
   }
 }
 
-// WAVES waves a row; ITER pieces of 512 * WAVES columns.
+template <int CTRL>
+__device__ __forceinline__ double dpp_move64(double x) {
+  struct Two { float lo, hi; };
+  const Two t = __builtin_bit_cast(Two, x);
+  return __builtin_bit_cast(double, Two{dpp_move<CTRL>(t.lo), dpp_move<CTRL>(t.hi)});
+}
+// Sum of a row's squares over its waves, the same in every lane.
+template <int WAVES>
+__device__ __forceinline__ double row_sum64(double x, double* at) {
+  x += dpp_move64<0xB1>(x);
+  x += dpp_move64<0x4E>(x);
+  x += dpp_move64<0x141>(x);
+  x += dpp_move64<0x140>(x);
+  x += __shfl_xor(x, 16);
+  x += __shfl_xor(x, 32);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) x += at[w];
+  }
+  return x;
+}
+// 1 / sqrt(x) to a few 2^-53: the hardware's, and one step of Newton's.
+__device__ __forceinline__ double row_rsqrt(double x) {
+  const double r = __builtin_amdgcn_rsq(x);
+  return r * fma(-0.5 * x * r, r, 1.5);
+}
+
+// WAVES waves a row; ITER pieces of 512 * WAVES columns.  Squares are summed in fp64: a tenth of
+// the time that the row's bytes take, and what decides between codes is then exact.
 template <typename E, int WAVES, int ITER, bool VEC>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel(
     const E* x, const E* res, const float* __restrict__ w, E* sum, E* __restrict__ y,
     uint8_t* __restrict__ q, float* __restrict__ scale, AddNormArgs s) {
-  __shared__ float at[WAVES][1];
+  __shared__ double at[WAVES];
   const long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
   if (m >= s.M) return;  // (with more than one wave never)
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-  float v[ITER][8], total[1] = {0.f};
+  float v[ITER][8];
 #pragma unroll
   for (int k = 0; k < ITER; ++k) load8<VEC>(x + m * s.x_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
   if (res) {
@@ -64,17 +95,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
       if (sum) store8<VEC>(sum + m * s.sum_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
     }
   }
+  double total = 0.0;
 #pragma unroll
   for (int k = 0; k < ITER; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) total[0] = fmaf(v[k][i], v[k][i], total[0]);
-  row_sum<WAVES>(total, at);
-  const float inv = 1.f / sqrtf(total[0] / s.D + s.eps);
+    for (int i = 0; i < 8; ++i) total = fma(static_cast<double>(v[k][i]), static_cast<double>(v[k][i]), total);
+  total = row_sum64<WAVES>(total, at);
+  const double inv64 = row_rsqrt(total / s.D + s.eps);
+  const float inv = static_cast<float>(inv64);
   const int kb = (s.D + kF8Block - 1) / kF8Block;
 #pragma unroll
   for (int k = 0; k < ITER; ++k) {
     const int c = (k * 64 * WAVES + lane) * 8;
-    float wv[8];
+    float wv[8], out[8];
     if (w) {
       load8<VEC>(w, c, s.D, wv);
     } else {
@@ -82,15 +115,32 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
       for (int i = 0; i < 8; ++i) wv[i] = 1.f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * inv * wv[i];
-    if (y) store8<VEC>(y + m * s.y_row, c, s.D, v[k]);
+    for (int i = 0; i < 8; ++i) out[i] = v[k][i] * inv * wv[i];
+    if (y) store8<VEC>(y + m * s.y_row, c, s.D, out);
     if (q) {
       float t = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t = fmaxf(t, fabsf(v[k][i]));
-      const float sc = f8_scale(max_row16(t));
+      for (int i = 0; i < 8; ++i) t = fmaxf(t, fabsf(out[i]));
+      const float sc = f8_scale(max_row16(t)), by = 1.f / sc;
       if ((lane & 15) == 0 && c < s.D) scale[m * kb + c / kF8Block] = sc;
-      store8_codes<VEC>(q + m * s.q_row, c, s.D, f8_codes8(v[k], 1.f / sc));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i] *= by;
+      // out and the block's largest value are off by up to 2.5 steps of fp32 each, their quotient by 6
+      if (__any(f8_near_middle<8>(out))) {
+        double exact[8], top = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          exact[i] = v[k][i] * inv64 * wv[i];
+          top = fmax(top, fabs(exact[i]));
+        }
+        top = fmax(top, dpp_move64<0xB1>(top));
+        top = fmax(top, dpp_move64<0x4E>(top));
+        top = fmax(top, dpp_move64<0x141>(top));
+        top = f8_scale(fmax(top, dpp_move64<0x140>(top)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = f8_odd(exact[i] / top);
+      }
+      store8_codes<VEC>(q + m * s.q_row, c, s.D, f8_pack8(out));
     }
   }
 }

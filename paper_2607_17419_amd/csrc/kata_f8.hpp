@@ -1,10 +1,14 @@
 // kata_f8.hpp -- codes of 8 bits (e4m3: sign, 4 bits of exponent, 3 of mantissa; largest
 // 448, no infinity) with an fp32 scale for each block, and the quantiser:
 //
-//   scale = max(max |x| over the block / 448, 2^-126),   q = e4m3(x * (1 / scale)),
+//   scale = max(max |x| over the block / 448, 2^-126),   q = e4m3(x / scale),
 //
 // rounded to nearest, ties to even.  x / scale is at most 448 (1 + 2^-22), which rounds to
-// 448, so nothing saturates.  A NaN is left out of the maximum and becomes a NaN code; an
+// 448, so nothing saturates.  The quotient is formed in fp32 as x (1 / scale), and where that
+// comes so near to the middle between two codes that its own roundings could decide between
+// them, for the eight values of each lane of the wave once more in fp64 (one value in 10^5: a
+// few instructions each to look, and hardly ever more).  Quotients of bf16 inputs of the
+// quantiser often are such middles exactly; they stay as fp32 gives them.  A NaN is left out of the maximum and becomes a NaN code; an
 // infinity makes its block's scale infinite and its own code NaN.
 //
 // Blocks are 128 columns of one row (KATA_BLOCK_ROWS) or 128 x 128.  A workgroup holds a
@@ -72,9 +76,42 @@ __device__ __forceinline__ void store8_codes(uint8_t* row, int c, int n, uint2 q
       if (c + i < n) row[c + i] = static_cast<uint8_t>((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
   }
 }
-__device__ __forceinline__ uint2 f8_codes8(const float (&v)[8], float inv) {
-  return make_uint2(f8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                    f8_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+// Whether one of eight quotients is within N fp32 steps of a middle between two codes (of codes
+// in their normal range, which have 20 bits less).
+template <int N>
+__device__ __forceinline__ bool f8_near_middle(const float (&v)[8]) {
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) least = min(least, (__float_as_uint(v[i]) - (0x80000u - N)) & 0xFFFFFu);
+  return least <= 2 * N;
+}
+// fp64 to the fp32 that rounds to the same code: to odd where it is not exact.
+__device__ __forceinline__ float f8_odd(double v) {
+  const float f = static_cast<float>(v);
+  const double d = fabs(v) - fabs(static_cast<double>(f));
+  uint32_t b = __float_as_uint(f);
+  if (d < 0.0) b = (b - 1u) | 1u;
+  else if (d > 0.0) b |= 1u;
+  return __uint_as_float(b);
+}
+__device__ __forceinline__ double f8_scale(double top) { return fmax(top / 448.0, 0x1p-126); }
+__device__ __forceinline__ uint2 f8_pack8(const float (&v)[8]) {
+  return make_uint2(f8_pack4(v[0], v[1], v[2], v[3]), f8_pack4(v[4], v[5], v[6], v[7]));
+}
+// Codes of eight values of a block whose largest magnitude is `top`, inv = 1 / its scale.
+template <bool EXACT>
+__device__ __forceinline__ uint2 f8_codes8(const float (&x)[8], float inv, float top) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = x[i] * inv;
+  if constexpr (EXACT) {
+    if (__any(f8_near_middle<4>(v))) {
+      const double scale = f8_scale(static_cast<double>(top));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = f8_odd(x[i] / scale);
+    }
+  }
+  return f8_pack8(v);
 }
 
 // ROWS: rows of a block (1 or 128).  VEC: x in whole aligned pieces of eight elements;
@@ -85,6 +122,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
                                                        float* __restrict__ scale,
                                                        uint8_t* __restrict__ qt,
                                                        float* __restrict__ scale_t, F8QuantArgs s) {
+  constexpr bool EXACT = sizeof(E) == 4;
   __shared__ float top[4][kF8Block];
   __shared__ uint2 turned[kF8Block][17];  // [column][eight rows], a piece of padding
   const int col = threadIdx.x & 15, group = threadIdx.x >> 4, wave = threadIdx.x >> 6;
@@ -101,7 +139,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
     }
   }
   const int kb = (s.K + kF8Block - 1) / kF8Block, mb = (s.M + kF8Block - 1) / kF8Block;
-  float block_inv = 0.f;
+  float block_inv = 0.f, block_top = 0.f;
   if constexpr (ROWS != 1) {
     float t = 0.f;
 #pragma unroll
@@ -115,7 +153,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
     __syncthreads();
     t = fmaxf(fmaxf(top[0][0], top[0][1]), fmaxf(top[0][2], top[0][3]));
     const float sc = f8_scale(t);
-    block_inv = 1.f / sc;
+    block_inv = 1.f / sc, block_top = t;
     if (threadIdx.x == 0) {
       if (scale) scale[static_cast<size_t>(tm) * kb + tk] = sc;
       if (scale_t) scale_t[static_cast<size_t>(tk) * mb + tm] = sc;
@@ -124,19 +162,22 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
   if (q) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float inv = block_inv;
+      float inv = block_inv, t = block_top;
       if constexpr (ROWS == 1) {
-        float t = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) t = fmaxf(t, fabsf(v[i][j]));
-        const float sc = f8_scale(max_row16(t));
+        t = max_row16(t);
+        const float sc = f8_scale(t);
         inv = 1.f / sc;
         if (col == 0 && m0 + i < s.M) scale[static_cast<size_t>(m0 + i) * kb + tk] = sc;
       }
-      if (m0 + i < s.M) store8_codes<VQ>(q + (m0 + i) * s.q_row, k0, s.K, f8_codes8(v[i], inv));
+      if (m0 + i < s.M) store8_codes<VQ>(q + (m0 + i) * s.q_row, k0, s.K, f8_codes8<EXACT>(v[i], inv, t));
     }
   }
   if (!qt) return;
+  const auto column_top = [&](int c) {
+    return ROWS == 1 ? fmaxf(fmaxf(top[0][c], top[1][c]), fmaxf(top[2][c], top[3][c])) : block_top;
+  };
   float inv[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) inv[j] = block_inv;
@@ -154,8 +195,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = col * 8 + j;
-      const float sc =
-          f8_scale(fmaxf(fmaxf(top[0][c], top[1][c]), fmaxf(top[2][c], top[3][c])));
+      const float sc = f8_scale(column_top(c));
       inv[j] = 1.f / sc;
       if (group == 0 && k0 + j < s.K) scale_t[static_cast<size_t>(k0 + j) * mb + tm] = sc;
     }
@@ -163,7 +203,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const E* __restrict__ x,
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float down[8] = {v[0][j], v[1][j], v[2][j], v[3][j], v[4][j], v[5][j], v[6][j], v[7][j]};
-    turned[col * 8 + j][group] = f8_codes8(down, inv[j]);
+    turned[col * 8 + j][group] = f8_codes8<EXACT>(down, inv[j], column_top(col * 8 + j));
   }
   __syncthreads();
   // eight lanes write a transposed row's 128 bytes

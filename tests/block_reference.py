@@ -30,9 +30,11 @@ def to_e4m3(v):
     return torch.where(v.isnan(), v, torch.round(v / step) * step)
 
 
-def quantise(x, rows):
-    """x [M,K] fp32 -> (codes' values, scales fp32), every step rounded as the library defines it:
-    fp32 division, fp32 reciprocal, fp32 product, then to e4m3."""
+def quantise(x, rows, bf16=False):
+    """x [M,K] fp32 -> (codes' values, scales fp32), as the library defines them: the scale an fp32
+    division; codes of fp32 values to nearest of x / scale (fp64: x 448 is exact in it, and a
+    quotient of 24 bits by 24 that is no middle itself is further from one than 2^-52 of it), of
+    bf16 values (bf16) fp32's reciprocal and product, then to nearest."""
     M, K = x.shape
     mb, kb = -(-M // rows), blocks(K)
     cut = torch.zeros((mb * rows, kb * BLOCK), dtype=torch.float32)
@@ -40,8 +42,13 @@ def quantise(x, rows):
     cut = cut.view(mb, rows, kb, BLOCK)
     top = cut.abs().nan_to_num(nan=0.0, posinf=float("inf")).amax((1, 3))
     scale = torch.maximum(top / torch.tensor(448.0), torch.tensor(2.0 ** -126))
-    q = to_e4m3((cut * (torch.tensor(1.0) / scale)[:, None, :, None]).double())
-    return q.reshape(mb * rows, kb * BLOCK)[:M, :K], scale
+    if bf16:
+        v = (cut * (torch.tensor(1.0) / scale)[:, None, :, None]).double()
+    else:
+        whole = top.double() / 448 > 2.0 ** -126
+        v = torch.where(whole[:, None, :, None], cut.double() * 448 / top.double()[:, None, :, None],
+                        cut.double() * 2.0 ** 126)
+    return to_e4m3(v).reshape(mb * rows, kb * BLOCK)[:M, :K], scale
 
 
 def spread(scale, rows, M, K):
