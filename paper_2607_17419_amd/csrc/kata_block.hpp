@@ -54,6 +54,7 @@ struct RecurArgs {
   float* part;      // [B * spans][3 D]: sums for dlam, drb, dib
   unsigned* ticket;  // the chain: see kata_recur.hpp
   uint64_t* words;
+  const float* slopes;  // [D]: c softplus(lam), or null
   int B, T, D, spans, tiles, cols;
   long long xb, xt, rb_, rt, ib_, it, yb, yt;  // y, or dy in the backward
   long long dxb, dxt, drb, drt, dib, dit;

@@ -91,7 +91,7 @@ __device__ __forceinline__ RecurChannel recur_channel(const RecurArgs& s, int c)
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int at = min(c + k, s.D - 1);
-    p.slope[k] = recur_slope(s.lam[at], s.c);
+    p.slope[k] = s.slopes ? s.slopes[at] : recur_slope(s.lam[at], s.c);
     p.rb[k] = s.rb ? -kLog2e * s.rb[at] : 0.f;
     p.ib[k] = s.ib ? -kLog2e * s.ib[at] : 0.f;
   }
@@ -241,11 +241,14 @@ __device__ __forceinline__ float recur_before(const RecurArgs& s, const RecurTur
   return h;
 }
 
-// No words yet, no turn taken: 16 bytes a thread, the first 256 bytes zero.
-__global__ __launch_bounds__(256) void recur_clear_kernel(uint4* ws, size_t n) {
+// No words yet, no turn taken: 16 bytes a thread, the first 256 bytes zero; and the channels'
+// slopes, which each lane of the spans' workgroups would form again (7% of their instructions).
+__global__ __launch_bounds__(256) void recur_clear_kernel(uint4* ws, size_t n, const float* lam, float c,
+                                                          float* slopes, int D) {
   const size_t id = blockIdx.x * 256ull + threadIdx.x;
   const uint32_t v = id < 16 ? 0u : ~0u;
   if (id < n) ws[id] = make_uint4(v, v, v, v);
+  else if (id - n < static_cast<size_t>(D)) slopes[id - n] = recur_slope(lam[id - n], c);
 }
 
 // ---- forward ------------------------------------------------------------------------
@@ -550,11 +553,14 @@ __global__ __launch_bounds__(256) void recur_step_kernel(float* __restrict__ h, 
 
 int recur_spans(int T) { return (T + kRecurSpan - 1) / kRecurSpan; }
 
-// Bytes of the chain of `spans` spans of each column: the counter, the words.
-inline size_t recur_chain_bytes(int B, int D, int spans) {
+// Bytes of the chain of `spans` spans of each column: the counter, the words; then the slopes.
+inline size_t recur_word_bytes(int B, int D, int spans) {
   const size_t cols = static_cast<size_t>(B) * ((D + kRecurCols - 1) / kRecurCols);
-  if (spans < 2) return 0;
   return 256 + cols * (spans + spans / kRecurGroup) * kRecurCols * sizeof(uint64_t);
+}
+inline size_t recur_chain_bytes(int B, int D, int spans) {
+  if (spans < 2) return 0;
+  return recur_word_bytes(B, D, spans) + ((D * sizeof(float) + 255) & ~static_cast<size_t>(255));
 }
 // A chain; gradients: partial sums, and the states before the spans.
 size_t recur_workspace_bytes(int B, int T, int D, bool backward) {
@@ -573,7 +579,7 @@ bool recur_vec(const RecurArgs& s) {
          ptr_aligned({s.x, s.r, s.i, s.dy, s.y, s.dx, s.dr, s.di}, 2 * sizeof(E));
 }
 
-// The chain in `ws`, cleared; the grid.
+// The chain in `ws`, cleared, and the slopes; the grid.
 inline hipError_t recur_chain(RecurArgs& s, int spans, void* ws, unsigned& blocks, hipStream_t st) {
   s.spans = spans;
   s.tiles = (s.D + kRecurCols - 1) / kRecurCols;
@@ -581,9 +587,13 @@ inline hipError_t recur_chain(RecurArgs& s, int spans, void* ws, unsigned& block
   s.ticket = static_cast<unsigned*>(ws);
   s.words = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + 256);
   blocks = static_cast<unsigned>(static_cast<long long>(s.cols) * spans);
+  s.slopes = nullptr;
   if (spans < 2) return hipSuccess;
-  const size_t n = recur_chain_bytes(s.B, s.D, spans) / 16;
-  recur_clear_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(static_cast<uint4*>(ws), n);
+  const size_t words = recur_word_bytes(s.B, s.D, spans), n = words / 16;
+  float* slopes = reinterpret_cast<float*>(static_cast<char*>(ws) + words);
+  s.slopes = slopes;
+  recur_clear_kernel<<<static_cast<unsigned>((n + s.D + 255) / 256), 256, 0, st>>>(
+      static_cast<uint4*>(ws), n, s.lam, s.c, slopes, s.D);
   return hipGetLastError();
 }
 
