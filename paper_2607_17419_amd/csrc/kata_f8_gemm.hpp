@@ -196,6 +196,13 @@ struct F8Int {
   static constexpr int value = V;
 };
 
+// 8192 x 8192 x 8192 to bf16: 490-540 us on different cards, 2.0-2.25 PFLOP/s (a library product with one
+// scale for all 2.71, with a scale per row 2.34); the matrix units are busy 54% of the cycles at
+// 1.9 GHz.  Without the copies 427 us, without the scaled sums 355 (timing copies): the sums
+// are half of the matrix time on the vector units and overlap it in part only.  Tried and not
+// kept: tiles of 32 x 32 (v_mfma_f32_32x32x64: 513 us, spills), a block's first fragments read
+// during the block before (spills; in tiles of 128 x 128 634 for 589), touching the lines of the
+// block after the next for the L2 (578 for 540), wave priorities (nothing).
 // WM x WN waves.  ROWS: rows of a block of b.  FAST: aligned rows.
 template <typename E, int BM, int BN, int WM, int WN, int ROWS, bool FAST>
 __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) {
@@ -367,6 +374,8 @@ __global__ __launch_bounds__(256) void f8_join_kernel(F8GemmArgs s) {
 // ---- few rows of a --------------------------------------------------------------
 // A workgroup forms 16 columns of c of all rows (16 MT of them); its eight waves take every
 // eighth block of K, both operands straight from memory to registers, and are joined in LDS.
+// 8 rows, 8192 x 4096: 10.3 us, b at 3.3 TB/s (one launch's loads are all on their way at once, so
+// latency counts as much as the rate).
 template <typename E, int MT, int ROWS>
 __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
   constexpr bool F16 = sizeof(E) == 4;

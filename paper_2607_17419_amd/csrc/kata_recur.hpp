@@ -16,6 +16,13 @@
 // in one fixed order, so that results do not depend on the order in which workgroups run.
 // L and not the product of the a: where a = 1 - m 2^-24, its products round to 1 - (m + n) 2^-24
 // token by token, always to the same side (state after 20000 tokens at rates of 2e-5: 1.2e-5 off).
+//
+// 131072 tokens of 1024 channels, bf16: 255-265 us, 4.1 TB/s of the 1.07 GB that are read and
+// written once (three launches that form the spans' sums, join them and read everything again:
+// 874); the vector units are busy 66% of the cycles (45 instructions an element, a sixth of
+// them exponentials, reciprocals and roots at 2.5 times an addition's time), loads and
+// arithmetic of the two workgroups of a CU overlap in part.  Training step of 8 x 4096 tokens:
+// forward 84 us, gradients 172.  Runs of 8 tokens a wave: long 298, training 257 us.
 #pragma once
 
 #include "kata_block.hpp"
