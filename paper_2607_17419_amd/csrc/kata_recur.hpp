@@ -30,6 +30,12 @@
 
 namespace kata {
 
+// Within fp32's range, NaN as it is: so that a shut gate (a sigmoid of 0) is a rate of 0 and a gate
+// of -inf stays shut, whatever finite parameters they meet.
+__device__ __forceinline__ float recur_finite(float v) {
+  return v > 3e38f ? 3e38f : v < -3e38f ? -3e38f : v;
+}
+
 // c softplus(lam) = c (max(lam, 0) + log(1 + e)), e = exp(-|lam|) <= 1: the logarithm as
 // 2 atanh(z), z = e / (2 + e) <= 1/3, by its series (the first term left out is 2e-8 of it).
 __device__ __forceinline__ float recur_slope(float lam, float c) {
@@ -40,7 +46,7 @@ __device__ __forceinline__ float recur_slope(float lam, float c) {
   s = fmaf(q, s, 1.f / 5.f);
   s = fmaf(q, s, 1.f / 3.f);
   s = fmaf(q, s, 1.f);
-  return c * (fmaxf(lam, 0.f) + 2.f * z * s);
+  return recur_finite(c * (fmaxf(lam, 0.f) + 2.f * z * s));
 }
 
 // sigmoid of a gate and what is left of 1, both to a few 2^-24 of themselves: v log2(e) + b is the
@@ -99,8 +105,8 @@ __device__ __forceinline__ RecurChannel recur_channel(const RecurArgs& s, int c)
   for (int k = 0; k < 2; ++k) {
     const int at = min(c + k, s.D - 1);
     p.slope[k] = s.slopes ? s.slopes[at] : recur_slope(s.lam[at], s.c);
-    p.rb[k] = s.rb ? -kLog2e * s.rb[at] : 0.f;
-    p.ib[k] = s.ib ? -kLog2e * s.ib[at] : 0.f;
+    p.rb[k] = s.rb ? recur_finite(-kLog2e * s.rb[at]) : 0.f;
+    p.ib[k] = s.ib ? recur_finite(-kLog2e * s.ib[at]) : 0.f;
   }
   p.near = __all(p.slope[0] < kRecurNear && p.slope[1] < kRecurNear);
   return p;

@@ -451,6 +451,32 @@ def test_recur_extreme_gates(kata):
     assert all((g == 0).all() for g in grads if g is not None)
 
 
+@pytest.mark.parametrize("T,lengths", ((20, [5, 20]), (300, [130, 64])))
+def test_recur_extreme_parameters(kata, T, lengths):
+    """Parameters at fp32's ends, in padded batches: a rate without bound (the state forgets all),
+    biases that hold a gate open or shut, a rate of 0 (the state stays)."""
+    big = 3.3e38
+    lam = torch.tensor([big, 0.0, 0.0, -big, big], device=DEV)
+    rb = torch.tensor([0.0, big, -big, 0.0, -big], device=DEV)
+    ib = torch.tensor([0.0, big, 0.0, 0.0, -big], device=DEV)
+    x = torch.linspace(-2, 2, 2 * T * 5, device=DEV).view(2, T, 5)
+    gate = torch.zeros_like(x)
+    h0 = torch.full((2, 5), 0.75, device=DEV)
+    ln = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    y = torch.full_like(x, 7.0)
+    y, h = kata.recur_fwd(x, gate, gate, lam, rb, ib, state=h0, lengths=ln, y=y, final_state=True)
+    there = (torch.arange(T, device=DEV)[None] < ln[:, None])
+    assert torch.isfinite(y).all() and torch.isfinite(h).all() and (y[~there] == 7.0).all()
+    assert torch.equal(y[..., 0][there], x[..., 0][there] * 0.5)        # take = 1/2, a = 0
+    assert (y[..., 2:][there] == 0.75).all() and (h[:, 2:] == 0.75).all()
+    grads = kata.recur_bwd(x, gate, gate, lam, rb, ib, torch.ones_like(x), state=h0, lengths=ln)
+    assert all(torch.isfinite(g).all() for g in grads)
+    for b in range(2):
+        one = kata.recur_fwd(x[b:b + 1, :lengths[b]], gate[:1, :lengths[b]], gate[:1, :lengths[b]], lam, rb, ib,
+                             state=h0[:1])
+        assert torch.equal(one[0], y[b, :lengths[b]])
+
+
 def test_recur_non_finite_stays_ahead(kata):
     x = torch.ones((2, 300, 6), dtype=F32, device=DEV)
     x[0, 140, 2], x[0, 200, 3] = float("inf"), float("nan")
