@@ -512,7 +512,8 @@ __global__ __launch_bounds__(64 * kRecurWaves, sizeof(E) == 2 ? 4 : 2) void recu
       const float u = take * xv[e], G = dyv[e] + g[e], ag = a[k][e] * G;
       // rate / beta -> 0 with the rate
       const float ratio = beta > 0.f ? rate[k][e] * __builtin_amdgcn_rcpf(beta) : 0.f;
-      const float by_rate = ag * (u * a[k][e] * ratio - rate[k][e] * before[k][e]);
+      // (a shut state, a = 0, meets its rate before anything else, so that no product is 0 inf)
+      const float by_rate = ag * (u * a[k][e] * ratio) - ag * rate[k][e] * before[k][e];
       const float du = G * beta;
       ox[e] = du * take;
       orr[e] = by_rate * rest;

@@ -429,6 +429,27 @@ def test_recur_padded_batch_then_steps(kata, dtype, D):
             h = h2
 
 
+def test_recur_lengths_at_groups_of_spans(kata):
+    """Sequences that end where spans, and groups of sixteen spans, of either direction end."""
+    lengths, T, D = [1023, 1024, 1025, 2047, 2048, 2049, 4096, 4100], 4100, 10
+    B = len(lengths)
+    gen, x, r, i, lam, rb, ib = recur_inputs(B, T, D, F32, 77)
+    h0, dh, dy = normal(gen, B, D, dtype=F32), normal(gen, B, D, dtype=F32), normal(gen, B, T, D, dtype=F32)
+    leaf = [t.clone().requires_grad_() for t in (x, r, i, lam, rb, ib, h0)]
+    y, h = ref.recur(*leaf[:6], 8.0, leaf[6], lengths)
+    grads = torch.autograd.grad((y * dy).sum() + (h * dh).sum(), leaf)
+    err = ref.recur_errors(x, r, i, lam, rb, ib, 8.0, h0, lengths, dy, dh)
+    dev, ln = [up(t) for t in (x, r, i, lam, rb, ib)], torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    out, last = kata.recur_fwd(*dev, state=up(h0), lengths=ln, y=torch.zeros((B, T, D), device=DEV), final_state=True)
+    near(out, y.detach(), EPS * y.detach().abs() + err["y"], "y")
+    near(last, h.detach(), err["h"] + EPS * h.detach().abs(), "state")
+    for starts in (None, kata.recur_fwd_train(*dev, state=up(h0), lengths=ln)[1]):
+        back = torch.empty((B, D), device=DEV)
+        got = kata.recur_bwd(*dev, up(dy), starts, state=up(h0), lengths=ln, dstate=up(dh), dstate_in=back)
+        for g, w, name in zip((*got, back), grads, ("dx", "dr", "di", "dlam", "drb", "dib", "dstate")):
+            near(g, w, EPS * w.abs() + err[name], name)
+
+
 def test_recur_extreme_gates(kata):
     """Gates shut and open to their limits: rates of 0 (a = 1) and far past 1."""
     B, T, D = 1, 140, 8
@@ -475,6 +496,21 @@ def test_recur_extreme_parameters(kata, T, lengths):
         one = kata.recur_fwd(x[b:b + 1, :lengths[b]], gate[:1, :lengths[b]], gate[:1, :lengths[b]], lam, rb, ib,
                              state=h0[:1])
         assert torch.equal(one[0], y[b, :lengths[b]])
+
+
+@pytest.mark.parametrize("lam,r", ((3.3e38, 0.0), (1e30, 3.0), (300.0, 50.0)))
+def test_recur_gradients_without_memory(kata, lam, r):
+    """Rates at which a = 0: h = sigmoid(i) x, so that dx = dy / 2, di = dy x / 4 and the rest is 0,
+    with states far above 1.  Powers of two: nothing is rounded but sigmoid(0) = rcp(2), exact."""
+    x = torch.tensor([2.0, -64.0, 1024.0], device=DEV).repeat(2, 70, 1)
+    gate, dy = torch.zeros_like(x), torch.full_like(x, 4.0)
+    h0 = torch.full((2, 3), 4096.0, device=DEV)
+    lam, zeros, dh = torch.full((3,), lam, device=DEV), torch.zeros(3, device=DEV), torch.empty_like(h0)
+    dx, dr, di, dlam, drb, dib = kata.recur_bwd(x, torch.full_like(x, r), gate, lam, zeros, zeros, dy, state=h0,
+                                                dstate_in=dh)
+    assert (dx == 2).all() and torch.equal(di, x) and torch.equal(dib, x.sum((0, 1)))
+    for zero in (dr, dlam, drb, dh):
+        assert (zero.abs() <= 1e-30).all()
 
 
 def test_recur_non_finite_stays_ahead(kata):
