@@ -17,51 +17,40 @@
 
 namespace kata {
 
-// Sum over the WAVES waves of a row (a workgroup, or one wave), the same in every lane; `at`
-// holds one number a wave and is free again after the next barrier.
-template <int WAVES, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float (*at)[N]) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = sum_group<64>(v[k]);
-  if constexpr (WAVES > 1) {
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) at[wave][k] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      v[k] = 0.f;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) v[k] += at[w][k];
-    }
-  }
-}
-
 template <int CTRL>
 __device__ __forceinline__ double dpp_move64(double x) {
   struct Two { float lo, hi; };
   const Two t = __builtin_bit_cast(Two, x);
   return __builtin_bit_cast(double, Two{dpp_move<CTRL>(t.lo), dpp_move<CTRL>(t.hi)});
 }
-// Sum of a row's squares over its waves, the same in every lane.
-template <int WAVES>
-__device__ __forceinline__ double row_sum64(double x, double* at) {
-  x += dpp_move64<0xB1>(x);
-  x += dpp_move64<0x4E>(x);
-  x += dpp_move64<0x141>(x);
-  x += dpp_move64<0x140>(x);
-  x += __shfl_xor(x, 16);
-  x += __shfl_xor(x, 32);
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.0;
+// Sums over the WAVES waves of a row (a workgroup, or one wave), the same in every lane; `at`
+// holds them for each wave and is free again after the next barrier.
+template <int WAVES, int N>
+__device__ __forceinline__ void row_sum(double (&v)[N], double (*at)[N]) {
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) x += at[w];
+  for (int k = 0; k < N; ++k) {
+    double x = v[k];
+    x += dpp_move64<0xB1>(x);
+    x += dpp_move64<0x4E>(x);
+    x += dpp_move64<0x141>(x);
+    x += dpp_move64<0x140>(x);
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    v[k] = x;
   }
-  return x;
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) at[threadIdx.x >> 6][k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = 0.0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v[k] += at[w][k];
+    }
+  }
 }
 // 1 / sqrt(x) to a few 2^-53: the hardware's, and one step of Newton's.
 __device__ __forceinline__ double row_rsqrt(double x) {
@@ -75,7 +64,7 @@ template <typename E, int WAVES, int ITER, bool VEC>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel(
     const E* x, const E* res, const float* __restrict__ w, E* sum, E* __restrict__ y,
     uint8_t* __restrict__ q, float* __restrict__ scale, AddNormArgs s) {
-  __shared__ double at[WAVES];
+  __shared__ double at[WAVES][1];
   const long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
   if (m >= s.M) return;  // (with more than one wave never)
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -97,13 +86,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
       if (sum) store8<VEC>(sum + m * s.sum_row, (k * 64 * WAVES + lane) * 8, s.D, v[k]);
     }
   }
-  double total = 0.0;
+  double total[1] = {0.0};
 #pragma unroll
   for (int k = 0; k < ITER; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) total = fma(static_cast<double>(v[k][i]), static_cast<double>(v[k][i]), total);
-  total = row_sum64<WAVES>(total, at);
-  const double inv64 = row_rsqrt(total / s.D + s.eps);
+    for (int i = 0; i < 8; ++i) total[0] = fma(static_cast<double>(v[k][i]), static_cast<double>(v[k][i]), total[0]);
+  row_sum<WAVES>(total, at);
+  const double inv64 = row_rsqrt(total[0] / s.D + s.eps);
   const float inv = static_cast<float>(inv64);
   const int kb = (s.D + kF8Block - 1) / kF8Block;
 #pragma unroll
@@ -153,7 +142,7 @@ template <typename E, typename G, int WAVES, int ITER, bool VEC>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_kernel(
     const E* __restrict__ sum, const float* __restrict__ w, const G* __restrict__ dy,
     const E* __restrict__ dsum, E* __restrict__ dx, float* __restrict__ part, AddNormArgs s) {
-  __shared__ float at[2][WAVES][2];
+  __shared__ double at[2][WAVES][2];
   __shared__ float red[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * ITER * 8 : 1];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   float dw[ITER][8] = {}, wv[ITER][8];
@@ -170,7 +159,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_ke
   int turn = 0;
   for (long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x; m < s.M;
        m += step, turn ^= 1) {
-    float v[ITER][8], g[ITER][8], d[ITER][8], sums[2] = {0.f, 0.f};
+    float v[ITER][8], g[ITER][8], d[ITER][8], along = 0.f;
+    double sums[2] = {0.0, 0.0};
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
       const int c = (k * 64 * WAVES + lane) * 8;
@@ -187,12 +177,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_ke
     for (int k = 0; k < ITER; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        sums[0] = fmaf(v[k][i], v[k][i], sums[0]);
-        sums[1] = fmaf(v[k][i], g[k][i] * wv[k][i], sums[1]);
+        // (in fp64 as in the forward: fp32 has no squares of rows from 1e19 on)
+        sums[0] = fma(static_cast<double>(v[k][i]), static_cast<double>(v[k][i]), sums[0]);
+        along = fmaf(v[k][i], g[k][i] * wv[k][i], along);
       }
+    sums[1] = along;
     row_sum<WAVES>(sums, at[turn]);
-    const float inv = 1.f / sqrtf(sums[0] / s.D + s.eps);
-    const float dot = sums[1] * inv / s.D;  // mean(g hat)
+    const double inv64 = row_rsqrt(sums[0] / s.D + s.eps);
+    const float inv = static_cast<float>(inv64);
+    const float dot = static_cast<float>(sums[1] * inv64 / s.D);  // mean(g hat)
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
 #pragma unroll

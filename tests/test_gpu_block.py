@@ -132,6 +132,24 @@ def test_add_norm_non_finite_and_zero_rows(kata):
     assert torch.equal(bits(q)[0], bits(q)[5])
 
 
+@pytest.mark.parametrize("size", (1e25, 1e-25))
+@pytest.mark.parametrize("M,D", ((5, 130), (3, 4100), (2100, 96)))
+def test_add_norm_rows_whose_squares_leave_fp32(kata, M, D, size):
+    gen = torch.Generator().manual_seed(M)
+    s, w, dy = (normal(gen, *n, dtype=F32) for n in ((M, D), (D,), (M, D)))
+    s = (s * size).float().double()
+    y, _ = kata.add_norm_fwd(up(s), up(w), eps=0.0)
+    leaf = [s.clone().requires_grad_(), w.clone().requires_grad_()]
+    want = ref.norm(*leaf, 0.0)
+    near(y, want.detach(), (D / 2 + 22) * EPS * want.detach().abs(), "y")
+    grads = torch.autograd.grad(want, leaf, dy)
+    dx, dw = kata.add_norm_bwd(up(s), up(w), up(dy), eps=0.0)
+    inv = 1 / torch.sqrt(s.square().mean(-1, keepdim=True))
+    g, hat = (dy * w).abs(), (s * inv).abs()
+    near(dx, grads[0], (2 * D + 40) * EPS * inv * (g + hat * (g * hat).mean(-1, keepdim=True)), "dx")
+    near(dw, grads[1], (M // 1024 + D / 2 + 60) * EPS * (dy.abs() * hat).sum(0), "dw")
+
+
 # ---- e4m3 ------------------------------------------------------------------------------
 
 QUANT = [(1, 1), (1, 200), (128, 128), (130, 257), (7, 1000), (257, 64), (300, 384), (129, 131)]
