@@ -150,6 +150,22 @@ def test_add_norm_rows_whose_squares_leave_fp32(kata, M, D, size):
     near(dw, grads[1], (M // 1024 + D / 2 + 60) * EPS * (dy.abs() * hat).sum(0), "dw")
 
 
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("M,D", ((2048, 1000), (200, 5000)))
+def test_add_norm_codes_are_the_exact_ones(kata, M, D, dtype):
+    """Codes to nearest of the exact quotients, wherever fp64 can tell the two apart: weights are
+    of 24 bits, so that a quotient within 2^-40 of a middle would be chance (none is)."""
+    gen = torch.Generator().manual_seed(D)
+    x, w = normal(gen, M, D, dtype=dtype), normal(gen, D, dtype=F32)
+    q, _, _ = kata.add_norm_f8_fwd(up(x, dtype), up(w))
+    want = ref.norm(x, w, float(torch.tensor(1e-6)))  # the call takes eps in fp32
+    kb = ref.blocks(D)
+    top = torch.nn.functional.pad(want.abs(), (0, kb * 128 - D)).unflatten(1, (kb, 128)).amax(-1)
+    v = want * 448 / ref.spread(top, 1, M, D)
+    assert torch.equal(ref.to_e4m3(v * (1 - 2.0 ** -40)), ref.to_e4m3(v * (1 + 2.0 ** -40)).clamp(-448, 448))
+    assert torch.equal(q.float().cpu().double(), ref.to_e4m3(v))
+
+
 # ---- e4m3 ------------------------------------------------------------------------------
 
 QUANT = [(1, 1), (1, 200), (128, 128), (130, 257), (7, 1000), (257, 64), (300, 384), (129, 131)]
@@ -178,6 +194,28 @@ def test_f8_quant_is_its_definition(kata, M, K, rows, dtype):
     tight = [torch.empty((M, K), dtype=F8, device=DEV), torch.empty((K, M), dtype=F8, device=DEV)]
     out = kata.f8_quant(up(x, dtype), rows=rows, transposed=True, q=tight[0], qt=tight[1])
     assert torch.equal(bits(out[0]), bits(got[0])) and torch.equal(bits(out[2]), bits(got[2]))
+
+
+@pytest.mark.parametrize("rows", (1, 128))
+def test_f8_quant_beside_the_middles(kata, rows):
+    """fp32 values within three steps of the middles between neighbouring codes, the least
+    (subnormal) codes' too."""
+    gen = torch.Generator().manual_seed(3)
+    codes = torch.arange(127, dtype=torch.uint8).view(F8).float().double()  # 0 to 448
+    middles = (codes[1:] + codes[:-1]) / 2
+    M = 640
+    x = torch.empty((M, 128), dtype=F32)
+    x[:, 0] = torch.rand(M, generator=gen) + 1.0
+    x[:, 0] = x[torch.arange(M) // 128 * 128, 0]  # one for each block of either form
+    x[:, 1:127] = (middles * x[:, :1].double() / 448).float()
+    x[:, 127] = 0.0
+    for k in range(3):
+        x[:, 1:127] = torch.where((torch.arange(M) % 7 > 3 + k)[:, None], x[:, 1:127].nextafter(torch.tensor(9.0)), x[:, 1:127])
+        x[:, 1:127] = torch.where((torch.arange(M) % 7 < 3 - k)[:, None], x[:, 1:127].nextafter(torch.tensor(0.0)), x[:, 1:127])
+    got = kata.f8_quant(up(x), rows=rows, transposed=True)
+    want = (*ref.quantise(x, rows), *ref.quantise(x.t(), rows))
+    for g, w, name in zip(got, want, ("q", "scale", "qt", "scale_t")):
+        assert torch.equal(g.float().cpu().double(), w.double()), name
 
 
 def test_f8_quant_writes_its_rows_only_and_keeps_non_finite_in_their_blocks(kata):
