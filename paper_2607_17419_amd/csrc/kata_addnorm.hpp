@@ -23,21 +23,21 @@ __device__ __forceinline__ double dpp_move64(double x) {
   const Two t = __builtin_bit_cast(Two, x);
   return __builtin_bit_cast(double, Two{dpp_move<CTRL>(t.lo), dpp_move<CTRL>(t.hi)});
 }
+__device__ __forceinline__ float wave_sum(float x) { return sum_group<64>(x); }
+__device__ __forceinline__ double wave_sum(double x) {
+  x += dpp_move64<0xB1>(x);
+  x += dpp_move64<0x4E>(x);
+  x += dpp_move64<0x141>(x);
+  x += dpp_move64<0x140>(x);
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
 // Sums over the WAVES waves of a row (a workgroup, or one wave), the same in every lane; `at`
 // holds them for each wave and is free again after the next barrier.
-template <int WAVES, int N>
-__device__ __forceinline__ void row_sum(double (&v)[N], double (*at)[N]) {
+template <int WAVES, int N, typename F>
+__device__ __forceinline__ void row_sum(F (&v)[N], F (*at)[N]) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    double x = v[k];
-    x += dpp_move64<0xB1>(x);
-    x += dpp_move64<0x4E>(x);
-    x += dpp_move64<0x141>(x);
-    x += dpp_move64<0x140>(x);
-    x += __shfl_xor(x, 16);
-    x += __shfl_xor(x, 32);
-    v[k] = x;
-  }
+  for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -46,7 +46,7 @@ __device__ __forceinline__ void row_sum(double (&v)[N], double (*at)[N]) {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      v[k] = 0.0;
+      v[k] = F(0);
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) v[k] += at[w][k];
     }
@@ -137,12 +137,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
 }
 
 // A workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ... (in fours with one wave a
-// row) and keeps its sums of dw in registers; part: [gridDim.x][D].
+// row) and keeps its sums of dw in registers; part: [gridDim.x][D].  Squares are summed in fp32,
+// and once more, scaled, in rows whose squares may have left its range (in fp64 at once:
+// training step 101 -> 129 us, a wave less on each SIMD).
 template <typename E, typename G, int WAVES, int ITER, bool VEC>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_kernel(
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES,
+                             ITER == 1 ? (WAVES == 1 ? 6 : 5) : WAVES == 16 || ITER == 2 ? 4 : 2) void add_norm_bwd_kernel(
     const E* __restrict__ sum, const float* __restrict__ w, const G* __restrict__ dy,
     const E* __restrict__ dsum, E* __restrict__ dx, float* __restrict__ part, AddNormArgs s) {
-  __shared__ double at[2][WAVES][2];
+  __shared__ float at[2][WAVES][2];
+  __shared__ float far[2][WAVES][1];
   __shared__ float red[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * ITER * 8 : 1];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   float dw[ITER][8] = {}, wv[ITER][8];
@@ -159,8 +163,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_ke
   int turn = 0;
   for (long long m = WAVES == 1 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x; m < s.M;
        m += step, turn ^= 1) {
-    float v[ITER][8], g[ITER][8], d[ITER][8], along = 0.f;
-    double sums[2] = {0.0, 0.0};
+    float v[ITER][8], g[ITER][8], d[ITER][8], sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
       const int c = (k * 64 * WAVES + lane) * 8;
@@ -177,15 +180,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_bwd_ke
     for (int k = 0; k < ITER; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        // (in fp64 as in the forward: fp32 has no squares of rows from 1e19 on)
-        sums[0] = fma(static_cast<double>(v[k][i]), static_cast<double>(v[k][i]), sums[0]);
-        along = fmaf(v[k][i], g[k][i] * wv[k][i], along);
+        sums[0] = fmaf(v[k][i], v[k][i], sums[0]);
+        sums[1] = fmaf(v[k][i], g[k][i] * wv[k][i], sums[1]);
       }
-    sums[1] = along;
     row_sum<WAVES>(sums, at[turn]);
-    const double inv64 = row_rsqrt(sums[0] / s.D + s.eps);
-    const float inv = static_cast<float>(inv64);
-    const float dot = static_cast<float>(sums[1] * inv64 / s.D);  // mean(g hat)
+    float inv = 1.f / sqrtf(sums[0] / s.D + s.eps);
+    if (!(sums[0] > 1e-20f && sums[0] < 1e38f)) {  // the same in the whole row
+      const float by = sums[0] < 1.f ? 0x1p80f : 0x1p-80f;
+      float total[1] = {0.f};
+#pragma unroll
+      for (int k = 0; k < ITER; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total[0] = fmaf(v[k][i] * by, v[k][i] * by, total[0]);
+      row_sum<WAVES>(total, far[turn]);
+      inv = static_cast<float>(row_rsqrt(static_cast<double>(total[0]) / by / by / s.D + s.eps));
+    }
+    const float dot = sums[1] * inv / s.D;  // mean(g hat)
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
 #pragma unroll
