@@ -615,7 +615,7 @@ KATA_API kata_status_t kata_add_norm_fwd(const void* x, const void* res, const f
 /* Its gradients from sum (s; x without res) and dy, the gradient of y before it is quantised, in
  * dy_dtype (fp32, or dtype): dx [M][D], the gradient of x and of res alike, to which dsum (nullable:
  * none), the gradient that reaches s by the residual's own way, is added; dw [D], nullable.
- * Squares are summed in fp32 here, scaled where a row's leave its range.  workspace as for kata_conv_bwd_ws. */
+ * A row's sums are formed in fp32 here, in fp64 where they leave its range.  workspace as for kata_conv_bwd_ws. */
 KATA_API kata_status_t kata_add_norm_bwd_ws(const void* sum, const float* w, const void* dy,
                                             const void* dsum, void* dx, float* dw, int M, int D,
                                             long long sum_row, long long dy_row,

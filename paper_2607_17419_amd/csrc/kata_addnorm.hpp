@@ -47,7 +47,7 @@ __device__ __forceinline__ void row_sum(F (&v)[N], F (*at)[N]) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       v[k] = F(0);
-#pragma unroll
+#pragma unroll 4  // (all sixteen at once in fp64 take the registers of the row)
       for (int w = 0; w < WAVES; ++w) v[k] += at[w][k];
     }
   }
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES,
     const E* __restrict__ sum, const float* __restrict__ w, const G* __restrict__ dy,
     const E* __restrict__ dsum, E* __restrict__ dx, float* __restrict__ part, AddNormArgs s) {
   __shared__ float at[2][WAVES][2];
-  __shared__ float far[2][WAVES][1];
+  __shared__ double far[2][WAVES][2];
   __shared__ float red[WAVES == 1 ? 3 : 1][WAVES == 1 ? 64 * ITER * 8 : 1];
   const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   float dw[ITER][8] = {}, wv[ITER][8];
@@ -185,17 +185,25 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES,
       }
     row_sum<WAVES>(sums, at[turn]);
     float inv = 1.f / sqrtf(sums[0] / s.D + s.eps);
-    if (!(sums[0] > 1e-20f && sums[0] < 1e38f)) {  // the same in the whole row
-      const float by = sums[0] < 1.f ? 0x1p80f : 0x1p-80f;
-      float total[1] = {0.f};
+    float dot = sums[1] * (inv / s.D);  // mean(g hat)
+    // the same in the whole row.  (A sum above 1e-30 has lost less than 2^-35 of itself to
+    // subnormal parts; one of 0 may have been smaller, or a row without gradients.)
+    const float size = fabsf(sums[1]);
+    if (!(sums[0] > 1e-20f && sums[0] < 1e38f && size > 1e-30f && size < 1e38f)) {
+      double total[2] = {0.0, 0.0};
 #pragma unroll
       for (int k = 0; k < ITER; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) total[0] = fmaf(v[k][i] * by, v[k][i] * by, total[0]);
+        for (int i = 0; i < 8; ++i) {
+          const double one = v[k][i];
+          total[0] = fma(one, one, total[0]);
+          total[1] = fma(one, static_cast<double>(g[k][i] * wv[k][i]), total[1]);
+        }
       row_sum<WAVES>(total, far[turn]);
-      inv = static_cast<float>(row_rsqrt(static_cast<double>(total[0]) / by / by / s.D + s.eps));
+      const double inv64 = row_rsqrt(total[0] / s.D + s.eps);
+      inv = static_cast<float>(inv64);
+      dot = static_cast<float>(total[1] * inv64 / s.D);
     }
-    const float dot = sums[1] * inv / s.D;  // mean(g hat)
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
 #pragma unroll
@@ -233,8 +241,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES,
 // ---- launches ---------------------------------------------------------------
 
 // A row to one wave where there are rows for two waves on each of the 1024 SIMDs, so that
-// sums need no barrier; fewer or wider rows to four waves, the widest to sixteen (whose rows of
-// 16384 and more spill some of their registers).
+// sums need no barrier; fewer or wider rows to four waves, the widest to sixteen (whose gradients
+// spill from 16385 columns on: 173 of the 256 values that a lane holds).
 inline int add_norm_waves(int M, int D) { return D > 8192 ? 16 : D > 2048 || M < 2048 ? 4 : 1; }
 
 // Pieces of 512 * waves columns: CALL(waves, pieces).
