@@ -101,6 +101,8 @@ __device__ __forceinline__ float f8_odd(double v) {
   return __uint_as_float(b);
 }
 __device__ __forceinline__ double f8_scale(double top) { return fmax(top / 448.0, 0x1p-126); }
+// The largest magnitude of a block, or what it is at the least scale.
+__device__ __forceinline__ double f8_most(double top) { return fmax(top, 448.0 * 0x1p-126); }
 __device__ __forceinline__ uint2 f8_pack8(const float (&v)[8]) {
   return make_uint2(f8_pack4(v[0], v[1], v[2], v[3]), f8_pack4(v[4], v[5], v[6], v[7]));
 }
@@ -112,9 +114,11 @@ __device__ __forceinline__ uint2 f8_codes8(const float (&x)[8], float inv, float
   for (int i = 0; i < 8; ++i) v[i] = x[i] * inv;
   if constexpr (EXACT) {
     if (__any(f8_near_middle<4>(v))) {
-      const double scale = f8_scale(static_cast<double>(top));
+      // x 448 is exact, so that its quotient by the largest is a middle where x / scale is one
+      // (by a rounded top / 448, an eighth of them would fall to either side)
+      const double most = f8_most(top);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = f8_odd(x[i] / scale);
+      for (int i = 0; i < 8; ++i) v[i] = f8_odd(x[i] * 448.0 / most);
     }
   }
   return f8_pack8(v);

@@ -54,3 +54,28 @@ def test_add_norm_rows_without_gradients(kata, M, D):  # noqa: F811
     dx, dw = kata.add_norm_bwd(up(s, BF16), w, up(dy, BF16), up(dsum, BF16))
     assert torch.equal(dx.cpu().double()[out], dsum[out])
     assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
+
+
+# ---- e4m3: values that are middles between two codes -------------------------------------
+
+@pytest.mark.parametrize("rows", (1, 128))
+def test_f8_quant_middles_go_to_the_even_code(kata, rows):  # noqa: F811
+    """x = top v / 448 for the middles v that a top of 16 bits has in fp32 (those of significand 21,
+    and 7 below the normal range): x 448 / top is v itself, a tie, whatever top / 448 rounds to."""
+    gen = torch.Generator().manual_seed(5)
+    n = 640
+    middles = torch.tensor([21.0 * 2.0 ** k for k in range(-10, 5)] + [7 * 2.0 ** -10], dtype=torch.float64)
+    tops = torch.randint(1, 1 << 16, (n // 128, n // 128), generator=gen).double()
+    tops = tops.repeat_interleave(128, 0).repeat_interleave(128, 1)
+    v = middles[torch.randint(0, len(middles), (n, n), generator=gen)]
+    sign = torch.randint(0, 2, (n, n), generator=gen) * 2.0 - 1
+    x = sign * tops * v / 448
+    at = torch.arange(128)
+    for i in range(0, n, 128):
+        for j in range(0, n, 128):
+            x[i + at, j + at] = tops[i + at, j + at]  # the largest of every row and column of a block
+    assert torch.equal(x.float().double(), x) and torch.equal(x * 448 / tops, (x * 448 / tops).float().double())
+    x = x.float()
+    got = kata.f8_quant(up(x), rows=rows, transposed=True)
+    for g, w, name in zip(got, (*ref.quantise(x, rows), *ref.quantise(x.t(), rows)), ("q", "scale", "qt", "scale_t")):
+        assert torch.equal(g.float().cpu().double(), w.double()), name
