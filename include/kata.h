@@ -603,7 +603,7 @@ KATA_API kata_status_t kata_ssm_step(float* S, const void* x, const void* dt, co
  *     s = x + res (rounded to dtype; without res: x),   y = s w / sqrt(mean(s^2) + eps).
  *   x, res, sum, y : [M][D] in dtype;  w : [D], nullable (ones).
  *   res, sum : both or neither; sum receives s, and may be res itself with its row stride.
- *   y, or q and scale (y in 8 bits, quantised from fp32, blocks of one row), or all three.
+ *   y, or q and scale (y in 8 bits, quantised before it is rounded, blocks of one row), or all three.
  *   D <= 32768, else KATA_ERR_UNSUPPORTED.  Squares are summed in fp64;
  *   mean + eps has to lie between 2^-250 and 2^250.
  */

@@ -116,20 +116,24 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
       if ((lane & 15) == 0 && c < s.D) scale[m * kb + c / kF8Block] = sc;
 #pragma unroll
       for (int i = 0; i < 8; ++i) out[i] *= by;
-      // out and the block's largest value are off by up to 2.5 steps of fp32 each, their quotient by 6
+      // out and the block's largest value are off by up to 2.5 steps of fp32 each, their quotient by 6.
+      // The row's factor stands in both and is left out: s w 448 is exact in fp64 (51 bits), so that its
+      // quotient by the block's largest s w is a middle only where it is one.
       if (__any(f8_near_middle<8>(out))) {
         double exact[8], top = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          exact[i] = v[k][i] * inv64 * wv[i];
+          exact[i] = static_cast<double>(v[k][i]) * wv[i];
           top = fmax(top, fabs(exact[i]));
         }
         top = fmax(top, dpp_move64<0xB1>(top));
         top = fmax(top, dpp_move64<0x4E>(top));
         top = fmax(top, dpp_move64<0x141>(top));
-        top = f8_scale(fmax(top, dpp_move64<0x140>(top)));
+        top = fmax(top, dpp_move64<0x140>(top));
+        const bool least = !(f8_most(top * inv64) > f8_most(0.0));  // (a NaN row too)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = f8_odd(exact[i] / top);
+        for (int i = 0; i < 8; ++i)
+          out[i] = f8_odd(least ? exact[i] * (inv64 * 0x1p126) : exact[i] * 448.0 / top);
       }
       store8_codes<VEC>(q + m * s.q_row, c, s.D, f8_pack8(out));
     }

@@ -100,7 +100,6 @@ __device__ __forceinline__ float f8_odd(double v) {
   else if (d > 0.0) b |= 1u;
   return __uint_as_float(b);
 }
-__device__ __forceinline__ double f8_scale(double top) { return fmax(top / 448.0, 0x1p-126); }
 // The largest magnitude of a block, or what it is at the least scale.
 __device__ __forceinline__ double f8_most(double top) { return fmax(top, 448.0 * 0x1p-126); }
 __device__ __forceinline__ uint2 f8_pack8(const float (&v)[8]) {

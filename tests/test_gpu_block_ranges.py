@@ -79,3 +79,36 @@ def test_f8_quant_middles_go_to_the_even_code(kata, rows):  # noqa: F811
     got = kata.f8_quant(up(x), rows=rows, transposed=True)
     for g, w, name in zip(got, (*ref.quantise(x, rows), *ref.quantise(x.t(), rows)), ("q", "scale", "qt", "scale_t")):
         assert torch.equal(g.float().cpu().double(), w.double()), name
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("weight", (False, True))
+@pytest.mark.parametrize("M,D", ((2048, 1000), (200, 3100)))
+def test_add_norm_middles_go_to_the_even_code(kata, M, D, weight, dtype):  # noqa: F811
+    """Rows (and weights) of 8 bits, whose quotients by their block's largest are middles in one of
+    500 values.  The row's factor stands in both and leaves the quotient; products of 16 bits
+    times 448 are exact in fp64, and so is a quotient that has few bits."""
+    gen = torch.Generator().manual_seed(D)
+    x = normal(gen, M, D, dtype=BF16)
+    w = normal(gen, D, dtype=BF16) if weight else None
+    q, _, _ = kata.add_norm_f8_fwd(up(x, dtype), up(w))
+    v = x if w is None else x * w
+    top = torch.nn.functional.pad(v.abs(), (0, -D % 128)).unflatten(1, (-1, 128)).amax(-1)
+    v = v * 448 / ref.spread(top, 1, M, D)
+    ties = ref.to_e4m3(v * (1 - 2.0 ** -40)) != ref.to_e4m3(v * (1 + 2.0 ** -40)).clamp(-448, 448)
+    assert 1e-4 * v.numel() < int(ties.sum())
+    assert torch.equal(q.float().cpu().double(), ref.to_e4m3(v))
+
+
+def test_add_norm_codes_at_the_least_scale(kata):  # noqa: F811
+    """A block whose largest value is at most 448 x 2^-126: codes of y 2^126."""
+    gen = torch.Generator().manual_seed(2)
+    x, w = normal(gen, 5, 300, dtype=F32), normal(gen, 300, dtype=F32)
+    w[128:256] = (w[128:256] * 2.0 ** -121).float().double()
+    q, scale, _ = kata.add_norm_f8_fwd(up(x), up(w))
+    want = ref.norm(x, w, float(torch.tensor(1e-6)))
+    assert (scale[:, 1] == 2.0 ** -126).all()
+    v = want[:, 128:256] * 2.0 ** 126
+    # w is of 24 bits: no middles but by chance (none within 2^-40)
+    assert torch.equal(ref.to_e4m3(v * (1 - 2.0 ** -40)), ref.to_e4m3(v * (1 + 2.0 ** -40)))
+    assert torch.equal(q.float().cpu().double()[:, 128:256], ref.to_e4m3(v))
