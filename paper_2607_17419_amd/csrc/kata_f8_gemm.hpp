@@ -134,6 +134,20 @@ __device__ __forceinline__ i32x8 f8_operand(uint4 lo, uint4 hi) {
   return __builtin_bit_cast(i32x8, Two{lo, hi});
 }
 
+// Whether a scale's product with one of the other operand may leave fp32's normal range: two that
+// are not far are between 2^-124 and 2^126.  0 and the quantisers' least scale, whose blocks hold no
+// value above 2^-117, are not: such a block's part of a result is off by up to 2^-125.  A far scale
+// counts as 0 in the kernels' loops; blocks that have one are gone through once more behind them,
+// for the results that they left out, in fp64.  (Both ways in one loop spill.)
+constexpr uint32_t kF8Least = 0x00800000, kF8Low = 0x20800000, kF8High = 0x5F000000;  // 2^-126, 2^-62, 2^63
+__device__ __forceinline__ bool f8_far(float scale) {
+  const uint32_t m = __float_as_uint(scale) & 0x7FFFFFFFu;
+  return m - kF8Low > kF8High - kF8Low && (m & ~kF8Least) != 0;
+}
+__device__ __forceinline__ float f8_far_sum(float p, float sa, float sb, float acc) {
+  return f8_far(sa) || f8_far(sb) ? static_cast<float>(static_cast<double>(p) * sa * sb + acc) : acc;
+}
+
 // Four neighbouring columns of a row of the result.
 template <typename E>
 __device__ __forceinline__ void f8_store4(E* row, int n, int N, bool whole, const float (&v)[4]) {
@@ -212,6 +226,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) 
   static_assert(ROWS_ALL <= 64 * WAVES && (BM / 8) % WAVES == 0 && (BN / 8) % WAVES == 0, "");
   __shared__ __align__(16) char lds[2 * STAGE];
   __shared__ __align__(16) float scales[2][4][ROWS_ALL];
+  __shared__ int any_far;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int split, tm, tn;
   f8_place(s, split, tm, tn);
@@ -254,7 +269,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) 
 #pragma unroll
     for (int k = 0; k < 4; ++k) four[k] = srow[min(kb + k, s.kb - 1)];
   };
+  unsigned long long far = 0;
   const auto put = [&](int group) {
+    // hardly ever more than this one look at four of them (as words: a negative one is looked at, too)
+    uint32_t most = 0, least = ~0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      most = max(most, __float_as_uint(four[k]));
+      least = min(least, __float_as_uint(four[k]));
+    }
+    if (__any(most > kF8High || least < kF8Low)) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool one = f8_far(four[k]);
+        far |= __ballot(one);
+        if (one) four[k] = 0.f;
+      }
+    }
     if (threadIdx.x < ROWS_ALL) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) scales[group & 1][k][threadIdx.x] = four[k];
@@ -268,6 +299,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) 
   } else {
     stage_slow(first, lds);
   }
+  if (threadIdx.x == 0) any_far = 0;
   fetch(first);
   put(0);
   const auto block = [&](int kb, auto with_copies) {
@@ -334,6 +366,34 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8GemmArgs s) 
     for (; kb + 1 < min(last, whole); ++kb) block(kb, F8Int<1>());
   }
   for (; kb < last; ++kb) block(kb, F8Int<0>());
+  if (far) any_far = 1;
+  __syncthreads();
+  if (any_far) {
+    float* sc = scales[0][0];
+    for (kb = first; kb < last; ++kb) {
+      const float one = srow[kb];
+      if (!__syncthreads_or(f8_far(one))) continue;
+      __syncthreads();  // the block before has been read
+      stage_slow(kb, lds);
+      if (threadIdx.x < ROWS_ALL) sc[threadIdx.x] = one;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const F8Operand<F16> fa(f8_fragment(lds, (wm * TM + i) * 16));
+        const float sa = sc[(wm * TM + i) * 16 + (lane & 15)];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const F8Operand<F16> fb(f8_fragment(lds + BM * 128, (wn * TN + j) * 16));
+          const f32x4 p = f8_block(fb, fa);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = f8_far_sum(
+                p[e], sa, sc[BM + wn * TN * 16 + (ROWS == 1 ? j * 16 + 4 * (lane >> 4) + e : 0)], acc[i][j][e]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
   const bool pieces = s.part ? s.N % 4 == 0
                              : s.c_row % 4 == 0 &&
                                    (reinterpret_cast<uintptr_t>(s.c) & (4 * sizeof(E) - 1)) == 0;
@@ -386,6 +446,12 @@ __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
   const int nr = min(n0 + r, s.N - 1);
   const uint8_t* brow = s.b + nr * s.b_row;
   f32x4 acc[MT] = {};
+  int far = 0;
+  const auto ordinary = [&](float scale) {
+    const bool one = f8_far(scale);
+    far = one ? 1 : far;
+    return one ? 0.f : scale;
+  };
   // N blocks from kb on, every eighth; TAIL: the one that K ends in
   const auto blocks = [&](int kb, auto count, auto tail) {
     constexpr int N = decltype(count)::value;
@@ -420,20 +486,46 @@ __global__ __launch_bounds__(512) void f8_rows_kernel(F8GemmArgs s) {
       }
     }
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+    for (int u = 0; u < N; ++u) {
+#pragma unroll
+      for (int e = 0; e < (ROWS == 1 ? 4 : 1); ++e) sb[u][e] = ordinary(sb[u][e]);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const f32x4 p = f8_block(F8Operand<F16>(f8_operand(fb[u][0], fb[u][1])),
                                  F8Operand<F16>(f8_operand(fa[u][i][0], fa[u][i][1])));
+        const float si = ordinary(sa[u][i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[i][e] = fmaf(p[e], sa[u][i] * sb[u][ROWS == 1 ? e : 0], acc[i][e]);
+          acc[i][e] = fmaf(p[e], si * sb[u][ROWS == 1 ? e : 0], acc[i][e]);
       }
+    }
   };
   int kb = wave;
   for (; kb + 8 * (U - 1) < whole; kb += 8 * U) blocks(kb, F8Int<U>(), F8Int<0>());
   for (; kb < whole; kb += 8) blocks(kb, F8Int<1>(), F8Int<0>());
   if (kb < s.kb) blocks(kb, F8Int<1>(), F8Int<1>());
+  if (__any(far)) {
+    for (kb = wave; kb < s.kb; kb += 8) {
+      const int k = kb * 128 + g * 32;
+      const F8Operand<F16> fb(f8_operand(f8_chunk<true>(brow, k, s.K, nr == s.N - 1),
+                                         f8_chunk<true>(brow, k + 16, s.K, nr == s.N - 1)));
+      float sb[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sb[e] = s.sb[static_cast<size_t>(min(n0 + 4 * g + e, s.N - 1) / ROWS) * s.kb + kb];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int m = min(i * 16 + r, s.M - 1);
+        const uint8_t* arow = s.a + m * s.a_row;
+        const F8Operand<F16> fa(f8_operand(f8_chunk<true>(arow, k, s.K, m == s.M - 1),
+                                           f8_chunk<true>(arow, k + 16, s.K, m == s.M - 1)));
+        const f32x4 p = f8_block(fb, fa);
+        const float sa = s.sa[static_cast<size_t>(m) * s.kb + kb];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][e] = f8_far_sum(p[e], sa, sb[e], acc[i][e]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll

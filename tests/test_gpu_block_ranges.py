@@ -112,3 +112,95 @@ def test_add_norm_codes_at_the_least_scale(kata):  # noqa: F811
     # w is of 24 bits: no middles but by chance (none within 2^-40)
     assert torch.equal(ref.to_e4m3(v * (1 - 2.0 ** -40)), ref.to_e4m3(v * (1 + 2.0 ** -40)))
     assert torch.equal(q.float().cpu().double()[:, 128:256], ref.to_e4m3(v))
+
+
+# ---- product: scales whose product leaves fp32 -------------------------------------------
+
+def far_operands(gen, M, N, K, rows, how):
+    """Codes and scales: `apart`: every third block's scales are about 2^66 each and its codes share
+    no k (a product of 0), the others' 2^90 and 2^-90; `faint`: 2^66 each, codes of 2^-9;
+    `low`: 2^-70 and 2^-50; `least`: blocks without values beside ordinary ones."""
+    (a, sa), (b, sb) = operand(gen, M, K, 1), operand(gen, N, K, rows)
+    kb, k = torch.arange(sa.shape[1]), torch.arange(K)
+    third = kb % 3 == 0
+    if how == "apart":
+        sa = torch.where(third, sa * 2.0 ** 72, sa * 2.0 ** 90)
+        sb = torch.where(third, sb * 2.0 ** 72, sb * 2.0 ** -90)
+        of = third[k // 128]
+        a[:, of & (k % 128 >= 64)] = 0.0
+        b[:, of & (k % 128 < 64)] = 0.0
+    elif how == "faint":
+        a, b = a.sign() * 2.0 ** -9, b.sign() * 2.0 ** -9
+        sa, sb = torch.full_like(sa, 2.0 ** 66), torch.full_like(sb, 2.0 ** 66)
+    elif how == "low":
+        sa, sb = sa * 2.0 ** -70, sb * 2.0 ** -50
+    else:
+        a[:, third[k // 128]] = 0.0
+        sa = torch.where(third, 2.0 ** -126, sa)
+        b[:, ~third[k // 128]] = 0.0
+        sb = torch.where(third, sb, 2.0 ** -126)
+    return (a, sa.float()), (b, sb.float())
+
+
+FAR = [(33, 130, 1000, "even"), (64, 40, 4500, "even"), (8, 8200, 700, "even"), (100, 300, 1152, "even"),
+       (100, 300, 1152, "odd"), (70, 200, 2500, "even"), (70, 200, 2500, "odd")]
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("rows", (1, 128))
+@pytest.mark.parametrize("M,N,K,lay", FAR)
+def test_f8_gemm_scales_whose_product_leaves_fp32(kata, M, N, K, lay, rows, dtype):  # noqa: F811
+    gen = torch.Generator().manual_seed(M + N + K)
+    for how in ("apart", "faint", "low", "least"):
+        (a, sa), (b, sb) = far_operands(gen, M, N, K, rows, how)
+        want, mag, top = ref.product(a, sa, b, sb, rows)
+        assert float(want.abs().max()) < 3e38
+        tol = ref.ROUND[dtype] * want.abs() + (2 * min(K, 128) + ref.blocks(K) + 32) * EPS * mag + LEAST[dtype]
+        if dtype == BF16:
+            tol = tol + 7 * 2.0 ** -13 * top
+        log(f"case f8_gemm scales {how} M{M} N{N} K{K} rows{rows} {dtype} {lay}")
+        c = kata.f8_gemm(laid(a, lay), up(sa), laid(b, lay), up(sb), dtype=dtype)
+        near(c, want, tol, "c")
+
+
+@pytest.mark.parametrize("lay", ("even", "odd"))
+@pytest.mark.parametrize("rows", (1, 128))
+def test_f8_gemm_large_tiles(kata, rows, lay):  # noqa: F811
+    """The largest tiles, on aligned and unaligned rows, of ordinary scales and of far ones."""
+    M, N, K = 4096, 4097, 700
+    gen = torch.Generator().manual_seed(rows)
+    at = torch.randperm(M, generator=gen)[:24]
+    at[:4] = torch.tensor([0, M - 1, M // 2, 255])
+    for how in ("ordinary", "apart", "low"):
+        log(f"case f8_gemm large {how} rows{rows} {lay}")
+        if how == "ordinary":
+            (a, sa), (b, sb) = operand(gen, M, K, 1), operand(gen, N, K, rows)
+        else:
+            (a, sa), (b, sb) = far_operands(gen, M, N, K, rows, how)
+        c = kata.f8_gemm(laid(a, lay), up(sa), laid(b, lay), up(sb))
+        want, mag, top = ref.product(a[at], sa[at], b, sb, rows)
+        tol = 2.0 ** -8 * want.abs() + (256 + ref.blocks(K) + 32) * EPS * mag + 7 * 2.0 ** -13 * top
+        near(c[at.to(DEV)], want, tol, "rows")
+        whole = (a.double() * ref.spread(sa, 1, M, K)) @ (b.double() * ref.spread(sb, rows, N, K)).t()
+        off = float((c.cpu().double() - whole).norm() / whole.norm())
+        assert off <= 2.0 ** -8, off
+
+
+def test_f8_gemm_far_scales_in_one_block_only(kata):  # noqa: F811
+    """Far scales in one group of blocks and ordinary ones in the others, and the ones that spread."""
+    gen = torch.Generator().manual_seed(11)
+    M, N, K = 150, 200, 1700
+    for at, dtype in ((0, F32), (5, F32), (13, F32), (5, BF16)):
+        (a, sa), (b, sb) = operand(gen, M, K, 1), operand(gen, N, K, 128)
+        a[:, at * 128:at * 128 + 128] = 0.0
+        sa[:, at], sb[:, at] = 3e19, 3e19
+        want, mag, top = ref.product(a, sa, b, sb, 128)
+        tol = ref.ROUND[dtype] * want.abs() + (288 + ref.blocks(K)) * EPS * mag + (7 * 2.0 ** -13 * top if dtype == BF16 else 0)
+        near(kata.f8_gemm(laid(a, "even"), up(sa), laid(b, "even"), up(sb), dtype=dtype), want, tol, "c")
+        sa[7, at] = float("inf")
+        sb[1, (at + 1) % 13] = float("nan")
+        c = kata.f8_gemm(laid(a, "even"), up(sa), laid(b, "even"), up(sb), dtype=dtype).cpu()
+        bad = torch.zeros((M, N), dtype=torch.bool)
+        bad[7] = bad[:, 128:] = True
+        assert torch.equal(~torch.isfinite(c), bad)
+        assert torch.equal(c[~bad].double().sub(want[~bad]).abs() <= tol[~bad], torch.ones(int((~bad).sum()), dtype=torch.bool))
