@@ -204,3 +204,33 @@ def test_f8_gemm_far_scales_in_one_block_only(kata):  # noqa: F811
         bad[7] = bad[:, 128:] = True
         assert torch.equal(~torch.isfinite(c), bad)
         assert torch.equal(c[~bad].double().sub(want[~bad]).abs() <= tol[~bad], torch.ones(int((~bad).sum()), dtype=torch.bool))
+
+
+# ---- gated linear recurrence: gates that cancel their biases --------------------------------
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_recur_gates_that_cancel_their_biases(kata, dtype):  # noqa: F811
+    """Biases up to 3000 against gates as far on the other side: what is left of them is exact, and
+    results are as near as without either."""
+    B, T, D = 2, 200, 16
+    gen = torch.Generator().manual_seed(7)
+    base = torch.tensor([20.0, -20.0, 43.0, -43.0, 300.0, -300.0, 3008.0, -3008.0], dtype=torch.float64).repeat(2)
+    x, dy = normal(gen, B, T, D, dtype=dtype), normal(gen, B, T, D, dtype=dtype)
+    r, i = ((base + normal(gen, B, T, D)).to(dtype).double() for _ in range(2))
+    bias = (-base + 0.37).float().double()
+    lam = (torch.rand(D, generator=gen, dtype=torch.float64) * 4 - 5).float().double()
+    dev = [up(t, dtype) for t in (x, r, i)] + [up(lam), up(bias), up(bias)]
+    log(f"case recur cancelled gates {dtype}")
+    leaf = [t.clone().requires_grad_() for t in (x, r, i, lam, bias, bias)]
+    want, h = ref.recur(*leaf)
+    err = ref.recur_errors(x, r, i, lam, bias, bias, 8.0, None, None, dy)
+    y, last = kata.recur_fwd(*dev, final_state=True)
+    near(y, want, ref.ROUND[dtype] * want.abs() + err["y"], "y")
+    near(last, h, err["h"] + EPS * h.abs(), "state")
+    grads = torch.autograd.grad((want * dy).sum(), leaf)
+    for g, w, name in zip(kata.recur_bwd(*dev, up(dy, dtype)), grads, ("dx", "dr", "di", "dlam", "drb", "dib")):
+        near(g, w, (ref.ROUND[dtype] if g.dim() == 3 else EPS) * w.abs() + err[name], name)
+    state = torch.zeros((B, D), device=DEV)
+    out = kata.recur_step(state, *(t[:, 0].contiguous() for t in dev[:3]), *dev[3:])
+    near(state, want[:, 0], err["y"][:, 0] + EPS * want[:, 0].abs(), "step")
+    near(out, want[:, 0], ref.ROUND[dtype] * want[:, 0].abs() + err["y"][:, 0], "step's output")
