@@ -131,9 +131,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void add_norm_kernel
         top = fmax(top, dpp_move64<0x141>(top));
         top = fmax(top, dpp_move64<0x140>(top));
         const bool least = !(f8_most(top * inv64) > f8_most(0.0));  // (a NaN row too)
+        const double times = least ? inv64 * 0x1p126 : 448.0;
+        if (least) top = 1.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          out[i] = f8_odd(least ? exact[i] * (inv64 * 0x1p126) : exact[i] * 448.0 / top);
+        for (int i = 0; i < 8; ++i) out[i] = f8_odd(exact[i] * times / top);
       }
       store8_codes<VEC>(q + m * s.q_row, c, s.D, f8_pack8(out));
     }
