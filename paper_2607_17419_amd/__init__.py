@@ -1167,7 +1167,8 @@ def f8_quant(x, rows: int = 1, transposed: bool = False, q=None, scale=None, qt=
 def f8_gemm(a, a_scale, b, b_scale, out=None, dtype=None, workspace=None):
     """a b^T of 8-bit operands (kata_f8_gemm_ws): a [..,K] with a_scale [..,ceil(K/128)], b [N,K]
     with b_scale [ceil(N/128),ceil(K/128)] (128 x 128 blocks) or [N,ceil(K/128)] (blocks of a
-    row); returns [..,N] in dtype (fp32 or bf16, the default)."""
+    row); returns [..,N] in dtype: bf16 (the default), whose products keep 13 bits of the largest
+    of eight, or fp32, whose products are exact."""
     import torch
     M, K, a_row = _rows(a, "a [..,K]")
     N, Kb = _dims(b, 2, "b [N,K]")

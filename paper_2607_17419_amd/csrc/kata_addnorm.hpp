@@ -8,9 +8,11 @@
 //   dx = dsum + inv (g - hat mean(g hat)),   dw = sum over rows of dy hat.
 //
 // HBM bound: a row stays in the registers of one to sixteen waves from its load to its
-// store, eight neighbouring columns a lane, so every tensor is read or written once.
-// 32768 rows of 1024, bf16: forward 46 us (268 MB, 5.8 TB/s), gradients 47 us (268 MB, 5.7 TB/s)
-// and 5 us for their sums; 256 rows to 8 bits 4 us, the launch's latency.
+// store, eight neighbouring columns a lane, so every tensor is read or written once (but in the
+// gradients of rows of more than 16384 columns, which spill).  32768 rows of 1024, bf16: forward 46 us
+// (268 MB, 5.8 TB/s), to codes 44 us (236 MB, 5.4 TB/s), gradients 48 us (268 MB, 5.6 TB/s; 51 us
+// where all of dy is 0) and 5 us for their sums; 256 rows to 8 bits 4 us, the launch's latency.
+// 2048 rows of 16384: 55 and 58 us, 1024 of 32768: 57 and 270.
 #pragma once
 
 #include "kata_f8.hpp"

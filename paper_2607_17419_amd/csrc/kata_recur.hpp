@@ -17,12 +17,14 @@
 // L and not the product of the a: where a = 1 - m 2^-24, its products round to 1 - (m + n) 2^-24
 // token by token, always to the same side (state after 20000 tokens at rates of 2e-5: 1.2e-5 off).
 //
-// 131072 tokens of 1024 channels, bf16: 255-265 us, 4.1 TB/s of the 1.07 GB that are read and
+// 131072 tokens of 1024 channels, bf16: 251 us, 4.3 TB/s of the 1.07 GB that are read and
 // written once (three launches that form the spans' sums, join them and read everything again:
-// 874); the vector units are busy 66% of the cycles (45 instructions an element, a sixth of
+// 874); the vector units are busy 69% of the cycles (44 instructions an element, a sixth of
 // them exponentials, reciprocals and roots at 2.5 times an addition's time), loads and
 // arithmetic of the two workgroups of a CU overlap in part.  Training step of 8 x 4096 tokens:
-// forward 84 us, gradients 172.  Runs of 8 tokens a wave: long 298, training 257 us.
+// forward 75-81 us, gradients 164-175.  Runs of 8 tokens a wave: long 298 (for 268 then), training
+// 257 (for 251).  fp32: 65536 tokens 206-217 us, training step of 8 x 2048 65-69 and 136-141 us, the
+// gradients with one workgroup on a CU (156 registers).
 #pragma once
 
 #include "kata_block.hpp"
