@@ -234,3 +234,28 @@ def test_recur_gates_that_cancel_their_biases(kata, dtype):  # noqa: F811
     out = kata.recur_step(state, *(t[:, 0].contiguous() for t in dev[:3]), *dev[3:])
     near(state, want[:, 0], err["y"][:, 0] + EPS * want[:, 0].abs(), "step")
     near(out, want[:, 0], ref.ROUND[dtype] * want[:, 0].abs() + err["y"][:, 0], "step's output")
+
+
+@pytest.mark.parametrize("T", (20, 70, 300))
+def test_recur_forgets_large_states(kata, T):  # noqa: F811
+    """Rates at which a = 0, or at which a run's tokens leave less than fp32 holds, meet states and
+    gradients of 1e37: what a run adds to what is left of them is at most 2^-149 of each."""
+    big, few = 1e37, 1e37 * 2.0 ** -148
+    x = torch.linspace(-2, 2, T * 2, device=DEV).view(1, T, 2)
+    gate, zeros = torch.zeros_like(x), torch.zeros(2, device=DEV)
+    lam = torch.tensor([3e38, 30.0], device=DEV)  # the second: 8 x 30 / 2 = 120 a token
+    h0 = torch.full((1, 2), big, device=DEV)
+    _, starts = kata.recur_fwd_train(x, gate, gate, lam, zeros, zeros, state=h0)
+    assert (starts[:, 1:].abs() <= 1.0 + few).all()  # sigmoid(0) x
+    dh = torch.empty_like(h0)
+    kata.recur_bwd(x, gate, gate, lam, zeros, zeros, torch.zeros_like(x), state=h0, dstate=h0, dstate_in=dh)
+    assert (dh.abs() <= few).all()
+    # 16 tokens of rate 6 leave e^-96 of a state, which fp32 has as a subnormal number: a run's
+    # factor is off by up to 2^-149, what it hands on decays on; rates are off by 16 2^-24
+    lam = torch.log(torch.expm1(torch.full((2,), 1.5, dtype=torch.float64))).float().to(DEV)
+    y = kata.recur_fwd(torch.zeros_like(x), gate, gate, lam, zeros, zeros, state=h0).cpu().double()[0]
+    t = torch.arange(T, dtype=torch.float64)
+    want = float(h0[0, 0]) * torch.exp(-6.0 * (t + 1))
+    tol = (6 * (t + 1) * 16 * EPS + 2.0 ** -20) * want + LEAST[F32]
+    tol = tol + (t >= 16) * few * torch.exp(-6.0 * (t % 16 + 1))
+    assert ((y - want[:, None]).abs() <= tol[:, None]).all()
